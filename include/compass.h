@@ -68,7 +68,10 @@ typedef enum compass_status {
 } compass_status;
 
 enum { COMPASS_OP_AG_GEMM = 0, COMPASS_OP_GEMM_RS = 1 };
-enum { COMPASS_DTYPE_BF16 = 0 };
+/* BF16 everywhere; FP32 only where an entry point names it (embedding, layer norm, weight gradients). */
+enum { COMPASS_DTYPE_BF16 = 0, COMPASS_DTYPE_FP32 = 1 };
+/* Type of token ids and targets. */
+enum { COMPASS_INDEX_INT64 = 0, COMPASS_INDEX_INT32 = 1 };
 /* GEMM+ReduceScatter variants.
  *   SEGMENTED_K: an output tile's accumulator runs over the P ranks' K-slices
  *     in ring order (the reduction tree is the tensor-core accumulator); one
@@ -347,6 +350,66 @@ int compass_mlp_workspace_bytes(const compass_mlp* mlp, size_t* bytes);
 int compass_mlp_block(const compass_mlp* mlp, const void* const* X, const void* const* W0, void* const* H,
                       const void* const* W1, void* const* Out, void* workspace, size_t workspace_bytes,
                       void* cuda_stream);
+
+/* ---- around the blocks: embedding, layer norm, output-layer loss -------------
+ * The operators a model needs at the two ends of its tensor-parallel blocks and
+ * between them.  Activations are split by rows over the P logical ranks as
+ * everywhere in this library: P pointers to [M/P x hidden].  Vocabulary tables
+ * are split by rows too: with s = ceil(vocab / P), W[r] holds rows
+ * [r*s, min((r+1)*s, vocab)); a shard without rows may be NULL.  Pointers are
+ * 16-byte aligned (vectors of M entries: 4-byte aligned; ids: their own size).
+ * M = 0 is legal in all of them: no row is read or written, and weight
+ * gradients are set to zero.  No call allocates, synchronises or waits for
+ * other work than what precedes it on its stream; all can be captured into CUDA
+ * graphs (first call on a device before any capture).  Results do not depend on
+ * timing: the same inputs give the same bits.  Outputs must not overlap inputs
+ * or one another unless an entry point says so. */
+
+/* Token embedding.  ids: M token ids on the device (every rank has all of
+ * them), COMPASS_INDEX_*.  An id outside [0, vocab) is padding: its output row
+ * is zero and it adds nothing to the gradient. */
+typedef struct compass_embed {
+  int32_t P;
+  int32_t dtype;        /* of W and Out / dOut: COMPASS_DTYPE_BF16 or _FP32 */
+  int32_t grad_dtype;   /* of dW */
+  int32_t index_dtype;  /* COMPASS_INDEX_* */
+  int64_t M, hidden, vocab;
+  float scale;          /* Out = scale * W[id] */
+  int32_t accumulate;   /* backward: 0 = every row of dW is written; 1 = added to the rows that occur (tied weights) */
+} compass_embed;
+/* Out[r] row i = scale * W[ids[r*M/P + i]], rounded once. */
+int compass_embedding(const compass_embed* embed, const void* ids, const void* const* W, void* const* Out, void* cuda_stream);
+/* dW[v] (+)= scale * sum of the rows of dOut whose id is v: summed in FP32 over
+ * tokens sorted by id (stable, so in ascending order of position), rounded once. */
+int compass_embedding_workspace_bytes(const compass_embed* embed, size_t* bytes);
+int compass_embedding_backward(const compass_embed* embed, const void* ids, const void* const* dOut, void* const* dW,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Layer norm over rows of `hidden` elements:
+ *   h = X (+ residual),  Y = (h - mean(h)) * rstd(h) * gamma + beta,
+ *   rstd = 1 / sqrt(mean((h - mean)^2) + eps).
+ * Statistics are FP32, the variance from the centred values. */
+typedef struct compass_norm {
+  int32_t P;
+  int32_t dtype;        /* of X, residual, summed, Y and their gradients */
+  int32_t param_dtype;  /* of gamma, beta and their gradients */
+  float eps;            /* >= 0 */
+  int64_t M, hidden;
+} compass_norm;
+/* residual, summed: both or neither NULL; `summed` receives h rounded to dtype,
+ * and the rounded values are what is normalised (the backward pass takes them as
+ * its X).  summed may be X or residual themselves (in place).  gamma / beta:
+ * NULL for 1 / 0.  mean, rstd: M FP32 values each, or NULL. */
+int compass_layer_norm(const compass_norm* norm, const void* const* X, const void* const* residual, const void* gamma,
+                       const void* beta, void* const* summed, void* const* Y, float* mean, float* rstd, void* cuda_stream);
+/* dX = rstd * (g dY - mean(g dY) - xhat * mean(g dY xhat)) (+ dsum), dgamma = sum
+ * over all M rows of dY * xhat, dbeta = sum of dY.  dsum: gradient that reaches h
+ * past the norm (the residual path), or NULL.  dgamma / dbeta: NULL to leave out.
+ * dX may be dY or dsum themselves (in place) for hidden <= 8192. */
+int compass_layer_norm_workspace_bytes(const compass_norm* norm, size_t* bytes);
+int compass_layer_norm_backward(const compass_norm* norm, const void* const* dY, const void* const* X, const void* gamma,
+                                const float* mean, const float* rstd, const void* const* dsum, void* const* dX,
+                                void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ---- models, individually (host) ----------------------------------------- */
 /* Eq. 2-3: (d-1)*max(T_comp,T_comm)/d*(alpha+beta*d) + T_comp/d + T_comm/d. */

@@ -19,7 +19,8 @@ OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_BUFFER_TOO_S
 ERR_SCRATCH_LIMIT = 8
 NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
 OP_AG_GEMM, OP_GEMM_RS = 0, 1
-DTYPE_BF16 = 0
+DTYPE_BF16, DTYPE_FP32 = 0, 1
+INDEX_INT64, INDEX_INT32 = 0, 1
 RS_SEGMENTED_K, RS_RING_RMW, RS_RING_RMW_F32 = 0, 1, 2
 STRATEGY_INTRAFUSION, STRATEGY_INTERDECOM = 0, 1
 ORDER_RANK_MAJOR, ORDER_STEP_MAJOR = 0, 1
@@ -39,6 +40,8 @@ EXPORTS = (
     "compass_last_cuda_error", "compass_kernel_launch_count", "compass_gemm_rs_sequential_noalloc",
     "compass_set_wait_limit_us", "compass_calib_fit_line", "compass_ag_gemm_push", "compass_read_kernel_clock",
     "compass_mlp_workspace_bytes", "compass_mlp_block", "compass_noalloc_read_status", "compass_select_ex", "compass_test_drop_flag_writes", "compass_tensor_map_cache_stats", "compass_decomp_comm", "compass_tile_plan",
+    "compass_embedding", "compass_embedding_workspace_bytes", "compass_embedding_backward",
+    "compass_layer_norm", "compass_layer_norm_workspace_bytes", "compass_layer_norm_backward",
 )
 
 
@@ -58,6 +61,16 @@ class Problem(C.Structure):
 class Mlp(C.Structure):
     _fields_ = [("P", C.c_int32), ("rings", C.c_int32), ("M", C.c_int64), ("hidden", C.c_int64), ("ffn", C.c_int64),
                 ("activation", C.c_int32), ("rs_variant", C.c_int32), ("order", C.c_int32), ("b_layout", C.c_int32)]
+
+
+class Embed(C.Structure):
+    _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("index_dtype", C.c_int32),
+                ("M", C.c_int64), ("hidden", C.c_int64), ("vocab", C.c_int64), ("scale", C.c_float), ("accumulate", C.c_int32)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("param_dtype", C.c_int32), ("eps", C.c_float),
+                ("M", C.c_int64), ("hidden", C.c_int64)]
 
 
 class SchedEntry(C.Structure):
@@ -125,6 +138,13 @@ def lib() -> C.CDLL:
                                          C.c_void_p, C.c_size_t, C.c_void_p]
         L.compass_gemm_rs_sequential_noalloc.argtypes = [C.POINTER(Problem), pp, pp, pp, C.c_void_p]
         L.compass_noalloc_read_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
+        vp = C.c_void_p
+        L.compass_embedding.argtypes = [C.POINTER(Embed), vp, pp, pp, vp]
+        L.compass_embedding_workspace_bytes.argtypes = [C.POINTER(Embed), C.POINTER(C.c_size_t)]
+        L.compass_embedding_backward.argtypes = [C.POINTER(Embed), vp, pp, pp, vp, C.c_size_t, vp]
+        L.compass_layer_norm.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, pp, pp, vp, vp, vp]
+        L.compass_layer_norm_workspace_bytes.argtypes = [C.POINTER(Norm), C.POINTER(C.c_size_t)]
+        L.compass_layer_norm_backward.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, vp, pp, pp, vp, vp, vp, C.c_size_t, vp]
         L.compass_set_wait_limit_us.argtypes = [C.c_uint32]
         L.compass_test_drop_flag_writes.argtypes = [C.c_int]
         L.compass_tensor_map_cache_stats.argtypes = [C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
@@ -347,6 +367,139 @@ def compass_mlp_block(mlp: Mlp, X: Sequence, W0: Sequence, H: Sequence, W1: Sequ
     p, n = _ws(workspace)
     _check(lib().compass_mlp_block(C.byref(mlp), _ptr_array(X), _ptr_array(W0), _ptr_array(H), _ptr_array(W1),
                                    _ptr_array(Out), p, n, _stream_handle(stream)), "compass_mlp_block")
+
+
+# ---- around the blocks: embedding, layer norm ------------------------------------------
+#
+# These take torch tensors and check type, shape and layout before the library sees the addresses
+# (ValueError); what the library itself refuses raises CompassError.
+
+_TORCH_DTYPES: dict = {}
+
+
+def _torch_dtype(kind: int):
+    if not _TORCH_DTYPES:
+        import torch
+        _TORCH_DTYPES.update({DTYPE_BF16: torch.bfloat16, DTYPE_FP32: torch.float32, "index": {INDEX_INT64: torch.int64, INDEX_INT32: torch.int32}})
+    if kind not in _TORCH_DTYPES:
+        raise ValueError(f"unknown element type {kind}")
+    return _TORCH_DTYPES[kind]
+
+
+def _tensor(name: str, t, dtype, shape) -> Optional[int]:
+    """Address of a dense CUDA tensor of this type and shape (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name}: want a contiguous CUDA tensor of {dtype} {tuple(shape)}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
+    return t.data_ptr() or None
+
+
+def _row_shards(name: str, tensors: Optional[Sequence], P: int, M: int, hidden: int, kind: int):
+    if tensors is None:
+        return None
+    if len(tensors) != P:
+        raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
+    dtype, shape = _torch_dtype(kind), (M // P, hidden)
+    return (C.c_void_p * P)(*[_tensor(name, t, dtype, shape) for t in tensors])
+
+
+def vocab_shard_rows(vocab: int, P: int, r: int) -> int:
+    """Rows of rank r's shard of a table of `vocab` rows: ceil(vocab / P) each, the last ones fewer."""
+    s = -(-vocab // P)
+    return max(0, min(s, vocab - s * r))
+
+
+def _vocab_shards(name: str, tensors: Sequence, P: int, vocab: int, hidden: int, kind: int):
+    if len(tensors) != P:
+        raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
+    dtype = _torch_dtype(kind)
+    return (C.c_void_p * P)(*[_tensor(name, t, dtype, (vocab_shard_rows(vocab, P, r), hidden)) for r, t in enumerate(tensors)])
+
+
+def _index(name: str, t, kind: int, M: int):
+    return _tensor(name, t, _torch_dtype("index")[kind], (M,))
+
+
+def _vector(name: str, t, n: int, kind: int = DTYPE_FP32):
+    return _tensor(name, t, _torch_dtype(kind), (n,))
+
+
+def _sized_workspace(nbytes: int, device):
+    import torch
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    compass_workspace_init(ws)
+    return ws
+
+
+def make_embedding(P: int, M: int, hidden: int, vocab: int, scale: float = 1.0, dtype: int = DTYPE_BF16,
+                   grad_dtype: Optional[int] = None, index_dtype: int = INDEX_INT64, accumulate: bool = False) -> Embed:
+    return Embed(P=P, dtype=dtype, grad_dtype=dtype if grad_dtype is None else grad_dtype, index_dtype=index_dtype, M=M,
+                 hidden=hidden, vocab=vocab, scale=scale, accumulate=int(accumulate))
+
+
+def compass_embedding(embed: Embed, ids, W: Sequence, Out: Sequence, stream=None) -> None:
+    """Out[r] = scale * W[ids of rank r's rows]; ids outside the vocabulary give zero rows."""
+    e = embed
+    _check(lib().compass_embedding(C.byref(e), _index("ids", ids, e.index_dtype, e.M), _vocab_shards("W", W, e.P, e.vocab, e.hidden, e.dtype),
+                                   _row_shards("Out", Out, e.P, e.M, e.hidden, e.dtype), _stream_handle(stream)), "compass_embedding")
+
+
+def compass_embedding_workspace_bytes(embed: Embed) -> int:
+    n = C.c_size_t(0)
+    _check(lib().compass_embedding_workspace_bytes(C.byref(embed), C.byref(n)), "compass_embedding_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_embedding_workspace(embed: Embed, device="cuda"):
+    return _sized_workspace(compass_embedding_workspace_bytes(embed), device)
+
+
+def compass_embedding_backward(embed: Embed, ids, dOut: Sequence, dW: Sequence, workspace, stream=None) -> None:
+    """dW (+)= scale * the rows of dOut summed by id, over tokens sorted by id."""
+    e = embed
+    p, n = _ws(workspace)
+    _check(lib().compass_embedding_backward(C.byref(e), _index("ids", ids, e.index_dtype, e.M),
+                                            _row_shards("dOut", dOut, e.P, e.M, e.hidden, e.dtype),
+                                            _vocab_shards("dW", dW, e.P, e.vocab, e.hidden, e.grad_dtype), p, n, _stream_handle(stream)),
+           "compass_embedding_backward")
+
+
+def make_layer_norm(P: int, M: int, hidden: int, eps: float = 1e-5, dtype: int = DTYPE_BF16, param_dtype: Optional[int] = None) -> Norm:
+    return Norm(P=P, dtype=dtype, param_dtype=dtype if param_dtype is None else param_dtype, eps=eps, M=M, hidden=hidden)
+
+
+def compass_layer_norm(norm: Norm, X: Sequence, gamma, beta, Y: Sequence, mean=None, rstd=None, residual: Optional[Sequence] = None,
+                       summed: Optional[Sequence] = None, stream=None) -> None:
+    """Y = layer norm of X, or of summed = X + residual; gamma and beta may be None (1 and 0)."""
+    n = norm
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype)  # noqa: E731
+    _check(lib().compass_layer_norm(C.byref(n), rows("X", X), rows("residual", residual), _vector("gamma", gamma, n.hidden, n.param_dtype),
+                                    _vector("beta", beta, n.hidden, n.param_dtype), rows("summed", summed), rows("Y", Y),
+                                    _vector("mean", mean, n.M), _vector("rstd", rstd, n.M), _stream_handle(stream)), "compass_layer_norm")
+
+
+def compass_layer_norm_workspace_bytes(norm: Norm) -> int:
+    n = C.c_size_t(0)
+    _check(lib().compass_layer_norm_workspace_bytes(C.byref(norm), C.byref(n)), "compass_layer_norm_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_layer_norm_workspace(norm: Norm, device="cuda"):
+    return _sized_workspace(compass_layer_norm_workspace_bytes(norm), device)
+
+
+def compass_layer_norm_backward(norm: Norm, dY: Sequence, X: Sequence, gamma, mean, rstd, dX: Sequence, dgamma, dbeta, workspace,
+                                dsum: Optional[Sequence] = None, stream=None) -> None:
+    """dX (+ dsum, the gradient that reaches X past the norm), dgamma and dbeta (None: left out) summed over all M rows."""
+    n = norm
+    p, size = _ws(workspace)
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype)  # noqa: E731
+    param = lambda name, t: _vector(name, t, n.hidden, n.param_dtype)  # noqa: E731
+    _check(lib().compass_layer_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), param("gamma", gamma), _vector("mean", mean, n.M),
+                                             _vector("rstd", rstd, n.M), rows("dsum", dsum), rows("dX", dX), param("dgamma", dgamma),
+                                             param("dbeta", dbeta), p, size, _stream_handle(stream)), "compass_layer_norm_backward")
 
 
 def compass_decomp(problem: Problem, A: Sequence, B: Sequence, out: Sequence, workspace, stream_compute=None,

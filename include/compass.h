@@ -411,6 +411,37 @@ int compass_layer_norm_backward(const compass_norm* norm, const void* const* dY,
                                 const float* mean, const float* rstd, const void* const* dsum, void* const* dX,
                                 void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Softmax cross entropy of the vocabulary-parallel output layer, without the
+ * logits: z = logit_scale * X * W^T exists only tile by tile.
+ *   lse_i  = log sum_v exp(z_iv)
+ *   loss_i = lse_i - (1 - e) * z_i,target - (e / vocab) * sum_v z_iv,   e = label_smoothing
+ * A target outside [0, vocab) marks a row that takes no part: its loss, lse and
+ * dX are zero, it costs no products, and nothing in its X (not even NaN) reaches
+ * a result.  X, W: BF16, hidden % 8 == 0; products accumulate in FP32. */
+typedef struct compass_head {
+  int32_t P;
+  int32_t dtype;        /* COMPASS_DTYPE_BF16 */
+  int32_t grad_dtype;   /* of dW: BF16 or FP32 */
+  int32_t index_dtype;  /* of targets */
+  int64_t M, hidden, vocab;
+  float logit_scale;
+  float label_smoothing;   /* in [0, 1) */
+} compass_head;
+/* backward = 0 / 1: workspace of compass_head_loss / compass_head_loss_backward
+ * (256-byte aligned, zeroed once with compass_workspace_init; afterwards
+ * compass_read_status reports a bounded wait that gave up). */
+int compass_head_workspace_bytes(const compass_head* head, int backward, size_t* bytes);
+/* loss, lse: M FP32 values each. */
+int compass_head_loss(const compass_head* head, const void* const* X, const void* const* W, const void* targets, float* loss,
+                      float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* lse: what the forward call wrote; dloss: gradient of every token's loss (M
+ * FP32 values).  dX[r] = [M/P x hidden] and dW[r] are written whole.  The logits
+ * are computed again, in pieces of the vocabulary whose gradient (BF16, scaled by
+ * dloss / max|dloss|) fits the workspace; sums are FP32, rounded once. */
+int compass_head_loss_backward(const compass_head* head, const void* const* X, const void* const* W, const void* targets,
+                               const float* lse, const float* dloss, void* const* dX, void* const* dW, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream);
+
 /* ---- models, individually (host) ----------------------------------------- */
 /* Eq. 2-3: (d-1)*max(T_comp,T_comm)/d*(alpha+beta*d) + T_comp/d + T_comm/d. */
 int compass_model_decomp_time(double t_comp, double t_comm, double alpha, double beta, int d, double* out);

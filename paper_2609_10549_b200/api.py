@@ -42,6 +42,7 @@ EXPORTS = (
     "compass_mlp_workspace_bytes", "compass_mlp_block", "compass_noalloc_read_status", "compass_select_ex", "compass_test_drop_flag_writes", "compass_tensor_map_cache_stats", "compass_decomp_comm", "compass_tile_plan",
     "compass_embedding", "compass_embedding_workspace_bytes", "compass_embedding_backward",
     "compass_layer_norm", "compass_layer_norm_workspace_bytes", "compass_layer_norm_backward",
+    "compass_head_workspace_bytes", "compass_head_loss", "compass_head_loss_backward",
 )
 
 
@@ -71,6 +72,12 @@ class Embed(C.Structure):
 class Norm(C.Structure):
     _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("param_dtype", C.c_int32), ("eps", C.c_float),
                 ("M", C.c_int64), ("hidden", C.c_int64)]
+
+
+class Head(C.Structure):
+    _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("index_dtype", C.c_int32),
+                ("M", C.c_int64), ("hidden", C.c_int64), ("vocab", C.c_int64), ("logit_scale", C.c_float),
+                ("label_smoothing", C.c_float)]
 
 
 class SchedEntry(C.Structure):
@@ -145,6 +152,9 @@ def lib() -> C.CDLL:
         L.compass_layer_norm.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, pp, pp, vp, vp, vp]
         L.compass_layer_norm_workspace_bytes.argtypes = [C.POINTER(Norm), C.POINTER(C.c_size_t)]
         L.compass_layer_norm_backward.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, vp, pp, pp, vp, vp, vp, C.c_size_t, vp]
+        L.compass_head_workspace_bytes.argtypes = [C.POINTER(Head), C.c_int, C.POINTER(C.c_size_t)]
+        L.compass_head_loss.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.compass_head_loss_backward.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, pp, pp, vp, C.c_size_t, vp]
         L.compass_set_wait_limit_us.argtypes = [C.c_uint32]
         L.compass_test_drop_flag_writes.argtypes = [C.c_int]
         L.compass_tensor_map_cache_stats.argtypes = [C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
@@ -369,7 +379,7 @@ def compass_mlp_block(mlp: Mlp, X: Sequence, W0: Sequence, H: Sequence, W1: Sequ
                                    _ptr_array(Out), p, n, _stream_handle(stream)), "compass_mlp_block")
 
 
-# ---- around the blocks: embedding, layer norm ------------------------------------------
+# ---- around the blocks: embedding, layer norm, output-layer loss -------------------
 #
 # These take torch tensors and check type, shape and layout before the library sees the addresses
 # (ValueError); what the library itself refuses raises CompassError.
@@ -500,6 +510,44 @@ def compass_layer_norm_backward(norm: Norm, dY: Sequence, X: Sequence, gamma, me
     _check(lib().compass_layer_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), param("gamma", gamma), _vector("mean", mean, n.M),
                                              _vector("rstd", rstd, n.M), rows("dsum", dsum), rows("dX", dX), param("dgamma", dgamma),
                                              param("dbeta", dbeta), p, size, _stream_handle(stream)), "compass_layer_norm_backward")
+
+
+def make_head(P: int, M: int, hidden: int, vocab: int, logit_scale: float = 1.0, label_smoothing: float = 0.0, dtype: int = DTYPE_BF16,
+              grad_dtype: Optional[int] = None, index_dtype: int = INDEX_INT64) -> Head:
+    return Head(P=P, dtype=dtype, grad_dtype=dtype if grad_dtype is None else grad_dtype, index_dtype=index_dtype, M=M, hidden=hidden,
+                vocab=vocab, logit_scale=logit_scale, label_smoothing=label_smoothing)
+
+
+def compass_head_workspace_bytes(head: Head, backward: bool = False) -> int:
+    n = C.c_size_t(0)
+    _check(lib().compass_head_workspace_bytes(C.byref(head), int(backward), C.byref(n)), "compass_head_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_head_workspace(head: Head, backward: bool = False, device="cuda"):
+    return _sized_workspace(compass_head_workspace_bytes(head, backward), device)
+
+
+def compass_head_loss(head: Head, X: Sequence, W: Sequence, targets, loss, lse, workspace, stream=None) -> None:
+    """Cross entropy of every token and its log-sum-exp, without the logits; targets outside the vocabulary take no part."""
+    h = head
+    p, n = _ws(workspace)
+    _check(lib().compass_head_loss(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype),
+                                   _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype), _index("targets", targets, h.index_dtype, h.M),
+                                   _vector("loss", loss, h.M), _vector("lse", lse, h.M), p, n, _stream_handle(stream)), "compass_head_loss")
+
+
+def compass_head_loss_backward(head: Head, X: Sequence, W: Sequence, targets, lse, dloss, dX: Sequence, dW: Sequence, workspace,
+                               stream=None) -> None:
+    """dX and dW from the gradient of every token's loss; the logits are computed again in pieces of the vocabulary."""
+    h = head
+    p, n = _ws(workspace)
+    _check(lib().compass_head_loss_backward(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype),
+                                            _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype),
+                                            _index("targets", targets, h.index_dtype, h.M), _vector("lse", lse, h.M),
+                                            _vector("dloss", dloss, h.M), _row_shards("dX", dX, h.P, h.M, h.hidden, h.dtype),
+                                            _vocab_shards("dW", dW, h.P, h.vocab, h.hidden, h.grad_dtype), p, n, _stream_handle(stream)),
+           "compass_head_loss_backward")
 
 
 def compass_decomp(problem: Problem, A: Sequence, B: Sequence, out: Sequence, workspace, stream_compute=None,

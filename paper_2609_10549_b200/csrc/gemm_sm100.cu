@@ -1423,6 +1423,10 @@ int device_info(DeviceInfo** out) {
 
 }  // namespace
 
+bool encode_tensor_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows) {
+  return encode_kmajor(map, ptr, rows, cols, box_rows);
+}
+
 void tensor_map_cache_stats(uint64_t* hits, uint64_t* misses) {
   *hits = g_map_hits.load(std::memory_order_relaxed);
   *misses = g_map_misses.load(std::memory_order_relaxed);

@@ -1,0 +1,1168 @@
+// Softmax cross entropy of the vocabulary-parallel output layer, forward and
+// backward, without the logits.
+//
+// Rows whose target lies outside the vocabulary take no part: head_rows_kernel
+// lists the others and head_gather_kernel copies them together, so that the
+// products run over real rows only, whatever the mask and the ranks' shards.
+// Then one kernel in four forms (tcgen05 products of BF16 with FP32 sums):
+//   STATS  logits of 256 vocabulary columns at a time; what leaves the epilogue
+//          is each row's maximum and sum of exponentials over 128 columns
+//   GRAD   the same product again; the epilogue writes the logits' gradient
+//          (BF16) of one piece of the vocabulary
+//   DX     that piece times the table: added to the FP32 sums of dX
+//   DW     that piece, transposed, times X: dW of the piece
+// The backward pass is bound by the tensor cores: 6 M hidden vocab operations.
+//
+// Tiles are computed by pairs of CTAs: 512 x 256 as long as they fill whole
+// rounds of the pairs (two accumulators that share one tile of B: 48 bytes of
+// operands per SM and clock at the tensor cores' full rate, against 64 for
+// 256 x 256), 256 x 256 for the rest.  Warp 0 loads (TMA), warp 1 issues the
+// products, warps 2..9 are the epilogue: two per quarter of the rows, 128
+// columns each, so that a whole accumulator is in registers, and its tensor
+// memory free again, before the exponentials begin.
+#include <mutex>
+
+#include "ptx_sm100.cuh"
+#include "row_ops.cuh"
+
+namespace compass {
+
+using namespace ptx;
+
+namespace {
+
+enum Form : int { STATS = 0, GRAD = 1, DX = 2, DW = 3 };
+
+constexpr int kThreads = 320;
+constexpr int kEpiWarps = 8;
+constexpr int kSlots = 4;
+constexpr int kChunkBytes = 128 * BK * 2;       // 16 KB: 128 rows (or columns) of one 64-wide k-atom
+constexpr int kHalfChunk = kChunkBytes / 2;     // an MN-major operand is two boxes of 64 columns x 64 k-rows
+constexpr int kChunks = 12;
+constexpr int kStageRow = 64 + 16;              // epilogue staging: 64 bytes of a row, padded
+constexpr int kStageWarp = 32 * kStageRow;
+constexpr int kGroup = 8;                       // row tiles that go through the columns together (their A stays in L2)
+constexpr int kSkew = 3;                        // stages at a tile's ends in which accumulator 0 runs ahead
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// 2^x, relative error 2^-22; results below 2^-126 are zero (of a sum that is at least 1, or of a BF16 gradient).
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// What the kernels before the products found out.
+struct Found {
+  int32_t rows;      // that take part
+  float top;         // max |dloss| over them (1 if that is not finite)
+};
+
+struct HeadParams {
+  CUtensorMap x_k;              // gathered X [pad][hidden]: boxes of 128 rows (A of the logits)
+  CUtensorMap x_mn;             // boxes of 64 rows (B of dW)
+  CUtensorMap d_k, d_mn;        // the piece's gradient [pad][piece_cols]: A of dX; A of dW
+  CUtensorMap w_k[kMaxP], w_mn[kMaxP];
+  void* dw[kMaxP];
+  const Found* found;
+  const int32_t* target;        // of the gathered rows
+  const float* lse2;            // in units of log 2
+  const float* weight;          // dloss of the gathered rows
+  float2* part;                 // [2 * vocab tiles][pad] (maximum, sum), in units of log 2
+  float* part_sum;              // [2 * vocab tiles][pad] sum of logits (label smoothing)
+  float* target_logit;          // [pad]
+  __nv_bfloat16* d;             // the piece's gradient
+  float4* acc;                  // FP32 sums of dX, in the order the epilogue's lanes hold them
+  StatusBlock* status;
+  int64_t hidden;
+  int32_t pad;                  // rows of the workspace's arrays, a multiple of 512
+  int32_t vocab_rows;           // rows per shard
+  int32_t vocab;
+  int32_t tiles_per_shard;
+  int32_t vt0, n_vt;            // the piece: vocabulary tiles [vt0, vt0 + n_vt)
+  int32_t piece_cols;           // row pitch of d
+  int32_t hidden_tiles;
+  int32_t splits;               // of dX's contraction
+  int32_t first_piece;
+  int32_t grad_fp32;
+  float z_scale;                // logit_scale * log2(e)
+  float out_scale;              // logit_scale
+  float smoothing, uniform;     // label_smoothing, label_smoothing / vocab
+  uint32_t wait_limit_us;
+};
+
+struct Control {
+  uint64_t full[kSlots], empty[kSlots];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t drain;
+  uint32_t tmem_base;
+  int abort;
+};
+
+constexpr size_t kSmemBytes = 1024 + size_t(kChunks) * kChunkBytes + sizeof(Control) + 16 + size_t(kEpiWarps) * kStageWarp;
+
+enum Site : int { SITE_EMPTY = 1, SITE_FULL = 2, SITE_ACC_EMPTY = 3, SITE_ACC_FULL = 4, SITE_DRAIN = 5 };
+
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Control* ctl, const HeadParams& p, int site, int tile) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  const uint64_t limit = uint64_t(p.wait_limit_us) * 1000ull;
+  for (uint32_t spins = 1; spins < (1u << 30); ++spins) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((spins & 0xFF) == 0) {
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) return false;
+      if (globaltimer_ns() - t0 > limit) break;
+    }
+  }
+  *reinterpret_cast<volatile int*>(&ctl->abort) = 1;
+  if (atomicCAS(&p.status->code, 0, int(COMPASS_ERR_TIMEOUT)) == 0) {
+    p.status->detail = site;
+    p.status->block_idx = int(blockIdx.x);
+    p.status->tile = tile;
+  }
+  return false;
+}
+
+// How a form's output is cut into tiles; the number of rows is known on the device only.
+struct Plan {
+  int big_rows;        // row tiles of 512
+  int odd;             // one more of 256
+  int cols;            // column tiles (of all splits)
+  int n_big, left;     // 512 x 256 tiles; slots left over, two 256 x 256 tiles each
+  int total;
+  int atoms;           // 64-wide k-atoms of a tile (an even number)
+};
+template <int kForm>
+__device__ __forceinline__ Plan make_plan(const HeadParams& p, int units) {
+  Plan q;
+  const int found = max(p.found->rows, 1);      // at least one tile: its zeros are what dW reads when no row takes part
+  const int halves = kForm == DW ? p.n_vt : (found + 255) / 256;
+  q.big_rows = halves / 2;
+  q.odd = halves & 1;
+  q.cols = kForm == DW ? p.hidden_tiles : kForm == DX ? p.hidden_tiles * p.splits : p.n_vt;
+  const int slots = q.big_rows * q.cols;
+  q.n_big = slots / units * units;
+  q.left = slots - q.n_big;
+  q.total = q.n_big + 2 * q.left + q.odd * q.cols;
+  q.atoms = kForm == DW ? (found + 127) / 128 * 2 : kForm == DX ? 4 * p.n_vt : int((p.hidden + 127) / 128) * 2;
+  return q;
+}
+struct Tile {
+  bool big;
+  int row0;            // first of 512 or 256 rows
+  int col;             // column tile
+  int atom0, atoms;    // range of the contraction
+};
+template <int kForm>
+__device__ __forceinline__ Tile tile_of(const HeadParams& p, const Plan& q, int t) {
+  Tile c;
+  c.big = t < q.n_big;
+  int slot = t, half = 0;
+  const int u = t - q.n_big;
+  if (!c.big && u >= 2 * q.left) {
+    c.row0 = q.big_rows * 512;
+    c.col = u - 2 * q.left;
+  } else {
+    if (!c.big) {
+      slot = q.n_big + (u >> 1);
+      half = u & 1;
+    }
+    const int g = slot / (kGroup * q.cols);
+    const int rest = slot - g * (kGroup * q.cols);
+    const int wide = min(kGroup, q.big_rows - g * kGroup);
+    c.col = rest / wide;
+    c.row0 = (g * kGroup + rest - c.col * wide) * 512 + half * 256;
+  }
+  c.atom0 = 0;
+  c.atoms = q.atoms;
+  if (kForm == DX && p.splits > 1) {
+    // whole vocabulary tiles (4 atoms) per split
+    const int s = c.col / p.hidden_tiles;
+    const int from = int(int64_t(p.n_vt) * s / p.splits), to = int(int64_t(p.n_vt) * (s + 1) / p.splits);
+    c.atom0 = 4 * from;
+    c.atoms = 4 * (to - from);
+  }
+  return c;
+}
+
+// This CTA's 128 rows of A of one k-atom.
+template <int kForm>
+__device__ __forceinline__ void load_a(const HeadParams& p, uint8_t* dst, uint32_t bar, int row, int atom, uint64_t pol) {
+  if (kForm == DW) {
+    tma_load_2d_pair_hint(dst, &p.d_mn, bar, row, atom * BK, pol);
+    tma_load_2d_pair_hint(dst + kHalfChunk, &p.d_mn, bar, row + 64, atom * BK, pol);
+  } else {
+    tma_load_2d_pair_hint(dst, kForm == DX ? &p.d_k : &p.x_k, bar, atom * BK, row, pol);
+  }
+}
+// This CTA's 128 columns of B of one k-atom.
+template <int kForm>
+__device__ __forceinline__ void load_b(const HeadParams& p, uint8_t* dst, uint32_t bar, int col_tile, int cta, int atom, uint64_t pol) {
+  if (kForm == DW) {
+    const int col = col_tile * 256 + cta * 128;
+    tma_load_2d_pair_hint(dst, &p.x_mn, bar, col, atom * BK, pol);
+    tma_load_2d_pair_hint(dst + kHalfChunk, &p.x_mn, bar, col + 64, atom * BK, pol);
+  } else if (kForm == DX) {
+    const int col = (p.splits > 1 ? col_tile % p.hidden_tiles : col_tile) * 256 + cta * 128;
+    const int vt = p.vt0 + (atom >> 2);
+    const int shard = vt / p.tiles_per_shard;
+    const int row = (vt - shard * p.tiles_per_shard) * 256 + (atom & 3) * BK;
+    tma_load_2d_pair_hint(dst, &p.w_mn[shard], bar, col, row, pol);
+    tma_load_2d_pair_hint(dst + kHalfChunk, &p.w_mn[shard], bar, col + 64, row, pol);
+  } else {
+    const int vt = p.vt0 + col_tile;
+    const int shard = vt / p.tiles_per_shard;
+    tma_load_2d_pair_hint(dst, &p.w_k[shard], bar, atom * BK, (vt - shard * p.tiles_per_shard) * 256 + cta * 128, pol);
+  }
+}
+
+// Vocabulary columns that exist in a tile.
+__device__ __forceinline__ int vocab_cols(const HeadParams& p, int vt, int* shard, int* row) {
+  *shard = vt / p.tiles_per_shard;
+  *row = (vt - *shard * p.tiles_per_shard) * 256;
+  const int64_t rows = min(int64_t(p.vocab_rows), int64_t(p.vocab) - int64_t(*shard) * p.vocab_rows);
+  return int(min(int64_t(256), rows - *row));
+}
+
+template <int kForm>
+__global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant__ HeadParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  Control* ctl = reinterpret_cast<Control*>(smem + kChunks * kChunkBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t cta = cluster_ctarank();
+  const bool leader = cta == 0;
+  const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->acc_full[b], 1);
+      mbar_init(&ctl->acc_empty[b], 2 * kEpiWarps);
+    }
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&ctl->tmem_base, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl->tmem_base;
+  launch_dependents();
+  wait_for_previous_kernel();
+  const Plan plan = make_plan<kForm>(p, units);
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      uint32_t j = 0;          // stages so far
+      int chunk = 0;           // ring cursor
+      bool ok = true;
+      for (int t = unit; ok && t < plan.total; t += units) {
+        const Tile tile = tile_of<kForm>(p, plan, t);
+        const int row = tile.row0 + int(cta) * (tile.big ? 256 : 128);
+        const int step = tile.big ? 1 : 2;
+        for (int a = 0; a < tile.atoms; a += step, ++j) {
+          // A 512x256 stage (3 chunks) follows only stages of its own kind: four of them fill the ring.  A 256x256 stage
+          // (4 chunks) overwrites nothing newer than the third stage before it.
+          const uint32_t depth = tile.big ? 4u : 3u;
+          if (j >= depth) {
+            const uint32_t r = j - depth;
+            if (!wait_bar(&ctl->empty[r & 3u], (r >> 2) & 1u, ctl, p, SITE_EMPTY, t)) {
+              ok = false;
+              break;
+            }
+          }
+          const uint32_t slot = j & 3u;
+          const uint32_t bar = map_to_cta(smem_u32(&ctl->full[slot]), 0);
+          const int n = tile.big ? 3 : 4;
+          if (leader) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * kChunkBytes));
+          uint8_t* c[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c[i] = smem + ((chunk + i) % kChunks) * kChunkBytes;
+          const int atom = tile.atom0 + a;
+          if (tile.big) {
+            load_a<kForm>(p, c[0], bar, row, atom, pol);
+            load_a<kForm>(p, c[1], bar, row + 128, atom, pol);
+            load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
+          } else {
+            load_a<kForm>(p, c[0], bar, row, atom, pol);
+            load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
+            load_a<kForm>(p, c[1], bar, row, atom + 1, pol);
+            load_b<kForm>(p, c[3], bar, tile.col, int(cta), atom + 1, pol);
+          }
+          chunk = (chunk + n) % kChunks;
+        }
+      }
+      // leave only when the last stages have been read (the leader's products read both CTAs' chunks)
+      const uint32_t back = j < 4u ? j : 4u;
+      for (uint32_t i = 1; i <= back; ++i) {
+        const uint32_t r = j - i;
+        if (!wait_bar(&ctl->empty[r & 3u], (r >> 2) & 1u, ctl, p, SITE_DRAIN, -1)) break;
+      }
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- MMA issuer
+    if (leader && lane == 0) {
+      constexpr bool kAMn = kForm == DW, kBMn = kForm == DW || kForm == DX;
+      constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | (kAMn ? kUmmaIdescAMnMajor : 0u) | (kBMn ? kUmmaIdescBMnMajor : 0u);
+      const uint64_t desc_k = umma_smem_desc_sw128(smem_u32(smem));
+      const uint64_t desc_mn = umma_smem_desc_sw128_mn(smem_u32(smem), kHalfChunk);
+      const uint64_t desc_a = kAMn ? desc_mn : desc_k, desc_b = kBMn ? desc_mn : desc_k;
+      constexpr uint64_t ak = kAMn ? 2048 >> 4 : 2, bk = kBMn ? 2048 >> 4 : 2;     // address step of 16 k-elements
+      uint32_t j = 0, uses[2] = {0, 0}, small = 0;
+      int chunk = 0;
+      auto at = [&](uint64_t base, int c) { return base + uint64_t(((c % kChunks) * kChunkBytes) >> 4); };
+      auto issue = [&](uint32_t acc, int a_chunk, int b_chunk, uint32_t first) {
+        const uint64_t da = at(desc_a, a_chunk), db = at(desc_b, b_chunk);
+#pragma unroll
+        for (int k = 0; k < BK / UMMA_K; ++k) umma_bf16_pair(acc, da + k * ak, db + k * bk, idesc, k ? 1u : first);
+      };
+      auto acc_free = [&](int b, int t) {
+        if (!wait_bar(&ctl->acc_empty[b], (uses[b] & 1u) ^ 1u, ctl, p, SITE_ACC_EMPTY, t)) return false;
+        tc_fence_after_sync();
+        return true;
+      };
+      auto landed = [&](uint32_t s, int t) {
+        if (!wait_bar(&ctl->full[s & 3u], (s >> 2) & 1u, ctl, p, SITE_FULL, t)) return false;
+        tc_fence_after_sync();
+        return true;
+      };
+      bool ok = true;
+      for (int t = unit; ok && t < plan.total; t += units) {
+        const Tile tile = tile_of<kForm>(p, plan, t);
+        if (tile.big) {
+          // Both accumulators are live for the whole tile, so nothing would hide the epilogue's reads if they ended
+          // together: for the first and last kSkew stages accumulator 0's products go first.  It is then complete early
+          // (its epilogue runs under accumulator 1's last products), and the next tile begins on it while accumulator 1
+          // is still being read.
+          const int n = tile.atoms;
+          const int skew = n >= 2 * kSkew ? kSkew : 0;
+          auto skewed = [&](int kb, bool begin) {
+            for (int s = 0; s < kSkew; ++s) {
+              if (!landed(j + s, t)) return false;
+              issue(tmem_base, chunk + 3 * s, chunk + 3 * s + 2, (kb + s) != 0 ? 1u : 0u);
+            }
+            if (begin) {
+              if (!acc_free(1, t)) return false;
+            } else {
+              umma_commit_pair(&ctl->acc_full[0], 0x3);
+            }
+            for (int s = 0; s < kSkew; ++s) {
+              issue(tmem_base + 256, chunk + 3 * s + 1, chunk + 3 * s + 2, (kb + s) != 0 ? 1u : 0u);
+              umma_commit_pair(&ctl->empty[(j + s) & 3u], 0x3);
+            }
+            j += kSkew;
+            chunk = (chunk + 3 * kSkew) % kChunks;
+            return true;
+          };
+          ok = acc_free(0, t);
+          if (ok) ok = skew ? skewed(0, true) : acc_free(1, t);
+          for (int kb = skew; ok && kb < n - skew; ++kb, ++j) {
+            if (!(ok = landed(j, t))) break;
+            const uint64_t a0 = at(desc_a, chunk), a1 = at(desc_a, chunk + 1), b = at(desc_b, chunk + 2);
+            const uint32_t first = kb != 0 ? 1u : 0u;
+#pragma unroll
+            for (int k = 0; k < BK / UMMA_K; ++k) {
+              umma_bf16_pair(tmem_base, a0 + k * ak, b + k * bk, idesc, k ? 1u : first);
+              umma_bf16_pair(tmem_base + 256, a1 + k * ak, b + k * bk, idesc, k ? 1u : first);
+            }
+            chunk = (chunk + 3) % kChunks;
+            umma_commit_pair(&ctl->empty[j & 3u], 0x3);
+          }
+          if (ok && skew) ok = skewed(n - skew, false);
+          else if (ok) umma_commit_pair(&ctl->acc_full[0], 0x3);
+          if (!ok) break;
+          umma_commit_pair(&ctl->acc_full[1], 0x3);
+          ++uses[0];
+          ++uses[1];
+        } else {
+          const int b = int(small & 1u);
+          if (!(ok = acc_free(b, t))) break;
+          for (int a = 0; a < tile.atoms; a += 2, ++j) {
+            if (!(ok = landed(j, t))) break;
+            issue(tmem_base + b * 256, chunk, chunk + 2, a != 0 ? 1u : 0u);
+            issue(tmem_base + b * 256, chunk + 1, chunk + 3, 1u);
+            chunk = (chunk + 4) % kChunks;
+            umma_commit_pair(&ctl->empty[j & 3u], 0x3);
+          }
+          if (!ok) break;
+          umma_commit_pair(&ctl->acc_full[b], 0x3);
+          ++uses[b];
+          ++small;
+        }
+      }
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+        // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
+        umma_commit_pair(&ctl->drain, 0x1);
+        wait_bar(&ctl->drain, 0, ctl, p, SITE_DRAIN, -2);
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* stage = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ctl + 1) + 15) & ~uintptr_t(15)) + (warp - 2) * kStageWarp;
+    const int rows = p.found->rows;
+    float out_scale = p.out_scale;
+    if (kForm == DW) out_scale *= p.found->top;
+    const float top_weight = kForm == GRAD ? p.found->top : 1.f;
+    uint32_t uses[2] = {0, 0}, small = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < plan.total; t += units) {
+      const Tile tile = tile_of<kForm>(p, plan, t);
+      for (int a = 0; a < (tile.big ? 2 : 1); ++a) {
+        const int b = tile.big ? a : int(small & 1u);
+        const int frag0 = tile.row0 + (tile.big ? int(cta) * 256 + a * 128 : int(cta) * 128);    // this CTA's 128 rows
+        const int row = frag0 + quarter * 32 + lane;
+        int target = -1;
+        float lse2 = 0.f, w = 0.f;
+        if (kForm == STATS || kForm == GRAD) {
+          if (row < rows) {
+            target = p.target[row];
+            if (kForm == GRAD) {
+              lse2 = p.lse2[row];
+              w = p.weight[row] / top_weight;
+            }
+          }
+        }
+        if (!(ok = wait_bar(&ctl->acc_full[b], uses[b] & 1u, ctl, p, SITE_ACC_FULL, t))) break;
+        tc_fence_after_sync();
+        uint32_t v[4][32];
+        const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(taddr + c * 32, v[c]);
+        tmem_ld_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+        ++uses[b];
+
+        if (kForm == STATS || kForm == GRAD) {
+          int shard, vrow;
+          const int cols = vocab_cols(p, p.vt0 + tile.col, &shard, &vrow) - half * 128;      // of this thread's 128
+          const int hit = target - (shard * p.vocab_rows + vrow + half * 128);               // the target among them?
+          const bool mine = target >= 0 && hit >= 0 && hit < min(cols, 128);
+          const bool any = __any_sync(0xffffffffu, mine);
+          if (kForm == STATS) {
+            float m = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                float z = __uint_as_float(v[c][i]) * p.z_scale;
+                if (cols < 128 && c * 32 + i >= cols) z = -INFINITY;
+                else if (p.smoothing != 0.f) sum += z;
+                v[c][i] = __float_as_uint(z);
+                m = fmaxf(m, z);
+              }
+            const float top = m == -INFINITY ? 0.f : m;
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) s[i & 3] += exp2_fast(__uint_as_float(v[c][i]) - top);
+            if (any) {
+              float z = 0.f;
+#pragma unroll
+              for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (hit == c * 32 + i) z = __uint_as_float(v[c][i]);
+              if (mine) p.target_logit[row] = z;
+            }
+            if (row < rows) {
+              const int64_t at = int64_t(2 * (p.vt0 + tile.col) + half) * p.pad + row;
+              p.part[at] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
+              if (p.smoothing != 0.f) p.part_sum[at] = sum;
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                float d = (exp2_fast(fmaf(__uint_as_float(v[c][i]), p.z_scale, -lse2)) - p.uniform) * w;
+                if (row >= rows || (cols < 128 && c * 32 + i >= cols)) d = 0.f;
+                v[c][i] = __float_as_uint(d);
+              }
+            if (any) {
+              const float off = (1.f - p.smoothing) * w;
+#pragma unroll
+              for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (mine && hit == c * 32 + i) v[c][i] = __float_as_uint(__uint_as_float(v[c][i]) - off);
+            }
+            __nv_bfloat16* out = p.d + int64_t(frag0 + quarter * 32) * p.piece_cols + tile.col * 256 + half * 128;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint4* srow = reinterpret_cast<uint4*>(stage + lane * kStageRow);
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const uint32_t* q = &v[c][g * 8];
+                srow[g] = make_uint4(pack_bf16x2(__uint_as_float(q[0]), __uint_as_float(q[1])), pack_bf16x2(__uint_as_float(q[2]), __uint_as_float(q[3])),
+                                     pack_bf16x2(__uint_as_float(q[4]), __uint_as_float(q[5])), pack_bf16x2(__uint_as_float(q[6]), __uint_as_float(q[7])));
+              }
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2);
+                *reinterpret_cast<uint4*>(out + int64_t(r) * p.piece_cols + c * 32 + (lane & 3) * 8) =
+                    *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
+              }
+              __syncwarp();
+            }
+          }
+        } else if (kForm == DX) {
+          // sums in the order the lanes hold them: 32 groups of 4 columns per warp, each group the lanes' 16 bytes in a row
+          const int64_t frag = (int64_t(frag0 >> 7) * plan.cols + tile.col) * 8 + quarter * 2 + half;
+          float4* sum = p.acc + frag * (32 * 32) + lane;
+          if (tile.atoms == 0) continue;      // a last piece of fewer vocabulary tiles than splits: nothing to add
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float4 old[8];
+            if (!p.first_piece) {
+#pragma unroll
+              for (int g = 0; g < 8; ++g) old[g] = __ldcg(sum + (c * 8 + g) * 32);
+            }
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              float4 x = make_float4(__uint_as_float(v[c][g * 4]), __uint_as_float(v[c][g * 4 + 1]), __uint_as_float(v[c][g * 4 + 2]),
+                                     __uint_as_float(v[c][g * 4 + 3]));
+              if (!p.first_piece) {
+                x.x += old[g].x;
+                x.y += old[g].y;
+                x.z += old[g].z;
+                x.w += old[g].w;
+              }
+              sum[(c * 8 + g) * 32] = x;
+            }
+          }
+        } else {
+          // rows are vocabulary rows: this CTA's fragment lies in one vocabulary tile
+          int shard, vrow;
+          const int vt_rows = vocab_cols(p, p.vt0 + (frag0 >> 8), &shard, &vrow);
+          const int in_tile = (frag0 & 255) + quarter * 32;
+          const int live = vt_rows - in_tile;                     // rows of this warp that exist
+          const int64_t first = int64_t(vrow) + in_tile;
+          const int col0 = tile.col * 256 + half * 128;
+          const int per = p.grad_fp32 ? 16 : 32;                  // columns in 64 bytes
+          const int passes = p.grad_fp32 ? 8 : 4;
+          uint8_t* out = static_cast<uint8_t*>(p.dw[shard]);
+          const int64_t pitch = p.hidden * (p.grad_fp32 ? 4 : 2);
+#pragma unroll
+          for (int pass = 0; pass < 8; ++pass) {
+            if (pass < passes) {
+              uint4* srow = reinterpret_cast<uint4*>(stage + lane * kStageRow);
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                float x[8];
+                if (p.grad_fp32) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[pass >> 1][(pass & 1) * 16 + g * 4 + i]) * out_scale;
+                  srow[g] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[pass & 3][g * 8 + i]) * out_scale;
+                  srow[g] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+                }
+              }
+              __syncwarp();
+              const int col = col0 + pass * per + (lane & 3) * (per / 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2);
+                if (r < live && col < p.hidden)
+                  *reinterpret_cast<uint4*>(out + (first + r) * pitch + int64_t(col) * (p.grad_fp32 ? 4 : 2)) =
+                      *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
+              }
+              __syncwarp();
+            }
+          }
+        }
+      }
+      if (!tile.big) ++small;
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---- which rows take part ------------------------------------------------------
+
+struct RowParams {
+  const void* targets;
+  const float* lse;         // backward
+  const float* dloss;
+  float* loss_out;          // forward: zeros for the others
+  float* lse_out;
+  Found* found;
+  int32_t* place;           // [M] place among the gathered rows, or -1
+  int32_t* origin;          // [pad] row that a gathered one comes from
+  int32_t* target;
+  float* lse2;
+  float* weight;
+  uint32_t M;
+  int32_t vocab;
+  int32_t wide;
+};
+
+constexpr int kRowItems = 4;
+__global__ void __launch_bounds__(1024, 1) head_rows_kernel(const __grid_constant__ RowParams p) {
+  __shared__ uint32_t counts[2][32];
+  __shared__ float tops[32];
+  launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t base = 0;
+  float top = 0.f;
+  bool bad = false;
+  for (uint32_t turn = 0, i0 = 0; i0 < p.M; i0 += 1024 * kRowItems, ++turn) {
+    // thread t takes kRowItems rows in a row, so that the order is kept
+    const uint32_t i = i0 + threadIdx.x * kRowItems;
+    int32_t target[kRowItems];
+    uint32_t n = 0;
+#pragma unroll
+    for (int k = 0; k < kRowItems; ++k) {
+      target[k] = -1;
+      if (i + k < p.M) {
+        const int64_t y = p.wide ? static_cast<const int64_t*>(p.targets)[i + k] : int64_t(static_cast<const int32_t*>(p.targets)[i + k]);
+        if (y >= 0 && y < p.vocab) {
+          target[k] = int32_t(y);
+          ++n;
+        }
+      }
+    }
+    uint32_t x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) counts[turn & 1][warp] = x;
+    __syncthreads();
+    uint32_t c = counts[turn & 1][lane], sum = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    uint32_t at = base + (x - n) + __shfl_sync(0xffffffffu, sum - c, warp);
+    base += __shfl_sync(0xffffffffu, sum, 31);
+#pragma unroll
+    for (int k = 0; k < kRowItems; ++k) {
+      if (i + k >= p.M) break;
+      if (target[k] < 0) {
+        p.place[i + k] = -1;
+        if (p.loss_out) p.loss_out[i + k] = 0.f;
+        if (p.lse_out) p.lse_out[i + k] = 0.f;
+        continue;
+      }
+      p.place[i + k] = int32_t(at);
+      p.origin[at] = int32_t(i + k);
+      p.target[at] = target[k];
+      if (p.dloss) {
+        const float g = p.dloss[i + k];
+        p.weight[at] = g;
+        p.lse2[at] = p.lse[i + k] * kLog2e;
+        top = fmaxf(top, fabsf(g));
+        bad |= !(fabsf(g) < INFINITY);
+      }
+      ++at;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  bad = __syncthreads_or(bad);
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 32; ++w) top = fmaxf(top, tops[w]);
+    p.found->rows = int32_t(base);
+    p.found->top = bad || top == 0.f ? 1.f : top;
+  }
+}
+
+struct GatherParams2 {
+  RowShards x, dx;
+  const Found* found;
+  const int32_t* place;
+  uint4* gathered;
+  uint32_t M;
+  uint32_t vecs;            // 16-byte vectors per row
+  int32_t zero_dx;
+};
+// The rows that take part, together; zeros behind them up to a multiple of 512 (dW contracts over these rows), and in the
+// dX of the others.
+__global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant__ GatherParams2 p) {
+  launch_dependents();
+  wait_for_previous_kernel();
+  const uint32_t rows = uint32_t(p.found->rows);
+  const uint32_t pad = (max(rows, 1u) + 511) / 512 * 512 - rows;
+  for (uint32_t i = blockIdx.x; i < p.M + pad; i += gridDim.x) {
+    const int32_t to = i < p.M ? p.place[i] : int32_t(rows + (i - p.M));
+    const uint4* from = i < p.M && to >= 0 ? p.x.row<uint4>(i, p.vecs) : nullptr;
+    uint4* out = to >= 0 ? p.gathered + int64_t(to) * p.vecs : p.zero_dx ? p.dx.row<uint4>(i, p.vecs) : nullptr;
+    if (out == nullptr) continue;
+    for (uint32_t c = threadIdx.x; c < p.vecs; c += 256) out[c] = from ? from[c] : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// ---- what the statistics say ---------------------------------------------------
+
+struct CombineParams {
+  const Found* found;
+  const int32_t* origin;
+  const float2* part;
+  const float* part_sum;
+  const float* target_logit;
+  float* loss;
+  float* lse;
+  int32_t parts, pad;
+  float smoothing, uniform;
+};
+// 32 rows per block, 32 threads a row.
+__global__ void __launch_bounds__(1024) head_combine_kernel(const __grid_constant__ CombineParams p) {
+  __shared__ float2 ms[32][33];
+  __shared__ float zs[32][33];
+  wait_for_previous_kernel();
+  const int rows = p.found->rows;
+  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
+  const int row = blockIdx.x * 32 + lane;
+  if (int(blockIdx.x) * 32 >= rows) return;
+  float m = -INFINITY, s = 0.f, z = 0.f;
+  if (row < rows) {
+#pragma unroll 4
+    for (int q = k; q < p.parts; q += 32) {
+      const float2 x = p.part[int64_t(q) * p.pad + row];
+      const float top = fmaxf(m, x.x);
+      // (no maximum: nothing but -inf, whose sum is 0, and NaN, whose sum is NaN)
+      if (top != -INFINITY) s = s * exp2f(m - top) + x.y * exp2f(x.x - top);
+      else s += x.y;
+      m = top;
+      if (p.smoothing != 0.f) z += p.part_sum[int64_t(q) * p.pad + row];
+    }
+  }
+  ms[k][lane] = make_float2(m, s);
+  zs[k][lane] = z;
+  __syncthreads();
+  if (k == 0 && row < rows) {
+    float top = -INFINITY;
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, ms[i][lane].x);
+    s = z = 0.f;
+    for (int i = 0; i < 32; ++i) {
+      s += top != -INFINITY ? ms[i][lane].y * exp2f(ms[i][lane].x - top) : ms[i][lane].y;
+      z += zs[i][lane];
+    }
+    const float lse2 = top + log2f(s);
+    const int to = p.origin[row];
+    p.lse[to] = lse2 * kLn2;
+    float l = lse2 - (1.f - p.smoothing) * p.target_logit[row];
+    if (p.smoothing != 0.f) l -= p.uniform * z;
+    p.loss[to] = l * kLn2;
+  }
+}
+
+// ---- dX from its FP32 sums -----------------------------------------------------
+
+struct FinishParams {
+  RowShards dx;
+  const Found* found;
+  const int32_t* origin;
+  const float4* acc;
+  int64_t hidden;
+  int32_t hidden_tiles, splits;
+  float out_scale;
+};
+// A block takes 32 gathered rows and 256 columns (what two warps of the products' epilogue hold).
+__global__ void __launch_bounds__(256) head_finish_kernel(const __grid_constant__ FinishParams p) {
+  __shared__ float tile[32][257];
+  wait_for_previous_kernel();
+  const int rows = p.found->rows;
+  const int row0 = blockIdx.x * 32;
+  if (row0 >= rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int cols = p.hidden_tiles * p.splits;
+  const float scale = p.out_scale * p.found->top;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int g = warp * 8 + i;                 // group of 4 columns among the tile's 64
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < p.splits; ++s) {
+      const int64_t frag = (int64_t(row0 >> 7) * cols + s * p.hidden_tiles + blockIdx.y) * 8 + ((row0 >> 5) & 3) * 2 + (g >> 5);
+      const float4 y = p.acc[frag * (32 * 32) + (g & 31) * 32 + lane];
+      x.x += y.x;
+      x.y += y.y;
+      x.z += y.z;
+      x.w += y.w;
+    }
+    tile[lane][g * 4] = x.x * scale;
+    tile[lane][g * 4 + 1] = x.y * scale;
+    tile[lane][g * 4 + 2] = x.z * scale;
+    tile[lane][g * 4 + 3] = x.w * scale;
+  }
+  __syncthreads();
+  for (int r = warp; r < 32 && row0 + r < rows; r += 8) {
+    const int64_t c = int64_t(blockIdx.y) * 256 + lane * 8;
+    if (c < p.hidden) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = tile[r][lane * 8 + i];
+      store_vec(p.dx.row<__nv_bfloat16>(uint32_t(p.origin[row0 + r]), p.hidden) + c, x);
+    }
+  }
+}
+
+// ---- host ----------------------------------------------------------------------
+
+int check_head(const compass_head* h) {
+  if (h == nullptr) return COMPASS_ERR_INVALID_ARG;
+  int st = check_rows(h->P, h->M, h->hidden);
+  if (st != COMPASS_OK) return st;
+  if (h->vocab <= 0) return COMPASS_ERR_SHAPE;
+  if (h->vocab > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  if (h->index_dtype != COMPASS_INDEX_INT64 && h->index_dtype != COMPASS_INDEX_INT32) return COMPASS_ERR_INVALID_ARG;
+  st = check_dtype(h->dtype, false);
+  if (st == COMPASS_OK) st = check_dtype(h->grad_dtype, true);
+  if (st != COMPASS_OK) return st;
+  if (!(h->label_smoothing >= 0.f && h->label_smoothing < 1.f)) return COMPASS_ERR_INVALID_ARG;
+  if (!(h->logit_scale - h->logit_scale == 0.f)) return COMPASS_ERR_INVALID_ARG;      // not finite
+  return h->hidden % 8 == 0 ? COMPASS_OK : COMPASS_ERR_ALIGNMENT;
+}
+
+// Pairs of CTAs that a launch counts on (one CTA per SM of the B200's 148); fewer co-resident ones only take more rounds.
+constexpr int kPairs = 74;
+// Bytes of the logits' gradient that are held at a time.
+constexpr int64_t kPieceBytes = int64_t(256) << 20;
+
+struct HeadPlan {
+  int64_t pad;
+  int tiles_per_shard, vocab_tiles, hidden_tiles, splits, piece_tiles;
+  size_t ints, part, part_sum, gathered, acc, d;      // sections of the workspace, in bytes
+  size_t bytes;
+};
+HeadPlan head_plan(const compass_head* h, bool backward) {
+  HeadPlan q = {};
+  q.pad = int64_t(round_up(size_t(h->M), 512));
+  const int64_t rows = vocab_shard_rows(h->vocab, h->P);
+  q.tiles_per_shard = int(ceil_div(rows, 256));
+  for (int r = 0; r < h->P; ++r) q.vocab_tiles += int(ceil_div(rows_of_vocab_shard(h->vocab, h->P, r), 256));
+  q.hidden_tiles = int(ceil_div(h->hidden, 256));
+  // dX has few tiles when rows are few: its contraction over the vocabulary is then split over the pairs
+  const int64_t dx_tiles = ceil_div(h->M, 256) * q.hidden_tiles;
+  q.splits = dx_tiles > 0 && dx_tiles < kPairs ? int(kPairs / dx_tiles) : 1;
+  if (q.splits > q.vocab_tiles) q.splits = q.vocab_tiles;
+  // pieces of equal size, an even number of vocabulary tiles each (512-row tiles of dW)
+  int64_t most = kPieceBytes / (q.pad * 512 + 1);
+  if (most < 2) most = 2;
+  const int64_t pieces = ceil_div(q.vocab_tiles, most);
+  q.piece_tiles = int(round_up(size_t(ceil_div(q.vocab_tiles, pieces)), 2));
+  if (q.splits > q.piece_tiles) q.splits = q.piece_tiles;
+  q.ints = round_up(size_t(q.pad) * 4, 256);
+  q.gathered = size_t(q.pad) * size_t(h->hidden) * 2;
+  if (backward) {
+    q.acc = size_t(q.pad / 128) * size_t(q.hidden_tiles) * size_t(q.splits) * (128 * 256 * 4);
+    q.d = size_t(q.pad) * size_t(q.piece_tiles) * 512;
+    q.bytes = 512 + 5 * q.ints + round_up(q.gathered, 256) + q.acc + q.d;
+  } else {
+    q.part = round_up(size_t(q.pad) * size_t(q.vocab_tiles) * 2 * 8, 256);
+    q.part_sum = h->label_smoothing != 0.f ? q.part / 2 : 0;
+    q.part_sum = round_up(q.part_sum, 256);
+    q.bytes = 512 + 4 * q.ints + round_up(q.gathered, 256) + q.part + q.part_sum;
+  }
+  return q;
+}
+
+struct DeviceFacts {
+  bool ready = false;
+  int pairs = 0;
+};
+int device_facts(DeviceFacts** out) {
+  constexpr int kMaxDevices = 64;
+  static DeviceFacts facts[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return record_cuda_error(e);
+  if (dev < 0 || dev >= kMaxDevices) return COMPASS_ERR_UNSUPPORTED;
+  std::lock_guard<std::mutex> lock(mu);
+  DeviceFacts& f = facts[dev];
+  if (!f.ready) {
+    const void* kernels[] = {reinterpret_cast<const void*>(head_kernel<STATS>), reinterpret_cast<const void*>(head_kernel<GRAD>),
+                             reinterpret_cast<const void*>(head_kernel<DX>), reinterpret_cast<const void*>(head_kernel<DW>)};
+    for (const void* k : kernels) {
+      e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
+      if (e != cudaSuccess) return record_cuda_error(e);
+    }
+    int sms = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(sms / 2 * 2));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&f.pairs, head_kernel<STATS>, &cfg);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    if (f.pairs < 1) return COMPASS_ERR_UNSUPPORTED;
+    f.ready = true;
+  }
+  *out = &f;
+  return COMPASS_OK;
+}
+
+int launch_form(int form, const HeadParams& p, int64_t most_tiles, const DeviceFacts& f, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(2 * (most_tiles < f.pairs ? most_tiles : f.pairs)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaError_t e;
+  if (form == STATS) e = cudaLaunchKernelEx(&cfg, head_kernel<STATS>, p);
+  else if (form == GRAD) e = cudaLaunchKernelEx(&cfg, head_kernel<GRAD>, p);
+  else if (form == DX) e = cudaLaunchKernelEx(&cfg, head_kernel<DX>, p);
+  else e = cudaLaunchKernelEx(&cfg, head_kernel<DW>, p);
+  count_kernel_launch();
+  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}
+
+// The part of both directions that lists and gathers the rows.
+struct Common {
+  HeadPlan q;
+  DeviceFacts* facts;
+  uint8_t* at;            // next free byte of the workspace
+  RowParams rows;
+  GatherParams2 gather;
+  HeadParams p;
+  uint8_t* take(size_t n) {
+    uint8_t* was = at;
+    at += n;
+    return was;
+  }
+};
+
+int begin(const compass_head* h, const void* const* X, const void* const* W, const void* targets, void* ws, size_t ws_bytes, bool backward,
+          Common* c) {
+  int st = check_head(h);
+  if (st != COMPASS_OK) return st;
+  if (h->M > 0 && targets == nullptr) return COMPASS_ERR_INVALID_ARG;
+  if (!is_aligned(targets, h->index_dtype == COMPASS_INDEX_INT64 ? 8 : 4)) return COMPASS_ERR_ALIGNMENT;
+  st = fill_shards(X, h->P, h->M, &c->gather.x);
+  if (st == COMPASS_OK) st = check_vocab_shards(W, h->P, h->vocab);
+  if (st != COMPASS_OK) return st;
+  c->q = head_plan(h, backward);
+  // tiles are numbered in 32 bits
+  const int64_t cols = c->q.vocab_tiles > c->q.hidden_tiles * c->q.splits ? c->q.vocab_tiles : c->q.hidden_tiles * c->q.splits;
+  if ((h->M / 256 + 1) * cols > kMaxDim || int64_t(c->q.vocab_tiles) * c->q.hidden_tiles > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  return check_workspace(ws, ws_bytes, c->q.bytes);
+}
+
+int gather_rows(const compass_head* h, const void* const* W, const void* targets, void* ws, Common* c, cudaStream_t stream) {
+  int st = device_facts(&c->facts);
+  if (st != COMPASS_OK) return st;
+  const HeadPlan& q = c->q;
+  HeadParams& p = c->p;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  Found* found = reinterpret_cast<Found*>(base + 256);
+  c->at = base + 512;
+  RowParams& r = c->rows;
+  r.targets = targets;
+  r.found = found;
+  r.place = reinterpret_cast<int32_t*>(c->take(q.ints));
+  r.origin = reinterpret_cast<int32_t*>(c->take(q.ints));
+  r.target = reinterpret_cast<int32_t*>(c->take(q.ints));
+  r.M = uint32_t(h->M);
+  r.vocab = int32_t(h->vocab);
+  r.wide = h->index_dtype == COMPASS_INDEX_INT64;
+  if (r.dloss) {
+    r.lse2 = reinterpret_cast<float*>(c->take(q.ints));
+    r.weight = reinterpret_cast<float*>(c->take(q.ints));
+  } else {
+    p.target_logit = reinterpret_cast<float*>(c->take(q.ints));
+  }
+  uint8_t* gathered = c->take(round_up(q.gathered, 256));
+  p.found = found;
+  p.target = r.target;
+  p.lse2 = r.lse2;
+  p.weight = r.weight;
+  p.status = static_cast<StatusBlock*>(ws);
+  p.hidden = h->hidden;
+  p.pad = int32_t(q.pad);
+  p.vocab_rows = int32_t(vocab_shard_rows(h->vocab, h->P));
+  p.vocab = int32_t(h->vocab);
+  p.tiles_per_shard = q.tiles_per_shard;
+  p.hidden_tiles = q.hidden_tiles;
+  p.splits = q.splits;
+  p.z_scale = h->logit_scale * kLog2e;
+  p.out_scale = h->logit_scale;
+  p.smoothing = h->label_smoothing;
+  p.uniform = float(double(h->label_smoothing) / double(h->vocab));
+  p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
+  bool ok = encode_tensor_map(&p.x_k, gathered, q.pad, h->hidden, 128);
+  for (int s = 0; s < h->P; ++s) {
+    const int64_t n = rows_of_vocab_shard(h->vocab, h->P, s);
+    if (n > 0) ok = ok && encode_tensor_map(&p.w_k[s], W[s], n, h->hidden, 128);
+    if (n > 0 && r.dloss) ok = ok && encode_tensor_map(&p.w_mn[s], W[s], n, h->hidden, 64);
+  }
+  if (r.dloss) ok = ok && encode_tensor_map(&p.x_mn, gathered, q.pad, h->hidden, 64);
+  if (!ok) return record_cuda_error(cudaErrorUnknown);
+  GatherParams2& g = c->gather;
+  g.found = found;
+  g.place = r.place;
+  g.gathered = reinterpret_cast<uint4*>(gathered);
+  g.M = uint32_t(h->M);
+  g.vecs = uint32_t(h->hidden / 8);
+  st = launch(head_rows_kernel, 1, 1024, 0, stream, false, r);
+  if (st != COMPASS_OK) return st;
+  const int64_t most = h->M + 512;
+  return launch(head_gather_kernel, most < 2048 ? most : 2048, 256, 0, stream, true, g);
+}
+
+// Tiles of a form at most, counted as 256 x 256.
+int64_t most_tiles(const compass_head* h, const HeadPlan& q, int64_t cols) { return ceil_div(h->M, 256) * cols; }
+
+}  // namespace
+
+}  // namespace compass
+
+using namespace compass;
+
+extern "C" int compass_head_workspace_bytes(const compass_head* h, int backward, size_t* bytes) {
+  if (bytes == nullptr) return COMPASS_ERR_INVALID_ARG;
+  const int st = check_head(h);
+  if (st != COMPASS_OK) return st;
+  *bytes = head_plan(h, backward != 0).bytes;
+  return COMPASS_OK;
+}
+
+extern "C" int compass_head_loss(const compass_head* h, const void* const* X, const void* const* W, const void* targets, float* loss,
+                                 float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Common c = {};
+  int st = begin(h, X, W, targets, ws, ws_bytes, false, &c);
+  if (st != COMPASS_OK) return st;
+  if (h->M > 0 && (loss == nullptr || lse == nullptr)) return COMPASS_ERR_INVALID_ARG;
+  if (!is_aligned(loss, 4) || !is_aligned(lse, 4)) return COMPASS_ERR_ALIGNMENT;
+  if (h->M == 0) return COMPASS_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  c.rows.loss_out = loss;
+  c.rows.lse_out = lse;
+  st = gather_rows(h, W, targets, ws, &c, s);
+  if (st != COMPASS_OK) return st;
+  HeadParams& p = c.p;
+  p.part = reinterpret_cast<float2*>(c.take(c.q.part));
+  p.part_sum = reinterpret_cast<float*>(c.take(c.q.part_sum));
+  p.n_vt = c.q.vocab_tiles;
+  st = launch_form(STATS, p, most_tiles(h, c.q, c.q.vocab_tiles), *c.facts, s);
+  if (st != COMPASS_OK) return st;
+  CombineParams m = {};
+  m.found = p.found;
+  m.origin = c.rows.origin;
+  m.part = p.part;
+  m.part_sum = p.part_sum;
+  m.target_logit = p.target_logit;
+  m.loss = loss;
+  m.lse = lse;
+  m.parts = 2 * c.q.vocab_tiles;
+  m.pad = int32_t(c.q.pad);
+  m.smoothing = p.smoothing;
+  m.uniform = p.uniform;
+  return launch(head_combine_kernel, ceil_div(h->M, 32), 1024, 0, s, true, m);
+}
+
+extern "C" int compass_head_loss_backward(const compass_head* h, const void* const* X, const void* const* W, const void* targets,
+                                          const float* lse, const float* dloss, void* const* dX, void* const* dW, void* ws,
+                                          size_t ws_bytes, void* stream) {
+  Common c = {};
+  int st = begin(h, X, W, targets, ws, ws_bytes, true, &c);
+  if (st != COMPASS_OK) return st;
+  if (h->M > 0 && (lse == nullptr || dloss == nullptr)) return COMPASS_ERR_INVALID_ARG;
+  if (!is_aligned(lse, 4) || !is_aligned(dloss, 4)) return COMPASS_ERR_ALIGNMENT;
+  st = fill_shards(dX, h->P, h->M, &c.gather.dx);
+  if (st == COMPASS_OK) st = check_vocab_shards(dW, h->P, h->vocab);
+  if (st != COMPASS_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (h->M == 0) {
+    for (int r = 0; r < h->P; ++r) {
+      const int64_t n = rows_of_vocab_shard(h->vocab, h->P, r);
+      if (n == 0) continue;
+      const cudaError_t e = cudaMemsetAsync(dW[r], 0, size_t(n) * size_t(h->hidden) * dtype_size(h->grad_dtype), s);
+      if (e != cudaSuccess) return record_cuda_error(e);
+    }
+    return COMPASS_OK;
+  }
+  c.rows.lse = lse;
+  c.rows.dloss = dloss;
+  c.gather.zero_dx = 1;
+  st = gather_rows(h, W, targets, ws, &c, s);
+  if (st != COMPASS_OK) return st;
+  const HeadPlan& q = c.q;
+  HeadParams& p = c.p;
+  p.acc = reinterpret_cast<float4*>(c.take(q.acc));
+  p.d = reinterpret_cast<__nv_bfloat16*>(c.take(q.d));
+  p.grad_fp32 = h->grad_dtype == COMPASS_DTYPE_FP32;
+  p.piece_cols = q.piece_tiles * 256;
+  for (int r = 0; r < h->P; ++r) p.dw[r] = dW[r];
+  if (!encode_tensor_map(&p.d_k, p.d, q.pad, p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, q.pad, p.piece_cols, 64))
+    return record_cuda_error(cudaErrorUnknown);
+  for (int vt = 0; vt < q.vocab_tiles; vt += q.piece_tiles) {
+    p.vt0 = vt;
+    p.n_vt = q.vocab_tiles - vt < q.piece_tiles ? q.vocab_tiles - vt : q.piece_tiles;
+    p.first_piece = vt == 0;
+    st = launch_form(GRAD, p, most_tiles(h, q, p.n_vt), *c.facts, s);
+    if (st == COMPASS_OK) st = launch_form(DX, p, most_tiles(h, q, int64_t(q.hidden_tiles) * q.splits), *c.facts, s);
+    if (st == COMPASS_OK) st = launch_form(DW, p, int64_t(p.n_vt) * q.hidden_tiles, *c.facts, s);
+    if (st != COMPASS_OK) return st;
+  }
+  FinishParams f = {};
+  f.dx = c.gather.dx;
+  f.found = p.found;
+  f.origin = c.rows.origin;
+  f.acc = p.acc;
+  f.hidden = h->hidden;
+  f.hidden_tiles = q.hidden_tiles;
+  f.splits = q.splits;
+  f.out_scale = p.out_scale;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(ceil_div(h->M, 32)), unsigned(q.hidden_tiles));
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, head_finish_kernel, f);
+  count_kernel_launch();
+  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}

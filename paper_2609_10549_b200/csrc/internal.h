@@ -179,6 +179,9 @@ struct TilePlan {
 // gemm_sm100.cu
 TilePlan plan_tiles(const GemmLaunch& launch, int max_pairs);
 int launch_gemm(const GemmLaunch& launch, cudaStream_t stream);
+// Tensor map of a dense BF16 matrix [rows x cols]: boxes of BK columns x box_rows rows, 128-byte swizzle, zero fill outside
+// (kept in the calling thread's table of encoded maps).
+bool encode_tensor_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows);
 size_t gemm_smem_bytes();
 void tensor_map_cache_stats(uint64_t* hits, uint64_t* misses);
 int gemm_tile_rows(int mode, int rows_per_block);   // rows of one scheduling tile: 256 (CTA pair) or 128

@@ -149,6 +149,7 @@ __device__ __forceinline__ uint64_t umma_smem_desc_sw128_mn(uint32_t smem_addr, 
 __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32(uint32_t m, uint32_t n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
+constexpr uint32_t kUmmaIdescAMnMajor = 1u << 15;      // A operand stored with M contiguous
 constexpr uint32_t kUmmaIdescBMnMajor = 1u << 16;      // B operand stored with N contiguous
 
 // D[tmem] (+)= A[smem] * B[smem]; issued by ONE thread.

@@ -39,8 +39,6 @@ constexpr int kSlots = 4;
 constexpr int kChunkBytes = 128 * BK * 2;       // 16 KB: 128 rows (or columns) of one 64-wide k-atom
 constexpr int kHalfChunk = kChunkBytes / 2;     // an MN-major operand is two boxes of 64 columns x 64 k-rows
 constexpr int kChunks = 12;
-constexpr int kStageRow = 64 + 16;              // epilogue staging: 64 bytes of a row, padded
-constexpr int kStageWarp = 32 * kStageRow;
 constexpr int kGroup = 8;                       // row tiles that go through the columns together (their A stays in L2)
 constexpr int kSkew = 3;                        // stages at a tile's ends in which accumulator 0 runs ahead
 constexpr float kLog2e = 1.4426950408889634f;
@@ -86,6 +84,7 @@ struct HeadParams {
   int32_t splits;               // of dX's contraction
   int32_t first_piece;
   int32_t grad_fp32;
+  int32_t dw_wide;              // dW's rows are whole 32-byte sectors
   float z_scale;                // logit_scale * log2(e)
   float out_scale;              // logit_scale
   float smoothing, uniform;     // label_smoothing, label_smoothing / vocab
@@ -100,7 +99,7 @@ struct Control {
   int abort;
 };
 
-constexpr size_t kSmemBytes = 1024 + size_t(kChunks) * kChunkBytes + sizeof(Control) + 16 + size_t(kEpiWarps) * kStageWarp;
+constexpr size_t kSmemBytes = 1024 + size_t(kChunks) * kChunkBytes + sizeof(Control);
 
 enum Site : int { SITE_EMPTY = 1, SITE_FULL = 2, SITE_ACC_EMPTY = 3, SITE_ACC_FULL = 4, SITE_DRAIN = 5 };
 
@@ -214,6 +213,23 @@ __device__ __forceinline__ void load_b(const HeadParams& p, uint8_t* dst, uint32
     const int vt = p.vt0 + col_tile;
     const int shard = vt / p.tiles_per_shard;
     tma_load_2d_pair_hint(dst, &p.w_k[shard], bar, atom * BK, (vt - shard * p.tiles_per_shard) * 256 + cta * 128, pol);
+  }
+}
+
+// 32 bytes, one sector, at a 32-byte boundary.
+__device__ __forceinline__ void store_32(void* p, const uint32_t (&q)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]), "r"(q[4]),
+               "r"(q[5]), "r"(q[6]), "r"(q[7])
+               : "memory");
+}
+// The same at a 16-byte boundary where rows are not whole sectors, `both` halves or the first.
+__device__ __forceinline__ void store_row_piece(void* p, const uint32_t (&q)[8], bool wide, bool both) {
+  if (wide) {
+    store_32(p, q);
+  } else {
+    uint4* o = static_cast<uint4*>(p);
+    o[0] = make_uint4(q[0], q[1], q[2], q[3]);
+    if (both) o[1] = make_uint4(q[4], q[5], q[6], q[7]);
   }
 }
 
@@ -412,7 +428,6 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    uint8_t* stage = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ctl + 1) + 15) & ~uintptr_t(15)) + (warp - 2) * kStageWarp;
     const int rows = p.found->rows;
     float out_scale = p.out_scale;
     if (kForm == DW) out_scale *= p.found->top;
@@ -426,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         const int frag0 = tile.row0 + (tile.big ? int(cta) * 256 + a * 128 : int(cta) * 128);    // this CTA's 128 rows
         const int row = frag0 + quarter * 32 + lane;
         int target = -1;
-        float lse2 = 0.f, w = 0.f;
+        float lse2 = INFINITY, w = 0.f;       // a row past the last gives zeros
         if (kForm == STATS || kForm == GRAD) {
           if (row < rows) {
             target = p.target[row];
@@ -445,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         tmem_ld_wait();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
         ++uses[b];
 
         if (kForm == STATS || kForm == GRAD) {
@@ -490,11 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                float d = (exp2_fast(fmaf(__uint_as_float(v[c][i]), p.z_scale, -lse2)) - p.uniform) * w;
-                if (row >= rows || (cols < 128 && c * 32 + i >= cols)) d = 0.f;
-                v[c][i] = __float_as_uint(d);
-              }
+              for (int i = 0; i < 32; ++i)
+                v[c][i] = __float_as_uint((exp2_fast(fmaf(__uint_as_float(v[c][i]), p.z_scale, -lse2)) - p.uniform) * w);
             if (any) {
               const float off = (1.f - p.smoothing) * w;
 #pragma unroll
@@ -503,24 +515,23 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
                 for (int i = 0; i < 32; ++i)
                   if (mine && hit == c * 32 + i) v[c][i] = __float_as_uint(__uint_as_float(v[c][i]) - off);
             }
-            __nv_bfloat16* out = p.d + int64_t(frag0 + quarter * 32) * p.piece_cols + tile.col * 256 + half * 128;
+            if (cols < 128) {       // past the shard's last row
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint4* srow = reinterpret_cast<uint4*>(stage + lane * kStageRow);
+              for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                const uint32_t* q = &v[c][g * 8];
-                srow[g] = make_uint4(pack_bf16x2(__uint_as_float(q[0]), __uint_as_float(q[1])), pack_bf16x2(__uint_as_float(q[2]), __uint_as_float(q[3])),
-                                     pack_bf16x2(__uint_as_float(q[4]), __uint_as_float(q[5])), pack_bf16x2(__uint_as_float(q[6]), __uint_as_float(q[7])));
-              }
-              __syncwarp();
+                for (int i = 0; i < 32; ++i)
+                  if (c * 32 + i >= cols) v[c][i] = 0u;
+            }
+            // straight from the registers, 32 bytes of a row per lane: through shared memory the tensor cores' operand
+            // reads, which take most of its bandwidth, made this phase several times as long
+            __nv_bfloat16* out = p.d + int64_t(row) * p.piece_cols + tile.col * 256 + half * 128;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = i * 8 + (lane >> 2);
-                *reinterpret_cast<uint4*>(out + int64_t(r) * p.piece_cols + c * 32 + (lane & 3) * 8) =
-                    *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
-              }
-              __syncwarp();
+            for (int g = 0; g < 8; ++g) {
+              uint32_t q[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                q[i] = pack_bf16x2(__uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i]), __uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i + 1]));
+              store_32(out + g * 16, q);
             }
           }
         } else if (kForm == DX) {
@@ -553,40 +564,29 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           int shard, vrow;
           const int vt_rows = vocab_cols(p, p.vt0 + (frag0 >> 8), &shard, &vrow);
           const int in_tile = (frag0 & 255) + quarter * 32;
-          const int live = vt_rows - in_tile;                     // rows of this warp that exist
-          const int64_t first = int64_t(vrow) + in_tile;
           const int col0 = tile.col * 256 + half * 128;
-          const int per = p.grad_fp32 ? 16 : 32;                  // columns in 64 bytes
-          const int passes = p.grad_fp32 ? 8 : 4;
-          uint8_t* out = static_cast<uint8_t*>(p.dw[shard]);
-          const int64_t pitch = p.hidden * (p.grad_fp32 ? 4 : 2);
+          if (in_tile + lane < vt_rows) {
+            const int bytes = p.grad_fp32 ? 4 : 2;
+            uint8_t* out = static_cast<uint8_t*>(p.dw[shard]) + ((int64_t(vrow) + in_tile + lane) * p.hidden + col0) * bytes;
+            const int left = int(p.hidden) - col0;            // columns, a multiple of 8
+            if (p.grad_fp32) {
 #pragma unroll
-          for (int pass = 0; pass < 8; ++pass) {
-            if (pass < passes) {
-              uint4* srow = reinterpret_cast<uint4*>(stage + lane * kStageRow);
+              for (int g = 0; g < 16; ++g) {
+                uint32_t q[8];
 #pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                float x[8];
-                if (p.grad_fp32) {
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[pass >> 1][(pass & 1) * 16 + g * 4 + i]) * out_scale;
-                  srow[g] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[pass & 3][g * 8 + i]) * out_scale;
-                  srow[g] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-                }
+                for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__uint_as_float(v[g >> 2][(g & 3) * 8 + i]) * out_scale);
+                if (g * 8 < left) store_row_piece(out + g * 32, q, p.dw_wide, true);
               }
-              __syncwarp();
-              const int col = col0 + pass * per + (lane & 3) * (per / 4);
+            } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = i * 8 + (lane >> 2);
-                if (r < live && col < p.hidden)
-                  *reinterpret_cast<uint4*>(out + (first + r) * pitch + int64_t(col) * (p.grad_fp32 ? 4 : 2)) =
-                      *reinterpret_cast<const uint4*>(stage + r * kStageRow + (lane & 3) * 16);
+              for (int g = 0; g < 8; ++g) {
+                uint32_t q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  q[i] = pack_bf16x2(__uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i]) * out_scale,
+                                     __uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i + 1]) * out_scale);
+                if (g * 16 < left) store_row_piece(out + g * 32, q, p.dw_wide, g * 16 + 8 < left);
               }
-              __syncwarp();
             }
           }
         }
@@ -1132,7 +1132,11 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
   p.d = reinterpret_cast<__nv_bfloat16*>(c.take(q.d));
   p.grad_fp32 = h->grad_dtype == COMPASS_DTYPE_FP32;
   p.piece_cols = q.piece_tiles * 256;
-  for (int r = 0; r < h->P; ++r) p.dw[r] = dW[r];
+  p.dw_wide = h->hidden * int64_t(dtype_size(h->grad_dtype)) % 32 == 0;
+  for (int r = 0; r < h->P; ++r) {
+    p.dw[r] = dW[r];
+    if (!is_aligned(dW[r], 32)) p.dw_wide = 0;
+  }
   if (!encode_tensor_map(&p.d_k, p.d, q.pad, p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, q.pad, p.piece_cols, 64))
     return record_cuda_error(cudaErrorUnknown);
   for (int vt = 0; vt < q.vocab_tiles; vt += q.piece_tiles) {

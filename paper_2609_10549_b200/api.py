@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -105,11 +106,16 @@ class PlanBlock(C.Structure):
 
 
 _lib: Optional[C.CDLL] = None
+_raw_stream = _current_device = None      # torch's getters of the current stream's handle and of the current device
 
 
 def lib() -> C.CDLL:
-    global _lib
+    global _lib, _raw_stream, _current_device
     if _lib is None:
+        torch = sys.modules.get("torch")
+        if torch is not None:
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _current_device = torch.cuda.current_device
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_10549_b200.build` "
                                "(there is no CPU fallback)")
@@ -304,6 +310,8 @@ def _ptr_array(tensors: Sequence) -> C.Array:
 
 def _stream_handle(stream) -> C.c_void_p:
     if stream is None:
+        if _raw_stream is not None:       # torch.cuda.current_stream() builds an object around it, several microseconds a call
+            return C.c_void_p(_raw_stream(_current_device()))
         import torch
         stream = torch.cuda.current_stream()
     return C.c_void_p(int(stream.cuda_stream))

@@ -15,12 +15,12 @@ namespace {
 
 struct VocabShards {
   void* ptr[kMaxP];
-  uint32_t rows;      // per shard (the last ones hold fewer)
+  FastDiv rows;       // per shard (the last ones hold fewer)
   uint32_t vocab;
   template <typename T>
   __device__ __forceinline__ T* row(uint32_t v, int64_t pitch) const {
-    const uint32_t r = v / rows;
-    return static_cast<T*>(ptr[r]) + int64_t(v - r * rows) * pitch;
+    const uint32_t r = rows.div(v);
+    return static_cast<T*>(ptr[r]) + int64_t(v - r * rows.d) * pitch;
   }
 };
 
@@ -206,7 +206,7 @@ __device__ void sort_tile(const GradParams& p, SortShared& s) {
 
 // Zeros for every row of dW, by blocks first .. first + n - 1 of the grid.
 __device__ __forceinline__ void write_zeros(const GradParams& p, int64_t first, int64_t n) {
-  const uint32_t per = p.dw.rows;
+  const uint32_t per = p.dw.rows.d;
   for (uint32_t r = 0, v0 = 0; v0 < p.dw.vocab; ++r, v0 += per) {
     const int64_t rows = min(per, p.dw.vocab - v0);
     const int64_t bytes = rows * p.hidden * p.elem;
@@ -297,7 +297,30 @@ __global__ void __launch_bounds__(1024, 1) embedding_scan_kernel(const __grid_co
 // ---- gradient: sums ------------------------------------------------------------
 
 constexpr int kGradThreads = 128;
-constexpr int kAhead = 4;                  // tokens whose rows are in flight
+constexpr int kAhead = 8;                  // tokens whose rows are in flight
+
+// V FP32 sums, in accesses of 16 bytes where V allows.
+template <int V>
+__device__ __forceinline__ void store_sums(float* p, const float (&v)[V]) {
+  if constexpr (V == 1) {
+    *p = v[0];
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_sums(float (&v)[V], const float* p) {
+  if constexpr (V == 1) {
+    v[0] = __ldcg(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const float4 q = __ldcg(reinterpret_cast<const float4*>(p + j));
+      v[j] = q.x, v[j + 1] = q.y, v[j + 2] = q.z, v[j + 3] = q.w;
+    }
+  }
+}
 
 template <typename G, int V>
 __device__ __forceinline__ void finish_row(const GradParams& p, uint32_t id, int64_t c, const float (&acc)[V]) {
@@ -334,90 +357,115 @@ __device__ __forceinline__ void finish_row(const GradParams& p, uint32_t id, int
 template <typename T, typename G, int V>
 __global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __grid_constant__ GradParams p) {
   wait_for_previous_kernel();
-  extern __shared__ uint32_t tokens[];       // [run] positions, [run] ids
+  extern __shared__ uint4 raw[];
+  // where each token's row is (null: padding), and what to do behind it: kNone, or a run's end
+  enum : int { kNone = 0, kWrite = 1, kInherited = 2, kGoesOn = 3 };
+  const T** rows = reinterpret_cast<const T**>(raw);
+  int* what = reinterpret_cast<int*>(rows + p.run);
+  uint32_t* ids = reinterpret_cast<uint32_t*>(what + p.run);
   const int64_t piece = blockIdx.x;
   const int64_t first = piece * p.run;
   const int n = int(min(int64_t(p.run), int64_t(p.M) - first));
-  uint32_t* pos = tokens;
-  uint32_t* key = tokens + p.run;
-  for (int i = threadIdx.x; i < n; i += kGradThreads) {
-    pos[i] = p.pos_a[first + i];
-    key[i] = p.key_a[first + i];
+  for (int i = threadIdx.x; i < int(p.run); i += kGradThreads) {
+    rows[i] = nullptr;
+    what[i] = kNone;
+    if (i >= n) continue;
+    const uint32_t id = p.key_a[first + i];
+    ids[i] = id;
+    if (id >= p.dw.vocab) continue;
+    rows[i] = p.dout.row<T>(p.pos_a[first + i], p.hidden);
+    const bool goes_on = first + i + 1 < int64_t(p.M) && p.key_a[first + i + 1] == id;
+    if (!goes_on || i + 1 == n) {
+      const bool inherited = first > 0 && p.key_a[first] == id && p.key_a[first - 1] == id;
+      what[i] = inherited ? kInherited : goes_on ? kGoesOn : kWrite;
+    }
   }
-  const uint32_t before = first > 0 ? p.key_a[first - 1] : 0xffffffffu;
-  const uint32_t after = first + n < int64_t(p.M) ? p.key_a[first + n] : 0xffffffffu;
   __syncthreads();
   const int64_t c = (int64_t(blockIdx.y) * kGradThreads + threadIdx.x) * V;
   if (c >= p.hidden) return;
   float acc[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) acc[j] = 0.f;
-  Raw<T, V> ahead[kAhead];
-  auto fetch = [&](int i, Raw<T, V>& r) {
-    r.zero();
-    if (i < n && key[i] < p.dw.vocab) r.load(p.dout.row<T>(pos[i], p.hidden) + c);
-  };
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) fetch(i, ahead[i]);
-  bool inherited = n > 0 && key[0] == before;
   for (int i0 = 0; i0 < n; i0 += kAhead) {
+    Raw<T, V> ahead[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int i = i0 + k;
-      if (i < n && key[i] < p.dw.vocab) {
-        float x[V];
-        ahead[k].get(x);
+      const T* r = rows[i0 + k];          // (p.run is a multiple of kAhead)
+      if (r) ahead[k].load(r + c);
+      else ahead[k].zero();
+    }
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += x[j];
-        const uint32_t next = i + 1 < n ? key[i + 1] : after;
-        if (next != key[i] || i + 1 == n) {
-          const bool goes_on = next == key[i];
-          if (!inherited && !goes_on) {
-            finish_row<G, V>(p, key[i], c, acc);
-          } else {
-            float* out = p.partial + (piece * 2 + (inherited ? 0 : 1)) * p.hidden + c;
+    for (int k = 0; k < kAhead; ++k) {
+      float x[V];
+      ahead[k].get(x);
 #pragma unroll
-            for (int j = 0; j < V; ++j) out[j] = acc[j];
-          }
-          inherited = false;
-#pragma unroll
-          for (int j = 0; j < V; ++j) acc[j] = 0.f;
+      for (int j = 0; j < V; ++j) acc[j] += x[j];
+      const int end = what[i0 + k];
+      if (end != kNone) {
+        if (end == kWrite) {
+          finish_row<G, V>(p, ids[i0 + k], c, acc);
+        } else {
+          store_sums(p.partial + (piece * 2 + (end == kInherited ? 0 : 1)) * p.hidden + c, acc);
         }
-        fetch(i + kAhead, ahead[k]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.f;
       }
     }
   }
 }
 
-// The runs that cross pieces: the piece a run begins in adds up what it and the pieces after it left, in order.
+// The runs that cross pieces: where one begins, what its pieces left is added up in order, every kJoinWays-th by one group of
+// threads, and the groups' sums in turn.
+constexpr int kJoinWays = 8;
+constexpr int kJoinLanes = 32;
 template <typename G, int V>
-__global__ void __launch_bounds__(kGradThreads) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces) {
+__global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces) {
+  __shared__ float part[kJoinWays][kJoinLanes][V + 1];
   wait_for_previous_kernel();
   const int64_t piece = blockIdx.x;
   const int64_t first = piece * p.run, last = min(first + p.run, int64_t(p.M)) - 1;
   if (last + 1 >= int64_t(p.M)) return;
-  const uint32_t id = p.key_a[last];
-  if (id >= p.dw.vocab || p.key_a[last + 1] != id) return;            // nothing goes on
-  if (p.key_a[first] == id && first > 0 && p.key_a[first - 1] == id) return;   // it began earlier
-  const int64_t c = (int64_t(blockIdx.y) * kGradThreads + threadIdx.x) * V;
-  if (c >= p.hidden) return;
-  // pieces that it reaches into: the last one starts with it (found by bisection of the sorted ids)
-  int64_t lo = piece + 1, hi = int64_t(pieces) - 1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (p.key_a[mid * p.run] == id) lo = mid;
-    else hi = mid - 1;
+  // (four independent loads before the first branch)
+  const uint32_t id = p.key_a[last], next = p.key_a[last + 1], front = p.key_a[first], before = first > 0 ? p.key_a[first - 1] : 0xffffffffu;
+  if (id >= p.dw.vocab || next != id) return;        // nothing goes on
+  if (front == id && before == id) return;           // it began earlier
+  // the last piece that it reaches into starts with it; every warp looks at 32 pieces at a time
+  int64_t lo = piece;
+  for (;;) {
+    const int64_t q = lo + 1 + (threadIdx.x & 31);
+    const uint32_t same = __ballot_sync(0xffffffffu, q < int64_t(pieces) && p.key_a[q < int64_t(pieces) ? q * p.run : first] == id);
+    const int n = __ffs(~same) - 1;                  // (-1: all 32)
+    lo += n < 0 ? 32 : n;
+    if (n >= 0) break;
   }
-  const float* src = p.partial + c;
-  float acc[V];
+  const int lane = threadIdx.x % kJoinLanes, way = threadIdx.x / kJoinLanes;
+  for (int64_t c0 = int64_t(blockIdx.y) * kJoinLanes * V; c0 < p.hidden; c0 += int64_t(gridDim.y) * kJoinLanes * V) {
+    const int64_t c = c0 + lane * V;
+    float acc[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = src[(piece * 2 + 1) * p.hidden + j];
-#pragma unroll 8
-  for (int64_t q = piece + 1; q <= lo; ++q) {
+    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+    if (c < p.hidden) {
+      // (the piece where it begins left its part in slot 1, the others in slot 0)
+#pragma unroll 4
+      for (int64_t q = piece + way; q <= lo; q += kJoinWays) {
+        float x[V];
+        load_sums(x, p.partial + (q * 2 + (q == piece ? 1 : 0)) * p.hidden + c);
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += src[q * 2 * p.hidden + j];
+        for (int j = 0; j < V; ++j) acc[j] += x[j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) part[way][lane][j] = acc[j];
+    __syncthreads();
+    if (way == 0 && c < p.hidden) {
+#pragma unroll
+      for (int w = 1; w < kJoinWays; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += part[w][lane][j];
+      finish_row<G, V>(p, id, c, acc);
+    }
+    __syncthreads();
   }
-  finish_row<G, V>(p, id, c, acc);
 }
 
 // ---- host ----------------------------------------------------------------------
@@ -440,7 +488,7 @@ int check_ids(const void* ids, int64_t M, int index_dtype) {
 
 VocabShards vocab_shards(const void* const* w, int P, int64_t vocab) {
   VocabShards s = {};
-  s.rows = uint32_t(vocab_shard_rows(vocab, P));
+  s.rows.set(uint32_t(vocab_shard_rows(vocab, P)));
   s.vocab = uint32_t(vocab);
   for (int r = 0; r < P; ++r) s.ptr[r] = const_cast<void*>(w[r]);
   return s;
@@ -460,8 +508,8 @@ int pick_lookup(const LookupParams& p, int sms, cudaStream_t stream) {
   return blocks >= 8 * sms ? run_lookup<T, V, 4>(p, stream) : run_lookup<T, V, 1>(p, stream);
 }
 
-// Sorted tokens per piece: 32, more where that would be over 2048 pieces.
-uint32_t run_length(int64_t M) { return uint32_t(M <= 65536 ? 32 : round_up(size_t(ceil_div(M, 2048)), 32)); }
+// Sorted tokens per piece: 8 (whose loads a thread has in flight together), more where that would be over 1024 pieces.
+uint32_t run_length(int64_t M) { return uint32_t(M <= 8192 ? 8 : round_up(size_t(ceil_div(M, 1024)), 8)); }
 
 struct GradPlan {
   uint32_t tiles, run, pieces;
@@ -486,7 +534,7 @@ int run_grad(const GradParams& p, const GradPlan& g, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(g.pieces, slabs);
   cfg.blockDim = dim3(kGradThreads);
-  cfg.dynamicSmemBytes = size_t(g.run) * 8;
+  cfg.dynamicSmemBytes = size_t(g.run) * 16;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -498,6 +546,8 @@ int run_grad(const GradParams& p, const GradPlan& g, cudaStream_t stream) {
   if (e != cudaSuccess) return record_cuda_error(e);
   if (g.pieces == 1) return COMPASS_OK;
   cfg.dynamicSmemBytes = 0;
+  cfg.gridDim = dim3(g.pieces, unsigned(ceil_div(p.hidden, kJoinLanes * V) < 4 ? ceil_div(p.hidden, kJoinLanes * V) : 4));
+  cfg.blockDim = dim3(kJoinWays * kJoinLanes);
   e = cudaLaunchKernelEx(&cfg, embedding_join_kernel<G, V>, p, g.pieces);
   count_kernel_launch();
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);

@@ -1,8 +1,8 @@
 // Softmax cross entropy of the vocabulary-parallel output layer, forward and
 // backward, without the logits.
 //
-// Rows whose target lies outside the vocabulary take no part: head_rows_kernel
-// lists the others and head_gather_kernel copies them together, so that the
+// Rows whose target lies outside the vocabulary take no part: head_count_kernel
+// counts the others and head_gather_kernel copies them together, so that the
 // products run over real rows only, whatever the mask and the ranks' shards.
 // Then one kernel in four forms (tcgen05 products of BF16 with FP32 sums):
 //   STATS  logits of 256 vocabulary columns at a time; what leaves the epilogue
@@ -83,6 +83,7 @@ struct HeadParams {
   int32_t hidden_tiles;
   int32_t splits;               // of dX's contraction
   int32_t first_piece;
+  int32_t one_row_tile;         // M <= 256
   int32_t grad_fp32;
   int32_t dw_wide;              // dW's rows are whole 32-byte sectors
   float z_scale;                // logit_scale * log2(e)
@@ -275,13 +276,25 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
   tc_fence_after_sync();
   const uint32_t tmem_base = ctl->tmem_base;
   launch_dependents();
+  const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+  // The first stages' tiles of the table do not depend on the kernels before (which list and gather the rows): with one row
+  // tile, whose place among the tiles is known, they are on their way before those are done.
+  int early = 0;
+  if ((kForm == STATS || kForm == GRAD) && p.one_row_tile && threadIdx.x == 0 && unit < p.n_vt) {
+    const int stages = min(3, int((p.hidden + 127) / 128));
+    for (; early < stages; ++early) {
+      const uint32_t bar = map_to_cta(smem_u32(&ctl->full[early]), 0);
+      if (leader) mbar_arrive_expect_tx(&ctl->full[early], uint32_t(8 * kChunkBytes));
+      for (int i = 0; i < 2; ++i)
+        load_b<kForm>(p, smem + (early * 4 + 2 + i) * kChunkBytes, bar, unit, int(cta), early * 2 + i, pol);
+    }
+  }
   wait_for_previous_kernel();
   const Plan plan = make_plan<kForm>(p, units);
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
       uint32_t j = 0;          // stages so far
       int chunk = 0;           // ring cursor
       bool ok = true;
@@ -303,7 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           const uint32_t slot = j & 3u;
           const uint32_t bar = map_to_cta(smem_u32(&ctl->full[slot]), 0);
           const int n = tile.big ? 3 : 4;
-          if (leader) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * kChunkBytes));
+          const bool b_sent = j < uint32_t(early);
+          if (leader && !b_sent) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * kChunkBytes));
           uint8_t* c[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) c[i] = smem + ((chunk + i) % kChunks) * kChunkBytes;
@@ -314,9 +328,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
             load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
           } else {
             load_a<kForm>(p, c[0], bar, row, atom, pol);
-            load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
+            if (!b_sent) load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
             load_a<kForm>(p, c[1], bar, row, atom + 1, pol);
-            load_b<kForm>(p, c[3], bar, tile.col, int(cta), atom + 1, pol);
+            if (!b_sent) load_b<kForm>(p, c[3], bar, tile.col, int(cta), atom + 1, pol);
           }
           chunk = (chunk + n) % kChunks;
         }
@@ -607,120 +621,165 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 
 // ---- which rows take part ------------------------------------------------------
 
+constexpr int kCountRows = 1024;      // rows counted together
+constexpr int kGatherRows = 4;        // rows a block copies, two warps each
+
 struct RowParams {
+  RowShards x, dx;          // dx: backward, zeros for the rows that take no part
   const void* targets;
   const float* lse;         // backward
   const float* dloss;
-  float* loss_out;          // forward: zeros for the others
+  float* loss_out;          // forward: zeros for the rows that take no part
   float* lse_out;
+  int32_t* counts;          // [ceil(M / kCountRows)] rows that take part
+  float* tops;              // the same: max |dloss| over them, infinite where one is not finite
   Found* found;
-  int32_t* place;           // [M] place among the gathered rows, or -1
   int32_t* origin;          // [pad] row that a gathered one comes from
   int32_t* target;
   float* lse2;
   float* weight;
+  uint4* gathered;
   uint32_t M;
+  uint32_t vecs;            // 16-byte vectors per row
   int32_t vocab;
   int32_t wide;
 };
 
-constexpr int kRowItems = 4;
-__global__ void __launch_bounds__(1024, 1) head_rows_kernel(const __grid_constant__ RowParams p) {
-  __shared__ uint32_t counts[2][32];
-  __shared__ float tops[32];
+// A row's target, or -1 when it takes no part.
+__device__ __forceinline__ int32_t target_of(const RowParams& p, uint32_t i) {
+  const int64_t y = p.wide ? static_cast<const int64_t*>(p.targets)[i] : int64_t(static_cast<const int32_t*>(p.targets)[i]);
+  return y >= 0 && y < p.vocab ? int32_t(y) : -1;
+}
+
+__global__ void __launch_bounds__(256) head_count_kernel(const __grid_constant__ RowParams p) {
+  __shared__ int32_t counts[8];
+  __shared__ float tops[8];
   launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t base = 0;
+  int32_t n = 0;
   float top = 0.f;
-  bool bad = false;
-  for (uint32_t turn = 0, i0 = 0; i0 < p.M; i0 += 1024 * kRowItems, ++turn) {
-    // thread t takes kRowItems rows in a row, so that the order is kept
-    const uint32_t i = i0 + threadIdx.x * kRowItems;
-    int32_t target[kRowItems];
-    uint32_t n = 0;
 #pragma unroll
-    for (int k = 0; k < kRowItems; ++k) {
-      target[k] = -1;
-      if (i + k < p.M) {
-        const int64_t y = p.wide ? static_cast<const int64_t*>(p.targets)[i + k] : int64_t(static_cast<const int32_t*>(p.targets)[i + k]);
-        if (y >= 0 && y < p.vocab) {
-          target[k] = int32_t(y);
-          ++n;
-        }
-      }
-    }
-    uint32_t x = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) counts[turn & 1][warp] = x;
-    __syncthreads();
-    uint32_t c = counts[turn & 1][lane], sum = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
-    uint32_t at = base + (x - n) + __shfl_sync(0xffffffffu, sum - c, warp);
-    base += __shfl_sync(0xffffffffu, sum, 31);
-#pragma unroll
-    for (int k = 0; k < kRowItems; ++k) {
-      if (i + k >= p.M) break;
-      if (target[k] < 0) {
-        p.place[i + k] = -1;
-        if (p.loss_out) p.loss_out[i + k] = 0.f;
-        if (p.lse_out) p.lse_out[i + k] = 0.f;
-        continue;
-      }
-      p.place[i + k] = int32_t(at);
-      p.origin[at] = int32_t(i + k);
-      p.target[at] = target[k];
-      if (p.dloss) {
-        const float g = p.dloss[i + k];
-        p.weight[at] = g;
-        p.lse2[at] = p.lse[i + k] * kLog2e;
-        top = fmaxf(top, fabsf(g));
-        bad |= !(fabsf(g) < INFINITY);
-      }
-      ++at;
+  for (int k = 0; k < kCountRows / 256; ++k) {
+    const uint32_t i = blockIdx.x * kCountRows + k * 256 + threadIdx.x;
+    if (i >= p.M) continue;
+    const float g = p.dloss ? fabsf(p.dloss[i]) : 0.f;
+    if (target_of(p, i) >= 0) {
+      ++n;
+      top = fmaxf(top, g < INFINITY ? g : INFINITY);      // (NaN too)
+    } else if (p.loss_out) {
+      p.loss_out[i] = 0.f;
+      p.lse_out[i] = 0.f;
     }
   }
+  n = __reduce_add_sync(0xffffffffu, n);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  bad = __syncthreads_or(bad);
-  if (lane == 0) tops[warp] = top;
+  if (lane == 0) {
+    counts[warp] = n;
+    tops[warp] = top;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < 32; ++w) top = fmaxf(top, tops[w]);
-    p.found->rows = int32_t(base);
-    p.found->top = bad || top == 0.f ? 1.f : top;
+    for (int w = 1; w < 8; ++w) {
+      n += counts[w];
+      top = fmaxf(top, tops[w]);
+    }
+    p.counts[blockIdx.x] = n;
+    p.tops[blockIdx.x] = top;
   }
 }
 
-struct GatherParams2 {
-  RowShards x, dx;
-  const Found* found;
-  const int32_t* place;
-  uint4* gathered;
-  uint32_t M;
-  uint32_t vecs;            // 16-byte vectors per row
-  int32_t zero_dx;
-};
-// The rows that take part, together; zeros behind them up to a multiple of 512 (dW contracts over these rows), and in the
-// dX of the others.
-__global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant__ GatherParams2 p) {
+// Sum over the block; all its threads take part.
+__device__ __forceinline__ int2 block_add(int2 v, int2* part) {
+  v.x = __reduce_add_sync(0xffffffffu, v.x);
+  v.y = __reduce_add_sync(0xffffffffu, v.y);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int w = 1; w < 8; ++w) {
+    v.x += part[w].x;
+    v.y += part[w].y;
+  }
+  return v;
+}
+
+// The rows that take part, together and in order.  The k-th row that takes none zeroes the k-th row behind them, up to a
+// multiple of 512 (dW contracts over whole tiles of these rows), and its own dX.
+__global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant__ RowParams p) {
+  __shared__ int2 part[8];
+  __shared__ int32_t places[kGatherRows];
   launch_dependents();
   wait_for_previous_kernel();
-  const uint32_t rows = uint32_t(p.found->rows);
-  const uint32_t pad = (max(rows, 1u) + 511) / 512 * 512 - rows;
-  for (uint32_t i = blockIdx.x; i < p.M + pad; i += gridDim.x) {
-    const int32_t to = i < p.M ? p.place[i] : int32_t(rows + (i - p.M));
-    const uint4* from = i < p.M && to >= 0 ? p.x.row<uint4>(i, p.vecs) : nullptr;
-    uint4* out = to >= 0 ? p.gathered + int64_t(to) * p.vecs : p.zero_dx ? p.dx.row<uint4>(i, p.vecs) : nullptr;
-    if (out == nullptr) continue;
-    for (uint32_t c = threadIdx.x; c < p.vecs; c += 256) out[c] = from ? from[c] : make_uint4(0u, 0u, 0u, 0u);
+  const uint32_t row0 = blockIdx.x * kGatherRows;
+  const uint32_t chunk = row0 / kCountRows, chunks = (p.M + kCountRows - 1) / kCountRows;
+  int2 sum = make_int2(0, 0);       // rows that take part: before row0, in all
+  float top = 0.f;
+  for (uint32_t b = threadIdx.x; b < chunks; b += 256) {
+    const int32_t n = p.counts[b];
+    if (b < chunk) sum.x += n;
+    sum.y += n;
+    top = fmaxf(top, p.tops[b]);
+  }
+  for (uint32_t i = chunk * kCountRows + threadIdx.x; i < row0; i += 256) sum.x += target_of(p, i) >= 0;
+  sum = block_add(sum, part);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x == 0) {
+    __shared__ float tops[8];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
+      p.found->rows = sum.y;
+      p.found->top = top > 0.f && top < INFINITY ? top : 1.f;
+    }
+  }
+  if (warp == 0) {
+    const uint32_t i = row0 + lane;
+    const bool in = lane < kGatherRows && i < p.M;
+    const int32_t target = in ? target_of(p, i) : -1;
+    const uint32_t valid = __ballot_sync(0xffffffffu, target >= 0);
+    const int32_t at = sum.x + __popc(valid & ((1u << lane) - 1u));
+    if (target >= 0) {
+      p.origin[at] = int32_t(i);
+      p.target[at] = target;
+      if (p.dloss) {
+        p.weight[at] = p.dloss[i];
+        p.lse2[at] = p.lse[i] * kLog2e;
+      }
+    }
+    // a row that takes no part, the (i - at)-th of them: its place is behind the others, as ~place
+    if (lane < kGatherRows) places[lane] = target >= 0 ? at : ~(sum.y + int32_t(i) - at);
+  }
+  __syncthreads();
+  const int32_t padded = (max(sum.y, 1) + 511) / 512 * 512;
+  const uint32_t i = row0 + (warp >> 1);
+  if (i >= p.M) return;
+  const int32_t place = places[warp >> 1];
+  const uint32_t c0 = threadIdx.x & 63;
+  if (place >= 0) {
+    const uint4* from = p.x.row<uint4>(i, p.vecs);
+    uint4* to = p.gathered + int64_t(place) * p.vecs;
+    uint32_t c = c0;
+    for (; c + 7 * 64 < p.vecs; c += 8 * 64) {
+      uint4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __ldcs(from + c + k * 64);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) to[c + k * 64] = v[k];
+    }
+    for (; c < p.vecs; c += 64) to[c] = __ldcs(from + c);
+  } else {
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    uint4* to = p.gathered + int64_t(~place) * p.vecs;
+    if (~place < padded)
+      for (uint32_t c = c0; c < p.vecs; c += 64) to[c] = zero;
+    if (p.dloss) {
+      to = p.dx.row<uint4>(i, p.vecs);
+      for (uint32_t c = c0; c < p.vecs; c += 64) to[c] = zero;
+    }
   }
 }
 
@@ -790,41 +849,51 @@ struct FinishParams {
   int32_t hidden_tiles, splits;
   float out_scale;
 };
-// A block takes 32 gathered rows and 256 columns (what two warps of the products' epilogue hold).
+// A block takes 32 gathered rows and 128 columns: what one warp of the products' epilogue holds.
 __global__ void __launch_bounds__(256) head_finish_kernel(const __grid_constant__ FinishParams p) {
-  __shared__ float tile[32][257];
+  __shared__ float tile[32][129];
   wait_for_previous_kernel();
   const int rows = p.found->rows;
   const int row0 = blockIdx.x * 32;
   if (row0 >= rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int cols = p.hidden_tiles * p.splits;
   const float scale = p.out_scale * p.found->top;
+  const int64_t step = int64_t(p.hidden_tiles) * 8 * (32 * 32);            // from one split's sums to the next one's
+  const int64_t frag = (int64_t(row0 >> 7) * p.hidden_tiles * p.splits + (blockIdx.y >> 1)) * 8 + ((row0 >> 5) & 3) * 2 + (blockIdx.y & 1);
+  const float4* in = p.acc + frag * (32 * 32) + warp * 4 * 32 + lane;      // 4 of the 32 groups of 4 columns per warp
+  float4 x[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int g = warp * 8 + i;                 // group of 4 columns among the tile's 64
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < p.splits; ++s) {
-      const int64_t frag = (int64_t(row0 >> 7) * cols + s * p.hidden_tiles + blockIdx.y) * 8 + ((row0 >> 5) & 3) * 2 + (g >> 5);
-      const float4 y = p.acc[frag * (32 * 32) + (g & 31) * 32 + lane];
-      x.x += y.x;
-      x.y += y.y;
-      x.z += y.z;
-      x.w += y.w;
+  for (int i = 0; i < 4; ++i) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 y = __ldcs(in + s * step + i * 32);
+      x[i].x += y.x;
+      x[i].y += y.y;
+      x[i].z += y.z;
+      x[i].w += y.w;
     }
-    tile[lane][g * 4] = x.x * scale;
-    tile[lane][g * 4 + 1] = x.y * scale;
-    tile[lane][g * 4 + 2] = x.z * scale;
-    tile[lane][g * 4 + 3] = x.w * scale;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float* t = &tile[lane][(warp * 4 + i) * 4];
+    t[0] = x[i].x * scale;
+    t[1] = x[i].y * scale;
+    t[2] = x[i].z * scale;
+    t[3] = x[i].w * scale;
   }
   __syncthreads();
-  for (int r = warp; r < 32 && row0 + r < rows; r += 8) {
-    const int64_t c = int64_t(blockIdx.y) * 256 + lane * 8;
-    if (c < p.hidden) {
-      float x[8];
+  // 16 lanes a row, 8 columns each
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = tile[r][lane * 8 + i];
-      store_vec(p.dx.row<__nv_bfloat16>(uint32_t(p.origin[row0 + r]), p.hidden) + c, x);
+  for (int k = 0; k < 2; ++k) {
+    const int r = k * 16 + (threadIdx.x >> 4);
+    const int64_t c = int64_t(blockIdx.y) * 128 + (threadIdx.x & 15) * 8;
+    if (row0 + r < rows && c < p.hidden) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = tile[r][(threadIdx.x & 15) * 8 + i];
+      store_vec(p.dx.row<__nv_bfloat16>(uint32_t(p.origin[row0 + r]), p.hidden) + c, y);
     }
   }
 }
@@ -854,7 +923,7 @@ constexpr int64_t kPieceBytes = int64_t(256) << 20;
 struct HeadPlan {
   int64_t pad;
   int tiles_per_shard, vocab_tiles, hidden_tiles, splits, piece_tiles;
-  size_t ints, part, part_sum, gathered, acc, d;      // sections of the workspace, in bytes
+  size_t ints, chunks, part, part_sum, gathered, acc, d;      // sections of the workspace, in bytes
   size_t bytes;
 };
 HeadPlan head_plan(const compass_head* h, bool backward) {
@@ -875,16 +944,17 @@ HeadPlan head_plan(const compass_head* h, bool backward) {
   q.piece_tiles = int(round_up(size_t(ceil_div(q.vocab_tiles, pieces)), 2));
   if (q.splits > q.piece_tiles) q.splits = q.piece_tiles;
   q.ints = round_up(size_t(q.pad) * 4, 256);
-  q.gathered = size_t(q.pad) * size_t(h->hidden) * 2;
+  q.chunks = round_up(size_t(ceil_div(h->M, kCountRows)) * 4, 256);
+  q.gathered = size_t(h->M) * size_t(h->hidden) * 2;
   if (backward) {
     q.acc = size_t(q.pad / 128) * size_t(q.hidden_tiles) * size_t(q.splits) * (128 * 256 * 4);
     q.d = size_t(q.pad) * size_t(q.piece_tiles) * 512;
-    q.bytes = 512 + 5 * q.ints + round_up(q.gathered, 256) + q.acc + q.d;
+    q.bytes = 512 + 2 * q.chunks + 4 * q.ints + round_up(q.gathered, 256) + q.acc + q.d;
   } else {
     q.part = round_up(size_t(q.pad) * size_t(q.vocab_tiles) * 2 * 8, 256);
     q.part_sum = h->label_smoothing != 0.f ? q.part / 2 : 0;
     q.part_sum = round_up(q.part_sum, 256);
-    q.bytes = 512 + 4 * q.ints + round_up(q.gathered, 256) + q.part + q.part_sum;
+    q.bytes = 512 + 2 * q.chunks + 3 * q.ints + round_up(q.gathered, 256) + q.part + q.part_sum;
   }
   return q;
 }
@@ -963,7 +1033,6 @@ struct Common {
   DeviceFacts* facts;
   uint8_t* at;            // next free byte of the workspace
   RowParams rows;
-  GatherParams2 gather;
   HeadParams p;
   uint8_t* take(size_t n) {
     uint8_t* was = at;
@@ -978,7 +1047,7 @@ int begin(const compass_head* h, const void* const* X, const void* const* W, con
   if (st != COMPASS_OK) return st;
   if (h->M > 0 && targets == nullptr) return COMPASS_ERR_INVALID_ARG;
   if (!is_aligned(targets, h->index_dtype == COMPASS_INDEX_INT64 ? 8 : 4)) return COMPASS_ERR_ALIGNMENT;
-  st = fill_shards(X, h->P, h->M, &c->gather.x);
+  st = fill_shards(X, h->P, h->M, &c->rows.x);
   if (st == COMPASS_OK) st = check_vocab_shards(W, h->P, h->vocab);
   if (st != COMPASS_OK) return st;
   c->q = head_plan(h, backward);
@@ -999,7 +1068,8 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   RowParams& r = c->rows;
   r.targets = targets;
   r.found = found;
-  r.place = reinterpret_cast<int32_t*>(c->take(q.ints));
+  r.counts = reinterpret_cast<int32_t*>(c->take(q.chunks));
+  r.tops = reinterpret_cast<float*>(c->take(q.chunks));
   r.origin = reinterpret_cast<int32_t*>(c->take(q.ints));
   r.target = reinterpret_cast<int32_t*>(c->take(q.ints));
   r.M = uint32_t(h->M);
@@ -1023,30 +1093,27 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   p.vocab = int32_t(h->vocab);
   p.tiles_per_shard = q.tiles_per_shard;
   p.hidden_tiles = q.hidden_tiles;
+  p.one_row_tile = h->M <= 256;
   p.splits = q.splits;
   p.z_scale = h->logit_scale * kLog2e;
   p.out_scale = h->logit_scale;
   p.smoothing = h->label_smoothing;
   p.uniform = float(double(h->label_smoothing) / double(h->vocab));
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
-  bool ok = encode_tensor_map(&p.x_k, gathered, q.pad, h->hidden, 128);
+  // (rows past M are not loaded: they read as zeros)
+  bool ok = encode_tensor_map(&p.x_k, gathered, h->M, h->hidden, 128);
   for (int s = 0; s < h->P; ++s) {
     const int64_t n = rows_of_vocab_shard(h->vocab, h->P, s);
     if (n > 0) ok = ok && encode_tensor_map(&p.w_k[s], W[s], n, h->hidden, 128);
     if (n > 0 && r.dloss) ok = ok && encode_tensor_map(&p.w_mn[s], W[s], n, h->hidden, 64);
   }
-  if (r.dloss) ok = ok && encode_tensor_map(&p.x_mn, gathered, q.pad, h->hidden, 64);
+  if (r.dloss) ok = ok && encode_tensor_map(&p.x_mn, gathered, h->M, h->hidden, 64);
   if (!ok) return record_cuda_error(cudaErrorUnknown);
-  GatherParams2& g = c->gather;
-  g.found = found;
-  g.place = r.place;
-  g.gathered = reinterpret_cast<uint4*>(gathered);
-  g.M = uint32_t(h->M);
-  g.vecs = uint32_t(h->hidden / 8);
-  st = launch(head_rows_kernel, 1, 1024, 0, stream, false, r);
+  r.gathered = reinterpret_cast<uint4*>(gathered);
+  r.vecs = uint32_t(h->hidden / 8);
+  st = launch(head_count_kernel, ceil_div(h->M, kCountRows), 256, 0, stream, false, r);
   if (st != COMPASS_OK) return st;
-  const int64_t most = h->M + 512;
-  return launch(head_gather_kernel, most < 2048 ? most : 2048, 256, 0, stream, true, g);
+  return launch(head_gather_kernel, ceil_div(h->M, kGatherRows), 256, 0, stream, true, r);
 }
 
 // Tiles of a form at most, counted as 256 x 256.
@@ -1108,7 +1175,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
   if (st != COMPASS_OK) return st;
   if (h->M > 0 && (lse == nullptr || dloss == nullptr)) return COMPASS_ERR_INVALID_ARG;
   if (!is_aligned(lse, 4) || !is_aligned(dloss, 4)) return COMPASS_ERR_ALIGNMENT;
-  st = fill_shards(dX, h->P, h->M, &c.gather.dx);
+  st = fill_shards(dX, h->P, h->M, &c.rows.dx);
   if (st == COMPASS_OK) st = check_vocab_shards(dW, h->P, h->vocab);
   if (st != COMPASS_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -1123,7 +1190,6 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
   }
   c.rows.lse = lse;
   c.rows.dloss = dloss;
-  c.gather.zero_dx = 1;
   st = gather_rows(h, W, targets, ws, &c, s);
   if (st != COMPASS_OK) return st;
   const HeadPlan& q = c.q;
@@ -1137,7 +1203,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
     p.dw[r] = dW[r];
     if (!is_aligned(dW[r], 32)) p.dw_wide = 0;
   }
-  if (!encode_tensor_map(&p.d_k, p.d, q.pad, p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, q.pad, p.piece_cols, 64))
+  if (!encode_tensor_map(&p.d_k, p.d, h->M, p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, h->M, p.piece_cols, 64))
     return record_cuda_error(cudaErrorUnknown);
   for (int vt = 0; vt < q.vocab_tiles; vt += q.piece_tiles) {
     p.vt0 = vt;
@@ -1149,7 +1215,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
     if (st != COMPASS_OK) return st;
   }
   FinishParams f = {};
-  f.dx = c.gather.dx;
+  f.dx = c.rows.dx;
   f.found = p.found;
   f.origin = c.rows.origin;
   f.acc = p.acc;
@@ -1158,7 +1224,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
   f.splits = q.splits;
   f.out_scale = p.out_scale;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(ceil_div(h->M, 32)), unsigned(q.hidden_tiles));
+  cfg.gridDim = dim3(unsigned(ceil_div(h->M, 32)), unsigned(2 * q.hidden_tiles));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr;

@@ -13,6 +13,11 @@ namespace compass {
 
 namespace {
 
+// Elements of a row per thread: what a row costs every thread (sums over the row, addresses) is shared by this many.  16 where
+// they are loaded packed, two to a register; 8 in FP32 and in rows that are not whole vectors.
+template <typename T, int V>
+constexpr int kElems = V == 8 ? 16 : 8;
+
 struct NormParams {
   RowShards x, residual, summed, y;      // forward
   RowShards dy, dsum, dx;                // backward (x above: the normalised input)
@@ -58,132 +63,219 @@ __device__ __forceinline__ void load_param(float (&out)[V], const void* p, bool 
   }
 }
 
-// Sum of two values over the `tpr` threads of a row; every thread gets it.  `red`: two floats per warp of the block, a
-// buffer that no earlier call since the last barrier used.  All threads of the block take part.
+// Sum of two values over the `tpr` threads of a row; every thread gets it.  `red`: a float2 per warp of the block, a buffer
+// that no call since the last but one used.  The rows of a block do not wait for one another: each has a barrier of its own.
 __device__ __forceinline__ float2 row_sum(float a, float b, int tpr, float2* red) {
   a = warp_sum(a);
   b = warp_sum(b);
   if (tpr == 32) return make_float2(a, b);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n = tpr >> 5, group = warp / n;
   if (lane == 0) red[warp] = make_float2(a, b);
-  __syncthreads();
-  const int n = tpr >> 5, first = warp / n * n;
-  const float2 v = lane < n ? red[first + lane] : make_float2(0.f, 0.f);
+  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
+  const float2 v = lane < n ? red[group * n + lane] : make_float2(0.f, 0.f);
   return make_float2(warp_sum(v.x), warp_sum(v.y));
 }
 
-// ---- forward -------------------------------------------------------------------
-// One row per group of `tpr` threads, NVT vectors of V elements per thread, all in registers.
+__device__ __forceinline__ float row_sum(float a, int tpr, float* red) {
+  a = warp_sum(a);
+  if (tpr == 32) return a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n = tpr >> 5, group = warp / n;
+  if (lane == 0) red[warp] = a;
+  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
+  return warp_sum(lane < n ? red[group * n + lane] : 0.f);
+}
+
+// NVT vectors of V elements of type T, a word per 4 bytes, and their values two by two.  (BF16 in rows that are not whole
+// vectors: an element a word.)
 template <typename T, int V, int NVT>
-__global__ void __launch_bounds__(1024) norm_forward_kernel(const __grid_constant__ NormParams p) {
-  __shared__ float2 red[2][32];
-  const int t = threadIdx.x % p.tpr;
-  const uint32_t row = uint32_t(blockIdx.x) * (blockDim.x / p.tpr) + threadIdx.x / p.tpr;
-  const bool live = row < p.M;
-  const int64_t H = p.hidden;
-  float h[NVT][V];
-  float sum = 0.f;
-  if (live) {
-    const T* x = p.x.row<T>(row, H);
-    const T* r = p.has_residual ? p.residual.row<T>(row, H) : nullptr;
-    T* s = p.has_residual ? p.summed.row<T>(row, H) : nullptr;
-    Raw<T, V> xr[NVT], rr[NVT];
-#pragma unroll
-    for (int i = 0; i < NVT; ++i) {
-      const int64_t c = int64_t(i * p.tpr + t) * V;
-      xr[i].zero();
-      rr[i].zero();
-      if (c < H) {
-        xr[i].load(x + c);
-        if (r) rr[i].load(r + c);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NVT; ++i) {
-      const int64_t c = int64_t(i * p.tpr + t) * V;
-      xr[i].get(h[i]);
-      if (r) {
-        float b[V];
-        rr[i].get(b);
-        // what is stored is normalised, so that the backward pass, which reads it, sees the same values
-#pragma unroll
-        for (int j = 0; j < V; ++j) h[i][j] = round_to<T>(h[i][j] + b[j]);
-        if (c < H) store_vec(s + c, h[i]);
-      }
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum += h[i][j];
+struct Words {
+  static constexpr int kPer = V * int(sizeof(T)) >= 4 ? V * int(sizeof(T)) / 4 : 1;
+  static constexpr int kPairs = V * NVT / 2;
+  uint32_t w[NVT][kPer];
+  __device__ __forceinline__ F2 pair(int k) const {
+    if constexpr (V == 8) {
+      const uint32_t q = w[k / 4][k % 4];
+      return f2(__uint_as_float(q << 16), __uint_as_float(q & 0xFFFF0000u));
+    } else if constexpr (sizeof(T) == 2) {
+      return f2(__uint_as_float(w[2 * k][0] << 16), __uint_as_float(w[2 * k + 1][0] << 16));
+    } else {
+      return f2(__uint_as_float(w[2 * k / V][2 * k % V]), __uint_as_float(w[(2 * k + 1) / V][(2 * k + 1) % V]));
     }
   }
-  const float inv = 1.0f / float(H);
-  const float mean = row_sum(sum, 0.f, p.tpr, red[0]).x * inv;
-  float sq = 0.f;
-  if (live) {
+  // a + b, rounded to T
+  __device__ __forceinline__ void add(const Words& o) {
 #pragma unroll
     for (int i = 0; i < NVT; ++i)
-      if (int64_t(i * p.tpr + t) * V < H) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          h[i][j] -= mean;
-          sq = fmaf(h[i][j], h[i][j], sq);
-        }
+      for (int k = 0; k < kPer; ++k) {
+        if constexpr (sizeof(T) == 2) asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(w[i][k]) : "r"(w[i][k]), "r"(o.w[i][k]));
+        else w[i][k] = __float_as_uint(__uint_as_float(w[i][k]) + __uint_as_float(o.w[i][k]));
       }
   }
-  const float var = row_sum(sq, 0.f, p.tpr, red[1]).x * inv;
-  const float rstd = 1.0f / sqrtf(var + p.eps);
-  if (!live) return;
-  T* y = p.y.row<T>(row, H);
+  __device__ __forceinline__ void set(const F2 (&v)[kPairs]) {
 #pragma unroll
-  for (int i = 0; i < NVT; ++i) {
-    const int64_t c = int64_t(i * p.tpr + t) * V;
-    if (c < H) {
-      float g[V], b[V];
-      load_param(g, p.gamma, p.param_fp32, c, 1.f);
-      load_param(b, p.beta, p.param_fp32, c, 0.f);
-#pragma unroll
-      for (int j = 0; j < V; ++j) g[j] = fmaf(h[i][j] * rstd, g[j], b[j]);
-      store_vec(y + c, g);
+    for (int k = 0; k < kPairs; ++k) {
+      const float2 q = of(v[k]);
+      if constexpr (V == 8) {
+        w[k / 4][k % 4] = bf16x2_of(q.x, q.y);
+      } else if constexpr (sizeof(T) == 2) {
+        w[2 * k][0] = bf16x2_of(q.x, 0.f);
+        w[2 * k + 1][0] = bf16x2_of(q.y, 0.f);
+      } else {
+        w[2 * k / V][2 * k % V] = __float_as_uint(q.x);
+        w[(2 * k + 1) / V][(2 * k + 1) % V] = __float_as_uint(q.y);
+      }
     }
   }
-  if (t == 0) {
-    if (p.mean) p.mean[row] = mean;
-    if (p.rstd) p.rstd[row] = rstd;
+  __device__ __forceinline__ void store(T* row, int tpr, int t, int H) const {
+#pragma unroll
+    for (int i = 0; i < NVT; ++i) {
+      const int c = (i * tpr + t) * V;
+      if (c < H) {
+        if constexpr (kPer == 4) *reinterpret_cast<uint4*>(row + c) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+        else if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(row + c) = w[i][0];
+        else *reinterpret_cast<unsigned short*>(row + c) = static_cast<unsigned short>(w[i][0]);
+      }
+    }
+  }
+};
+// A row's gamma or beta, two by two.
+template <int V, int NVT>
+__device__ __forceinline__ void load_params(F2 (&out)[V * NVT / 2], const void* p, bool fp32, float none, int tpr, int t, int H) {
+  float v[NVT][V];
+#pragma unroll
+  for (int i = 0; i < NVT; ++i) {
+    const int c = (i * tpr + t) * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[i][j] = 0.f;
+    if (c < H) load_param(v[i], p, fp32, c, none);
+  }
+#pragma unroll
+  for (int k = 0; k < V * NVT / 2; ++k) out[k] = f2(v[2 * k / V][2 * k % V], v[(2 * k + 1) / V][(2 * k + 1) % V]);
+}
+
+// ---- forward -------------------------------------------------------------------
+// A row per group of `tpr` threads, NVT vectors of V elements a thread, all in registers; the rows after it are on their way
+// meanwhile.  kKeep: gamma and beta stay in registers too.
+template <typename T, int V, int NVT, int kThreads, bool kKeep, bool kResidual>
+__global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_constant__ NormParams p) {
+  using Ring = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>;
+  __shared__ float red[4][32];
+  extern __shared__ uint4 raw[];
+  const int groups = blockDim.x / p.tpr, group = threadIdx.x / p.tpr, t = threadIdx.x - group * p.tpr;
+  const int H = int(p.hidden);
+  const float inv = 1.0f / float(H);
+  Ring ring(raw);
+  auto fetch = [&](int which, uint32_t row) {
+    const bool live = row < p.M;
+    const RowAt at = p.x.at(row, H);
+    if constexpr (kResidual) {
+      const T* const from[2] = {live ? p.x.row<T>(at) : nullptr, live ? p.residual.row<T>(at) : nullptr};
+      ring.fetch(which, from, p.tpr, t, H);
+    } else {
+      const T* const from[1] = {live ? p.x.row<T>(at) : nullptr};
+      ring.fetch(which, from, p.tpr, t, H);
+    }
+  };
+  const uint32_t stride = gridDim.x * groups;
+  uint32_t row = blockIdx.x * groups + group;
+#pragma unroll 1
+  for (int k = 0; k < Ring::kDepth; ++k) fetch(k, row + k * stride);
+  constexpr int kPairs = V * NVT / 2;
+  F2 g[kPairs], b[kPairs];
+  if constexpr (kKeep) {
+    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
+    load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, p.tpr, t, H);
+  }
+  const int own = min(NVT, max(0, (H / V - t + p.tpr - 1) / p.tpr)) * V;      // elements of a row that this thread holds
+  for (uint32_t turn = 0; row < p.M; ++turn, row += stride) {
+    const RowAt at = p.x.at(row, H);
+    Words<T, V, NVT> x;
+    ring.wait();
+#pragma unroll
+    for (int i = 0; i < NVT; ++i) ring.take(x.w[i], 0, i, p.tpr, t, H);
+    if constexpr (kResidual) {
+      // what is stored is normalised, so that the backward pass, which reads it, sees the same values
+      Words<T, V, NVT> r;
+#pragma unroll
+      for (int i = 0; i < NVT; ++i) ring.take(r.w[i], 1, i, p.tpr, t, H);
+      x.add(r);
+      x.store(p.summed.row<T>(at), p.tpr, t, H);
+    }
+    ring.advance();
+    fetch(Ring::kDepth - 1, row + Ring::kDepth * stride);
+    F2 h[kPairs], sum[2] = {f2(0.f), f2(0.f)};
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      h[k] = x.pair(k);
+      sum[k & 1] = sum[k & 1] + h[k];
+    }
+    const float mean = row_sum(sum_of(sum[0] + sum[1]), p.tpr, red[2 * (turn & 1)]) * inv;
+    F2 sq[2] = {f2(0.f), f2(0.f)};
+    const F2 minus = f2(-mean);
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      h[k] = h[k] + minus;
+      if (2 * k + 1 >= own) h[k] = 2 * k < own ? f2(of(h[k]).x, 0.f) : f2(0.f);      // past the row's end
+      sq[k & 1] = fma2(h[k], h[k], sq[k & 1]);
+    }
+    const float var = row_sum(sum_of(sq[0] + sq[1]), p.tpr, red[2 * (turn & 1) + 1]) * inv;
+    const float rstd = 1.0f / sqrtf(var + p.eps);
+    if constexpr (!kKeep) {
+      load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
+      load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, p.tpr, t, H);
+    }
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) h[k] = fma2(h[k] * f2(rstd), g[k], b[k]);
+    x.set(h);
+    x.store(p.y.row<T>(at), p.tpr, t, H);
+    if (t == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
   }
 }
 
 // Rows that do not fit the registers of a block: one block per row, three passes over it (the later ones out of L2).
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const __grid_constant__ NormParams p) {
-  __shared__ float2 red[2][32];
+  __shared__ float red[2][32];
   const uint32_t row = blockIdx.x;
   const int64_t H = p.hidden;
   const T* x = p.x.row<T>(row, H);
   const T* r = p.has_residual ? p.residual.row<T>(row, H) : nullptr;
   T* s = p.has_residual ? p.summed.row<T>(row, H) : nullptr;
-  float a[1], b[1], sum = 0.f, sq = 0.f;
-  for (int64_t c = threadIdx.x; c < H; c += blockDim.x) {
+  float a[V], b[V], sum = 0.f, sq = 0.f;
+  for (int64_t c = threadIdx.x * V; c < H; c += 1024 * V) {
     load_vec(a, x + c);
     if (r) {
       load_vec(b, r + c);
-      a[0] = round_to<T>(a[0] + b[0]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) a[j] = round_to<T>(a[j] + b[j]);
       store_vec(s + c, a);
     }
-    sum += a[0];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += a[j];
   }
   const T* h = r ? s : x;       // a thread reads back only what it wrote itself
   const float inv = 1.0f / float(H);
-  const float mean = row_sum(sum, 0.f, p.tpr, red[0]).x * inv;
-  for (int64_t c = threadIdx.x; c < H; c += blockDim.x) {
+  const float mean = row_sum(sum, 1024, red[0]) * inv;
+  for (int64_t c = threadIdx.x * V; c < H; c += 1024 * V) {
     load_vec(a, h + c);
-    sq = fmaf(a[0] - mean, a[0] - mean, sq);
+#pragma unroll
+    for (int j = 0; j < V; ++j) sq = fmaf(a[j] - mean, a[j] - mean, sq);
   }
-  const float rstd = 1.0f / sqrtf(row_sum(sq, 0.f, p.tpr, red[1]).x * inv + p.eps);
+  const float rstd = 1.0f / sqrtf(row_sum(sq, 1024, red[1]) * inv + p.eps);
   T* y = p.y.row<T>(row, H);
-  for (int64_t c = threadIdx.x; c < H; c += blockDim.x) {
-    float g[1];
+  for (int64_t c = threadIdx.x * V; c < H; c += 1024 * V) {
+    float g[V];
     load_vec(a, h + c);
     load_param(g, p.gamma, p.param_fp32, c, 1.f);
     load_param(b, p.beta, p.param_fp32, c, 0.f);
-    a[0] = fmaf((a[0] - mean) * rstd, g[0], b[0]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) a[j] = fmaf((a[j] - mean) * rstd, g[j], b[j]);
     store_vec(y + c, a);
   }
   if (threadIdx.x == 0) {
@@ -193,120 +285,106 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const __grid_co
 }
 
 // ---- backward ------------------------------------------------------------------
-// One block per SM walks the rows; a thread keeps its columns' sums of dY * xhat and dY in registers and has the next
-// row's loads in flight while it works on this one.  The block's groups add their sums up in shared memory and leave one
-// partial row each for norm_reduce_kernel: fixed order, so the bits do not depend on timing.
-constexpr int kBackThreads = 512;
-constexpr int kBackElems = 16;      // elements of a row per thread
-
-template <typename T, int V, int NVT>
-__global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __grid_constant__ NormParams p) {
-  static_assert(V * NVT <= kBackElems, "");
+// One block per SM walks the rows; a thread keeps its columns' sums of dY * xhat and dY in registers while the next rows are
+// on their way.  A block's rows add their sums up in shared memory and leave one partial row for norm_reduce_kernel: fixed
+// order, so the bits do not depend on timing.
+template <typename T, int V, int NVT, int kThreads, bool kDsum>
+__global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid_constant__ NormParams p) {
+  static_assert(V * NVT == kElems<T, V>, "");
+  using Ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>;
   __shared__ float2 red[2][32];
-  extern __shared__ float sums[];           // [groups][hidden], only with more than one group
-  const int groups = blockDim.x / p.tpr, group = threadIdx.x / p.tpr, t = threadIdx.x % p.tpr;
-  const int64_t H = p.hidden;
+  extern __shared__ uint4 raw[];
+  const int groups = blockDim.x / p.tpr, group = threadIdx.x / p.tpr, t = threadIdx.x - group * p.tpr;
+  const int H = int(p.hidden);
   const float inv = 1.0f / float(H);
-  float g[NVT][V], dg[NVT][V], db[NVT][V];
+  constexpr int kPairs = V * NVT / 2;
+  F2 dg[kPairs], db[kPairs];
 #pragma unroll
-  for (int i = 0; i < NVT; ++i) {
-    const int64_t c = int64_t(i * p.tpr + t) * V;
-    if (c < H) load_param(g[i], p.gamma, p.param_fp32, c, 1.f);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      if (c >= H) g[i][j] = 0.f;
-      dg[i][j] = db[i][j] = 0.f;
-    }
-  }
-  Raw<T, V> xr[NVT], yr[NVT], sr[NVT];
-  float mean = 0.f, rstd = 0.f;
-  auto fetch = [&](uint32_t row) {
+  for (int k = 0; k < kPairs; ++k) dg[k] = db[k] = f2(0.f);
+  const int own = min(NVT, max(0, (H / V - t + p.tpr - 1) / p.tpr)) * V;      // elements of a row that this thread holds
+  Ring ring(raw);
+  auto fetch = [&](int which, uint32_t row) {
     const bool live = row < p.M;
-    const T* x = live ? p.x.row<T>(row, H) : nullptr;
-    const T* dy = live ? p.dy.row<T>(row, H) : nullptr;
-    const T* ds = live && p.has_dsum ? p.dsum.row<T>(row, H) : nullptr;
-#pragma unroll
-    for (int i = 0; i < NVT; ++i) {
-      const int64_t c = int64_t(i * p.tpr + t) * V;
-      xr[i].zero();
-      yr[i].zero();
-      sr[i].zero();
-      if (live && c < H) {
-        xr[i].load(x + c);
-        yr[i].load(dy + c);
-        if (ds) sr[i].load(ds + c);
-      }
+    const RowAt at = p.x.at(row, H);
+    if constexpr (kDsum) {
+      const T* const from[3] = {live ? p.x.row<T>(at) : nullptr, live ? p.dy.row<T>(at) : nullptr, live ? p.dsum.row<T>(at) : nullptr};
+      ring.fetch(which, from, p.tpr, t, H);
+    } else {
+      const T* const from[2] = {live ? p.x.row<T>(at) : nullptr, live ? p.dy.row<T>(at) : nullptr};
+      ring.fetch(which, from, p.tpr, t, H);
     }
-    mean = live ? p.mean[row] : 0.f;
-    rstd = live ? p.rstd[row] : 0.f;
   };
   const uint32_t stride = gridDim.x * groups;
   uint32_t row = blockIdx.x * groups + group;
-  fetch(row);
-  // every group takes the same number of turns: the row sums have barriers in them
-  const uint32_t turns = (p.M - blockIdx.x * groups + stride - 1) / stride;
-  for (uint32_t turn = 0; turn < turns; ++turn, row += stride) {
-    float xh[NVT][V], d[NVT][V], s[NVT][V];
-    const float r = rstd, m = mean;
-    float c1 = 0.f, c2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < NVT; ++i) {
-      const bool in = int64_t(i * p.tpr + t) * V < H;
-      xr[i].get(xh[i]);
-      yr[i].get(d[i]);
-      sr[i].get(s[i]);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        xh[i][j] = in ? (xh[i][j] - m) * r : 0.f;
-        dg[i][j] = fmaf(d[i][j], xh[i][j], dg[i][j]);
-        db[i][j] += d[i][j];
-        d[i][j] *= g[i][j];
-        c1 += d[i][j];
-        c2 = fmaf(d[i][j], xh[i][j], c2);
-      }
+#pragma unroll 1
+  for (int k = 0; k < Ring::kDepth; ++k) fetch(k, row + k * stride);
+  float mean = row < p.M ? p.mean[row] : 0.f, rstd = row < p.M ? p.rstd[row] : 0.f;
+  for (uint32_t turn = 0; row < p.M; ++turn, row += stride) {
+    F2 xh[kPairs], d[kPairs];
+    const float r = rstd;
+    const F2 minus = f2(-mean), r2 = f2(r);
+    const RowAt at = p.x.at(row, H);
+    if (row + stride < p.M) {
+      mean = p.mean[row + stride];
+      rstd = p.rstd[row + stride];
     }
-    const bool live = row < p.M;
-    fetch(row + stride);
-    const float2 c = row_sum(c1, c2, p.tpr, red[turn & 1]);
-    if (live) {
-      T* dx = p.dx.row<T>(row, H);
+    Words<T, V, NVT> w;
+    ring.wait();
 #pragma unroll
-      for (int i = 0; i < NVT; ++i) {
-        const int64_t col = int64_t(i * p.tpr + t) * V;
-        if (col < H) {
+    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 0, i, p.tpr, t, H);
 #pragma unroll
-          for (int j = 0; j < V; ++j) d[i][j] = fmaf(r, d[i][j] - c.x * inv - xh[i][j] * (c.y * inv), s[i][j]);
-          store_vec(dx + col, d[i]);
-        }
-      }
+    for (int k = 0; k < kPairs; ++k) {
+      xh[k] = (w.pair(k) + minus) * r2;
+      if (2 * k + 1 >= own) xh[k] = 2 * k < own ? f2(of(xh[k]).x, 0.f) : f2(0.f);      // past the row's end
     }
+#pragma unroll
+    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 1, i, p.tpr, t, H);
+    load_params<V, NVT>(d, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);      // (from the L1 cache; kept in registers they would spill)
+    F2 c1 = f2(0.f), c2 = f2(0.f);
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      const F2 dy = w.pair(k);
+      dg[k] = fma2(dy, xh[k], dg[k]);
+      db[k] = db[k] + dy;
+      d[k] = d[k] * dy;
+      c1 = c1 + d[k];
+      c2 = fma2(d[k], xh[k], c2);
+    }
+    const float2 c = row_sum(sum_of(c1), sum_of(c2), p.tpr, red[turn & 1]);
+    const F2 a1 = f2(-c.x * inv), a2 = f2(-c.y * inv);
+    if constexpr (kDsum) {
+#pragma unroll
+      for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 2, i, p.tpr, t, H);
+    }
+    ring.advance();
+    fetch(Ring::kDepth - 1, row + Ring::kDepth * stride);
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      const F2 v = fma2(xh[k], a2, d[k] + a1);
+      d[k] = kDsum ? fma2(v, r2, w.pair(k)) : v * r2;
+    }
+    w.set(d);
+    w.store(p.dx.row<T>(at), p.tpr, t, H);
   }
+  float* sums = reinterpret_cast<float*>(raw);      // [groups][hidden], over the ring, whose last copies were of no row
+  asm volatile("cp.async.wait_all;" ::: "memory");
   // this block's sums, one array after the other through shared memory
   launch_dependents();
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float* out = p.partial + (int64_t(which) * p.n_partial + blockIdx.x) * H;
-    if (groups == 1) {
+    if (groups > 1) __syncthreads();
 #pragma unroll
-      for (int i = 0; i < NVT; ++i) {
-        const int64_t c = int64_t(i * p.tpr + t) * V;
-        if (c < H) {
+    for (int k = 0; k < kPairs; ++k)
 #pragma unroll
-          for (int j = 0; j < V; ++j) out[c + j] = which ? db[i][j] : dg[i][j];
-        }
+      for (int e = 0; e < 2; ++e) {
+        const int c = ((2 * k + e) / V * p.tpr + t) * V + (2 * k + e) % V;
+        const float2 q = of(which ? db[k] : dg[k]);
+        if (c < H) (groups > 1 ? sums + group * H : out)[c] = e ? q.y : q.x;
       }
-    } else {
+    if (groups > 1) {
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NVT; ++i) {
-        const int64_t c = int64_t(i * p.tpr + t) * V;
-        if (c < H) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) sums[group * H + c + j] = which ? db[i][j] : dg[i][j];
-        }
-      }
-      __syncthreads();
-      for (int64_t c = threadIdx.x; c < H; c += blockDim.x) {
+      for (int c = threadIdx.x; c < H; c += blockDim.x) {
         float a = 0.f;
         for (int k = 0; k < groups; ++k) a += sums[k * H + c];
         out[c] = a;
@@ -405,68 +483,86 @@ bool vectorised(const compass_norm* n) { return n->hidden % (n->dtype == COMPASS
 
 // Threads per row, a multiple of 32, when each holds `elems` elements.
 int threads_per_row(int64_t hidden, int elems) { return int(round_up(size_t(ceil_div(hidden, elems)), 32)); }
+// Rows a block of at most `threads` works on side by side (each has a named barrier: 8 at most).
+int rows_per_block(int tpr, int threads) { return tpr * 8 >= threads ? threads / tpr : 8; }
 
-// The backward pass keeps a row in the registers of at most kBackThreads threads.
-constexpr int64_t kBackWidest = int64_t(kBackThreads) * kBackElems;
+constexpr int kSms = 148;           // blocks are counted for a B200; fewer SMs only take them in turns
+constexpr int64_t kWidest = 8192;   // elements of a row that stay in the registers of a block
 constexpr int kWideParts = 64;      // row ranges of the wide form's column sums
 
 struct BackwardPlan {
   bool wide;
-  int tpr, groups, grid, n_partial;
+  int tpr, groups, threads, n_partial;
 };
-int backward_plan(const compass_norm* n, BackwardPlan* b) {
-  int sms = 0;
-  const int st = sm_count(&sms);
-  if (st != COMPASS_OK) return st;
-  b->wide = n->hidden > kBackWidest;
-  if (b->wide) {
-    b->tpr = 1024;
-    b->groups = 1;
-    b->n_partial = int(n->M < kWideParts ? n->M : kWideParts);
-    b->grid = 0;
-    return COMPASS_OK;
-  }
-  b->tpr = threads_per_row(n->hidden, kBackElems);
-  b->groups = kBackThreads / b->tpr;
-  const int64_t need = ceil_div(n->M, b->groups);
-  b->grid = int(need < sms ? need : sms);
-  b->n_partial = b->grid;
-  return COMPASS_OK;
+BackwardPlan backward_plan(const compass_norm* n) {
+  BackwardPlan b;
+  const bool packed = n->dtype == COMPASS_DTYPE_BF16 && vectorised(n);
+  b.wide = n->hidden > kWidest;
+  b.tpr = b.wide ? 1024 : threads_per_row(n->hidden, packed ? 16 : 8);
+  b.threads = b.tpr > 512 ? 1024 : 512;        // 128 registers a thread unless a row needs more than 512 threads
+  b.groups = b.wide ? 1 : rows_per_block(b.tpr, b.threads);
+  const int64_t most = b.wide ? kWideParts : kSms;
+  const int64_t need = b.wide ? n->M : ceil_div(n->M, b.groups);
+  b.n_partial = int(need < most ? need : most);
+  return b;
 }
 
-template <typename T, int V, int NVT>
+template <typename T, int V, int NVT, int kThreads, bool kKeep, bool kResidual>
 int run_forward(const NormParams& p, int tpr, cudaStream_t stream) {
+  constexpr size_t smem = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>::kSmemBytes;
+  auto kernel = norm_forward_kernel<T, V, NVT, kThreads, kKeep, kResidual>;
+  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem);
+  if (st != COMPASS_OK) return st;
   NormParams q = p;
   q.tpr = tpr;
-  const int groups = tpr >= 128 ? 1 : 128 / tpr;
-  return launch(norm_forward_kernel<T, V, NVT>, ceil_div(p.M, groups), tpr * groups, 0, stream, false, q);
+  // few rows: a block each, for the shortest way through; else blocks of several that walk the rows
+  const int groups = p.M <= kSms || tpr * 2 > kThreads ? 1 : rows_per_block(tpr, kThreads);
+  const int64_t need = ceil_div(p.M, groups), most = smem ? kSms : kSms * (kThreads / (tpr * groups));
+  return launch(kernel, need < most ? need : most, tpr * groups, smem, stream, false, q);
 }
 
-// Elements per thread: few where rows are few (latency: more threads a row, shorter chains), else 16 (32 where a row would
-// need more than 1024 threads).
-template <typename T, int V>
-int pick_forward(const NormParams& p, int sms, cudaStream_t stream) {
+// Up to 8192 elements a row: gamma and beta in registers.  Up to 16384: 16 elements per thread.
+template <typename T, int V, bool kResidual>
+int pick_forward(const NormParams& p, cudaStream_t stream) {
   const int64_t H = p.hidden;
-  constexpr int one = V == 1 ? 4 : V, two = V == 1 ? 16 : 16, four = 32;
-  if (int64_t(p.M) <= 2 * sms && H <= one * 1024) return run_forward<T, V, one / V>(p, threads_per_row(H, one), stream);
-  if (H <= two * 512) return run_forward<T, V, two / V>(p, threads_per_row(H, two), stream);
-  return run_forward<T, V, four / V>(p, threads_per_row(H, four), stream);
+  constexpr int E = kElems<T, V>, kThreads = int(kWidest) / E;
+  if (H <= kWidest) return run_forward<T, V, E / V, kThreads, true, kResidual>(p, threads_per_row(H, E), stream);
+  return run_forward<T, V, 16 / V, 1024, false, kResidual>(p, threads_per_row(H, 16), stream);
+}
+template <typename T, int V>
+int pick_forward(const NormParams& p, cudaStream_t stream) {
+  return p.has_residual ? pick_forward<T, V, true>(p, stream) : pick_forward<T, V, false>(p, stream);
 }
 
 template <typename T>
-int forward_of(const NormParams& p, bool vec, int sms, cudaStream_t stream) {
-  if (p.hidden > 32 * 1024) {
+int forward_of(const NormParams& p, bool vec, cudaStream_t stream) {
+  if (p.hidden > 2 * kWidest) {
     NormParams q = p;
     q.tpr = 1024;
-    return launch(norm_forward_wide_kernel<T>, p.M, 1024, 0, stream, false, q);
+    return vec ? launch(norm_forward_wide_kernel<T, 16 / int(sizeof(T))>, p.M, 1024, 0, stream, false, q)
+               : launch(norm_forward_wide_kernel<T, 1>, p.M, 1024, 0, stream, false, q);
   }
-  return vec ? pick_forward<T, 16 / int(sizeof(T))>(p, sms, stream) : pick_forward<T, 1>(p, sms, stream);
+  return vec ? pick_forward<T, 16 / int(sizeof(T))>(p, stream) : pick_forward<T, 1>(p, stream);
 }
 
-template <typename T, int V, int NVT>
+template <typename T, int V, int kThreads, bool kDsum>
 int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
-  return launch(norm_backward_kernel<T, V, NVT>, b.grid, b.tpr * b.groups, b.groups > 1 ? size_t(b.groups) * p.hidden * 4 : 0, stream,
-                false, p);
+  constexpr int NVT = kElems<T, V> / V;
+  constexpr size_t ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>::kSmemBytes;
+  auto kernel = norm_backward_kernel<T, V, NVT, kThreads, kDsum>;
+  const size_t sums = b.groups > 1 ? size_t(b.groups) * p.hidden * 4 : 0, smem = ring > sums ? ring : sums;
+  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem);
+  if (st != COMPASS_OK) return st;
+  return launch(kernel, b.n_partial, b.tpr * b.groups, smem, stream, false, p);
+}
+template <typename T, int V, int kThreads>
+int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
+  return p.has_dsum ? run_backward<T, V, kThreads, true>(p, b, stream) : run_backward<T, V, kThreads, false>(p, b, stream);
+}
+template <typename T, int V>
+int pick_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
+  if constexpr (V == 8) return run_backward<T, V, 512>(p, b, stream);
+  else return b.threads == 512 ? run_backward<T, V, 512>(p, b, stream) : run_backward<T, V, 1024>(p, b, stream);
 }
 
 template <typename T>
@@ -487,11 +583,16 @@ int backward_of(const NormParams& p, const BackwardPlan& b, bool vec, cudaStream
     count_kernel_launch();
     return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
   }
-  constexpr int V = 16 / int(sizeof(T));
-  return vec ? run_backward<T, V, kBackElems / V>(p, b, stream) : run_backward<T, 1, kBackElems>(p, b, stream);
+  return vec ? pick_backward<T, 16 / int(sizeof(T))>(p, b, stream) : pick_backward<T, 1>(p, b, stream);
 }
 
 }  // namespace
+
+int allow_smem(const void* kernel, size_t bytes) {
+  if (bytes <= 48 * 1024) return COMPASS_OK;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}
 
 int sm_count(int* out) {
   constexpr int kMaxDevices = 64;
@@ -527,9 +628,6 @@ extern "C" int compass_layer_norm(const compass_norm* n, const void* const* X, c
   if (st != COMPASS_OK) return st;
   if (!is_aligned(gamma, 16) || !is_aligned(beta, 16) || !is_aligned(mean, 4) || !is_aligned(rstd, 4)) return COMPASS_ERR_ALIGNMENT;
   if (n->M == 0) return COMPASS_OK;
-  int sms = 0;
-  st = sm_count(&sms);
-  if (st != COMPASS_OK) return st;
   p.gamma = gamma;
   p.beta = beta;
   p.mean = mean;
@@ -540,7 +638,7 @@ extern "C" int compass_layer_norm(const compass_norm* n, const void* const* X, c
   p.param_fp32 = n->param_dtype == COMPASS_DTYPE_FP32;
   p.eps = n->eps;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return n->dtype == COMPASS_DTYPE_FP32 ? forward_of<float>(p, vectorised(n), sms, s) : forward_of<__nv_bfloat16>(p, vectorised(n), sms, s);
+  return n->dtype == COMPASS_DTYPE_FP32 ? forward_of<float>(p, vectorised(n), s) : forward_of<__nv_bfloat16>(p, vectorised(n), s);
 }
 
 // Workspace: the partial column sums, then (wide rows) two sums per row.
@@ -548,11 +646,8 @@ extern "C" int compass_layer_norm_workspace_bytes(const compass_norm* n, size_t*
   if (bytes == nullptr) return COMPASS_ERR_INVALID_ARG;
   const int st = check_norm(n);
   if (st != COMPASS_OK) return st;
-  // an upper bound that needs no device: a block per SM at most (kWideParts row ranges with wide rows)
-  const bool wide = n->hidden > kBackWidest;
-  const int64_t parts = wide ? kWideParts : 256;
-  const int64_t most = n->M < parts ? n->M : parts;
-  *bytes = 256 + round_up(size_t(2 * most) * size_t(n->hidden) * 4, 256) + (wide ? size_t(n->M) * 8 : 0);
+  const BackwardPlan b = backward_plan(n);
+  *bytes = 256 + round_up(size_t(2 * b.n_partial) * size_t(n->hidden) * 4, 256) + (b.wide ? size_t(n->M) * 8 : 0);
   return COMPASS_OK;
 }
 
@@ -582,10 +677,7 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
       }
     return COMPASS_OK;
   }
-  BackwardPlan b;
-  st = backward_plan(n, &b);
-  if (st != COMPASS_OK) return st;
-  if (b.n_partial > 256) return COMPASS_ERR_UNSUPPORTED;
+  const BackwardPlan b = backward_plan(n);
   p.gamma = gamma;
   p.mean = const_cast<float*>(mean);
   p.rstd = const_cast<float*>(rstd);

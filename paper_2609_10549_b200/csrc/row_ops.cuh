@@ -10,14 +10,40 @@
 
 namespace compass {
 
-// Activations split by rows over the ranks.  A 32-bit division finds the shard: M <= 2^30.
+// Division of n < 2^31 by a divisor that the host knows: (n * mul) >> shift with shift = 31 + ceil(log2 d) and mul =
+// floor(2^shift / d) + 1, which is below 2^32 (exact: Granlund and Montgomery's bound).  A quarter of the instructions of a
+// division, which rows of a few elements per thread feel.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  __host__ void set(uint32_t divisor) {
+    d = divisor;
+    uint32_t l = 0;
+    while ((uint64_t(1) << l) < d) ++l;
+    shift = 31 + l;
+    mul = d ? uint32_t((uint64_t(1) << shift) / d + 1) : 0;
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return uint32_t((uint64_t(n) * mul) >> shift); }
+};
+
+// Activations split by rows over the ranks (M <= 2^30), `rows` each.
+struct RowAt {
+  uint32_t shard;
+  int64_t offset;      // elements from the shard's start
+};
 struct RowShards {
   void* ptr[kMaxP];
-  uint32_t rows;      // per shard
+  FastDiv rows;
+  __device__ __forceinline__ RowAt at(uint32_t i, int64_t pitch) const {
+    const uint32_t r = rows.div(i);
+    return RowAt{r, int64_t(i - r * rows.d) * pitch};
+  }
+  template <typename T>
+  __device__ __forceinline__ T* row(const RowAt& a) const {
+    return static_cast<T*>(ptr[a.shard]) + a.offset;
+  }
   template <typename T>
   __device__ __forceinline__ T* row(uint32_t i, int64_t pitch) const {
-    const uint32_t r = i / rows;
-    return static_cast<T*>(ptr[r]) + int64_t(i - r * rows) * pitch;
+    return row<T>(at(i, pitch));
   }
 };
 
@@ -111,6 +137,103 @@ struct Raw {
   }
 };
 
+// The next rows of kArrays tensors on their way from HBM: every thread copies its own elements to shared memory, kDepth rows
+// ahead, and reads back only what it copied, so that no barrier is needed and nothing is held in registers.  Elements of two
+// bytes (rows that are not whole vectors) cannot be copied this way: those are loaded when they are taken.
+template <typename T, int V, int NVT, int kArrays, int kThreads>
+struct RowRing {
+  static constexpr int kBytes = V * int(sizeof(T));
+  static constexpr bool kAsync = kBytes >= 4;
+  static constexpr int kRowBytes = kArrays * NVT * kThreads * kBytes;
+  static constexpr int kRoom = 192 * 1024;
+  static constexpr int kDepth = !kAsync ? 1 : kRoom / kRowBytes > 8 ? 8 : kRoom / kRowBytes < 1 ? 1 : kRoom / kRowBytes;
+  static constexpr size_t kSmemBytes = kAsync ? size_t(kDepth) * kRowBytes : 0;
+  uint32_t base;      // this thread's slot 0
+  int at = 0;         // oldest row
+  const T* src[kArrays] = {};
+  __device__ __forceinline__ explicit RowRing(void* smem)
+      : base(static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + threadIdx.x * kBytes) {}
+  // Row `which` (0 = the oldest) is to come from `p` (elements of this row; null: no row).
+  __device__ __forceinline__ void fetch(int which, const T* const (&p)[kArrays], int tpr, int t, int H) {
+    if constexpr (kAsync) {
+      const int slot = at + which >= kDepth ? at + which - kDepth : at + which;
+#pragma unroll
+      for (int a = 0; a < kArrays; ++a)
+#pragma unroll
+        for (int i = 0; i < NVT; ++i) {
+          const int c = (i * tpr + t) * V;
+          if (p[a] != nullptr && c < H) {
+            const uint32_t to = base + ((slot * kArrays + a) * NVT + i) * (kThreads * kBytes);
+            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p[a] + c) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(p[a] + c) : "memory");
+          }
+        }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    } else {
+#pragma unroll
+      for (int a = 0; a < kArrays; ++a) src[a] = p[a];
+    }
+  }
+  // The oldest row has landed.
+  __device__ __forceinline__ void wait() {
+    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+  }
+  // V elements of it as they are stored (zeros past the row's end): one word per 4 bytes.
+  static constexpr int kWords = kBytes >= 4 ? kBytes / 4 : 1;
+  __device__ __forceinline__ void take(uint32_t (&w)[kWords], int array, int i, int tpr, int t, int H) const {
+    const int c = (i * tpr + t) * V;
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = 0u;
+    if (c < H) {
+      if constexpr (kAsync) {
+        const uint32_t from = base + ((at * kArrays + array) * NVT + i) * (kThreads * kBytes);
+        if constexpr (kBytes == 16)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory");
+        else
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(from) : "memory");
+      } else {
+        w[0] = uint32_t(*reinterpret_cast<const unsigned short*>(src[array] + c));
+      }
+    }
+  }
+  __device__ __forceinline__ void advance() { at = at + 1 == kDepth ? 0 : at + 1; }
+};
+
+// Two FP32 values per instruction (add, mul and fma on pairs).
+struct F2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float2 of(F2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float sum_of(F2 a) {
+  const float2 q = of(a);
+  return q.x + q.y;
+}
+
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
@@ -149,7 +272,7 @@ inline int64_t rows_of_vocab_shard(int64_t vocab, int P, int r) {
 }
 // P row shards; with rows == 0 nothing is read and nothing is asked of the pointers.
 inline int fill_shards(const void* const* p, int P, int64_t M, RowShards* out) {
-  out->rows = uint32_t(M / P);
+  out->rows.set(uint32_t(M / P));
   if (M == 0) return COMPASS_OK;
   if (p == nullptr) return COMPASS_ERR_INVALID_ARG;
   for (int r = 0; r < P; ++r) {
@@ -192,6 +315,8 @@ int launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, cuda
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
 }
 
+// Lets a kernel have this much dynamic shared memory on the current device.
+int allow_smem(const void* kernel, size_t bytes);
 // Streaming multiprocessors of the current device (148 on a B200), looked up once per device.
 int sm_count(int* out);
 

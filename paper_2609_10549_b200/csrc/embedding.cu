@@ -414,10 +414,11 @@ __global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __gr
   }
 }
 
-// The runs that cross pieces: where one begins, what its pieces left is added up in order, every kJoinWays-th by one group of
-// threads, and the groups' sums in turn.
-constexpr int kJoinWays = 8;
+// The runs that cross pieces: where one begins, what its pieces left is added up in order; of a long run, every kJoinWays-th
+// piece by one group of threads, and the groups' sums in turn.
+constexpr int kJoinWays = 4;
 constexpr int kJoinLanes = 32;
+constexpr int kJoinShort = 16;      // up to this many pieces: a thread adds up a column's by itself
 template <typename G, int V>
 __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces) {
   __shared__ float part[kJoinWays][kJoinLanes][V + 1];
@@ -437,6 +438,21 @@ __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(
     const int n = __ffs(~same) - 1;                  // (-1: all 32)
     lo += n < 0 ? 32 : n;
     if (n >= 0) break;
+  }
+  if (lo - piece < kJoinShort) {
+    for (int64_t c = (int64_t(blockIdx.y) * blockDim.x + threadIdx.x) * V; c < p.hidden; c += int64_t(gridDim.y) * blockDim.x * V) {
+      float acc[V];
+      load_sums(acc, p.partial + (piece * 2 + 1) * p.hidden + c);
+#pragma unroll 4
+      for (int64_t q = piece + 1; q <= lo; ++q) {
+        float x[V];
+        load_sums(x, p.partial + q * 2 * p.hidden + c);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += x[j];
+      }
+      finish_row<G, V>(p, id, c, acc);
+    }
+    return;
   }
   const int lane = threadIdx.x % kJoinLanes, way = threadIdx.x / kJoinLanes;
   for (int64_t c0 = int64_t(blockIdx.y) * kJoinLanes * V; c0 < p.hidden; c0 += int64_t(gridDim.y) * kJoinLanes * V) {

@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
     load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, p.tpr, t, H);
   }
   const int own = min(NVT, max(0, (H / V - t + p.tpr - 1) / p.tpr)) * V;      // elements of a row that this thread holds
+  const bool ragged = p.tpr * (NVT * V) != H;
   for (uint32_t turn = 0; row < p.M; ++turn, row += stride) {
     const RowAt at = p.x.at(row, H);
     Words<T, V, NVT> x;
@@ -216,11 +217,14 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
     F2 sq[2] = {f2(0.f), f2(0.f)};
     const F2 minus = f2(-mean);
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) {
-      h[k] = h[k] + minus;
-      if (2 * k + 1 >= own) h[k] = 2 * k < own ? f2(of(h[k]).x, 0.f) : f2(0.f);      // past the row's end
-      sq[k & 1] = fma2(h[k], h[k], sq[k & 1]);
+    for (int k = 0; k < kPairs; ++k) h[k] = h[k] + minus;
+    if (ragged) {
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k)
+        if (2 * k + 1 >= own) h[k] = 2 * k < own ? f2(of(h[k]).x, 0.f) : f2(0.f);      // past the row's end
     }
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) sq[k & 1] = fma2(h[k], h[k], sq[k & 1]);
     const float var = row_sum(sum_of(sq[0] + sq[1]), p.tpr, red[2 * (turn & 1) + 1]) * inv;
     const float rstd = 1.0f / sqrtf(var + p.eps);
     if constexpr (!kKeep) {
@@ -301,8 +305,15 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
   F2 dg[kPairs], db[kPairs];
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) dg[k] = db[k] = f2(0.f);
-  const int own = min(NVT, max(0, (H / V - t + p.tpr - 1) / p.tpr)) * V;      // elements of a row that this thread holds
-  Ring ring(raw);
+  // gamma in FP32, every thread its own elements (in registers they would spill); the ring behind it
+  F2* gamma = reinterpret_cast<F2*>(raw) + threadIdx.x;
+  {
+    F2 g[kPairs];
+    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) gamma[k * kThreads] = g[k];
+  }
+  Ring ring(reinterpret_cast<F2*>(raw) + kPairs * kThreads);
   auto fetch = [&](int which, uint32_t row) {
     const bool live = row < p.M;
     const RowAt at = p.x.at(row, H);
@@ -333,20 +344,16 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 0, i, p.tpr, t, H);
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) {
-      xh[k] = (w.pair(k) + minus) * r2;
-      if (2 * k + 1 >= own) xh[k] = 2 * k < own ? f2(of(xh[k]).x, 0.f) : f2(0.f);      // past the row's end
-    }
+    for (int k = 0; k < kPairs; ++k) xh[k] = (w.pair(k) + minus) * r2;
 #pragma unroll
     for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 1, i, p.tpr, t, H);
-    load_params<V, NVT>(d, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);      // (from the L1 cache; kept in registers they would spill)
     F2 c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-      const F2 dy = w.pair(k);
+      const F2 dy = w.pair(k);      // (past the row's end: 0, so that xhat's value there does not matter)
       dg[k] = fma2(dy, xh[k], dg[k]);
       db[k] = db[k] + dy;
-      d[k] = d[k] * dy;
+      d[k] = gamma[k * kThreads] * dy;
       c1 = c1 + d[k];
       c2 = fma2(d[k], xh[k], c2);
     }
@@ -548,7 +555,7 @@ int forward_of(const NormParams& p, bool vec, cudaStream_t stream) {
 template <typename T, int V, int kThreads, bool kDsum>
 int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
   constexpr int NVT = kElems<T, V> / V;
-  constexpr size_t ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>::kSmemBytes;
+  constexpr size_t ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>::kSmemBytes + size_t(kElems<T, V>) * kThreads * 4;
   auto kernel = norm_backward_kernel<T, V, NVT, kThreads, kDsum>;
   const size_t sums = b.groups > 1 ? size_t(b.groups) * p.hidden * 4 : 0, smem = ring > sums ? ring : sums;
   const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem);

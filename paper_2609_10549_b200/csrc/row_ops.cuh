@@ -145,7 +145,7 @@ struct RowRing {
   static constexpr int kBytes = V * int(sizeof(T));
   static constexpr bool kAsync = kBytes >= 4;
   static constexpr int kRowBytes = kArrays * NVT * kThreads * kBytes;
-  static constexpr int kRoom = 192 * 1024;
+  static constexpr int kRoom = 160 * 1024;
   static constexpr int kDepth = !kAsync ? 1 : kRoom / kRowBytes > 8 ? 8 : kRoom / kRowBytes < 1 ? 1 : kRoom / kRowBytes;
   static constexpr size_t kSmemBytes = kAsync ? size_t(kDepth) * kRowBytes : 0;
   uint32_t base;      // this thread's slot 0

@@ -650,9 +650,9 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   if (e->M == 0) return p.fill ? launch(embedding_zero_kernel, 2 * sms, kSortThreads, 0, s, false, p) : COMPASS_OK;
   if (g.tiles == 1) {
     static_assert(sizeof(SortShared) <= 227 * 1024, "");
-    const cudaError_t err =
-        cudaFuncSetAttribute(embedding_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(SortShared)));
-    if (err != cudaSuccess) return record_cuda_error(err);
+    static std::atomic<uint64_t> allowed{0};
+    st = allow_smem(reinterpret_cast<const void*>(embedding_sort_kernel), sizeof(SortShared), &allowed);
+    if (st != COMPASS_OK) return st;
     st = launch(embedding_sort_kernel, p.fill ? sms : 1, kSortThreads, sizeof(SortShared), s, false, p);
   } else {
     p.key_b = reinterpret_cast<uint32_t*>(take(g.key));

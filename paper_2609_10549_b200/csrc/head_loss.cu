@@ -4,13 +4,15 @@
 // Rows whose target lies outside the vocabulary take no part: head_count_kernel
 // counts the others and head_gather_kernel copies them together, so that the
 // products run over real rows only, whatever the mask and the ranks' shards.
-// Then one kernel in four forms (tcgen05 products of BF16 with FP32 sums):
+// Then one kernel in three forms (tcgen05 products of BF16 with FP32 sums):
 //   STATS  logits of 256 vocabulary columns at a time; what leaves the epilogue
 //          is each row's maximum and sum of exponentials over 128 columns
 //   GRAD   the same product again; the epilogue writes the logits' gradient
 //          (BF16) of one piece of the vocabulary
-//   DX     that piece times the table: added to the FP32 sums of dX
-//   DW     that piece, transposed, times X: dW of the piece
+//   SUMS   the two products of that piece, in one launch, so that the one's
+//          tiles fill the other's last round: DX, the piece times the table,
+//          added to the FP32 sums of dX, and DW, the piece, transposed, times X:
+//          dW of the piece
 // The backward pass is bound by the tensor cores: 6 M hidden vocab operations.
 //
 // Tiles are computed by pairs of CTAs: 512 x 256 as long as they fill whole
@@ -21,6 +23,7 @@
 // columns each, so that a whole accumulator is in registers, and its tensor
 // memory free again, before the exponentials begin.
 #include <mutex>
+#include <type_traits>
 
 #include "ptx_sm100.cuh"
 #include "row_ops.cuh"
@@ -31,7 +34,7 @@ using namespace ptx;
 
 namespace {
 
-enum Form : int { STATS = 0, GRAD = 1, DX = 2, DW = 3 };
+enum Form : int { STATS = 0, GRAD = 1, SUMS = 2, DX = 3, DW = 4 };      // (DX and DW: of a SUMS tile)
 
 constexpr int kThreads = 320;
 constexpr int kEpiWarps = 8;
@@ -124,8 +127,8 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Control
   return false;
 }
 
-// How a form's output is cut into tiles; the number of rows is known on the device only.
-struct Plan {
+// How a product's output is cut into tiles; the number of rows is known on the device only.
+struct Part {
   int big_rows;        // row tiles of 512
   int odd;             // one more of 256
   int cols;            // column tiles (of all splits)
@@ -133,30 +136,52 @@ struct Plan {
   int total;
   int atoms;           // 64-wide k-atoms of a tile (an even number)
 };
-template <int kForm>
-__device__ __forceinline__ Plan make_plan(const HeadParams& p, int units) {
-  Plan q;
+// Whole rounds of the units take 512 x 256 tiles, what is left 256 x 256 ones.  `before`: tiles of the launch that come first;
+// the tiles go to the units in turn, so that a unit that has had one of its last, smaller ones gets its share of these later.
+__device__ __forceinline__ Part make_part(const HeadParams& p, int form, int units, int before) {
+  Part q;
   const int found = max(p.found->rows, 1);      // at least one tile: its zeros are what dW reads when no row takes part
-  const int halves = kForm == DW ? p.n_vt : (found + 255) / 256;
+  const int halves = form == DW ? p.n_vt : (found + 255) / 256;
   q.big_rows = halves / 2;
   q.odd = halves & 1;
-  q.cols = kForm == DW ? p.hidden_tiles : kForm == DX ? p.hidden_tiles * p.splits : p.n_vt;
+  q.cols = form == DW ? p.hidden_tiles : form == DX ? p.hidden_tiles * p.splits : p.n_vt;
   const int slots = q.big_rows * q.cols;
-  q.n_big = slots / units * units;
-  q.left = slots - q.n_big;
+  q.left = min(slots, (before + slots) % units);
+  q.n_big = slots - q.left;
   q.total = q.n_big + 2 * q.left + q.odd * q.cols;
-  q.atoms = kForm == DW ? (found + 127) / 128 * 2 : kForm == DX ? 4 * p.n_vt : int((p.hidden + 127) / 128) * 2;
+  q.atoms = form == DW ? (found + 127) / 128 * 2 : form == DX ? 4 * p.n_vt : int((p.hidden + 127) / 128) * 2;
+  return q;
+}
+struct Plan {
+  Part part[2];        // SUMS: DX, DW; else the first alone
+  int total;
+};
+template <int kForm>
+__device__ __forceinline__ Plan make_plan(const HeadParams& p, int units) {
+  Plan q = {};
+  if (kForm == SUMS) {
+    q.part[0] = make_part(p, DX, units, 0);
+    q.part[1] = make_part(p, DW, units, q.part[0].total);
+  } else {
+    q.part[0] = make_part(p, kForm, units, 0);
+  }
+  q.total = q.part[0].total + q.part[1].total;
   return q;
 }
 struct Tile {
+  int form;
   bool big;
   int row0;            // first of 512 or 256 rows
   int col;             // column tile
   int atom0, atoms;    // range of the contraction
 };
 template <int kForm>
-__device__ __forceinline__ Tile tile_of(const HeadParams& p, const Plan& q, int t) {
+__device__ __forceinline__ Tile tile_of(const HeadParams& p, const Plan& plan, int t) {
   Tile c;
+  const bool second = kForm == SUMS && t >= plan.part[0].total;
+  const Part& q = plan.part[second ? 1 : 0];
+  if (second) t -= plan.part[0].total;
+  c.form = kForm != SUMS ? kForm : second ? int(DW) : int(DX);
   c.big = t < q.n_big;
   int slot = t, half = 0;
   const int u = t - q.n_big;
@@ -176,7 +201,7 @@ __device__ __forceinline__ Tile tile_of(const HeadParams& p, const Plan& q, int 
   }
   c.atom0 = 0;
   c.atoms = q.atoms;
-  if (kForm == DX && p.splits > 1) {
+  if (c.form == DX && p.splits > 1) {
     // whole vocabulary tiles (4 atoms) per split
     const int s = c.col / p.hidden_tiles;
     const int from = int(int64_t(p.n_vt) * s / p.splits), to = int(int64_t(p.n_vt) * (s + 1) / p.splits);
@@ -187,23 +212,21 @@ __device__ __forceinline__ Tile tile_of(const HeadParams& p, const Plan& q, int 
 }
 
 // This CTA's 128 rows of A of one k-atom.
-template <int kForm>
-__device__ __forceinline__ void load_a(const HeadParams& p, uint8_t* dst, uint32_t bar, int row, int atom, uint64_t pol) {
-  if (kForm == DW) {
+__device__ __forceinline__ void load_a(const HeadParams& p, int form, uint8_t* dst, uint32_t bar, int row, int atom, uint64_t pol) {
+  if (form == DW) {
     tma_load_2d_pair_hint(dst, &p.d_mn, bar, row, atom * BK, pol);
     tma_load_2d_pair_hint(dst + kHalfChunk, &p.d_mn, bar, row + 64, atom * BK, pol);
   } else {
-    tma_load_2d_pair_hint(dst, kForm == DX ? &p.d_k : &p.x_k, bar, atom * BK, row, pol);
+    tma_load_2d_pair_hint(dst, form == DX ? &p.d_k : &p.x_k, bar, atom * BK, row, pol);
   }
 }
 // This CTA's 128 columns of B of one k-atom.
-template <int kForm>
-__device__ __forceinline__ void load_b(const HeadParams& p, uint8_t* dst, uint32_t bar, int col_tile, int cta, int atom, uint64_t pol) {
-  if (kForm == DW) {
+__device__ __forceinline__ void load_b(const HeadParams& p, int form, uint8_t* dst, uint32_t bar, int col_tile, int cta, int atom, uint64_t pol) {
+  if (form == DW) {
     const int col = col_tile * 256 + cta * 128;
     tma_load_2d_pair_hint(dst, &p.x_mn, bar, col, atom * BK, pol);
     tma_load_2d_pair_hint(dst + kHalfChunk, &p.x_mn, bar, col + 64, atom * BK, pol);
-  } else if (kForm == DX) {
+  } else if (form == DX) {
     const int col = (p.splits > 1 ? col_tile % p.hidden_tiles : col_tile) * 256 + cta * 128;
     const int vt = p.vt0 + (atom >> 2);
     const int shard = vt / p.tiles_per_shard;
@@ -286,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
       const uint32_t bar = map_to_cta(smem_u32(&ctl->full[early]), 0);
       if (leader) mbar_arrive_expect_tx(&ctl->full[early], uint32_t(8 * kChunkBytes));
       for (int i = 0; i < 2; ++i)
-        load_b<kForm>(p, smem + (early * 4 + 2 + i) * kChunkBytes, bar, unit, int(cta), early * 2 + i, pol);
+        load_b(p, kForm, smem + (early * 4 + 2 + i) * kChunkBytes, bar, unit, int(cta), early * 2 + i, pol);
     }
   }
   wait_for_previous_kernel();
@@ -296,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
       uint32_t j = 0;          // stages so far
+      uint32_t last_small = 0u - 4u;   // the last 256x256 one
       int chunk = 0;           // ring cursor
       bool ok = true;
       for (int t = unit; ok && t < plan.total; t += units) {
@@ -303,9 +327,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         const int row = tile.row0 + int(cta) * (tile.big ? 256 : 128);
         const int step = tile.big ? 1 : 2;
         for (int a = 0; a < tile.atoms; a += step, ++j) {
-          // A 512x256 stage (3 chunks) follows only stages of its own kind: four of them fill the ring.  A 256x256 stage
-          // (4 chunks) overwrites nothing newer than the third stage before it.
-          const uint32_t depth = tile.big ? 4u : 3u;
+          // Four 512x256 stages (3 chunks each) fill the ring; with a 256x256 stage (4 chunks) among the last three, a stage
+          // must not overwrite anything newer than the third before it.
+          const uint32_t depth = tile.big && j - last_small > 3u ? 4u : 3u;
+          if (!tile.big) last_small = j;
           if (j >= depth) {
             const uint32_t r = j - depth;
             if (!wait_bar(&ctl->empty[r & 3u], (r >> 2) & 1u, ctl, p, SITE_EMPTY, t)) {
@@ -323,14 +348,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           for (int i = 0; i < 4; ++i) c[i] = smem + ((chunk + i) % kChunks) * kChunkBytes;
           const int atom = tile.atom0 + a;
           if (tile.big) {
-            load_a<kForm>(p, c[0], bar, row, atom, pol);
-            load_a<kForm>(p, c[1], bar, row + 128, atom, pol);
-            load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
+            load_a(p, tile.form, c[0], bar, row, atom, pol);
+            load_a(p, tile.form, c[1], bar, row + 128, atom, pol);
+            load_b(p, tile.form, c[2], bar, tile.col, int(cta), atom, pol);
           } else {
-            load_a<kForm>(p, c[0], bar, row, atom, pol);
-            if (!b_sent) load_b<kForm>(p, c[2], bar, tile.col, int(cta), atom, pol);
-            load_a<kForm>(p, c[1], bar, row, atom + 1, pol);
-            if (!b_sent) load_b<kForm>(p, c[3], bar, tile.col, int(cta), atom + 1, pol);
+            load_a(p, tile.form, c[0], bar, row, atom, pol);
+            if (!b_sent) load_b(p, tile.form, c[2], bar, tile.col, int(cta), atom, pol);
+            load_a(p, tile.form, c[1], bar, row, atom + 1, pol);
+            if (!b_sent) load_b(p, tile.form, c[3], bar, tile.col, int(cta), atom + 1, pol);
           }
           chunk = (chunk + n) % kChunks;
         }
@@ -345,20 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issuer
     if (leader && lane == 0) {
-      constexpr bool kAMn = kForm == DW, kBMn = kForm == DW || kForm == DX;
-      constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | (kAMn ? kUmmaIdescAMnMajor : 0u) | (kBMn ? kUmmaIdescBMnMajor : 0u);
       const uint64_t desc_k = umma_smem_desc_sw128(smem_u32(smem));
       const uint64_t desc_mn = umma_smem_desc_sw128_mn(smem_u32(smem), kHalfChunk);
-      const uint64_t desc_a = kAMn ? desc_mn : desc_k, desc_b = kBMn ? desc_mn : desc_k;
-      constexpr uint64_t ak = kAMn ? 2048 >> 4 : 2, bk = kBMn ? 2048 >> 4 : 2;     // address step of 16 k-elements
       uint32_t j = 0, uses[2] = {0, 0}, small = 0;
       int chunk = 0;
       auto at = [&](uint64_t base, int c) { return base + uint64_t(((c % kChunks) * kChunkBytes) >> 4); };
-      auto issue = [&](uint32_t acc, int a_chunk, int b_chunk, uint32_t first) {
-        const uint64_t da = at(desc_a, a_chunk), db = at(desc_b, b_chunk);
-#pragma unroll
-        for (int k = 0; k < BK / UMMA_K; ++k) umma_bf16_pair(acc, da + k * ak, db + k * bk, idesc, k ? 1u : first);
-      };
       auto acc_free = [&](int b, int t) {
         if (!wait_bar(&ctl->acc_empty[b], (uses[b] & 1u) ^ 1u, ctl, p, SITE_ACC_EMPTY, t)) return false;
         tc_fence_after_sync();
@@ -370,8 +386,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         return true;
       };
       bool ok = true;
-      for (int t = unit; ok && t < plan.total; t += units) {
-        const Tile tile = tile_of<kForm>(p, plan, t);
+      // Operands are contiguous along the contraction, or (B of both sums, A of DW) across it: then an atom is two boxes, and
+      // a step of 16 k-elements is two groups of 8 rows (2048 bytes) instead of 32 bytes of a row.
+      auto run = [&](auto across, const Tile& tile, int t) {
+        constexpr bool kAMn = decltype(across)::value, kBMn = kForm == SUMS;
+        constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | (kAMn ? kUmmaIdescAMnMajor : 0u) | (kBMn ? kUmmaIdescBMnMajor : 0u);
+        constexpr uint64_t ak = kAMn ? 2048 >> 4 : 2, bk = kBMn ? 2048 >> 4 : 2;
+        const uint64_t desc_a = kAMn ? desc_mn : desc_k, desc_b = kBMn ? desc_mn : desc_k;
+        auto issue = [&](uint32_t acc, int a_chunk, int b_chunk, uint32_t first) {
+          const uint64_t da = at(desc_a, a_chunk), db = at(desc_b, b_chunk);
+#pragma unroll
+          for (int k = 0; k < BK / UMMA_K; ++k) umma_bf16_pair(acc, da + k * ak, db + k * bk, idesc, k ? 1u : first);
+        };
         if (tile.big) {
           // Both accumulators are live for the whole tile, so nothing would hide the epilogue's reads if they ended
           // together: for the first and last kSkew stages accumulator 0's products go first.  It is then complete early
@@ -413,13 +439,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           }
           if (ok && skew) ok = skewed(n - skew, false);
           else if (ok) umma_commit_pair(&ctl->acc_full[0], 0x3);
-          if (!ok) break;
+          if (!ok) return;
           umma_commit_pair(&ctl->acc_full[1], 0x3);
           ++uses[0];
           ++uses[1];
         } else {
           const int b = int(small & 1u);
-          if (!(ok = acc_free(b, t))) break;
+          if (!(ok = acc_free(b, t))) return;
           for (int a = 0; a < tile.atoms; a += 2, ++j) {
             if (!(ok = landed(j, t))) break;
             issue(tmem_base + b * 256, chunk, chunk + 2, a != 0 ? 1u : 0u);
@@ -427,11 +453,16 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
             chunk = (chunk + 4) % kChunks;
             umma_commit_pair(&ctl->empty[j & 3u], 0x3);
           }
-          if (!ok) break;
+          if (!ok) return;
           umma_commit_pair(&ctl->acc_full[b], 0x3);
           ++uses[b];
           ++small;
         }
+      };
+      for (int t = unit; ok && t < plan.total; t += units) {
+        const Tile tile = tile_of<kForm>(p, plan, t);
+        if (kForm == SUMS && tile.form == DW) run(std::true_type{}, tile, t);
+        else run(std::false_type{}, tile, t);
       }
       if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
         // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
@@ -443,8 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     const int rows = p.found->rows;
-    float out_scale = p.out_scale;
-    if (kForm == DW) out_scale *= p.found->top;
+    const float out_scale = kForm == SUMS ? p.out_scale * p.found->top : 0.f;
     const float top_weight = kForm == GRAD ? p.found->top : 1.f;
     uint32_t uses[2] = {0, 0}, small = 0;
     bool ok = true;
@@ -548,29 +578,29 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
               store_32(out + g * 16, q);
             }
           }
-        } else if (kForm == DX) {
+        } else if (tile.form == DX) {
           // sums in the order the lanes hold them: 32 groups of 4 columns per warp, each group the lanes' 16 bytes in a row
-          const int64_t frag = (int64_t(frag0 >> 7) * plan.cols + tile.col) * 8 + quarter * 2 + half;
+          const int64_t frag = (int64_t(frag0 >> 7) * plan.part[0].cols + tile.col) * 8 + quarter * 2 + half;
           float4* sum = p.acc + frag * (32 * 32) + lane;
           if (tile.atoms == 0) continue;      // a last piece of fewer vocabulary tiles than splits: nothing to add
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float4 old[8];
+          for (int c = 0; c < 8; ++c) {
+            float4 old[4];
             if (!p.first_piece) {
 #pragma unroll
-              for (int g = 0; g < 8; ++g) old[g] = __ldcg(sum + (c * 8 + g) * 32);
+              for (int g = 0; g < 4; ++g) old[g] = __ldcg(sum + (c * 4 + g) * 32);
             }
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-              float4 x = make_float4(__uint_as_float(v[c][g * 4]), __uint_as_float(v[c][g * 4 + 1]), __uint_as_float(v[c][g * 4 + 2]),
-                                     __uint_as_float(v[c][g * 4 + 3]));
+            for (int g = 0; g < 4; ++g) {
+              const uint32_t* q = &v[c >> 1][(c & 1) * 16 + g * 4];
+              float4 x = make_float4(__uint_as_float(q[0]), __uint_as_float(q[1]), __uint_as_float(q[2]), __uint_as_float(q[3]));
               if (!p.first_piece) {
                 x.x += old[g].x;
                 x.y += old[g].y;
                 x.z += old[g].z;
                 x.w += old[g].w;
               }
-              sum[(c * 8 + g) * 32] = x;
+              sum[(c * 4 + g) * 32] = x;
             }
           }
         } else {
@@ -975,7 +1005,7 @@ int device_facts(DeviceFacts** out) {
   DeviceFacts& f = facts[dev];
   if (!f.ready) {
     const void* kernels[] = {reinterpret_cast<const void*>(head_kernel<STATS>), reinterpret_cast<const void*>(head_kernel<GRAD>),
-                             reinterpret_cast<const void*>(head_kernel<DX>), reinterpret_cast<const void*>(head_kernel<DW>)};
+                             reinterpret_cast<const void*>(head_kernel<SUMS>)};
     for (const void* k : kernels) {
       e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
       if (e != cudaSuccess) return record_cuda_error(e);
@@ -1021,8 +1051,7 @@ int launch_form(int form, const HeadParams& p, int64_t most_tiles, const DeviceF
   cudaError_t e;
   if (form == STATS) e = cudaLaunchKernelEx(&cfg, head_kernel<STATS>, p);
   else if (form == GRAD) e = cudaLaunchKernelEx(&cfg, head_kernel<GRAD>, p);
-  else if (form == DX) e = cudaLaunchKernelEx(&cfg, head_kernel<DX>, p);
-  else e = cudaLaunchKernelEx(&cfg, head_kernel<DW>, p);
+  else e = cudaLaunchKernelEx(&cfg, head_kernel<SUMS>, p);
   count_kernel_launch();
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
 }
@@ -1210,8 +1239,8 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
     p.n_vt = q.vocab_tiles - vt < q.piece_tiles ? q.vocab_tiles - vt : q.piece_tiles;
     p.first_piece = vt == 0;
     st = launch_form(GRAD, p, most_tiles(h, q, p.n_vt), *c.facts, s);
-    if (st == COMPASS_OK) st = launch_form(DX, p, most_tiles(h, q, int64_t(q.hidden_tiles) * q.splits), *c.facts, s);
-    if (st == COMPASS_OK) st = launch_form(DW, p, int64_t(p.n_vt) * q.hidden_tiles, *c.facts, s);
+    if (st == COMPASS_OK)
+      st = launch_form(SUMS, p, most_tiles(h, q, int64_t(q.hidden_tiles) * q.splits) + int64_t(p.n_vt) * q.hidden_tiles, *c.facts, s);
     if (st != COMPASS_OK) return st;
   }
   FinishParams f = {};

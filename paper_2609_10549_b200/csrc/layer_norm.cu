@@ -518,7 +518,8 @@ template <typename T, int V, int NVT, int kThreads, bool kKeep, bool kResidual>
 int run_forward(const NormParams& p, int tpr, cudaStream_t stream) {
   constexpr size_t smem = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>::kSmemBytes;
   auto kernel = norm_forward_kernel<T, V, NVT, kThreads, kKeep, kResidual>;
-  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem);
+  static std::atomic<uint64_t> allowed{0};
+  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem, &allowed);
   if (st != COMPASS_OK) return st;
   NormParams q = p;
   q.tpr = tpr;
@@ -557,8 +558,10 @@ int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream
   constexpr int NVT = kElems<T, V> / V;
   constexpr size_t ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>::kSmemBytes + size_t(kElems<T, V>) * kThreads * 4;
   auto kernel = norm_backward_kernel<T, V, NVT, kThreads, kDsum>;
-  const size_t sums = b.groups > 1 ? size_t(b.groups) * p.hidden * 4 : 0, smem = ring > sums ? ring : sums;
-  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem);
+  constexpr size_t sums = size_t(kThreads) * kElems<T, V> * 4;      // [groups][hidden] at most
+  constexpr size_t smem = ring > sums ? ring : sums;
+  static std::atomic<uint64_t> allowed{0};
+  const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem, &allowed);
   if (st != COMPASS_OK) return st;
   return launch(kernel, b.n_partial, b.tpr * b.groups, smem, stream, false, p);
 }
@@ -595,10 +598,17 @@ int backward_of(const NormParams& p, const BackwardPlan& b, bool vec, cudaStream
 
 }  // namespace
 
-int allow_smem(const void* kernel, size_t bytes) {
+int allow_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>* done) {
   if (bytes <= 48 * 1024) return COMPASS_OK;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
-  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return record_cuda_error(e);
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev < 64 && (done->load(std::memory_order_acquire) & bit)) return COMPASS_OK;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+  if (e != cudaSuccess) return record_cuda_error(e);
+  if (dev < 64) done->fetch_or(bit, std::memory_order_release);
+  return COMPASS_OK;
 }
 
 int sm_count(int* out) {

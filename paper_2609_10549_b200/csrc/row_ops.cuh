@@ -3,6 +3,7 @@
 // their start with the end of the kernel before them.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
 
@@ -315,8 +316,8 @@ int launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, cuda
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
 }
 
-// Lets a kernel have this much dynamic shared memory on the current device.
-int allow_smem(const void* kernel, size_t bytes);
+// Lets a kernel have this much dynamic shared memory on the current device; `done`: the devices where it does already.
+int allow_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>* done);
 // Streaming multiprocessors of the current device (148 on a B200), looked up once per device.
 int sm_count(int* out);
 

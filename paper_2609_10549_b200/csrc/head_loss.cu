@@ -61,7 +61,7 @@ struct Found {
 };
 
 struct HeadParams {
-  CUtensorMap x_k;              // gathered X [pad][hidden]: boxes of 128 rows (A of the logits)
+  CUtensorMap x_k;              // gathered X [pad][hidden]: boxes of 128 rows (A of the logits), of few_cols with few rows
   CUtensorMap x_mn;             // boxes of 64 rows (B of dW)
   CUtensorMap d_k, d_mn;        // the piece's gradient [pad][piece_cols]: A of dX; A of dW
   CUtensorMap w_k[kMaxP], w_mn[kMaxP];
@@ -87,6 +87,7 @@ struct HeadParams {
   int32_t splits;               // of dX's contraction
   int32_t first_piece;
   int32_t one_row_tile;         // M <= 256
+  int32_t few_cols;             // head_few_kernel: M rounded up to a multiple of 16
   int32_t grad_fp32;
   int32_t dw_wide;              // dW's rows are whole 32-byte sectors
   float z_scale;                // logit_scale * log2(e)
@@ -649,6 +650,239 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
   }
 }
 
+// ---- statistics of few rows ----------------------------------------------------
+// Up to kFewRows rows the forward product only has to read the table.  Here the table's rows are the products' M side (128 at
+// a time) and X's the N side, so that all the loads but a few are of the table and fill the whole ring (the form above spends
+// half of its ring on rows of X that are not there).  Single CTAs; warp 0 loads, warp 1 multiplies, warps 2..5 transpose the
+// accumulator through shared memory and take each row's statistics over their 32 vocabulary rows.
+// Measured on 16 rows, 4096 x 32000: 66 us in the form above, 49 us here; the table's bytes take 40 us.
+constexpr int kFewRows = 128;
+constexpr int kFewThreads = 192;
+constexpr int kFewAhead = 8;              // stages behind the ring whose part of the table is fetched into L2 meanwhile
+constexpr int kFewRoom = 192 * 1024;
+struct FewControl {
+  uint64_t full[8], empty[8];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t drain;
+  uint32_t tmem_base;
+  int abort;
+};
+struct FewShared {
+  float z[4][32][33];        // [warp][token][vocabulary row]
+  float2 part[4][32];
+  float sum[4][32];
+};
+__host__ __device__ constexpr int few_stage_bytes(int n) { return 2 * (kChunkBytes + n * BK * 2); }      // two k-atoms
+__host__ __device__ constexpr int few_stages(int n) { return kFewRoom / few_stage_bytes(n) < 8 ? kFewRoom / few_stage_bytes(n) : 8; }
+constexpr size_t kFewSmemBytes = 1024 + kFewRoom + sizeof(FewControl) + 16 + sizeof(FewShared);
+
+__device__ __forceinline__ bool wait_few(uint64_t* bar, uint32_t parity, FewControl* ctl, const HeadParams& p, int site, int tile) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  const uint64_t limit = uint64_t(p.wait_limit_us) * 1000ull;
+  for (uint32_t spins = 1; spins < (1u << 30); ++spins) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((spins & 0xFF) == 0) {
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) return false;
+      if (globaltimer_ns() - t0 > limit) break;
+    }
+  }
+  *reinterpret_cast<volatile int*>(&ctl->abort) = 1;
+  if (atomicCAS(&p.status->code, 0, int(COMPASS_ERR_TIMEOUT)) == 0) {
+    p.status->detail = site;
+    p.status->block_idx = int(blockIdx.x);
+    p.status->tile = tile;
+  }
+  return false;
+}
+
+__global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_constant__ HeadParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  FewControl* ctl = reinterpret_cast<FewControl*>(smem + kFewRoom);
+  FewShared* sh = reinterpret_cast<FewShared*>((reinterpret_cast<uintptr_t>(ctl + 1) + 15) & ~uintptr_t(15));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_cols = p.few_cols;
+  const int stage_bytes = few_stage_bytes(n_cols), stages = few_stages(n_cols);
+  const int tiles = 2 * p.n_vt;                        // of 128 vocabulary rows
+  const int ksteps = int((p.hidden + 127) / 128);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < 8; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->acc_full[b], 1);
+      mbar_init(&ctl->acc_empty[b], 4);
+    }
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&ctl->tmem_base, 256);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl->tmem_base;
+  launch_dependents();
+  // the vocabulary rows of a tile that exist (0: none, the tile is left out by everyone)
+  auto rows_of = [&](int t, int* shard, int* row) {
+    const int rows = vocab_cols(p, t >> 1, shard, row) - (t & 1) * 128;
+    *row += (t & 1) * 128;
+    return max(0, min(128, rows));
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      auto load_table = [&](uint8_t* dst, uint64_t* bar, int shard, int row, int k) {
+        mbar_arrive_expect_tx(bar, uint32_t(stage_bytes));
+        tma_load_2d_hint(dst, &p.w_k[shard], bar, k * 2 * BK, row, pol);
+        tma_load_2d_hint(dst + kChunkBytes, &p.w_k[shard], bar, (k * 2 + 1) * BK, row, pol);
+      };
+      // the first stages' part of the table is on its way before the rows of X are gathered
+      int shard, row, early = 0;
+      if (int(blockIdx.x) < tiles && rows_of(blockIdx.x, &shard, &row) > 0)
+        for (; early < min(stages, ksteps); ++early) load_table(smem + early * stage_bytes, &ctl->full[early], shard, row, early);
+      for (int i = 2 * early; early > 0 && i < min(2 * (early + kFewAhead), 2 * ksteps); ++i) tma_prefetch_l2_2d(&p.w_k[shard], i * BK, row);
+      wait_for_previous_kernel();
+      int j = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        if (rows_of(t, &shard, &row) == 0) continue;
+        for (int k = 0; k < ksteps; ++k, ++j) {
+          const int slot = j % stages;
+          if (j >= stages && !wait_few(&ctl->empty[slot], uint32_t(j / stages - 1) & 1u, ctl, p, SITE_EMPTY, t)) {
+            ok = false;
+            break;
+          }
+          uint8_t* dst = smem + slot * stage_bytes;
+          if (j >= early) load_table(dst, &ctl->full[slot], shard, row, k);
+          for (int i = 0; i < 2; ++i)
+            tma_load_2d_hint(dst + 2 * kChunkBytes + i * n_cols * BK * 2, &p.x_k, &ctl->full[slot], (k * 2 + i) * BK, 0, pol);
+        }
+      }
+      // leave only when everything that was loaded has landed and been read
+      for (int i = max(0, j - stages); i < j; ++i)
+        if (!wait_few(&ctl->empty[i % stages], uint32_t(i / stages) & 1u, ctl, p, SITE_DRAIN, -1)) break;
+    } else {
+      wait_for_previous_kernel();
+    }
+  } else if (warp == 1) {
+    wait_for_previous_kernel();
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_bf16_f32(128, uint32_t(n_cols));
+      const uint64_t desc = umma_smem_desc_sw128(smem_u32(smem));
+      int j = 0;
+      uint32_t it = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        int shard, row;
+        if (rows_of(t, &shard, &row) == 0) continue;
+        const uint32_t b = it & 1u;
+        if (!(ok = wait_few(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, ctl, p, SITE_ACC_EMPTY, t))) break;
+        tc_fence_after_sync();
+        for (int k = 0; k < ksteps; ++k, ++j) {
+          const int slot = j % stages;
+          if (!(ok = wait_few(&ctl->full[slot], uint32_t(j / stages) & 1u, ctl, p, SITE_FULL, t))) break;
+          tc_fence_after_sync();
+          const uint64_t da = desc + uint64_t((slot * stage_bytes) >> 4), db = da + uint64_t((2 * kChunkBytes) >> 4);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            umma_bf16(tmem_base + b * 128, da + uint64_t((i >> 2) * (kChunkBytes >> 4) + (i & 3) * 2),
+                      db + uint64_t((i >> 2) * ((n_cols * BK * 2) >> 4) + (i & 3) * 2), idesc, (k | i) ? 1u : 0u);
+          umma_commit(&ctl->empty[slot]);
+        }
+        if (!ok) break;
+        umma_commit(&ctl->acc_full[b]);
+        ++it;
+      }
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+        umma_commit(&ctl->drain);
+        wait_few(&ctl->drain, 0, ctl, p, SITE_DRAIN, -2);
+      }
+    }
+  } else {
+    wait_for_previous_kernel();
+    const int quarter = warp & 3;
+    const int rows = p.found->rows;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      int shard, vrow;
+      const int live = rows_of(t, &shard, &vrow) - quarter * 32;        // of this warp's 32 vocabulary rows
+      const uint32_t b = it & 1u;
+      const bool empty = live + quarter * 32 == 0;
+      if (!empty) {
+        if (!(ok = wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t))) break;
+        tc_fence_after_sync();
+      }
+      for (int c = 0; c < n_cols; c += 32) {
+        const int token = c + lane;
+        float m = -INFINITY, s = 0.f, sum = 0.f;
+        if (!empty) {
+          uint32_t v[32];
+          tmem_ld_32x32b_x32(tmem_base + (uint32_t(quarter * 32) << 16) + b * 128 + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sh->z[quarter][i][lane] = __uint_as_float(v[i]) * p.z_scale;
+          __syncwarp();
+          const float* z = sh->z[quarter][lane];
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < live) m = fmaxf(m, z[i]);
+          const float top = m == -INFINITY ? 0.f : m;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < live) {
+              s += exp2_fast(z[i] - top);
+              sum += z[i];
+            }
+          if (token < rows) {
+            const int hit = p.target[token] - (shard * p.vocab_rows + vrow + quarter * 32);
+            if (hit >= 0 && hit < min(live, 32)) p.target_logit[token] = z[hit];
+          }
+        }
+        // the four warps' statistics as one
+        sh->part[quarter][lane] = make_float2(m, s);
+        sh->sum[quarter][lane] = sum;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (quarter == 0 && token < rows) {
+          float top = -INFINITY;
+          s = sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) top = fmaxf(top, sh->part[w][lane].x);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 x = sh->part[w][lane];
+            s += top == -INFINITY || x.x == -INFINITY ? x.y : x.y * exp2_fast(x.x - top);
+            sum += sh->sum[w][lane];
+          }
+          const int64_t at = int64_t(t) * p.pad + token;
+          p.part[at] = make_float2(top, s);
+          if (p.smoothing != 0.f) p.part_sum[at] = sum;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+      }
+      if (!empty) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl->acc_empty[b]);
+        ++it;
+      }
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, 256);
+  }
+}
+
 // ---- which rows take part ------------------------------------------------------
 
 constexpr int kCountRows = 1024;      // rows counted together
@@ -681,6 +915,9 @@ __device__ __forceinline__ int32_t target_of(const RowParams& p, uint32_t i) {
   return y >= 0 && y < p.vocab ? int32_t(y) : -1;
 }
 
+// |g|, infinite where g is not finite.
+__device__ __forceinline__ float finite_size(float g) { return fabsf(g) < INFINITY ? fabsf(g) : INFINITY; }
+
 __global__ void __launch_bounds__(256) head_count_kernel(const __grid_constant__ RowParams p) {
   __shared__ int32_t counts[8];
   __shared__ float tops[8];
@@ -692,10 +929,10 @@ __global__ void __launch_bounds__(256) head_count_kernel(const __grid_constant__
   for (int k = 0; k < kCountRows / 256; ++k) {
     const uint32_t i = blockIdx.x * kCountRows + k * 256 + threadIdx.x;
     if (i >= p.M) continue;
-    const float g = p.dloss ? fabsf(p.dloss[i]) : 0.f;
+    const float g = p.dloss ? finite_size(p.dloss[i]) : 0.f;
     if (target_of(p, i) >= 0) {
       ++n;
-      top = fmaxf(top, g < INFINITY ? g : INFINITY);      // (NaN too)
+      top = fmaxf(top, g);
     } else if (p.loss_out) {
       p.loss_out[i] = 0.f;
       p.lse_out[i] = 0.f;
@@ -742,16 +979,30 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
   launch_dependents();
   wait_for_previous_kernel();
   const uint32_t row0 = blockIdx.x * kGatherRows;
-  const uint32_t chunk = row0 / kCountRows, chunks = (p.M + kCountRows - 1) / kCountRows;
   int2 sum = make_int2(0, 0);       // rows that take part: before row0, in all
   float top = 0.f;
-  for (uint32_t b = threadIdx.x; b < chunks; b += 256) {
-    const int32_t n = p.counts[b];
-    if (b < chunk) sum.x += n;
-    sum.y += n;
-    top = fmaxf(top, p.tops[b]);
+  if (p.M <= kCountRows) {
+    // few enough for every block to count them (there was no head_count_kernel)
+    for (uint32_t i = threadIdx.x; i < p.M; i += 256) {
+      const bool in = target_of(p, i) >= 0;
+      sum.x += in && i < row0;
+      sum.y += in;
+      if (p.dloss && in) top = fmaxf(top, finite_size(p.dloss[i]));
+      if (p.loss_out && !in && i - row0 < kGatherRows) {
+        p.loss_out[i] = 0.f;
+        p.lse_out[i] = 0.f;
+      }
+    }
+  } else {
+    const uint32_t chunk = row0 / kCountRows, chunks = (p.M + kCountRows - 1) / kCountRows;
+    for (uint32_t b = threadIdx.x; b < chunks; b += 256) {
+      const int32_t n = p.counts[b];
+      if (b < chunk) sum.x += n;
+      sum.y += n;
+      top = fmaxf(top, p.tops[b]);
+    }
+    for (uint32_t i = chunk * kCountRows + threadIdx.x; i < row0; i += 256) sum.x += target_of(p, i) >= 0;
   }
-  for (uint32_t i = chunk * kCountRows + threadIdx.x; i < row0; i += 256) sum.x += target_of(p, i) >= 0;
   sum = block_add(sum, part);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (blockIdx.x == 0) {
@@ -826,39 +1077,51 @@ struct CombineParams {
   int32_t parts, pad;
   float smoothing, uniform;
 };
-// 32 rows per block, 32 threads a row.
+// 32 rows per block: every warp a share of their parts, then every warp one row.
 __global__ void __launch_bounds__(1024) head_combine_kernel(const __grid_constant__ CombineParams p) {
   __shared__ float2 ms[32][33];
   __shared__ float zs[32][33];
   wait_for_previous_kernel();
   const int rows = p.found->rows;
-  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
-  const int row = blockIdx.x * 32 + lane;
-  if (int(blockIdx.x) * 32 >= rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row0 = blockIdx.x * 32;
+  if (row0 >= rows) return;
   float m = -INFINITY, s = 0.f, z = 0.f;
-  if (row < rows) {
-#pragma unroll 4
-    for (int q = k; q < p.parts; q += 32) {
-      const float2 x = p.part[int64_t(q) * p.pad + row];
-      const float top = fmaxf(m, x.x);
+  if (row0 + lane < rows) {
+    for (int q0 = warp; q0 < p.parts; q0 += 32 * 8) {
+      float2 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int q = q0 + i * 32;
+        x[i] = make_float2(-INFINITY, 0.f);
+        if (q < p.parts) {
+          x[i] = p.part[int64_t(q) * p.pad + row0 + lane];
+          if (p.smoothing != 0.f) z += p.part_sum[int64_t(q) * p.pad + row0 + lane];
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i].x);
       // (no maximum: nothing but -inf, whose sum is 0, and NaN, whose sum is NaN)
-      if (top != -INFINITY) s = s * exp2f(m - top) + x.y * exp2f(x.x - top);
-      else s += x.y;
+      const float at = top == -INFINITY ? 0.f : top;
+      s = m == -INFINITY ? s : s * exp2f(m - at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += x[i].x == -INFINITY ? x[i].y : x[i].y * exp2f(x[i].x - at);
       m = top;
-      if (p.smoothing != 0.f) z += p.part_sum[int64_t(q) * p.pad + row];
     }
   }
-  ms[k][lane] = make_float2(m, s);
-  zs[k][lane] = z;
+  ms[warp][lane] = make_float2(m, s);
+  zs[warp][lane] = z;
   __syncthreads();
-  if (k == 0 && row < rows) {
-    float top = -INFINITY;
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, ms[i][lane].x);
-    s = z = 0.f;
-    for (int i = 0; i < 32; ++i) {
-      s += top != -INFINITY ? ms[i][lane].y * exp2f(ms[i][lane].x - top) : ms[i][lane].y;
-      z += zs[i][lane];
-    }
+  const int row = row0 + warp;
+  if (row >= rows) return;
+  const float2 x = ms[lane][warp];
+  float top = x.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  s = warp_sum(x.x == -INFINITY ? x.y : x.y * exp2f(x.x - top));
+  z = warp_sum(zs[lane][warp]);
+  if (lane == 0) {
     const float lse2 = top + log2f(s);
     const int to = p.origin[row];
     p.lse[to] = lse2 * kLn2;
@@ -991,7 +1254,7 @@ HeadPlan head_plan(const compass_head* h, bool backward) {
 
 struct DeviceFacts {
   bool ready = false;
-  int pairs = 0;
+  int pairs = 0, sms = 0;
 };
 int device_facts(DeviceFacts** out) {
   constexpr int kMaxDevices = 64;
@@ -1010,11 +1273,12 @@ int device_facts(DeviceFacts** out) {
       e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
       if (e != cudaSuccess) return record_cuda_error(e);
     }
-    int sms = 0;
-    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    e = cudaFuncSetAttribute(head_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kFewSmemBytes));
+    if (e != cudaSuccess) return record_cuda_error(e);
+    e = cudaDeviceGetAttribute(&f.sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return record_cuda_error(e);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(sms / 2 * 2));
+    cfg.gridDim = dim3(unsigned(f.sms / 2 * 2));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmemBytes;
     cudaLaunchAttribute attr;
@@ -1060,6 +1324,7 @@ int launch_form(int form, const HeadParams& p, int64_t most_tiles, const DeviceF
 struct Common {
   HeadPlan q;
   DeviceFacts* facts;
+  bool few;               // head_few_kernel takes the statistics
   uint8_t* at;            // next free byte of the workspace
   RowParams rows;
   HeadParams p;
@@ -1091,6 +1356,7 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   if (st != COMPASS_OK) return st;
   const HeadPlan& q = c->q;
   HeadParams& p = c->p;
+  if (c->few) p.few_cols = int32_t(round_up(size_t(h->M), 16));
   uint8_t* base = static_cast<uint8_t*>(ws);
   Found* found = reinterpret_cast<Found*>(base + 256);
   c->at = base + 512;
@@ -1130,7 +1396,7 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   p.uniform = float(double(h->label_smoothing) / double(h->vocab));
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
   // (rows past M are not loaded: they read as zeros)
-  bool ok = encode_tensor_map(&p.x_k, gathered, h->M, h->hidden, 128);
+  bool ok = encode_tensor_map(&p.x_k, gathered, h->M, h->hidden, c->few ? p.few_cols : 128);
   for (int s = 0; s < h->P; ++s) {
     const int64_t n = rows_of_vocab_shard(h->vocab, h->P, s);
     if (n > 0) ok = ok && encode_tensor_map(&p.w_k[s], W[s], n, h->hidden, 128);
@@ -1140,9 +1406,10 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   if (!ok) return record_cuda_error(cudaErrorUnknown);
   r.gathered = reinterpret_cast<uint4*>(gathered);
   r.vecs = uint32_t(h->hidden / 8);
-  st = launch(head_count_kernel, ceil_div(h->M, kCountRows), 256, 0, stream, false, r);
+  const bool counted = h->M > kCountRows;
+  if (counted) st = launch(head_count_kernel, ceil_div(h->M, kCountRows), 256, 0, stream, false, r);
   if (st != COMPASS_OK) return st;
-  return launch(head_gather_kernel, ceil_div(h->M, kGatherRows), 256, 0, stream, true, r);
+  return launch(head_gather_kernel, ceil_div(h->M, kGatherRows), 256, 0, stream, counted, r);
 }
 
 // Tiles of a form at most, counted as 256 x 256.
@@ -1173,13 +1440,19 @@ extern "C" int compass_head_loss(const compass_head* h, const void* const* X, co
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   c.rows.loss_out = loss;
   c.rows.lse_out = lse;
+  c.few = h->M <= kFewRows;
   st = gather_rows(h, W, targets, ws, &c, s);
   if (st != COMPASS_OK) return st;
   HeadParams& p = c.p;
   p.part = reinterpret_cast<float2*>(c.take(c.q.part));
   p.part_sum = reinterpret_cast<float*>(c.take(c.q.part_sum));
   p.n_vt = c.q.vocab_tiles;
-  st = launch_form(STATS, p, most_tiles(h, c.q, c.q.vocab_tiles), *c.facts, s);
+  if (c.few) {
+    const int64_t tiles = 2 * int64_t(c.q.vocab_tiles);
+    st = launch(head_few_kernel, tiles < c.facts->sms ? tiles : c.facts->sms, kFewThreads, kFewSmemBytes, s, true, p);
+  } else {
+    st = launch_form(STATS, p, most_tiles(h, c.q, c.q.vocab_tiles), *c.facts, s);
+  }
   if (st != COMPASS_OK) return st;
   CombineParams m = {};
   m.found = p.found;

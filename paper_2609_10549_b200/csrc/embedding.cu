@@ -2,11 +2,13 @@
 //
 // The lookup reads M rows and writes M rows.  The gradient reads M rows and
 // writes all vocab rows, most of them zeros: with a large vocabulary the zeros
-// are most of its bytes.  So one kernel sorts the ids on one SM while the other
-// SMs write the zeros, and a second one adds the tokens' rows up, run by run of
-// equal ids, and writes only the rows that occur.  Every sum runs over the sorted
-// tokens in fixed pieces and in fixed order: no atomics on results, the bits do
-// not depend on timing.
+// are most of its bytes.  So one kernel sorts the ids, on 8 SMs, while another
+// writes zeros; the third adds the tokens' rows up, run by run of equal ids, and
+// writes the rows that occur; the fourth joins the runs that were cut.  (Spreading the zeros over the later kernels, past the rows that
+// occur, was no faster: the sort is hidden behind them here, and was not then.)
+// Every sum runs over the sorted tokens in fixed pieces and in fixed order: no
+// atomics on results, the bits do not depend on timing.
+#include "ptx_sm100.cuh"
 #include "row_ops.cuh"
 
 namespace compass {
@@ -73,14 +75,18 @@ __global__ void __launch_bounds__(128) embedding_kernel(const __grid_constant__ 
 }
 
 // ---- gradient: sort ------------------------------------------------------------
-// Stable radix sort of (id, position), padding ids (= vocab) last, 9 bits a pass.
+// Stable radix sort of (id, position), padding ids (= vocab) last, 9 bits a pass.  Up to kClusterTokens tokens it is the work
+// of one cluster of 8 CTAs, which exchange digit counts and items through distributed shared memory; beyond, of a kernel for
+// each step.  (One CTA took 30 us for 16384 tokens, nearly all of it for the ranks; the cluster takes 15.)
 
 constexpr int kRadixBits = 9;
 constexpr int kRadix = 1 << kRadixBits;
-constexpr int kSortThreads = 1024;
-constexpr int kSortItems = 16;
-constexpr int kSortTile = kSortThreads * kSortItems;      // tokens one block sorts in its registers and shared memory
+constexpr int kSortThreads = 512;                         // (their registers fit beside a block that writes zeros)
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 16;                            // items per thread at most
+constexpr int kSortTile = kSortThreads * kSortItems;      // tokens of one block at most
+constexpr int kCluster = 8;
+constexpr int64_t kClusterTokens = int64_t(kCluster) * kSortTile;
 
 struct GradParams {
   VocabShards dw;
@@ -101,17 +107,17 @@ struct GradParams {
   float scale;
 };
 
-// Where each of a warp's items goes within the block: `rank` of every item among the block's items with the same digit,
-// items in order of position (warp-major, then item, then lane).  count[warp][digit] afterwards: items of that digit in
-// earlier warps; total[digit]: in the block.
-__device__ __forceinline__ void block_rank(const uint32_t (&digit)[kSortItems], uint32_t (&rank)[kSortItems], uint16_t* count,
-                                           uint32_t* total) {
+// Where each of a warp's items goes within the block: `rank` of every item among the warp's items with the same digit, items
+// in order of position (warp-major, then item, then lane).  count[warp][digit] afterwards: items of that digit in earlier
+// warps; total[digit]: in the block.
+template <int kItems>
+__device__ __forceinline__ void block_rank(const uint32_t (&digit)[kItems], uint32_t (&rank)[kItems], uint16_t* count, uint32_t* total) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint16_t* mine = count + warp * kRadix;
-  for (int d = lane; d < kRadix; d += 32) mine[d] = 0;
+  for (int d = lane; d < kRadix / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < kItems; ++i) {
     const uint32_t same = __match_any_sync(0xffffffffu, digit[i]);
     const uint32_t before = __popc(same & ((1u << lane) - 1u));
     const uint32_t base = mine[digit[i]];
@@ -121,82 +127,106 @@ __device__ __forceinline__ void block_rank(const uint32_t (&digit)[kSortItems], 
     rank[i] = base + before;
   }
   __syncthreads();
-  if (threadIdx.x < kRadix) {
-    uint32_t sum = 0;
-#pragma unroll 8
+  static_assert(kSortThreads == kRadix, "a thread per digit");
+  {
+    uint32_t sum = 0, c[kSortWarps];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) c[w] = count[w * kRadix + threadIdx.x];
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = count[w * kRadix + threadIdx.x];
       count[w * kRadix + threadIdx.x] = uint16_t(sum);
-      sum += c;
+      sum += c[w];
     }
     total[threadIdx.x] = sum;
   }
   __syncthreads();
 }
 
-// Exclusive sum over the kRadix totals of a block.
-__device__ __forceinline__ void scan_digits(uint32_t* total, uint32_t* warp_sums) {
+// Exclusive sum of a value per digit, one per thread.
+__device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t* warp_sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t v = 0, x = 0;
-  if (threadIdx.x < kRadix) {
-    v = x = total[threadIdx.x];
+  uint32_t x = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) warp_sums[warp] = x;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
   }
+  if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  if (threadIdx.x < kRadix) {
-    uint32_t before = 0;
-    for (int w = 0; w < warp; ++w) before += warp_sums[w];
-    total[threadIdx.x] = before + x - v;
-  }
-  __syncthreads();
+  uint32_t before = 0;
+  for (int w = 0; w < warp; ++w) before += warp_sums[w];
+  return before + x - v;
 }
 
 struct SortShared {
   uint32_t key[kSortTile], pos[kSortTile];
   uint16_t count[kSortWarps * kRadix];
-  uint32_t total[kRadix];
+  uint32_t total[kRadix], base[kRadix];
   uint32_t warp_sums[kRadix / 32];
 };
 
-// Sorts up to kSortTile tokens on one block.
-__device__ void sort_tile(const GradParams& p, SortShared& s) {
+__device__ __forceinline__ uint32_t load_cluster(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// Sorts up to kCluster * kSortThreads * kItems tokens on one cluster.
+template <int kItems>
+__device__ void sort_cluster(const GradParams& p, SortShared& s) {
+  using namespace ptx;
+  constexpr uint32_t kTile = kSortThreads * kItems;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t key[kSortItems], pos[kSortItems], digit[kSortItems], rank[kSortItems];
+  const uint32_t cta = cluster_ctarank();
+  const uint32_t own = warp * (32 * kItems) + lane;      // first of this thread's places in the tile, 32 apart
+  uint32_t key[kItems], pos[kItems], digit[kItems], rank[kItems];
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const uint32_t at = warp * (32 * kSortItems) + i * 32 + lane;
-    pos[i] = at;
+  for (int i = 0; i < kItems; ++i) {
+    pos[i] = cta * kTile + own + i * 32;
     // past the end: beyond every key, so that it stays behind the tokens in every pass
-    key[i] = at < p.M ? token_id(p.ids, p.wide_ids, at, p.dw.vocab) : 0xffffffffu;
+    key[i] = pos[i] < p.M ? token_id(p.ids, p.wide_ids, pos[i], p.dw.vocab) : 0xffffffffu;
   }
+  const uint32_t key_at = smem_u32(s.key), pos_at = smem_u32(s.pos), total_at = smem_u32(s.total);
   for (int shift = 0; shift < p.bits; shift += kRadixBits) {
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) digit[i] = (key[i] >> shift) & (kRadix - 1);
+    for (int i = 0; i < kItems; ++i) digit[i] = (key[i] >> shift) & (kRadix - 1);
     block_rank(digit, rank, s.count, s.total);
-    scan_digits(s.total, s.warp_sums);
+    cluster_arrive();      // every CTA's totals are there, and every CTA has read its items of the pass before
+    cluster_wait();
+    uint32_t all = 0, before = 0;
+    {
+      uint32_t t[kCluster];
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      const uint32_t to = s.total[digit[i]] + s.count[warp * kRadix + digit[i]] + rank[i];
-      s.key[to] = key[i];
-      s.pos[to] = pos[i];
+      for (int c = 0; c < kCluster; ++c) t[c] = load_cluster(map_to_cta(total_at + threadIdx.x * 4, c));
+#pragma unroll
+      for (int c = 0; c < kCluster; ++c) {
+        all += t[c];
+        if (uint32_t(c) < cta) before += t[c];
+      }
     }
+    const uint32_t first = scan_digits(all, s.warp_sums);
+    s.base[threadIdx.x] = first + before;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      const uint32_t at = warp * (32 * kSortItems) + i * 32 + lane;
-      key[i] = s.key[at];
-      pos[i] = s.pos[at];
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t to = s.base[digit[i]] + s.count[warp * kRadix + digit[i]] + rank[i];
+      store_cluster(map_to_cta(key_at + to % kTile * 4, to / kTile), key[i]);
+      store_cluster(map_to_cta(pos_at + to % kTile * 4, to / kTile), pos[i]);
     }
-    __syncthreads();
+    cluster_arrive();      // (and no CTA leaves while others still read its totals)
+    cluster_wait();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      key[i] = s.key[own + i * 32];
+      pos[i] = s.pos[own + i * 32];
+    }
   }
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const uint32_t at = warp * (32 * kSortItems) + i * 32 + lane;
+  for (int i = 0; i < kItems; ++i) {
+    const uint32_t at = cta * kTile + own + i * 32;
     if (at < p.M) {
       p.key_a[at] = key[i];
       p.pos_a[at] = pos[i];
@@ -204,33 +234,37 @@ __device__ void sort_tile(const GradParams& p, SortShared& s) {
   }
 }
 
-// Zeros for every row of dW, by blocks first .. first + n - 1 of the grid.
-__device__ __forceinline__ void write_zeros(const GradParams& p, int64_t first, int64_t n) {
-  const uint32_t per = p.dw.rows.d;
-  for (uint32_t r = 0, v0 = 0; v0 < p.dw.vocab; ++r, v0 += per) {
-    const int64_t rows = min(per, p.dw.vocab - v0);
-    const int64_t bytes = rows * p.hidden * p.elem;
-    uint8_t* base = static_cast<uint8_t*>(p.dw.ptr[r]);
-    const int64_t whole = bytes / 16;
-    for (int64_t i = (int64_t(blockIdx.x) - first) * blockDim.x + threadIdx.x; i < whole; i += n * blockDim.x)
-      __stcs(reinterpret_cast<uint4*>(base) + i, make_uint4(0u, 0u, 0u, 0u));
-    if (int64_t(blockIdx.x) == first)
-      for (int64_t b = whole * 16 + threadIdx.x * 2; b < bytes; b += blockDim.x * 2) *reinterpret_cast<uint16_t*>(base + b) = 0;
-  }
-}
-
-// Block 0 sorts; the others write the zeros meanwhile.
+template <int kItems>
 __global__ void __launch_bounds__(kSortThreads, 1) embedding_sort_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ uint4 raw[];
   launch_dependents();
-  if (blockIdx.x == 0) sort_tile(p, *reinterpret_cast<SortShared*>(raw));
-  else write_zeros(p, 1, int64_t(gridDim.x) - 1);
+  sort_cluster<kItems>(p, *reinterpret_cast<SortShared*>(raw));
 }
 
-// More tokens than one block sorts: per pass a histogram of every tile, their scan, and the scatter.
-__global__ void __launch_bounds__(kSortThreads, 1) embedding_zero_kernel(const __grid_constant__ GradParams p) {
-  write_zeros(p, 0, gridDim.x);
+// Zeros for every row of dW.  It may run beside the sort, but is not done before it: what follows waits for this one.
+// Many small blocks: 1.05 GB take 149 us with 64 of 256 threads per SM, 171 us with one of 1024.
+constexpr int kZeroThreads = 256;
+constexpr int kZeroAtOnce = 4;
+__global__ void __launch_bounds__(kZeroThreads) embedding_zero_kernel(const __grid_constant__ GradParams p) {
+  launch_dependents();
+  const int64_t n = int64_t(gridDim.x) * (kZeroThreads * kZeroAtOnce), own = int64_t(blockIdx.x) * (kZeroThreads * kZeroAtOnce) + threadIdx.x;
+  const uint32_t per = p.dw.rows.d;
+  for (uint32_t r = 0, v0 = 0; v0 < p.dw.vocab; ++r, v0 += per) {
+    const int64_t bytes = int64_t(min(per, p.dw.vocab - v0)) * p.hidden * p.elem;
+    uint8_t* base = static_cast<uint8_t*>(p.dw.ptr[r]);
+    const int64_t whole = bytes / 16;
+    for (int64_t i = own; i < whole; i += n) {
+#pragma unroll
+      for (int k = 0; k < kZeroAtOnce; ++k)
+        if (i + k * kZeroThreads < whole) __stcs(reinterpret_cast<uint4*>(base) + i + k * kZeroThreads, make_uint4(0u, 0u, 0u, 0u));
+    }
+    if (blockIdx.x == 0)
+      for (int64_t b = whole * 16 + threadIdx.x * 2; b < bytes; b += kZeroThreads * 2) *reinterpret_cast<uint16_t*>(base + b) = 0;
+  }
+  if (blockIdx.x == gridDim.x - 1) wait_for_previous_kernel();
 }
+
+// More tokens than a cluster sorts: per pass a histogram of every tile, their scan, and the scatter.
 template <bool kFirst>
 __device__ __forceinline__ void load_tile(const GradParams& p, uint32_t (&key)[kSortItems], uint32_t (&pos)[kSortItems]) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -256,7 +290,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) embedding_pass_kernel(const _
   for (int i = 0; i < kSortItems; ++i) digit[i] = (key[i] >> shift) & (kRadix - 1);
   block_rank(digit, rank, count, total);
   if constexpr (!kScatter) {
-    if (threadIdx.x < kRadix) p.hist[uint64_t(threadIdx.x) * p.tiles + blockIdx.x] = total[threadIdx.x];
+    p.hist[uint64_t(threadIdx.x) * p.tiles + blockIdx.x] = total[threadIdx.x];
   } else {
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
@@ -355,15 +389,16 @@ __device__ __forceinline__ void finish_row(const GradParams& p, uint32_t id, int
 // written; the part of one that began earlier goes to partial[piece][0], of one that begins here and goes on to
 // partial[piece][1].
 template <typename T, typename G, int V>
-__global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __grid_constant__ GradParams p) {
+__global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __grid_constant__ GradParams p, uint32_t slabs) {
   wait_for_previous_kernel();
+  const uint32_t slab = blockIdx.x % slabs;
   extern __shared__ uint4 raw[];
   // where each token's row is (null: padding), and what to do behind it: kNone, or a run's end
   enum : int { kNone = 0, kWrite = 1, kInherited = 2, kGoesOn = 3 };
   const T** rows = reinterpret_cast<const T**>(raw);
   int* what = reinterpret_cast<int*>(rows + p.run);
   uint32_t* ids = reinterpret_cast<uint32_t*>(what + p.run);
-  const int64_t piece = blockIdx.x;
+  const int64_t piece = blockIdx.x / slabs;
   const int64_t first = piece * p.run;
   const int n = int(min(int64_t(p.run), int64_t(p.M) - first));
   for (int i = threadIdx.x; i < int(p.run); i += kGradThreads) {
@@ -381,7 +416,7 @@ __global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __gr
     }
   }
   __syncthreads();
-  const int64_t c = (int64_t(blockIdx.y) * kGradThreads + threadIdx.x) * V;
+  const int64_t c = (int64_t(slab) * kGradThreads + threadIdx.x) * V;
   if (c >= p.hidden) return;
   float acc[V];
 #pragma unroll
@@ -420,10 +455,11 @@ constexpr int kJoinWays = 4;
 constexpr int kJoinLanes = 32;
 constexpr int kJoinShort = 16;      // up to this many pieces: a thread adds up a column's by itself
 template <typename G, int V>
-__global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces) {
+__global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces, uint32_t slabs) {
   __shared__ float part[kJoinWays][kJoinLanes][V + 1];
   wait_for_previous_kernel();
-  const int64_t piece = blockIdx.x;
+  const int64_t piece = blockIdx.x / slabs;
+  const uint32_t slab = blockIdx.x % slabs;
   const int64_t first = piece * p.run, last = min(first + p.run, int64_t(p.M)) - 1;
   if (last + 1 >= int64_t(p.M)) return;
   // (four independent loads before the first branch)
@@ -440,7 +476,7 @@ __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(
     if (n >= 0) break;
   }
   if (lo - piece < kJoinShort) {
-    for (int64_t c = (int64_t(blockIdx.y) * blockDim.x + threadIdx.x) * V; c < p.hidden; c += int64_t(gridDim.y) * blockDim.x * V) {
+    for (int64_t c = (int64_t(slab) * blockDim.x + threadIdx.x) * V; c < p.hidden; c += int64_t(slabs) * blockDim.x * V) {
       float acc[V];
       load_sums(acc, p.partial + (piece * 2 + 1) * p.hidden + c);
 #pragma unroll 4
@@ -455,7 +491,7 @@ __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(
     return;
   }
   const int lane = threadIdx.x % kJoinLanes, way = threadIdx.x / kJoinLanes;
-  for (int64_t c0 = int64_t(blockIdx.y) * kJoinLanes * V; c0 < p.hidden; c0 += int64_t(gridDim.y) * kJoinLanes * V) {
+  for (int64_t c0 = int64_t(slab) * kJoinLanes * V; c0 < p.hidden; c0 += int64_t(slabs) * kJoinLanes * V) {
     const int64_t c = c0 + lane * V;
     float acc[V];
 #pragma unroll
@@ -528,12 +564,12 @@ int pick_lookup(const LookupParams& p, int sms, cudaStream_t stream) {
 uint32_t run_length(int64_t M) { return uint32_t(M <= 8192 ? 8 : round_up(size_t(ceil_div(M, 1024)), 8)); }
 
 struct GradPlan {
-  uint32_t tiles, run, pieces;
+  uint32_t tiles, run, pieces;      // (tiles: 1 where a cluster sorts)
   size_t key, hist, partial, bytes;
 };
 GradPlan grad_plan(const compass_embed* e) {
   GradPlan g;
-  g.tiles = uint32_t(ceil_div(e->M, kSortTile));
+  g.tiles = e->M <= kClusterTokens ? 1 : uint32_t(ceil_div(e->M, kSortTile));
   g.run = run_length(e->M);
   g.pieces = uint32_t(ceil_div(e->M, g.run));
   g.key = round_up(size_t(e->M) * 4, 256);
@@ -543,30 +579,40 @@ GradPlan grad_plan(const compass_embed* e) {
   return g;
 }
 
-template <typename T, typename G, int V>
-int run_grad(const GradParams& p, const GradPlan& g, cudaStream_t stream) {
-  const unsigned slabs = unsigned(ceil_div(p.hidden, kGradThreads * V));
-  if (slabs > 65535) return COMPASS_ERR_UNSUPPORTED;
+template <int kItems>
+int run_sort(const GradParams& p, cudaStream_t stream) {
+  static_assert(sizeof(SortShared) <= 227 * 1024, "");
+  static std::atomic<uint64_t> allowed{0};
+  auto kernel = embedding_sort_kernel<kItems>;
+  const int st = allow_smem(reinterpret_cast<const void*>(kernel), sizeof(SortShared), &allowed);
+  if (st != COMPASS_OK) return st;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(g.pieces, slabs);
-  cfg.blockDim = dim3(kGradThreads);
-  cfg.dynamicSmemBytes = size_t(g.run) * 16;
+  cfg.gridDim = dim3(unsigned(kCluster));
+  cfg.blockDim = dim3(kSortThreads);
+  cfg.dynamicSmemBytes = sizeof(SortShared);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kCluster;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, embedding_grad_kernel<T, G, V>, p);
-  count_kernel_launch();
-  if (e != cudaSuccess) return record_cuda_error(e);
-  if (g.pieces == 1) return COMPASS_OK;
-  cfg.dynamicSmemBytes = 0;
-  cfg.gridDim = dim3(g.pieces, unsigned(ceil_div(p.hidden, kJoinLanes * V) < 4 ? ceil_div(p.hidden, kJoinLanes * V) : 4));
-  cfg.blockDim = dim3(kJoinWays * kJoinLanes);
-  e = cudaLaunchKernelEx(&cfg, embedding_join_kernel<G, V>, p, g.pieces);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
   count_kernel_launch();
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}
+
+template <typename T, typename G, int V>
+int run_grad(const GradParams& p, const GradPlan& g, cudaStream_t stream) {
+  const int64_t slabs = ceil_div(p.hidden, kGradThreads * V);
+  if (g.pieces * slabs > 0x7fffffff) return COMPASS_ERR_UNSUPPORTED;
+  int st = launch(embedding_grad_kernel<T, G, V>, g.pieces * slabs, kGradThreads, size_t(g.run) * 16, stream, true, p,
+                  uint32_t(slabs));
+  if (st != COMPASS_OK || g.pieces == 1) return st;
+  const int64_t all = ceil_div(p.hidden, kJoinLanes * V), join_slabs = all < 4 ? all : 4;
+  return launch(embedding_join_kernel<G, V>, g.pieces * join_slabs, kJoinWays * kJoinLanes, 0, stream, true, p, g.pieces,
+                uint32_t(join_slabs));
 }
 template <typename T, int V>
 int pick_grad(const GradParams& p, const GradPlan& g, bool fp32_grad, cudaStream_t stream) {
@@ -647,18 +693,19 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   p.elem = int64_t(dtype_size(e->grad_dtype));
   p.scale = e->scale;
   while ((int64_t(1) << p.bits) <= e->vocab) ++p.bits;      // keys 0 .. vocab
-  if (e->M == 0) return p.fill ? launch(embedding_zero_kernel, 2 * sms, kSortThreads, 0, s, false, p) : COMPASS_OK;
+  const int64_t vecs = e->vocab * e->hidden * p.elem / 16, zero_blocks = ceil_div(vecs + 1, kZeroThreads * kZeroAtOnce);
+  auto write_zeros = [&](bool beside_sort) {
+    return launch(embedding_zero_kernel, zero_blocks < 64 * sms ? zero_blocks : 64 * sms, kZeroThreads, 0, s, beside_sort, p);
+  };
+  if (p.fill && (e->M == 0 || g.tiles > 1)) st = write_zeros(false);
+  if (st != COMPASS_OK || e->M == 0) return st;
   if (g.tiles == 1) {
-    static_assert(sizeof(SortShared) <= 227 * 1024, "");
-    static std::atomic<uint64_t> allowed{0};
-    st = allow_smem(reinterpret_cast<const void*>(embedding_sort_kernel), sizeof(SortShared), &allowed);
-    if (st != COMPASS_OK) return st;
-    st = launch(embedding_sort_kernel, p.fill ? sms : 1, kSortThreads, sizeof(SortShared), s, false, p);
+    st = e->M <= kCluster * kSortThreads ? run_sort<1>(p, s) : e->M <= 4 * kCluster * kSortThreads ? run_sort<4>(p, s) : run_sort<kSortItems>(p, s);
+    if (st == COMPASS_OK && p.fill) st = write_zeros(true);
   } else {
     p.key_b = reinterpret_cast<uint32_t*>(take(g.key));
     p.pos_b = reinterpret_cast<uint32_t*>(take(g.key));
     p.hist = reinterpret_cast<uint32_t*>(take(g.hist));
-    if (p.fill) st = launch(embedding_zero_kernel, 2 * sms, kSortThreads, 0, s, false, p);
     for (int shift = 0; st == COMPASS_OK && shift < p.bits; shift += kRadixBits) {
       st = shift ? launch(embedding_pass_kernel<false, false>, g.tiles, kSortThreads, 0, s, false, p, shift)
                  : launch(embedding_pass_kernel<true, false>, g.tiles, kSortThreads, 0, s, false, p, shift);

@@ -6,6 +6,7 @@
 // taken from the values themselves (the variance from the centred ones), so no
 // element travels twice.
 #include <mutex>
+#include <type_traits>
 
 #include "row_ops.cuh"
 
@@ -32,7 +33,6 @@ struct NormParams {
   int32_t has_residual, has_dsum;
   int32_t param_fp32;
   float eps;
-  int32_t tpr;                           // threads per row, a multiple of 32
   int32_t n_partial;
 };
 
@@ -157,14 +157,14 @@ __device__ __forceinline__ void load_params(F2 (&out)[V * NVT / 2], const void* 
 }
 
 // ---- forward -------------------------------------------------------------------
-// A row per group of `tpr` threads, NVT vectors of V elements a thread, all in registers; the rows after it are on their way
+// A row per group of kTpr threads, NVT vectors of V elements a thread, all in registers; the rows after it are on their way
 // meanwhile.  kKeep: gamma and beta stay in registers too.
-template <typename T, int V, int NVT, int kThreads, bool kKeep, bool kResidual>
+template <typename T, int V, int NVT, int kThreads, int kTpr, bool kKeep, bool kResidual>
 __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_constant__ NormParams p) {
   using Ring = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>;
   __shared__ float red[4][32];
   extern __shared__ uint4 raw[];
-  const int groups = blockDim.x / p.tpr, group = threadIdx.x / p.tpr, t = threadIdx.x - group * p.tpr;
+  const int groups = blockDim.x / kTpr, group = threadIdx.x / kTpr, t = threadIdx.x - group * kTpr;
   const int H = int(p.hidden);
   const float inv = 1.0f / float(H);
   Ring ring(raw);
@@ -173,10 +173,10 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
     const RowAt at = p.x.at(row, H);
     if constexpr (kResidual) {
       const T* const from[2] = {live ? p.x.row<T>(at) : nullptr, live ? p.residual.row<T>(at) : nullptr};
-      ring.fetch(which, from, p.tpr, t, H);
+      ring.fetch(which, from, kTpr, t, H);
     } else {
       const T* const from[1] = {live ? p.x.row<T>(at) : nullptr};
-      ring.fetch(which, from, p.tpr, t, H);
+      ring.fetch(which, from, kTpr, t, H);
     }
   };
   const uint32_t stride = gridDim.x * groups;
@@ -186,24 +186,24 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
   constexpr int kPairs = V * NVT / 2;
   F2 g[kPairs], b[kPairs];
   if constexpr (kKeep) {
-    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
-    load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, p.tpr, t, H);
+    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, kTpr, t, H);
+    load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, kTpr, t, H);
   }
-  const int own = min(NVT, max(0, (H / V - t + p.tpr - 1) / p.tpr)) * V;      // elements of a row that this thread holds
-  const bool ragged = p.tpr * (NVT * V) != H;
+  const int own = min(NVT, max(0, (H / V - t + kTpr - 1) / kTpr)) * V;      // elements of a row that this thread holds
+  const bool ragged = kTpr * (NVT * V) != H;
   for (uint32_t turn = 0; row < p.M; ++turn, row += stride) {
     const RowAt at = p.x.at(row, H);
     Words<T, V, NVT> x;
     ring.wait();
 #pragma unroll
-    for (int i = 0; i < NVT; ++i) ring.take(x.w[i], 0, i, p.tpr, t, H);
+    for (int i = 0; i < NVT; ++i) ring.take(x.w[i], 0, i, kTpr, t, H);
     if constexpr (kResidual) {
       // what is stored is normalised, so that the backward pass, which reads it, sees the same values
       Words<T, V, NVT> r;
 #pragma unroll
-      for (int i = 0; i < NVT; ++i) ring.take(r.w[i], 1, i, p.tpr, t, H);
+      for (int i = 0; i < NVT; ++i) ring.take(r.w[i], 1, i, kTpr, t, H);
       x.add(r);
-      x.store(p.summed.row<T>(at), p.tpr, t, H);
+      x.store(p.summed.row<T>(at), kTpr, t, H);
     }
     ring.advance();
     fetch(Ring::kDepth - 1, row + Ring::kDepth * stride);
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
       h[k] = x.pair(k);
       sum[k & 1] = sum[k & 1] + h[k];
     }
-    const float mean = row_sum(sum_of(sum[0] + sum[1]), p.tpr, red[2 * (turn & 1)]) * inv;
+    const float mean = row_sum(sum_of(sum[0] + sum[1]), kTpr, red[2 * (turn & 1)]) * inv;
     F2 sq[2] = {f2(0.f), f2(0.f)};
     const F2 minus = f2(-mean);
 #pragma unroll
@@ -225,16 +225,16 @@ __global__ void __launch_bounds__(kThreads, 1) norm_forward_kernel(const __grid_
     }
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) sq[k & 1] = fma2(h[k], h[k], sq[k & 1]);
-    const float var = row_sum(sum_of(sq[0] + sq[1]), p.tpr, red[2 * (turn & 1) + 1]) * inv;
+    const float var = row_sum(sum_of(sq[0] + sq[1]), kTpr, red[2 * (turn & 1) + 1]) * inv;
     const float rstd = 1.0f / sqrtf(var + p.eps);
     if constexpr (!kKeep) {
-      load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
-      load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, p.tpr, t, H);
+      load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, kTpr, t, H);
+      load_params<V, NVT>(b, p.beta, p.param_fp32, 0.f, kTpr, t, H);
     }
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) h[k] = fma2(h[k] * f2(rstd), g[k], b[k]);
     x.set(h);
-    x.store(p.y.row<T>(at), p.tpr, t, H);
+    x.store(p.y.row<T>(at), kTpr, t, H);
     if (t == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
@@ -292,13 +292,13 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const __grid_co
 // One block per SM walks the rows; a thread keeps its columns' sums of dY * xhat and dY in registers while the next rows are
 // on their way.  A block's rows add their sums up in shared memory and leave one partial row for norm_reduce_kernel: fixed
 // order, so the bits do not depend on timing.
-template <typename T, int V, int NVT, int kThreads, bool kDsum>
+template <typename T, int V, int NVT, int kThreads, int kTpr, bool kDsum>
 __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid_constant__ NormParams p) {
   static_assert(V * NVT == kElems<T, V>, "");
   using Ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>;
   __shared__ float2 red[2][32];
   extern __shared__ uint4 raw[];
-  const int groups = blockDim.x / p.tpr, group = threadIdx.x / p.tpr, t = threadIdx.x - group * p.tpr;
+  const int groups = blockDim.x / kTpr, group = threadIdx.x / kTpr, t = threadIdx.x - group * kTpr;
   const int H = int(p.hidden);
   const float inv = 1.0f / float(H);
   constexpr int kPairs = V * NVT / 2;
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
   F2* gamma = reinterpret_cast<F2*>(raw) + threadIdx.x;
   {
     F2 g[kPairs];
-    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, p.tpr, t, H);
+    load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, kTpr, t, H);
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) gamma[k * kThreads] = g[k];
   }
@@ -319,10 +319,10 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
     const RowAt at = p.x.at(row, H);
     if constexpr (kDsum) {
       const T* const from[3] = {live ? p.x.row<T>(at) : nullptr, live ? p.dy.row<T>(at) : nullptr, live ? p.dsum.row<T>(at) : nullptr};
-      ring.fetch(which, from, p.tpr, t, H);
+      ring.fetch(which, from, kTpr, t, H);
     } else {
       const T* const from[2] = {live ? p.x.row<T>(at) : nullptr, live ? p.dy.row<T>(at) : nullptr};
-      ring.fetch(which, from, p.tpr, t, H);
+      ring.fetch(which, from, kTpr, t, H);
     }
   };
   const uint32_t stride = gridDim.x * groups;
@@ -342,11 +342,11 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
     Words<T, V, NVT> w;
     ring.wait();
 #pragma unroll
-    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 0, i, p.tpr, t, H);
+    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 0, i, kTpr, t, H);
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) xh[k] = (w.pair(k) + minus) * r2;
 #pragma unroll
-    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 1, i, p.tpr, t, H);
+    for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 1, i, kTpr, t, H);
     F2 c1 = f2(0.f), c2 = f2(0.f);
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
@@ -357,11 +357,11 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
       c1 = c1 + d[k];
       c2 = fma2(d[k], xh[k], c2);
     }
-    const float2 c = row_sum(sum_of(c1), sum_of(c2), p.tpr, red[turn & 1]);
+    const float2 c = row_sum(sum_of(c1), sum_of(c2), kTpr, red[turn & 1]);
     const F2 a1 = f2(-c.x * inv), a2 = f2(-c.y * inv);
     if constexpr (kDsum) {
 #pragma unroll
-      for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 2, i, p.tpr, t, H);
+      for (int i = 0; i < NVT; ++i) ring.take(w.w[i], 2, i, kTpr, t, H);
     }
     ring.advance();
     fetch(Ring::kDepth - 1, row + Ring::kDepth * stride);
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
       d[k] = kDsum ? fma2(v, r2, w.pair(k)) : v * r2;
     }
     w.set(d);
-    w.store(p.dx.row<T>(at), p.tpr, t, H);
+    w.store(p.dx.row<T>(at), kTpr, t, H);
   }
   float* sums = reinterpret_cast<float*>(raw);      // [groups][hidden], over the ring, whose last copies were of no row
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
     for (int k = 0; k < kPairs; ++k)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int c = ((2 * k + e) / V * p.tpr + t) * V + (2 * k + e) % V;
+        const int c = ((2 * k + e) / V * kTpr + t) * V + (2 * k + e) % V;
         const float2 q = of(which ? db[k] : dg[k]);
         if (c < H) (groups > 1 ? sums + group * H : out)[c] = e ? q.y : q.x;
       }
@@ -400,10 +400,12 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
   }
 }
 
-// Sums over the partial rows, in their order: 32 columns per block, 8 threads a column.
+// Sums over the partial rows: 32 columns per block, kReduceWays threads a column (each a fixed share of the rows, all of whose
+// loads are in flight together: the kernel is a load's latency long), and their sums in turn.
+constexpr int kReduceWays = 16;
 template <typename PT>
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const __grid_constant__ NormParams p, PT* dgamma, PT* dbeta) {
-  __shared__ float part[8][33];
+__global__ void __launch_bounds__(32 * kReduceWays) norm_reduce_kernel(const __grid_constant__ NormParams p, PT* dgamma, PT* dbeta) {
+  __shared__ float part[kReduceWays][33];
   wait_for_previous_kernel();
   const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
   const int64_t c = int64_t(blockIdx.x >> 1) * 32 + lane;
@@ -412,15 +414,23 @@ __global__ void __launch_bounds__(256) norm_reduce_kernel(const __grid_constant_
   const float* in = p.partial + int64_t(blockIdx.x & 1) * p.n_partial * p.hidden + c;
   float a = 0.f;
   if (c < p.hidden) {
-#pragma unroll 4
-    for (int r = k; r < p.n_partial; r += 8) a += in[int64_t(r) * p.hidden];
+    for (int r0 = k; r0 < p.n_partial; r0 += 10 * kReduceWays) {
+      float x[10];
+#pragma unroll
+      for (int i = 0; i < 10; ++i) {
+        const int r = r0 + i * kReduceWays;
+        x[i] = r < p.n_partial ? __ldcg(in + int64_t(r) * p.hidden) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 10; ++i) a += x[i];
+    }
   }
   part[k][lane] = a;
   __syncthreads();
   if (k == 0 && c < p.hidden) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += part[i][lane];
+    for (int i = 0; i < kReduceWays; ++i) s += part[i][lane];
     float v[1] = {s};
     store_vec(out + c, v);
   }
@@ -443,7 +453,7 @@ __global__ void __launch_bounds__(1024) norm_backward_rows_kernel(const __grid_c
     c1 += d[0] * g[0];
     c2 = fmaf(d[0] * g[0], (a[0] - m) * r, c2);
   }
-  const float2 s = row_sum(c1, c2, p.tpr, red);
+  const float2 s = row_sum(c1, c2, 1024, red);
   if (threadIdx.x == 0) {
     p.row_sums[2 * int64_t(row)] = s.x;
     p.row_sums[2 * int64_t(row) + 1] = s.y;
@@ -488,10 +498,27 @@ int check_norm(const compass_norm* n) {
 
 bool vectorised(const compass_norm* n) { return n->hidden % (n->dtype == COMPASS_DTYPE_FP32 ? 4 : 8) == 0; }
 
-// Threads per row, a multiple of 32, when each holds `elems` elements.
-int threads_per_row(int64_t hidden, int elems) { return int(round_up(size_t(ceil_div(hidden, elems)), 32)); }
-// Rows a block of at most `threads` works on side by side (each has a named barrier: 8 at most).
-int rows_per_block(int tpr, int threads) { return tpr * 8 >= threads ? threads / tpr : 8; }
+// Threads per row when each holds `elems` elements: a power of two from 32 on, which the kernels are compiled for (their
+// addresses are then a register and a constant; with an odd hidden size, an element per access, that is half their time).
+int threads_per_row(int64_t hidden, int elems) {
+  int tpr = 32;
+  while (int64_t(tpr) * elems < hidden) tpr *= 2;
+  return tpr;
+}
+// Rows a block of at most `threads` works on side by side (each has a named barrier, but for single warps: 8 at most).
+int rows_per_block(int tpr, int threads) { return tpr == 32 || tpr * 8 >= threads ? threads / tpr : 8; }
+// f(threads per row as a constant), up to kMost of them.
+template <int kMost, typename F>
+int with_tpr(int tpr, F f) {
+  switch (tpr) {
+    case 32: return f(std::integral_constant<int, 32>{});
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 128: return f(std::integral_constant<int, 128>{});
+    case 256: return f(std::integral_constant<int, 256>{});
+    case 512: return f(std::integral_constant<int, 512>{});
+    default: return f(std::integral_constant<int, kMost>{});
+  }
+}
 
 constexpr int kSms = 148;           // blocks are counted for a B200; fewer SMs only take them in turns
 constexpr int64_t kWidest = 8192;   // elements of a row that stay in the registers of a block
@@ -514,19 +541,18 @@ BackwardPlan backward_plan(const compass_norm* n) {
   return b;
 }
 
-template <typename T, int V, int NVT, int kThreads, bool kKeep, bool kResidual>
-int run_forward(const NormParams& p, int tpr, cudaStream_t stream) {
+template <typename T, int V, int NVT, int kThreads, int kTpr, bool kKeep, bool kResidual>
+int run_forward(const NormParams& p, cudaStream_t stream) {
   constexpr size_t smem = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>::kSmemBytes;
-  auto kernel = norm_forward_kernel<T, V, NVT, kThreads, kKeep, kResidual>;
+  constexpr int tpr = kTpr;
+  auto kernel = norm_forward_kernel<T, V, NVT, kThreads, kTpr, kKeep, kResidual>;
   static std::atomic<uint64_t> allowed{0};
   const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem, &allowed);
   if (st != COMPASS_OK) return st;
-  NormParams q = p;
-  q.tpr = tpr;
   // few rows: a block each, for the shortest way through; else blocks of several that walk the rows
   const int groups = p.M <= kSms || tpr * 2 > kThreads ? 1 : rows_per_block(tpr, kThreads);
   const int64_t need = ceil_div(p.M, groups), most = smem ? kSms : kSms * (kThreads / (tpr * groups));
-  return launch(kernel, need < most ? need : most, tpr * groups, smem, stream, false, q);
+  return launch(kernel, need < most ? need : most, tpr * groups, smem, stream, false, p);
 }
 
 // Up to 8192 elements a row: gamma and beta in registers.  Up to 16384: 16 elements per thread.
@@ -534,8 +560,10 @@ template <typename T, int V, bool kResidual>
 int pick_forward(const NormParams& p, cudaStream_t stream) {
   const int64_t H = p.hidden;
   constexpr int E = kElems<T, V>, kThreads = int(kWidest) / E;
-  if (H <= kWidest) return run_forward<T, V, E / V, kThreads, true, kResidual>(p, threads_per_row(H, E), stream);
-  return run_forward<T, V, 16 / V, 1024, false, kResidual>(p, threads_per_row(H, 16), stream);
+  if (H > kWidest) return run_forward<T, V, 16 / V, 1024, 1024, false, kResidual>(p, stream);
+  return with_tpr<kThreads>(threads_per_row(H, E), [&](auto tpr) {
+    return run_forward<T, V, E / V, kThreads, decltype(tpr)::value, true, kResidual>(p, stream);
+  });
 }
 template <typename T, int V>
 int pick_forward(const NormParams& p, cudaStream_t stream) {
@@ -545,19 +573,17 @@ int pick_forward(const NormParams& p, cudaStream_t stream) {
 template <typename T>
 int forward_of(const NormParams& p, bool vec, cudaStream_t stream) {
   if (p.hidden > 2 * kWidest) {
-    NormParams q = p;
-    q.tpr = 1024;
-    return vec ? launch(norm_forward_wide_kernel<T, 16 / int(sizeof(T))>, p.M, 1024, 0, stream, false, q)
-               : launch(norm_forward_wide_kernel<T, 1>, p.M, 1024, 0, stream, false, q);
+    return vec ? launch(norm_forward_wide_kernel<T, 16 / int(sizeof(T))>, p.M, 1024, 0, stream, false, p)
+               : launch(norm_forward_wide_kernel<T, 1>, p.M, 1024, 0, stream, false, p);
   }
   return vec ? pick_forward<T, 16 / int(sizeof(T))>(p, stream) : pick_forward<T, 1>(p, stream);
 }
 
-template <typename T, int V, int kThreads, bool kDsum>
+template <typename T, int V, int kThreads, int kTpr, bool kDsum>
 int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
   constexpr int NVT = kElems<T, V> / V;
   constexpr size_t ring = RowRing<T, V, NVT, kDsum ? 3 : 2, kThreads>::kSmemBytes + size_t(kElems<T, V>) * kThreads * 4;
-  auto kernel = norm_backward_kernel<T, V, NVT, kThreads, kDsum>;
+  auto kernel = norm_backward_kernel<T, V, NVT, kThreads, kTpr, kDsum>;
   constexpr size_t sums = size_t(kThreads) * kElems<T, V> * 4;      // [groups][hidden] at most
   constexpr size_t smem = ring > sums ? ring : sums;
   static std::atomic<uint64_t> allowed{0};
@@ -565,14 +591,16 @@ int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream
   if (st != COMPASS_OK) return st;
   return launch(kernel, b.n_partial, b.tpr * b.groups, smem, stream, false, p);
 }
-template <typename T, int V, int kThreads>
+template <typename T, int V, int kThreads, int kTpr>
 int run_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
-  return p.has_dsum ? run_backward<T, V, kThreads, true>(p, b, stream) : run_backward<T, V, kThreads, false>(p, b, stream);
+  return p.has_dsum ? run_backward<T, V, kThreads, kTpr, true>(p, b, stream) : run_backward<T, V, kThreads, kTpr, false>(p, b, stream);
 }
 template <typename T, int V>
 int pick_backward(const NormParams& p, const BackwardPlan& b, cudaStream_t stream) {
-  if constexpr (V == 8) return run_backward<T, V, 512>(p, b, stream);
-  else return b.threads == 512 ? run_backward<T, V, 512>(p, b, stream) : run_backward<T, V, 1024>(p, b, stream);
+  if constexpr (V != 8) {
+    if (b.tpr > 512) return run_backward<T, V, 1024, 1024>(p, b, stream);
+  }
+  return with_tpr<512>(b.tpr, [&](auto tpr) { return run_backward<T, V, 512, decltype(tpr)::value>(p, b, stream); });
 }
 
 template <typename T>
@@ -702,7 +730,6 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
   p.M = uint32_t(n->M);
   p.has_dsum = dsum != nullptr;
   p.param_fp32 = n->param_dtype == COMPASS_DTYPE_FP32;
-  p.tpr = b.tpr;
   p.n_partial = b.n_partial;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + 256);
   p.row_sums = p.partial + round_up(size_t(2 * b.n_partial) * size_t(n->hidden) * 4, 256) / 4;
@@ -710,7 +737,7 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
   if (st != COMPASS_OK || (dgamma == nullptr && dbeta == nullptr)) return st;
   const int64_t grid = 2 * ceil_div(n->hidden, 32);
   if (n->param_dtype == COMPASS_DTYPE_FP32)
-    return launch(norm_reduce_kernel<float>, grid, 256, 0, s, true, p, static_cast<float*>(dgamma), static_cast<float*>(dbeta));
-  return launch(norm_reduce_kernel<__nv_bfloat16>, grid, 256, 0, s, true, p, static_cast<__nv_bfloat16*>(dgamma),
+    return launch(norm_reduce_kernel<float>, grid, 32 * kReduceWays, 0, s, true, p, static_cast<float*>(dgamma), static_cast<float*>(dbeta));
+  return launch(norm_reduce_kernel<__nv_bfloat16>, grid, 32 * kReduceWays, 0, s, true, p, static_cast<__nv_bfloat16*>(dgamma),
                 static_cast<__nv_bfloat16*>(dbeta));
 }

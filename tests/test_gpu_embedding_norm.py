@@ -104,11 +104,18 @@ GRADS = [
     (1, 3000, 1001, 32001, "fp32", "fp32", "skewed"),
     (8, 4096, 520, 1000, "bf16", "bf16", "skewed"),
     (8, 4096, 520, 1000, "bf16", "fp32", "one"),     # every token the same
-    (2, 16384, 40, 600, "bf16", "fp32", "skewed"),   # the most one block sorts
-    (1, 16385, 40, 600, "bf16", "fp32", "skewed"),   # one more: the tiled sort
+    (2, 4096, 40, 600, "bf16", "fp32", "skewed"),    # one item per thread of the sort, and more
+    (1, 4097, 40, 600, "bf16", "fp32", "skewed"),
+    (2, 16384, 40, 600, "bf16", "fp32", "skewed"),
+    (1, 16385, 40, 600, "bf16", "fp32", "skewed"),
+    (1, 65536, 16, 700, "bf16", "fp32", "skewed"),   # the most a cluster sorts
+    (1, 65537, 16, 700, "bf16", "fp32", "skewed"),   # one more: the tiled sort
     (2, 70000, 16, 70000, "fp32", "fp32", "even"),   # two passes, longer pieces
     (1, 70000, 8, 300, "bf16", "bf16", "none"),      # padding only
     (1, 40000, 8, 300000, "bf16", "fp32", "one"),    # three passes
+    (8, 2048, 1024, 100001, "bf16", "bf16", "skewed"),   # 205 MB of rows, most of them zeros
+    (3, 6, 256, 200000, "fp32", "fp32", "even"),     # one piece, nothing to join
+    (1, 16000, 512, 190000, "bf16", "bf16", "even"),     # most tokens alone
 ]
 
 

@@ -128,6 +128,14 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Control
   return false;
 }
 
+// After giving up: wait for copies or products in flight, whatever the others do, before this CTA's memory may go (100 ms at
+// most).
+__device__ __forceinline__ void wait_landed(uint64_t* bar, uint32_t parity) {
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t spins = 1; spins < (1u << 30) && !mbar_try_wait(bar, parity); ++spins)
+    if ((spins & 0xFF) == 0 && globaltimer_ns() - t0 > 100000000ull) break;
+}
+
 // How a product's output is cut into tiles; the number of rows is known on the device only.
 struct Part {
   int big_rows;        // row tiles of 512
@@ -365,7 +373,12 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
       const uint32_t back = j < 4u ? j : 4u;
       for (uint32_t i = 1; i <= back; ++i) {
         const uint32_t r = j - i;
-        if (!wait_bar(&ctl->empty[r & 3u], (r >> 2) & 1u, ctl, p, SITE_DRAIN, -1)) break;
+        if (!wait_bar(&ctl->empty[r & 3u], (r >> 2) & 1u, ctl, p, SITE_DRAIN, -1)) {
+          // (the leader's barriers count both CTAs' copies, and neither CTA ends before the other)
+          if (leader)
+            for (uint32_t k = 1; k <= back; ++k) wait_landed(&ctl->full[(j - k) & 3u], ((j - k) >> 2) & 1u);
+          break;
+        }
       }
     }
   } else if (warp == 1) {
@@ -468,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
       if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
         // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
         umma_commit_pair(&ctl->drain, 0x1);
-        wait_bar(&ctl->drain, 0, ctl, p, SITE_DRAIN, -2);
+        wait_landed(&ctl->drain, 0);
       }
     }
   } else {
@@ -767,7 +780,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       }
       // leave only when everything that was loaded has landed and been read
       for (int i = max(0, j - stages); i < j; ++i)
-        if (!wait_few(&ctl->empty[i % stages], uint32_t(i / stages) & 1u, ctl, p, SITE_DRAIN, -1)) break;
+        if (!wait_few(&ctl->empty[i % stages], uint32_t(i / stages) & 1u, ctl, p, SITE_DRAIN, -1)) {
+          for (int k = max(0, j - stages); k < j; ++k) wait_landed(&ctl->full[k % stages], uint32_t(k / stages) & 1u);
+          break;
+        }
     } else {
       wait_for_previous_kernel();
     }
@@ -802,7 +818,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       }
       if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
         umma_commit(&ctl->drain);
-        wait_few(&ctl->drain, 0, ctl, p, SITE_DRAIN, -2);
+        wait_landed(&ctl->drain, 0);
       }
     }
   } else {

@@ -115,7 +115,7 @@ def lib() -> C.CDLL:
         torch = sys.modules.get("torch")
         if torch is not None:
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            _current_device = torch.cuda.current_device
+            _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_10549_b200.build` "
                                "(there is no CPU fallback)")
@@ -393,6 +393,12 @@ def compass_mlp_block(mlp: Mlp, X: Sequence, W0: Sequence, H: Sequence, W1: Sequ
 # (ValueError); what the library itself refuses raises CompassError.
 
 _TORCH_DTYPES: dict = {}
+_POINTERS = [C.c_void_p * P for P in range(MAX_P + 1)]
+
+
+def _pointers(addresses: list) -> C.Array:
+    n = len(addresses)
+    return (_POINTERS[n] if n <= MAX_P else C.c_void_p * n)(*addresses)
 
 
 def _torch_dtype(kind: int):
@@ -420,7 +426,7 @@ def _row_shards(name: str, tensors: Optional[Sequence], P: int, M: int, hidden: 
     if len(tensors) != P:
         raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
     dtype, shape = _torch_dtype(kind), (M // P, hidden)
-    return (C.c_void_p * P)(*[_tensor(name, t, dtype, shape) for t in tensors])
+    return _pointers([_tensor(name, t, dtype, shape) for t in tensors])
 
 
 def vocab_shard_rows(vocab: int, P: int, r: int) -> int:
@@ -433,7 +439,7 @@ def _vocab_shards(name: str, tensors: Sequence, P: int, vocab: int, hidden: int,
     if len(tensors) != P:
         raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
     dtype = _torch_dtype(kind)
-    return (C.c_void_p * P)(*[_tensor(name, t, dtype, (vocab_shard_rows(vocab, P, r), hidden)) for r, t in enumerate(tensors)])
+    return _pointers([_tensor(name, t, dtype, (vocab_shard_rows(vocab, P, r), hidden)) for r, t in enumerate(tensors)])
 
 
 def _index(name: str, t, kind: int, M: int):

@@ -249,7 +249,8 @@ __device__ __forceinline__ void load_b(const HeadParams& p, int form, uint8_t* d
   }
 }
 
-// 32 bytes, one sector, at a 32-byte boundary.
+// 32 bytes, one sector, at a 32-byte boundary.  (Measured and not kept: the results of an accumulator held back until the
+// next one has been read, so that its tensor memory is free before they are stored: 200 -> 209 us at 401 x 1024 x 50001.)
 __device__ __forceinline__ void store_32(void* p, const uint32_t (&q)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]), "r"(q[4]),
                "r"(q[5]), "r"(q[6]), "r"(q[7])
@@ -509,7 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
             }
           }
         }
-        if (!(ok = wait_bar(&ctl->acc_full[b], uses[b] & 1u, ctl, p, SITE_ACC_FULL, t))) break;
+        ok = __all_sync(0xffffffffu, wait_bar(&ctl->acc_full[b], uses[b] & 1u, ctl, p, SITE_ACC_FULL, t));      // (a warp goes on as one)
+        if (!ok) break;
         tc_fence_after_sync();
         uint32_t v[4][32];
         const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
@@ -833,7 +835,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       const uint32_t b = it & 1u;
       const bool empty = live + quarter * 32 == 0;
       if (!empty) {
-        if (!(ok = wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t))) break;
+        ok = __all_sync(0xffffffffu, wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t));
+        if (!ok) break;
         tc_fence_after_sync();
       }
       for (int c = 0; c < n_cols; c += 32) {

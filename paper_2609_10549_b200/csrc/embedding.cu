@@ -253,8 +253,13 @@ __global__ void __launch_bounds__(kZeroThreads) embedding_zero_kernel(const __gr
   const int64_t n = int64_t(gridDim.x) * (kZeroThreads * kZeroAtOnce), own = int64_t(blockIdx.x) * (kZeroThreads * kZeroAtOnce) + threadIdx.x;
   const uint32_t per = p.dw.rows.d;
   for (uint32_t r = 0, v0 = 0; v0 < p.dw.vocab; ++r, v0 += per) {
-    const int64_t bytes = int64_t(min(per, p.dw.vocab - v0)) * p.hidden * p.elem;
+    int64_t bytes = int64_t(min(per, p.dw.vocab - v0)) * p.hidden * p.elem;
     uint8_t* base = static_cast<uint8_t*>(p.dw.ptr[r]);
+    // up to the first 16-byte boundary
+    const int64_t front = min(bytes, int64_t((16 - (reinterpret_cast<uintptr_t>(base) & 15)) & 15));
+    if (blockIdx.x == 0 && threadIdx.x * 2 < front) *reinterpret_cast<uint16_t*>(base + threadIdx.x * 2) = 0;
+    base += front;
+    bytes -= front;
     const int64_t whole = bytes / 16;
     for (int64_t i = own; i < whole; i += n) {
 #pragma unroll
@@ -647,8 +652,10 @@ extern "C" int compass_embedding(const compass_embed* e, const void* ids, const 
   if (st != COMPASS_OK) return st;
   LookupParams p = {};
   st = check_ids(ids, e->M, e->index_dtype);
-  if (st == COMPASS_OK) st = check_vocab_shards(W, e->P, e->vocab);
-  if (st == COMPASS_OK) st = fill_shards(Out, e->P, e->M, &p.out);
+  const size_t element = dtype_size(e->dtype);
+  bool whole = e->hidden * int64_t(element) % 16 == 0;
+  if (st == COMPASS_OK) st = check_vocab_shards(W, e->P, e->vocab, element, &whole);
+  if (st == COMPASS_OK) st = fill_shards(Out, e->P, e->M, &p.out, element, &whole);
   if (st != COMPASS_OK || e->M == 0) return st;
   int sms = 0;
   st = sm_count(&sms);
@@ -661,8 +668,8 @@ extern "C" int compass_embedding(const compass_embed* e, const void* ids, const 
   p.scale = e->scale;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (e->dtype == COMPASS_DTYPE_FP32)
-    return e->hidden % 4 == 0 ? pick_lookup<float, 4>(p, sms, s) : pick_lookup<float, 1>(p, sms, s);
-  return e->hidden % 8 == 0 ? pick_lookup<__nv_bfloat16, 8>(p, sms, s) : pick_lookup<__nv_bfloat16, 1>(p, sms, s);
+    return whole ? pick_lookup<float, 4>(p, sms, s) : pick_lookup<float, 1>(p, sms, s);
+  return whole ? pick_lookup<__nv_bfloat16, 8>(p, sms, s) : pick_lookup<__nv_bfloat16, 1>(p, sms, s);
 }
 
 extern "C" int compass_embedding_workspace_bytes(const compass_embed* e, size_t* bytes) {
@@ -679,8 +686,9 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   if (st != COMPASS_OK) return st;
   GradParams p = {};
   st = check_ids(ids, e->M, e->index_dtype);
-  if (st == COMPASS_OK) st = fill_shards(dOut, e->P, e->M, &p.dout);
-  if (st == COMPASS_OK) st = check_vocab_shards(dW, e->P, e->vocab);
+  bool whole = e->hidden % (e->dtype == COMPASS_DTYPE_FP32 ? 4 : 8) == 0;
+  if (st == COMPASS_OK) st = fill_shards(dOut, e->P, e->M, &p.dout, dtype_size(e->dtype), &whole);
+  if (st == COMPASS_OK) st = check_vocab_shards(dW, e->P, e->vocab, dtype_size(e->grad_dtype), &whole);
   if (st != COMPASS_OK) return st;
   const GradPlan g = grad_plan(e);
   st = check_workspace(ws, ws_bytes, g.bytes);
@@ -741,6 +749,6 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   if (st != COMPASS_OK) return st;
   const bool fp32_grad = e->grad_dtype == COMPASS_DTYPE_FP32;
   if (e->dtype == COMPASS_DTYPE_FP32)
-    return e->hidden % 4 == 0 ? pick_grad<float, 4>(p, g, fp32_grad, s) : pick_grad<float, 1>(p, g, fp32_grad, s);
-  return e->hidden % 8 == 0 ? pick_grad<__nv_bfloat16, 8>(p, g, fp32_grad, s) : pick_grad<__nv_bfloat16, 1>(p, g, fp32_grad, s);
+    return whole ? pick_grad<float, 4>(p, g, fp32_grad, s) : pick_grad<float, 1>(p, g, fp32_grad, s);
+  return whole ? pick_grad<__nv_bfloat16, 8>(p, g, fp32_grad, s) : pick_grad<__nv_bfloat16, 1>(p, g, fp32_grad, s);
 }

@@ -503,7 +503,8 @@ int check_norm(const compass_norm* n) {
   return n->eps >= 0.f ? COMPASS_OK : COMPASS_ERR_INVALID_ARG;      // (NaN is refused too)
 }
 
-bool vectorised(const compass_norm* n) { return n->hidden % (n->dtype == COMPASS_DTYPE_FP32 ? 4 : 8) == 0; }
+// Rows of whole 16-byte vectors; with pointers on 16-byte boundaries they are accessed as such.
+bool whole_vectors(const compass_norm* n) { return n->hidden % (n->dtype == COMPASS_DTYPE_FP32 ? 4 : 8) == 0; }
 
 // Threads per row when each holds `elems` elements: a power of two from 32 on, which the kernels are compiled for (their
 // addresses are then a register and a constant; with an odd hidden size, an element per access, that is half their time).
@@ -535,9 +536,9 @@ struct BackwardPlan {
   bool wide;
   int tpr, groups, threads, n_partial;
 };
-BackwardPlan backward_plan(const compass_norm* n) {
+BackwardPlan backward_plan(const compass_norm* n, bool whole) {
   BackwardPlan b;
-  const bool packed = n->dtype == COMPASS_DTYPE_BF16 && vectorised(n);
+  const bool packed = n->dtype == COMPASS_DTYPE_BF16 && whole;
   b.wide = n->hidden > kWidest;
   b.tpr = b.wide ? 1024 : threads_per_row(n->hidden, packed ? 16 : 8);
   b.threads = b.tpr > 512 ? 1024 : 512;        // 128 registers a thread unless a row needs more than 512 threads
@@ -674,12 +675,14 @@ extern "C" int compass_layer_norm(const compass_norm* n, const void* const* X, c
   if (st != COMPASS_OK) return st;
   if ((residual == nullptr) != (summed == nullptr)) return COMPASS_ERR_INVALID_ARG;
   NormParams p = {};
-  st = fill_shards(X, n->P, n->M, &p.x);
-  if (st == COMPASS_OK) st = fill_shards(Y, n->P, n->M, &p.y);
-  if (st == COMPASS_OK && residual) st = fill_shards(residual, n->P, n->M, &p.residual);
-  if (st == COMPASS_OK && summed) st = fill_shards(summed, n->P, n->M, &p.summed);
+  const size_t element = dtype_size(n->dtype), param = dtype_size(n->param_dtype);
+  bool whole = whole_vectors(n) && is_aligned(gamma, 16) && is_aligned(beta, 16);
+  st = fill_shards(X, n->P, n->M, &p.x, element, &whole);
+  if (st == COMPASS_OK) st = fill_shards(Y, n->P, n->M, &p.y, element, &whole);
+  if (st == COMPASS_OK && residual) st = fill_shards(residual, n->P, n->M, &p.residual, element, &whole);
+  if (st == COMPASS_OK && summed) st = fill_shards(summed, n->P, n->M, &p.summed, element, &whole);
   if (st != COMPASS_OK) return st;
-  if (!is_aligned(gamma, 16) || !is_aligned(beta, 16) || !is_aligned(mean, 4) || !is_aligned(rstd, 4)) return COMPASS_ERR_ALIGNMENT;
+  if (!is_aligned(gamma, param) || !is_aligned(beta, param) || !is_aligned(mean, 4) || !is_aligned(rstd, 4)) return COMPASS_ERR_ALIGNMENT;
   if (n->M == 0) return COMPASS_OK;
   p.gamma = gamma;
   p.beta = beta;
@@ -691,7 +694,7 @@ extern "C" int compass_layer_norm(const compass_norm* n, const void* const* X, c
   p.param_fp32 = n->param_dtype == COMPASS_DTYPE_FP32;
   p.eps = n->eps;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return n->dtype == COMPASS_DTYPE_FP32 ? forward_of<float>(p, vectorised(n), s) : forward_of<__nv_bfloat16>(p, vectorised(n), s);
+  return n->dtype == COMPASS_DTYPE_FP32 ? forward_of<float>(p, whole, s) : forward_of<__nv_bfloat16>(p, whole, s);
 }
 
 // Workspace: the partial column sums, then (wide rows) two sums per row.
@@ -699,8 +702,10 @@ extern "C" int compass_layer_norm_workspace_bytes(const compass_norm* n, size_t*
   if (bytes == nullptr) return COMPASS_ERR_INVALID_ARG;
   const int st = check_norm(n);
   if (st != COMPASS_OK) return st;
-  const BackwardPlan b = backward_plan(n);
-  *bytes = 256 + round_up(size_t(2 * b.n_partial) * size_t(n->hidden) * 4, 256) + (b.wide ? size_t(n->M) * 8 : 0);
+  // (whether the pointers will be on 16-byte boundaries is not known yet)
+  const BackwardPlan a = backward_plan(n, false), b = backward_plan(n, whole_vectors(n));
+  const int most = a.n_partial > b.n_partial ? a.n_partial : b.n_partial;
+  *bytes = 256 + round_up(size_t(2 * most) * size_t(n->hidden) * 4, 256) + (b.wide ? size_t(n->M) * 8 : 0);
   return COMPASS_OK;
 }
 
@@ -711,13 +716,15 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
   int st = compass_layer_norm_workspace_bytes(n, &need);
   if (st != COMPASS_OK) return st;
   NormParams p = {};
-  st = fill_shards(dY, n->P, n->M, &p.dy);
-  if (st == COMPASS_OK) st = fill_shards(X, n->P, n->M, &p.x);
-  if (st == COMPASS_OK) st = fill_shards(dX, n->P, n->M, &p.dx);
-  if (st == COMPASS_OK && dsum) st = fill_shards(dsum, n->P, n->M, &p.dsum);
+  const size_t element = dtype_size(n->dtype), param = dtype_size(n->param_dtype);
+  bool whole = whole_vectors(n) && is_aligned(gamma, 16);
+  st = fill_shards(dY, n->P, n->M, &p.dy, element, &whole);
+  if (st == COMPASS_OK) st = fill_shards(X, n->P, n->M, &p.x, element, &whole);
+  if (st == COMPASS_OK) st = fill_shards(dX, n->P, n->M, &p.dx, element, &whole);
+  if (st == COMPASS_OK && dsum) st = fill_shards(dsum, n->P, n->M, &p.dsum, element, &whole);
   if (st != COMPASS_OK) return st;
   if (n->M > 0 && (mean == nullptr || rstd == nullptr)) return COMPASS_ERR_INVALID_ARG;
-  if (!is_aligned(gamma, 16) || !is_aligned(dgamma, 16) || !is_aligned(dbeta, 16) || !is_aligned(mean, 4) || !is_aligned(rstd, 4))
+  if (!is_aligned(gamma, param) || !is_aligned(dgamma, param) || !is_aligned(dbeta, param) || !is_aligned(mean, 4) || !is_aligned(rstd, 4))
     return COMPASS_ERR_ALIGNMENT;
   st = check_workspace(ws, ws_bytes, need);
   if (st != COMPASS_OK) return st;
@@ -730,7 +737,7 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
       }
     return COMPASS_OK;
   }
-  const BackwardPlan b = backward_plan(n);
+  const BackwardPlan b = backward_plan(n, whole);
   p.gamma = gamma;
   p.mean = const_cast<float*>(mean);
   p.rstd = const_cast<float*>(rstd);
@@ -741,7 +748,7 @@ extern "C" int compass_layer_norm_backward(const compass_norm* n, const void* co
   p.n_partial = b.n_partial;
   p.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + 256);
   p.row_sums = p.partial + round_up(size_t(2 * b.n_partial) * size_t(n->hidden) * 4, 256) / 4;
-  st = n->dtype == COMPASS_DTYPE_FP32 ? backward_of<float>(p, b, vectorised(n), s) : backward_of<__nv_bfloat16>(p, b, vectorised(n), s);
+  st = n->dtype == COMPASS_DTYPE_FP32 ? backward_of<float>(p, b, whole, s) : backward_of<__nv_bfloat16>(p, b, whole, s);
   if (st != COMPASS_OK || (dgamma == nullptr && dbeta == nullptr)) return st;
   const int64_t grid = 2 * ceil_div(n->hidden, 32);
   if (n->param_dtype == COMPASS_DTYPE_FP32)

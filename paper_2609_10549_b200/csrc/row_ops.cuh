@@ -271,8 +271,9 @@ inline int64_t rows_of_vocab_shard(int64_t vocab, int P, int r) {
   const int64_t left = vocab - s * r;
   return left < 0 ? 0 : (left < s ? left : s);
 }
-// P row shards; with rows == 0 nothing is read and nothing is asked of the pointers.
-inline int fill_shards(const void* const* p, int P, int64_t M, RowShards* out) {
+// P row shards; with rows == 0 nothing is read and nothing is asked of the pointers.  They are aligned to `align` bytes at
+// least; *whole is cleared where one is not to 16 (then every access is of one element).
+inline int fill_shards(const void* const* p, int P, int64_t M, RowShards* out, size_t align = 16, bool* whole = nullptr) {
   out->rows.set(uint32_t(M / P));
   if (M == 0) return COMPASS_OK;
   if (p == nullptr) return COMPASS_ERR_INVALID_ARG;
@@ -280,16 +281,20 @@ inline int fill_shards(const void* const* p, int P, int64_t M, RowShards* out) {
     if (p[r] == nullptr) return COMPASS_ERR_INVALID_ARG;
     out->ptr[r] = const_cast<void*>(p[r]);
   }
-  for (int r = 0; r < P; ++r)
-    if (!is_aligned(p[r], 16)) return COMPASS_ERR_ALIGNMENT;
+  for (int r = 0; r < P; ++r) {
+    if (!is_aligned(p[r], align)) return COMPASS_ERR_ALIGNMENT;
+    if (whole && !is_aligned(p[r], 16)) *whole = false;
+  }
   return COMPASS_OK;
 }
-inline int check_vocab_shards(const void* const* p, int P, int64_t vocab) {
+inline int check_vocab_shards(const void* const* p, int P, int64_t vocab, size_t align = 16, bool* whole = nullptr) {
   if (p == nullptr) return COMPASS_ERR_INVALID_ARG;
   for (int r = 0; r < P; ++r)
     if (p[r] == nullptr && rows_of_vocab_shard(vocab, P, r) > 0) return COMPASS_ERR_INVALID_ARG;
-  for (int r = 0; r < P; ++r)
-    if (!is_aligned(p[r], 16)) return COMPASS_ERR_ALIGNMENT;
+  for (int r = 0; r < P; ++r) {
+    if (!is_aligned(p[r], align)) return COMPASS_ERR_ALIGNMENT;
+    if (whole && !is_aligned(p[r], 16)) *whole = false;
+  }
   return COMPASS_OK;
 }
 inline int check_workspace(const void* ws, size_t have, size_t need) {

@@ -459,3 +459,66 @@ def test_offsets_beyond_32_bits():
     torch.nn.functional.layer_norm(xd, (H,)).backward(y[at].double())
     want = xd.grad + x[at].double()
     assert (dx[at].double() - want).abs().max() <= 2.0 ** -7 * want.abs().max()
+
+
+# ---- off the 16-byte boundaries -------------------------------------------------------------------------------------
+
+
+def shifted(t, by=1):
+    """The same values one element behind a 16-byte boundary."""
+    room = torch.zeros(t.numel() + by, device=t.device, dtype=t.dtype)
+    room[by:] = t.reshape(-1)
+    return room[by:].view(t.shape)
+
+
+@pytest.fixture
+def off_boundaries(monkeypatch):
+    import sys
+    here = sys.modules[__name__]
+    rows, vocab = split_rows, split_vocab
+    monkeypatch.setattr(here, "split_rows", lambda t, P: [shifted(s) for s in rows(t, P)])
+    monkeypatch.setattr(here, "split_vocab", lambda t, P: [shifted(s) for s in vocab(t, P)])
+
+
+@pytest.mark.parametrize("P,M,hidden,vocab,dtype", [(2, 6, 4096, 33, "bf16"), (1, 40, 64, 33, "fp32"), (3, 9, 7, 10, "bf16")])
+def test_embedding_off_boundaries(off_boundaries, P, M, hidden, vocab, dtype):
+    test_embedding(P, M, hidden, vocab, dtype, api.INDEX_INT64)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("P,M,hidden,vocab,dtype,grad", [(2, 600, 64, 33, "bf16", "bf16"), (1, 300, 64, 133, "bf16", "fp32"),
+                                                         (4, 400, 1001, 530, "fp32", "bf16"), (1, 5, 3, 1, "bf16", "bf16")])
+def test_embedding_backward_off_boundaries(off_boundaries, P, M, hidden, vocab, dtype, grad, accumulate):
+    test_embedding_backward(P, M, hidden, vocab, dtype, grad, "skewed", accumulate)
+
+
+@pytest.mark.parametrize("P,M,hidden,dtype,param", [(2, 302, 4096, "bf16", "fp32"), (1, 500, 64, "fp32", "bf16"), (1, 3, 8192, "bf16", "bf16"),
+                                                    (2, 4, 16384, "bf16", "fp32"), (1, 2, 40000, "fp32", "fp32")])
+def test_layer_norm_off_boundaries(off_boundaries, P, M, hidden, dtype, param):
+    for mode in ("plain", "residual", "bare"):
+        test_layer_norm(P, M, hidden, dtype, param, mode)
+    for dsum in (False, True):
+        test_layer_norm_backward(P, M, hidden, dtype, param, dsum)
+
+
+def test_any_pointer_off_its_boundary():
+    """One tensor off a 16-byte boundary at a time: results as with all of them there, to a rounding of the last place."""
+    M, H = 300, 512
+    x, r, gamma, beta = norm_inputs(1, M, H, "bf16", "fp32")
+    n = api.make_layer_norm(1, M, H, param_dtype=api.DTYPE_FP32)
+    ws = api.alloc_layer_norm_workspace(n)
+    mean, rstd = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+
+    def run(off):
+        t = {k: v.clone() for k, v in dict(x=x, r=r, g=gamma, b=beta, y=x, s=x, dx=x, dg=gamma, db=gamma).items()}
+        if off:
+            t[off] = shifted(t[off])
+        api.compass_layer_norm(n, [t["x"]], t["g"], t["b"], [t["y"]], mean=mean, rstd=rstd, residual=[t["r"]], summed=[t["s"]])
+        api.compass_layer_norm_backward(n, [t["r"]], [t["s"]], t["g"], mean, rstd, [t["dx"]], t["dg"], t["db"], ws, dsum=[t["x"]])
+        return [t[k] for k in ("y", "s", "dx", "dg", "db")]
+
+    want = run("")
+    for off in ("x", "r", "g", "b", "y", "s", "dx", "dg", "db"):
+        for got, w in zip(run(off), want):
+            # (sums over a row in another order: FP32 roundings, which now and then turn a BF16 one)
+            assert (got.double() - w.double()).norm() <= 2.0 ** -10 * w.double().norm(), off

@@ -57,8 +57,8 @@ def test_struct_layouts_match_the_header():
     assert C.sizeof(api.Head) == 4 * 4 + 3 * 8 + 2 * 4 and api.Head.label_smoothing.offset == 44
 
 
-# Addresses that are never read: every call below is refused on the host.
-A, ODD = 0x10000, 0x10008
+# Addresses that are never read: every call below is refused on the host.  ODD: on no element's boundary; HALF: not on 16 bytes.
+A, ODD, HALF = 0x10000, 0x10001, 0x10008
 
 
 def ptrs(*p):
@@ -104,7 +104,7 @@ def test_layer_norm_calls_that_are_refused():
 
 def test_head_calls_that_are_refused():
     h, L = api.make_head(2, 4, 16, 10), api.lib()
-    good, null, odd = ptrs(A, A), ptrs(None, A), ptrs(A, ODD)
+    good, null, odd = ptrs(A, A), ptrs(None, A), ptrs(A, HALF)
     need, need_back = api.compass_head_workspace_bytes(h), api.compass_head_workspace_bytes(h, True)
 
     def forward(x=good, w=good, y=A, loss=A, lse=A, ws=A, n=need):

@@ -677,9 +677,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 // a time) and X's the N side, so that all the loads but a few are of the table and fill the whole ring (the form above spends
 // half of its ring on rows of X that are not there).  Single CTAs; warp 0 loads, warp 1 multiplies, warps 2..5 transpose the
 // accumulator through shared memory and take each row's statistics over their 32 vocabulary rows.
-// Measured, whole calls, the form above and this one: 1 row, 4096 x 128000: 216 and 179 us (the table's bytes take 160);
-// 16 rows, 4096 x 32000: 76 and 55 (40); 128 rows: 66 and 62 us in a graph; 100 rows, 512 x 8000: 17.2 and 15.4.
-constexpr int kFewRows = 128;
+// Measured, whole calls in a graph, the form above and this one: 1 row, 4096 x 128000: 216 and 179 us (the table's bytes take
+// 160); 16 rows, 512 x 128000: 114 and 35; 64 rows, 4096 x 32000: 67 and 56, 200 x 65286: 42 and 28.  With more rows it is
+// this form's epilogue that takes the time: 128 rows, 512 x 128000: 43 and 58, 4096 x 32000: 66 and 62.
+constexpr int kFewRows = 64;
 constexpr int kFewThreads = 192;
 constexpr int kFewAhead = 8;              // stages behind the ring whose part of the table is fetched into L2 meanwhile
 constexpr int kFewRoom = 192 * 1024;

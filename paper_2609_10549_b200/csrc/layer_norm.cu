@@ -388,14 +388,25 @@ __global__ void __launch_bounds__(kThreads, 1) norm_backward_kernel(const __grid
   for (int which = 0; which < 2; ++which) {
     float* out = p.partial + (int64_t(which) * p.n_partial + blockIdx.x) * H;
     if (groups > 1) __syncthreads();
+    float* to = groups > 1 ? sums + group * H : out;
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k)
+    for (int i = 0; i < NVT; ++i) {
+      const int c = (i * kTpr + t) * V;
+      if (c < H) {
+        float x[V];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = ((2 * k + e) / V * kTpr + t) * V + (2 * k + e) % V;
-        const float2 q = of(which ? db[k] : dg[k]);
-        if (c < H) (groups > 1 ? sums + group * H : out)[c] = e ? q.y : q.x;
+        for (int j = 0; j < V; ++j) {
+          const float2 q = of(which ? db[(i * V + j) / 2] : dg[(i * V + j) / 2]);
+          x[j] = (i * V + j) & 1 ? q.y : q.x;
+        }
+        if constexpr (V == 1) {
+          to[c] = x[0];
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(to + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        }
       }
+    }
     if (groups > 1) {
       __syncthreads();
       for (int c = threadIdx.x; c < H; c += blockDim.x) {

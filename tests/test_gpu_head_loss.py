@@ -76,7 +76,9 @@ CASES = [
     (16, 16, 264, 1000, 0.2, 0.5, 0.2, "bf16"),
     (1, 16, 4096, 32000, 0.0, 1.0, 0.0, "bf16"),      # few rows, more tiles than SMs
     (5, 35, 200, 2600, 0.1, 1.0, 0.1, "bf16"),        # shards of 520 rows: tiles of 8 rows, and a half without any
-    (1, 127, 96, 40000, 0.0, 1.0, 0.0, "bf16"),       # two tiles and more per SM, the most of few rows
+    (1, 64, 96, 40000, 0.0, 1.0, 0.0, "bf16"),        # two tiles and more per SM, the most of few rows
+    (1, 65, 96, 40000, 0.0, 1.0, 0.0, "bf16"),        # one more
+    (1, 127, 96, 40000, 0.0, 1.0, 0.0, "bf16"),
     (1, 128, 128, 256, 0.0, 1.0, 0.0, "bf16"),        # whole tiles
     (1, 256, 256, 512, 0.0, 1.0, 0.0, "fp32"),
     (3, 129, 520, 257, 0.0, 1.0, 0.0, "bf16"),        # one more than a tile

@@ -682,6 +682,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 // this form's epilogue that takes the time: 128 rows, 512 x 128000: 43 and 58, 4096 x 32000: 66 and 62.
 constexpr int kFewRows = 64;
 constexpr int kFewThreads = 192;
+// A tile's contraction goes to this many accumulators in turn, which are added up in FP32: the tensor cores cut off what their
+// sums cannot hold, a little at each step, and shorter sums lose less (16 rows, hidden = 4096: losses 2e-6 to 4e-6 off with one
+// accumulator, 6e-7 with four, as with FP32 arithmetic).  The time is the table's either way.
+constexpr int kFewParts = 4;
 constexpr int kFewAhead = 8;              // stages behind the ring whose part of the table is fetched into L2 meanwhile
 constexpr int kFewRoom = 192 * 1024;
 struct FewControl {
@@ -744,7 +748,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
     fence_mbar_init();
   }
   if (warp == 1) {
-    tmem_alloc(&ctl->tmem_base, 256);
+    tmem_alloc(&ctl->tmem_base, 2 * kFewParts * kFewRows);
     tmem_relinquish();
   }
   tc_fence_before_sync();
@@ -819,8 +823,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
           const uint64_t da = desc + uint64_t((slot * stage_bytes) >> 4), db = da + uint64_t((2 * kChunkBytes) >> 4);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            umma_bf16(tmem_base + b * 128, da + uint64_t((i >> 2) * (kChunkBytes >> 4) + (i & 3) * 2),
-                      db + uint64_t((i >> 2) * ((n_cols * BK * 2) >> 4) + (i & 3) * 2), idesc, (k | i) ? 1u : 0u);
+            umma_bf16(tmem_base + (b * kFewParts + k % kFewParts) * kFewRows, da + uint64_t((i >> 2) * (kChunkBytes >> 4) + (i & 3) * 2),
+                      db + uint64_t((i >> 2) * ((n_cols * BK * 2) >> 4) + (i & 3) * 2), idesc, k >= kFewParts || i ? 1u : 0u);
           umma_commit(&ctl->empty[slot]);
         }
         if (!ok) break;
@@ -853,8 +857,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
         float m = -INFINITY, s = 0.f, sum = 0.f;
         if (!empty) {
           uint32_t v[32];
-          tmem_ld_32x32b_x32(tmem_base + (uint32_t(quarter * 32) << 16) + b * 128 + c, v);
+          const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * kFewParts * kFewRows + c;
+          tmem_ld_32x32b_x32(taddr, v);
           tmem_ld_wait();
+          for (int part = 1; part < min(kFewParts, ksteps); ++part) {
+            uint32_t w[32];
+            tmem_ld_32x32b_x32(taddr + part * kFewRows, w);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+          }
 #pragma unroll
           for (int i = 0; i < 32; ++i) sh->z[quarter][i][lane] = __uint_as_float(v[i]) * p.z_scale;
           __syncwarp();
@@ -907,7 +919,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
   __syncthreads();
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, 256);
+    tmem_dealloc(tmem_base, 2 * kFewParts * kFewRows);
   }
 }
 

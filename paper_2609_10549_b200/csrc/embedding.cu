@@ -583,7 +583,8 @@ int pick_lookup(const LookupParams& p, int sms, cudaStream_t stream) {
 
 // Sorted tokens per piece: 8 (whose loads a thread has in flight together), more where that would be over 512 pieces: fewer
 // of them leave runs to join (16384 tokens of 4096: sums and join 38 + 30 us at 8 a piece, 37 + 15 at 16, 36 + 8 at 32).
-uint32_t run_length(int64_t M) { return uint32_t(M <= 4096 ? 8 : round_up(size_t(ceil_div(M, 512)), 8)); }
+// At most 2048, whose positions a block keeps in shared memory.
+uint32_t run_length(int64_t M) { return uint32_t(M <= 4096 ? 8 : M > 512 * 2048 ? 2048 : round_up(size_t(ceil_div(M, 512)), 8)); }
 
 struct GradPlan {
   uint32_t tiles, run, pieces;      // (tiles: 1 where a cluster sorts)

@@ -113,6 +113,7 @@ GRADS = [
     (2, 70000, 16, 70000, "fp32", "fp32", "even"),   # two passes, longer pieces
     (1, 70000, 8, 300, "bf16", "bf16", "none"),      # padding only
     (1, 40000, 8, 300000, "bf16", "fp32", "one"),    # three passes
+    (1, 1100000, 8, 700, "bf16", "fp32", "skewed"),  # pieces of 2048 tokens, the most
     (8, 2048, 1024, 100001, "bf16", "bf16", "skewed"),   # 205 MB of rows, most of them zeros
     (3, 6, 256, 200000, "fp32", "fp32", "even"),     # one piece, nothing to join
     (1, 16000, 512, 190000, "bf16", "bf16", "even"),     # most tokens alone
@@ -152,8 +153,8 @@ def test_embedding_backward(P, M, hidden, vocab, dtype, grad, how, accumulate):
     want *= s
     if accumulate:
         want += f64(before)
-    # pieces of 8 tokens, or of as many as make 512 pieces, summed one after the other
-    run = 8 if M <= 4096 else -(-M // 4096) * 8
+    # pieces of 8 tokens, or of as many as make 512 pieces, but 2048 at most, summed one after the other
+    run = 8 if M <= 4096 else min(2048, -(-M // 4096) * 8)
     steps = np.minimum(count, run) + count / run + 3
     close(f64(dW), want, np.abs(want) * HALF_UNIT[grad] + steps[:, None] * 2.0 ** -24 * (size * s + (np.abs(f64(before)) if accumulate else 0)))
     if not accumulate:

@@ -1424,7 +1424,7 @@ int device_info(DeviceInfo** out) {
 }  // namespace
 
 bool encode_tensor_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows) {
-  return encode_kmajor(map, ptr, rows, cols, box_rows);
+  return encode_kmajor_uncached(map, ptr, rows, cols, box_rows);
 }
 
 void tensor_map_cache_stats(uint64_t* hits, uint64_t* misses) {

@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         const int frag0 = tile.row0 + (tile.big ? int(cta) * 256 + a * 128 : int(cta) * 128);    // this CTA's 128 rows
         const int row = frag0 + quarter * 32 + lane;
         int target = -1;
-        float lse2 = INFINITY, w = 0.f;       // a row past the last gives zeros
+        float lse2 = 0.f, w = 0.f;
         if (kForm == STATS || kForm == GRAD) {
           if (row < rows) {
             target = p.target[row];
@@ -582,12 +582,16 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
                 for (int i = 0; i < 32; ++i)
                   if (mine && hit == c * 32 + i) v[c][i] = __float_as_uint(__uint_as_float(v[c][i]) - off);
             }
-            if (cols < 128) {       // past the shard's last row
+            // Zeros past the shard's last row, and in the rows past the last that takes part, which DW sums over: selected, not
+            // computed, because such a row's X is zero, but 0 * inf is NaN where the table has an infinite entry (a word
+            // masked out).
+            const int live = row < rows ? cols : 0;
+            if (live < 128) {
 #pragma unroll
               for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                  if (c * 32 + i >= cols) v[c][i] = 0u;
+                  if (c * 32 + i >= live) v[c][i] = 0u;
             }
             // straight from the registers, 32 bytes of a row per lane: through shared memory the tensor cores' operand
             // reads, which take most of its bandwidth, made this phase several times as long

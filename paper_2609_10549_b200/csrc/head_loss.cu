@@ -728,6 +728,14 @@ __device__ __forceinline__ bool wait_few(uint64_t* bar, uint32_t parity, FewCont
   return false;
 }
 
+// Whether a wait of the four epilogue warps succeeded for all of them.  They meet at barrier 1 for every tile: a warp that gave
+// up alone, just before the others' wait was over, would leave them there for good.
+__device__ __forceinline__ bool few_agree(bool ok) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(uint32_t(ok)) : "memory");
+  return all != 0;
+}
+
 __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_constant__ HeadParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -852,7 +860,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       const uint32_t b = it & 1u;
       const bool empty = live + quarter * 32 == 0;
       if (!empty) {
-        ok = __all_sync(0xffffffffu, wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t));
+        ok = few_agree(__all_sync(0xffffffffu, wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t)));
         if (!ok) break;
         tc_fence_after_sync();
       }

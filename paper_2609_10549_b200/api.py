@@ -106,7 +106,15 @@ class PlanBlock(C.Structure):
 
 
 _lib: Optional[C.CDLL] = None
-_raw_stream = _current_device = None      # torch's getters of the current stream's handle and of the current device
+
+
+def _torch_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+_raw_stream = None                        # torch's getter of the current stream's handle, once the library is loaded
+_current_device = _torch_device           # and of the current device
 
 
 def lib() -> C.CDLL:
@@ -115,7 +123,7 @@ def lib() -> C.CDLL:
         torch = sys.modules.get("torch")
         if torch is not None:
             _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _current_device = getattr(torch._C, "_cuda_getDevice", _torch_device)
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_10549_b200.build` "
                                "(there is no CPU fallback)")
@@ -308,10 +316,10 @@ def _ptr_array(tensors: Sequence) -> C.Array:
     return (C.c_void_p * len(tensors))(*[int(t.data_ptr()) for t in tensors])
 
 
-def _stream_handle(stream) -> C.c_void_p:
+def _stream_handle(stream, here: Optional[int] = None) -> C.c_void_p:
     if stream is None:
         if _raw_stream is not None:       # torch.cuda.current_stream() builds an object around it, several microseconds a call
-            return C.c_void_p(_raw_stream(_current_device()))
+            return C.c_void_p(_raw_stream(_current_device() if here is None else here))
         import torch
         stream = torch.cuda.current_stream()
     return C.c_void_p(int(stream.cuda_stream))
@@ -389,8 +397,9 @@ def compass_mlp_block(mlp: Mlp, X: Sequence, W0: Sequence, H: Sequence, W1: Sequ
 
 # ---- around the blocks: embedding, layer norm, output-layer loss -------------------
 #
-# These take torch tensors and check type, shape and layout before the library sees the addresses
-# (ValueError); what the library itself refuses raises CompassError.
+# These take torch tensors and check type, shape, layout and device before the library sees the addresses
+# (ValueError); what the library itself refuses raises CompassError.  Everything lies on the current device,
+# where the call is launched (`here`, looked up once per call).
 
 _TORCH_DTYPES: dict = {}
 _POINTERS = [C.c_void_p * P for P in range(MAX_P + 1)]
@@ -410,23 +419,39 @@ def _torch_dtype(kind: int):
     return _TORCH_DTYPES[kind]
 
 
-def _tensor(name: str, t, dtype, shape) -> Optional[int]:
-    """Address of a dense CUDA tensor of this type and shape (None stays None)."""
+def _here() -> Optional[int]:
+    """Index of the current device (None without any: then no tensor is on it)."""
+    try:
+        return _current_device()
+    except (RuntimeError, AssertionError):
+        return None
+
+
+def _tensor(name: str, t, dtype, shape, here) -> Optional[int]:
+    """Address of a dense tensor of this type and shape on the current device (None stays None)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name}: want a contiguous CUDA tensor of {dtype} {tuple(shape)}, got "
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != here:
+        raise ValueError(f"{name}: want a contiguous tensor of {dtype} {tuple(shape)} on the current device (cuda:{here}), got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
     return t.data_ptr() or None
 
 
-def _row_shards(name: str, tensors: Optional[Sequence], P: int, M: int, hidden: int, kind: int):
+def _op_workspace(t, here):
+    """Address and bytes of a workspace on the current device."""
+    if not t.is_contiguous() or t.get_device() != here:
+        raise ValueError(f"workspace: want a contiguous tensor on the current device (cuda:{here}), got one on {t.device}, "
+                         f"strides {tuple(t.stride())}")
+    return _ws(t)
+
+
+def _row_shards(name: str, tensors: Optional[Sequence], P: int, M: int, hidden: int, kind: int, here):
     if tensors is None:
         return None
     if len(tensors) != P:
         raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
     dtype, shape = _torch_dtype(kind), (M // P, hidden)
-    return _pointers([_tensor(name, t, dtype, shape) for t in tensors])
+    return _pointers([_tensor(name, t, dtype, shape, here) for t in tensors])
 
 
 def vocab_shard_rows(vocab: int, P: int, r: int) -> int:
@@ -435,25 +460,26 @@ def vocab_shard_rows(vocab: int, P: int, r: int) -> int:
     return max(0, min(s, vocab - s * r))
 
 
-def _vocab_shards(name: str, tensors: Sequence, P: int, vocab: int, hidden: int, kind: int):
+def _vocab_shards(name: str, tensors: Sequence, P: int, vocab: int, hidden: int, kind: int, here):
     if len(tensors) != P:
         raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
     dtype = _torch_dtype(kind)
-    return _pointers([_tensor(name, t, dtype, (vocab_shard_rows(vocab, P, r), hidden)) for r, t in enumerate(tensors)])
+    return _pointers([_tensor(name, t, dtype, (vocab_shard_rows(vocab, P, r), hidden), here) for r, t in enumerate(tensors)])
 
 
-def _index(name: str, t, kind: int, M: int):
-    return _tensor(name, t, _torch_dtype("index")[kind], (M,))
+def _index(name: str, t, kind: int, M: int, here):
+    return _tensor(name, t, _torch_dtype("index")[kind], (M,), here)
 
 
-def _vector(name: str, t, n: int, kind: int = DTYPE_FP32):
-    return _tensor(name, t, _torch_dtype(kind), (n,))
+def _vector(name: str, t, n: int, here, kind: int = DTYPE_FP32):
+    return _tensor(name, t, _torch_dtype(kind), (n,), here)
 
 
 def _sized_workspace(nbytes: int, device):
     import torch
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    compass_workspace_init(ws)
+    with torch.cuda.device(ws.device):        # zeroed on the stream that its calls will follow
+        compass_workspace_init(ws)
     return ws
 
 
@@ -465,9 +491,9 @@ def make_embedding(P: int, M: int, hidden: int, vocab: int, scale: float = 1.0, 
 
 def compass_embedding(embed: Embed, ids, W: Sequence, Out: Sequence, stream=None) -> None:
     """Out[r] = scale * W[ids of rank r's rows]; ids outside the vocabulary give zero rows."""
-    e = embed
-    _check(lib().compass_embedding(C.byref(e), _index("ids", ids, e.index_dtype, e.M), _vocab_shards("W", W, e.P, e.vocab, e.hidden, e.dtype),
-                                   _row_shards("Out", Out, e.P, e.M, e.hidden, e.dtype), _stream_handle(stream)), "compass_embedding")
+    e, here = embed, _here()
+    _check(lib().compass_embedding(C.byref(e), _index("ids", ids, e.index_dtype, e.M, here), _vocab_shards("W", W, e.P, e.vocab, e.hidden, e.dtype, here),
+                                   _row_shards("Out", Out, e.P, e.M, e.hidden, e.dtype, here), _stream_handle(stream, here)), "compass_embedding")
 
 
 def compass_embedding_workspace_bytes(embed: Embed) -> int:
@@ -482,11 +508,11 @@ def alloc_embedding_workspace(embed: Embed, device="cuda"):
 
 def compass_embedding_backward(embed: Embed, ids, dOut: Sequence, dW: Sequence, workspace, stream=None) -> None:
     """dW (+)= scale * the rows of dOut summed by id, over tokens sorted by id."""
-    e = embed
-    p, n = _ws(workspace)
-    _check(lib().compass_embedding_backward(C.byref(e), _index("ids", ids, e.index_dtype, e.M),
-                                            _row_shards("dOut", dOut, e.P, e.M, e.hidden, e.dtype),
-                                            _vocab_shards("dW", dW, e.P, e.vocab, e.hidden, e.grad_dtype), p, n, _stream_handle(stream)),
+    e, here = embed, _here()
+    p, n = _op_workspace(workspace, here)
+    _check(lib().compass_embedding_backward(C.byref(e), _index("ids", ids, e.index_dtype, e.M, here),
+                                            _row_shards("dOut", dOut, e.P, e.M, e.hidden, e.dtype, here),
+                                            _vocab_shards("dW", dW, e.P, e.vocab, e.hidden, e.grad_dtype, here), p, n, _stream_handle(stream, here)),
            "compass_embedding_backward")
 
 
@@ -497,11 +523,11 @@ def make_layer_norm(P: int, M: int, hidden: int, eps: float = 1e-5, dtype: int =
 def compass_layer_norm(norm: Norm, X: Sequence, gamma, beta, Y: Sequence, mean=None, rstd=None, residual: Optional[Sequence] = None,
                        summed: Optional[Sequence] = None, stream=None) -> None:
     """Y = layer norm of X, or of summed = X + residual; gamma and beta may be None (1 and 0)."""
-    n = norm
-    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype)  # noqa: E731
-    _check(lib().compass_layer_norm(C.byref(n), rows("X", X), rows("residual", residual), _vector("gamma", gamma, n.hidden, n.param_dtype),
-                                    _vector("beta", beta, n.hidden, n.param_dtype), rows("summed", summed), rows("Y", Y),
-                                    _vector("mean", mean, n.M), _vector("rstd", rstd, n.M), _stream_handle(stream)), "compass_layer_norm")
+    n, here = norm, _here()
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
+    _check(lib().compass_layer_norm(C.byref(n), rows("X", X), rows("residual", residual), _vector("gamma", gamma, n.hidden, here, n.param_dtype),
+                                    _vector("beta", beta, n.hidden, here, n.param_dtype), rows("summed", summed), rows("Y", Y),
+                                    _vector("mean", mean, n.M, here), _vector("rstd", rstd, n.M, here), _stream_handle(stream, here)), "compass_layer_norm")
 
 
 def compass_layer_norm_workspace_bytes(norm: Norm) -> int:
@@ -517,13 +543,13 @@ def alloc_layer_norm_workspace(norm: Norm, device="cuda"):
 def compass_layer_norm_backward(norm: Norm, dY: Sequence, X: Sequence, gamma, mean, rstd, dX: Sequence, dgamma, dbeta, workspace,
                                 dsum: Optional[Sequence] = None, stream=None) -> None:
     """dX (+ dsum, the gradient that reaches X past the norm), dgamma and dbeta (None: left out) summed over all M rows."""
-    n = norm
-    p, size = _ws(workspace)
-    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype)  # noqa: E731
-    param = lambda name, t: _vector(name, t, n.hidden, n.param_dtype)  # noqa: E731
-    _check(lib().compass_layer_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), param("gamma", gamma), _vector("mean", mean, n.M),
-                                             _vector("rstd", rstd, n.M), rows("dsum", dsum), rows("dX", dX), param("dgamma", dgamma),
-                                             param("dbeta", dbeta), p, size, _stream_handle(stream)), "compass_layer_norm_backward")
+    n, here = norm, _here()
+    p, size = _op_workspace(workspace, here)
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
+    param = lambda name, t: _vector(name, t, n.hidden, here, n.param_dtype)  # noqa: E731
+    _check(lib().compass_layer_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), param("gamma", gamma), _vector("mean", mean, n.M, here),
+                                             _vector("rstd", rstd, n.M, here), rows("dsum", dsum), rows("dX", dX), param("dgamma", dgamma),
+                                             param("dbeta", dbeta), p, size, _stream_handle(stream, here)), "compass_layer_norm_backward")
 
 
 def make_head(P: int, M: int, hidden: int, vocab: int, logit_scale: float = 1.0, label_smoothing: float = 0.0, dtype: int = DTYPE_BF16,
@@ -544,23 +570,23 @@ def alloc_head_workspace(head: Head, backward: bool = False, device="cuda"):
 
 def compass_head_loss(head: Head, X: Sequence, W: Sequence, targets, loss, lse, workspace, stream=None) -> None:
     """Cross entropy of every token and its log-sum-exp, without the logits; targets outside the vocabulary take no part."""
-    h = head
-    p, n = _ws(workspace)
-    _check(lib().compass_head_loss(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype),
-                                   _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype), _index("targets", targets, h.index_dtype, h.M),
-                                   _vector("loss", loss, h.M), _vector("lse", lse, h.M), p, n, _stream_handle(stream)), "compass_head_loss")
+    h, here = head, _here()
+    p, n = _op_workspace(workspace, here)
+    _check(lib().compass_head_loss(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype, here),
+                                   _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype, here), _index("targets", targets, h.index_dtype, h.M, here),
+                                   _vector("loss", loss, h.M, here), _vector("lse", lse, h.M, here), p, n, _stream_handle(stream, here)), "compass_head_loss")
 
 
 def compass_head_loss_backward(head: Head, X: Sequence, W: Sequence, targets, lse, dloss, dX: Sequence, dW: Sequence, workspace,
                                stream=None) -> None:
     """dX and dW from the gradient of every token's loss; the logits are computed again in pieces of the vocabulary."""
-    h = head
-    p, n = _ws(workspace)
-    _check(lib().compass_head_loss_backward(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype),
-                                            _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype),
-                                            _index("targets", targets, h.index_dtype, h.M), _vector("lse", lse, h.M),
-                                            _vector("dloss", dloss, h.M), _row_shards("dX", dX, h.P, h.M, h.hidden, h.dtype),
-                                            _vocab_shards("dW", dW, h.P, h.vocab, h.hidden, h.grad_dtype), p, n, _stream_handle(stream)),
+    h, here = head, _here()
+    p, n = _op_workspace(workspace, here)
+    _check(lib().compass_head_loss_backward(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype, here),
+                                            _vocab_shards("W", W, h.P, h.vocab, h.hidden, h.dtype, here),
+                                            _index("targets", targets, h.index_dtype, h.M, here), _vector("lse", lse, h.M, here),
+                                            _vector("dloss", dloss, h.M, here), _row_shards("dX", dX, h.P, h.M, h.hidden, h.dtype, here),
+                                            _vocab_shards("dW", dW, h.P, h.vocab, h.hidden, h.grad_dtype, here), p, n, _stream_handle(stream, here)),
            "compass_head_loss_backward")
 
 

@@ -468,7 +468,10 @@ def _vocab_shards(name: str, tensors: Sequence, P: int, vocab: int, hidden: int,
 
 
 def _index(name: str, t, kind: int, M: int, here):
-    return _tensor(name, t, _torch_dtype("index")[kind], (M,), here)
+    kinds = _torch_dtype("index")
+    if kind not in kinds:
+        raise ValueError(f"unknown index type {kind}")
+    return _tensor(name, t, kinds[kind], (M,), here)
 
 
 def _vector(name: str, t, n: int, here, kind: int = DTYPE_FP32):

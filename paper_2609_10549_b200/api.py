@@ -450,7 +450,7 @@ def _row_shards(name: str, tensors: Optional[Sequence], P: int, M: int, hidden: 
         return None
     if len(tensors) != P:
         raise ValueError(f"{name}: want {P} shards, got {len(tensors)}")
-    dtype, shape = _torch_dtype(kind), (M // P, hidden)
+    dtype, shape = _torch_dtype(kind), (M // P if P else 0, hidden)       # (P = 0 is the library's to refuse)
     return _pointers([_tensor(name, t, dtype, shape, here) for t in tensors])
 
 

@@ -27,3 +27,13 @@ def test_unknown_types_of_ids_and_targets(here):
                  lambda: api.compass_head_loss_backward(h, x, w, ids, v, v, x, w, ws)):
         with pytest.raises(ValueError, match="index type"):
             call()
+
+
+def test_no_ranks(here):
+    _, _, ids, v, ws = tensors()
+    e, n, h = api.make_embedding(0, 4, 16, 10), api.make_layer_norm(0, 4, 16), api.make_head(0, 4, 16, 10)
+    for call in (lambda: api.compass_embedding(e, ids, [], []), lambda: api.compass_layer_norm(n, [], None, None, []),
+                 lambda: api.compass_head_loss(h, [], [], ids, v, v, ws)):
+        with pytest.raises(api.CompassError) as err:
+            call()
+        assert err.value.status == api.ERR_INVALID_ARG

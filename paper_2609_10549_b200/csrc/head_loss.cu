@@ -1195,19 +1195,22 @@ struct FinishParams {
   const float4* acc;
   int64_t hidden;
   int32_t hidden_tiles, splits;
+  FastDiv row_blocks;
   float out_scale;
 };
-// A block takes 32 gathered rows and 128 columns: what one warp of the products' epilogue holds.
+// A block takes 32 gathered rows and 128 columns: what one warp of the products' epilogue holds.  (One grid axis: the second
+// would end at 65535 blocks, 8.4 million columns.)
 __global__ void __launch_bounds__(256) head_finish_kernel(const __grid_constant__ FinishParams p) {
   __shared__ float tile[32][129];
   wait_for_previous_kernel();
   const int rows = p.found->rows;
-  const int row0 = blockIdx.x * 32;
+  const uint32_t slab = p.row_blocks.div(blockIdx.x);      // of 128 columns
+  const int row0 = int(blockIdx.x - slab * p.row_blocks.d) * 32;
   if (row0 >= rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float scale = p.out_scale * p.found->top;
   const int64_t step = int64_t(p.hidden_tiles) * 8 * (32 * 32);            // from one split's sums to the next one's
-  const int64_t frag = (int64_t(row0 >> 7) * p.hidden_tiles * p.splits + (blockIdx.y >> 1)) * 8 + ((row0 >> 5) & 3) * 2 + (blockIdx.y & 1);
+  const int64_t frag = (int64_t(row0 >> 7) * p.hidden_tiles * p.splits + int(slab >> 1)) * 8 + ((row0 >> 5) & 3) * 2 + int(slab & 1);
   const float4* in = p.acc + frag * (32 * 32) + warp * 4 * 32 + lane;      // 4 of the 32 groups of 4 columns per warp
   float4 x[4];
 #pragma unroll
@@ -1236,7 +1239,7 @@ __global__ void __launch_bounds__(256) head_finish_kernel(const __grid_constant_
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int r = k * 16 + (threadIdx.x >> 4);
-    const int64_t c = int64_t(blockIdx.y) * 128 + (threadIdx.x & 15) * 8;
+    const int64_t c = int64_t(slab) * 128 + (threadIdx.x & 15) * 8;
     if (row0 + r < rows && c < p.hidden) {
       float y[8];
 #pragma unroll
@@ -1582,17 +1585,7 @@ extern "C" int compass_head_loss_backward(const compass_head* h, const void* con
   f.hidden = h->hidden;
   f.hidden_tiles = q.hidden_tiles;
   f.splits = q.splits;
+  f.row_blocks.set(uint32_t(ceil_div(h->M, 32)));
   f.out_scale = p.out_scale;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(ceil_div(h->M, 32)), unsigned(2 * q.hidden_tiles));
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, head_finish_kernel, f);
-  count_kernel_launch();
-  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+  return launch(head_finish_kernel, int64_t(f.row_blocks.d) * 2 * q.hidden_tiles, 256, 0, s, true, f);
 }

@@ -105,7 +105,6 @@ struct GradParams {
   int32_t wide_ids;
   int32_t bits;                              // of a key
   int32_t accumulate;
-  int32_t fill;                              // zeros are written beside the sort
   int64_t elem;                              // bytes of an element of dW
   float scale;
 };
@@ -715,7 +714,6 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   p.run = g.run;
   p.wide_ids = e->index_dtype == COMPASS_INDEX_INT64;
   p.accumulate = e->accumulate != 0;
-  p.fill = !p.accumulate;
   p.elem = int64_t(dtype_size(e->grad_dtype));
   p.scale = e->scale;
   while ((int64_t(1) << p.bits) <= e->vocab) ++p.bits;      // keys 0 .. vocab
@@ -723,11 +721,11 @@ extern "C" int compass_embedding_backward(const compass_embed* e, const void* id
   auto write_zeros = [&](bool beside_sort) {
     return launch(embedding_zero_kernel, zero_blocks < 64 * sms ? zero_blocks : 64 * sms, kZeroThreads, 0, s, beside_sort, p);
   };
-  if (p.fill && (e->M == 0 || g.tiles > 1)) st = write_zeros(false);
+  if (!p.accumulate && (e->M == 0 || g.tiles > 1)) st = write_zeros(false);
   if (st != COMPASS_OK || e->M == 0) return st;
   if (g.tiles == 1) {
     st = e->M <= kCluster * kSortThreads ? run_sort<1>(p, s) : e->M <= 4 * kCluster * kSortThreads ? run_sort<4>(p, s) : run_sort<kSortItems>(p, s);
-    if (st == COMPASS_OK && p.fill) st = write_zeros(true);
+    if (st == COMPASS_OK && !p.accumulate) st = write_zeros(true);
   } else {
     p.key_b = reinterpret_cast<uint32_t*>(take(g.key));
     p.pos_b = reinterpret_cast<uint32_t*>(take(g.key));

@@ -48,12 +48,7 @@ struct RowShards {
   }
 };
 
-// V elements of type T as one access (V * sizeof(T) is 16 bytes, or one element).
-template <typename T, int V>
-struct Vec {
-  T v[V];
-};
-
+// V elements of a type as one access (16 bytes, or one element), as FP32.
 template <int V>
 __device__ __forceinline__ void load_vec(float (&out)[V], const float* p) {
   if constexpr (V == 4) {

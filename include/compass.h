@@ -441,7 +441,10 @@ int compass_head_loss(const compass_head* head, const void* const* X, const void
 /* lse: what the forward call wrote; dloss: gradient of every token's loss (M
  * FP32 values).  dX[r] = [M/P x hidden] and dW[r] are written whole.  The logits
  * are computed again, in pieces of the vocabulary whose gradient (BF16, scaled by
- * dloss / max|dloss|) fits the workspace; sums are FP32, rounded once. */
+ * dloss / max|dloss|) fits the workspace; sums are FP32, rounded once. That BF16
+ * rounding of every logit's gradient stays in the results whatever grad_dtype is:
+ * about 1e-3 relative (root mean square) in an FP32 dW, beside the 1.7e-3 of a
+ * result's own rounding in BF16. */
 int compass_head_loss_backward(const compass_head* head, const void* const* X, const void* const* W, const void* targets,
                                const float* lse, const float* dloss, void* const* dX, void* const* dW, void* workspace,
                                size_t workspace_bytes, void* cuda_stream);

@@ -582,7 +582,9 @@ def compass_head_loss(head: Head, X: Sequence, W: Sequence, targets, loss, lse, 
 
 def compass_head_loss_backward(head: Head, X: Sequence, W: Sequence, targets, lse, dloss, dX: Sequence, dW: Sequence, workspace,
                                stream=None) -> None:
-    """dX and dW from the gradient of every token's loss; the logits are computed again in pieces of the vocabulary."""
+    """dX and dW from the gradient of every token's loss; the logits are computed again in pieces of the vocabulary.
+
+    The logits' gradient is rounded to BF16 for its products: FP32 in grad_dtype saves dW its own rounding, not that one."""
     h, here = head, _here()
     p, n = _op_workspace(workspace, here)
     _check(lib().compass_head_loss_backward(C.byref(h), _row_shards("X", X, h.P, h.M, h.hidden, h.dtype, here),

@@ -19,8 +19,16 @@
 // limit (1.37); backward, 7392 rows, 4096 x 128000, 18.1 ms = 1.28 PFLOP/s at that
 // limit; backward, 401 rows, 1024 x 50001, 200 us = 0.62 PFLOP/s (every tile's part
 // of the table comes from HBM, and three launches ramp up and down).
+// With few rows or a small hidden size it is far from either bound: one row tile
+// takes 256 rows' work, launches and epilogues are what takes the time (backward,
+// 8 rows, 4096 x 32000: 232 us, 2.9 times the table's bytes; 8192 rows, 64 x 32000:
+// 685 us, 11 times its operations).
 // The tensor cores' FP32 sums cut off what they cannot hold: losses are 2e-6 to
 // 3e-6 off (relative, hidden = 4096), where FP32 arithmetic is 6e-7 off.
+// The logits' gradient is rounded to BF16 because its products take BF16 operands
+// (in two BF16 halves it would double both products, 4 of 6 M hidden vocab). What
+// that costs, relative and root mean square: dW in FP32 is 0.9e-3 to 1.4e-3 off,
+// gradients in BF16 1.9e-3 to 2.2e-3, of which their own rounding is 1.7e-3.
 //
 // Tiles are computed by pairs of CTAs: 512 x 256 as long as they fill whole
 // rounds of the pairs (two accumulators that share one tile of B: 48 bytes of
@@ -1268,7 +1276,11 @@ int check_head(const compass_head* h) {
 
 // Pairs of CTAs that a launch counts on (one CTA per SM of the B200's 148); fewer co-resident ones only take more rounds.
 constexpr int kPairs = 74;
-// Bytes of the logits' gradient that are held at a time.
+// Bytes of the logits' gradient that are held at a time.  Fewer, larger pieces mean fewer launches and sums read back, and that
+// outweighs a piece that stays in L2 even where hidden is small.  Backward, us, with pieces of 32, 64, 128, 256, 512 MB:
+// 8192 rows, 4096 x 64000: 12350, 10910, 10150, 9880, 9780; 1024 x 50000: 3040, 2740, 2460, 2270, 2180; 368 x 32000: 1390, 1250,
+// 900, 810, 780; 5926 rows, 96 x 5021: 187, 125, 130, 131 to 152, 125 to 150; 1000 rows, 4096 x 50001: 1170, 1117, 1070, 1065, 1065.
+// 512 would be 1 to 4 % faster on the large ones for twice the workspace.
 constexpr int64_t kPieceBytes = int64_t(256) << 20;
 
 struct HeadPlan {
@@ -1287,7 +1299,9 @@ HeadPlan head_plan(const compass_head* h, bool backward) {
   q.tiles_per_shard = int(ceil_div(rows, 256));
   for (int r = 0; r < h->P; ++r) q.vocab_tiles += int(ceil_div(rows_of_vocab_shard(h->vocab, h->P, r), 256));
   q.hidden_tiles = int(ceil_div(h->hidden, 256));
-  // dX has few tiles when rows are few: its contraction over the vocabulary is then split over the pairs
+  // dX has few tiles when rows are few: its contraction over the vocabulary is then split over the pairs.  Backward, us, split
+  // and not: 1 row, 4096 x 128000: 827, 1378; 16, 4096 x 32000: 230, 368; 64, 512 x 32000: 96, 240; 300, 4096 x 32000: 365, 421;
+  // 401, 1024 x 50001: 179, 409.
   const int64_t dx_tiles = ceil_div(h->M, 256) * q.hidden_tiles;
   q.splits = dx_tiles > 0 && dx_tiles < kPairs ? int(kPairs / dx_tiles) : 1;
   if (q.splits > q.vocab_tiles) q.splits = q.vocab_tiles;

@@ -181,7 +181,8 @@ TilePlan plan_tiles(const GemmLaunch& launch, int max_pairs);
 int launch_gemm(const GemmLaunch& launch, cudaStream_t stream);
 // Tensor map of a dense BF16 matrix [rows x cols]: boxes of BK columns x box_rows rows, 128-byte swizzle, zero fill outside.
 // Encoded anew at every call and not kept in the fused operators' table, so that nothing goes by an address that a later
-// tensor may have taken over. Timed in turn on the output-layer loss of 16 x 4096 x 32000, forward: 56.03 us, 56.02 with the table.
+// tensor may have taken over. Host time of enqueuing an output-layer loss, with the table's entries found: 16 ranks forward (17
+// maps) 33.3 us, 32.5 with the table; backward (36 maps) 56.7, 55.6; on the GPU no difference (16 x 4096 x 32000: 56.0, 56.0).
 bool encode_tensor_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows);
 size_t gemm_smem_bytes();
 void tensor_map_cache_stats(uint64_t* hits, uint64_t* misses);

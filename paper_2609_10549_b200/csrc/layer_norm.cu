@@ -8,10 +8,13 @@
 // instructions per element (55 in the first form, and most of the time): hence
 // FP32 in pairs, one position per row for all tensors, row widths compiled in,
 // 16 elements a thread.  Measured (of the copy rate, 6.55 TB/s): forward with
-// residual, 16384 x 8192 BF16: 168 us, 98 %; backward with the residual's
-// gradient, 8192 x 4096 BF16: 53.5 us, 77 % (half of its issue slots are busy, and
+// residual, 16384 x 8192 BF16: 190 us, 86 %; backward with the residual's
+// gradient, 8192 x 4096 BF16: 51 us, 80 % (half of its issue slots are busy, and
 // a row's sums hold up the rest); backward, 4095 x 1001 FP32, an element per
-// access: 21 us, 35 %; forward, 8 x 4096: 3.5 us, one way through.
+// access: 21 us, 35 %; 8192 x 1001 BF16, whose rows are not copied ahead either:
+// 33 us, 30 %; backward beyond 8192 elements, which passes over X and dY twice, an
+// element per access, 8192 x 12288 BF16: 665 us, 18 %, FP32 705 us, 35 %; forward,
+// 8 x 4096: 3.5 us, one way through.
 #include <mutex>
 #include <type_traits>
 
@@ -541,7 +544,10 @@ int with_tpr(int tpr, F f) {
 
 constexpr int kSms = 148;           // blocks are counted for a B200; fewer SMs only take them in turns
 constexpr int64_t kWidest = 8192;   // elements of a row that stay in the registers of a block
-constexpr int kWideParts = 64;      // row ranges of the wide form's column sums
+// Row ranges of the wide form's column sums: more of them are more threads, and more partial sums to read back.  Backward, us,
+// with 16, 32, 64, 128: 64 x 32768 BF16: 23.6, 25.5, 30.4, 30.4; 512 x 16384: 54.3, 51.8, 51.7, 54.0; 4096 x 12288: 301, 294,
+// 263, 260, in FP32 312, 304, 275, 272; 16384 x 8200 BF16: 994, 818, 763, 720.
+constexpr int kWideParts = 64;
 
 struct BackwardPlan {
   bool wide;

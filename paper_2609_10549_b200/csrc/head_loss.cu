@@ -23,8 +23,11 @@
 // takes 256 rows' work, launches and epilogues are what takes the time (backward,
 // 8 rows, 4096 x 32000: 232 us, 2.9 times the table's bytes; 8192 rows, 64 x 32000:
 // 685 us, 11 times its operations).
-// The tensor cores' FP32 sums cut off what they cannot hold: losses are 2e-6 to
-// 3e-6 off (relative, hidden = 4096), where FP32 arithmetic is 6e-7 off.
+// The tensor cores' FP32 sums cut off what they cannot hold, a little at each step.
+// The statistics' sums are therefore short, 1024 elements of the contraction, and
+// added up in FP32: losses and lse are 5e-7 to 7e-7 off (relative, root mean
+// square), as with FP32 arithmetic; in one sum they were 2.5e-6 off over 4096
+// elements and 5.5e-6 over 8192. What goes to BF16 afterwards keeps one sum.
 // The logits' gradient is rounded to BF16 because its products take BF16 operands
 // (in two BF16 halves it would double both products, 4 of 6 M hidden vocab). What
 // that costs, relative and root mean square: dW in FP32 is 0.9e-3 to 1.4e-3 off,
@@ -33,7 +36,8 @@
 // Tiles are computed by pairs of CTAs: 512 x 256 as long as they fill whole
 // rounds of the pairs (two accumulators that share one tile of B: 48 bytes of
 // operands per SM and clock at the tensor cores' full rate, against 64 for
-// 256 x 256), 256 x 256 for the rest.  Warp 0 loads (TMA), warp 1 issues the
+// 256 x 256), 256 x 256 for the rest, and for all of the statistics, whose short
+// sums need registers and the second accumulator for a tile.  Warp 0 loads (TMA), warp 1 issues the
 // products, warps 2..9 are the epilogue: two per quarter of the rows, 128
 // columns each, so that a whole accumulator is in registers, and its tensor
 // memory free again, before the exponentials begin.
@@ -59,6 +63,11 @@ constexpr int kHalfChunk = kChunkBytes / 2;     // an MN-major operand is two bo
 constexpr int kChunks = 12;
 constexpr int kGroup = 8;                       // row tiles that go through the columns together (their A stays in L2)
 constexpr int kSkew = 3;                        // stages at a tile's ends in which accumulator 0 runs ahead
+// The statistics' logits are summed up in ranges of the contraction, this many 64-wide k-atoms each, which the epilogue adds in
+// FP32.  8192 (7392) rows, 4096 x 32000, in one range with 512 x 256 tiles, in one with 256 x 256, in ranges of 32, 16 and 8:
+// 1470, 1495, 1550, 1572, 1634 us (before the additions were rid of spilled registers, which brought 16 to 1515); losses
+// 2.9e-6, 2.9e-6, 1.5e-6, 6.9e-7, 3.3e-7 off.  FP32 arithmetic: 6.4e-7.
+constexpr int kRangeAtoms = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -160,7 +169,7 @@ struct Part {
   int total;
   int atoms;           // 64-wide k-atoms of a tile (an even number)
 };
-// Whole rounds of the units take 512 x 256 tiles, what is left 256 x 256 ones.  `before`: tiles of the launch that come first;
+// Whole rounds of the units take 512 x 256 tiles, what is left, and all of STATS, 256 x 256 ones.  `before`: tiles of the launch that come first;
 // the tiles go to the units in turn, so that a unit that has had one of its last, smaller ones gets its share of these later.
 __device__ __forceinline__ Part make_part(const HeadParams& p, int form, int units, int before) {
   Part q;
@@ -170,12 +179,14 @@ __device__ __forceinline__ Part make_part(const HeadParams& p, int form, int uni
   q.odd = halves & 1;
   q.cols = form == DW ? p.hidden_tiles : form == DX ? p.hidden_tiles * p.splits : p.n_vt;
   const int slots = q.big_rows * q.cols;
-  q.left = min(slots, (before + slots) % units);
+  q.left = form == STATS ? slots : min(slots, (before + slots) % units);
   q.n_big = slots - q.left;
   q.total = q.n_big + 2 * q.left + q.odd * q.cols;
   q.atoms = form == DW ? (found + 127) / 128 * 2 : form == DX ? 4 * p.n_vt : int((p.hidden + 127) / 128) * 2;
   return q;
 }
+// Ranges of a 256 x 256 tile's contraction, the last one shorter.
+__device__ __forceinline__ int ranges_of(int form, int atoms) { return form == STATS ? (atoms + kRangeAtoms - 1) / kRangeAtoms : 1; }
 struct Plan {
   Part part[2];        // SUMS: DX, DW; else the first alone
   int total;
@@ -428,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
 #pragma unroll
           for (int k = 0; k < BK / UMMA_K; ++k) umma_bf16_pair(acc, da + k * ak, db + k * bk, idesc, k ? 1u : first);
         };
-        if (tile.big) {
+        if (kForm != STATS && tile.big) {
           // Both accumulators are live for the whole tile, so nothing would hide the epilogue's reads if they ended
           // together: for the first and last kSkew stages accumulator 0's products go first.  It is then complete early
           // (its epilogue runs under accumulator 1's last products), and the next tile begins on it while accumulator 1
@@ -474,19 +485,22 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           ++uses[0];
           ++uses[1];
         } else {
-          const int b = int(small & 1u);
-          if (!(ok = acc_free(b, t))) return;
-          for (int a = 0; a < tile.atoms; a += 2, ++j) {
-            if (!(ok = landed(j, t))) break;
-            issue(tmem_base + b * 256, chunk, chunk + 2, a != 0 ? 1u : 0u);
-            issue(tmem_base + b * 256, chunk + 1, chunk + 3, 1u);
-            chunk = (chunk + 4) % kChunks;
-            umma_commit_pair(&ctl->empty[j & 3u], 0x3);
+          const int ranges = ranges_of(kForm, tile.atoms);
+          for (int r = 0; r < ranges; ++r) {
+            const int b = int(small & 1u);
+            const int from = r * kRangeAtoms, to = ranges > 1 ? min(tile.atoms, from + kRangeAtoms) : tile.atoms;
+            if (!(ok = acc_free(b, t))) return;
+            for (int a = from; a < to; a += 2, ++j) {
+              if (!(ok = landed(j, t))) return;
+              issue(tmem_base + b * 256, chunk, chunk + 2, a != from ? 1u : 0u);
+              issue(tmem_base + b * 256, chunk + 1, chunk + 3, 1u);
+              chunk = (chunk + 4) % kChunks;
+              umma_commit_pair(&ctl->empty[j & 3u], 0x3);
+            }
+            umma_commit_pair(&ctl->acc_full[b], 0x3);
+            ++uses[b];
+            ++small;
           }
-          if (!ok) return;
-          umma_commit_pair(&ctl->acc_full[b], 0x3);
-          ++uses[b];
-          ++small;
         }
       };
       for (int t = unit; ok && t < plan.total; t += units) {
@@ -510,8 +524,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     bool ok = true;
     for (int t = unit; ok && t < plan.total; t += units) {
       const Tile tile = tile_of<kForm>(p, plan, t);
+      const int ranges = tile.big ? 1 : ranges_of(kForm, tile.atoms);
       for (int a = 0; a < (tile.big ? 2 : 1); ++a) {
-        const int b = tile.big ? a : int(small & 1u);
+        int b = tile.big ? a : int(small & 1u);
         const int frag0 = tile.row0 + (tile.big ? int(cta) * 256 + a * 128 : int(cta) * 128);    // this CTA's 128 rows
         const int row = frag0 + quarter * 32 + lane;
         int target = -1;
@@ -525,18 +540,47 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
             }
           }
         }
-        ok = __all_sync(0xffffffffu, wait_bar(&ctl->acc_full[b], uses[b] & 1u, ctl, p, SITE_ACC_FULL, t));      // (a warp goes on as one)
-        if (!ok) break;
-        tc_fence_after_sync();
+        // (A wait that gives up is looked at behind the last range: what is read until then is dropped.  Leaving in between cost
+        // 220 bytes of spilled registers a thread.)
         uint32_t v[4][32];
-        const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
+        bool gave_up = false;
+        auto take = [&](auto add) {
+          gave_up |= !wait_bar(&ctl->acc_full[b], uses[b] & 1u, ctl, p, SITE_ACC_FULL, t);
+          __syncwarp();
+          tc_fence_after_sync();
+          const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
+          if constexpr (decltype(add)::value) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(taddr + c * 32, v[c]);
-        tmem_ld_wait();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
-        ++uses[b];
+            for (int c = 0; c < 8; ++c) {      // (32 columns at a time would spill)
+              uint32_t more[16];
+              tmem_ld_32x32b_x16(taddr + c * 16, more);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                uint32_t& x = v[c >> 1][(c & 1) * 16 + i];
+                x = __float_as_uint(__uint_as_float(x) + __uint_as_float(more[i]));
+              }
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(taddr + c * 32, v[c]);
+            tmem_ld_wait();
+          }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+          ++uses[b];
+        };
+        take(std::false_type{});
+        if constexpr (kForm == STATS) {
+          for (int r = 1; r < ranges; ++r) {
+            ++small;
+            b = int(small & 1u);
+            take(std::true_type{});
+          }
+        }
+        ok = __all_sync(0xffffffffu, !gave_up);      // (a warp goes on as one)
+        if (!ok) break;
 
         if (kForm == STATS || kForm == GRAD) {
           int shard, vrow;
@@ -698,6 +742,9 @@ constexpr int kFewThreads = 192;
 // sums cannot hold, a little at each step, and shorter sums lose less (16 rows, hidden = 4096: losses 2e-6 to 4e-6 off with one
 // accumulator, 6e-7 with four, as with FP32 arithmetic).  The time is the table's either way.
 constexpr int kFewParts = 4;
+// Steps of 128 elements whose sums are read back together, so that an accumulator's are never longer than 1024 elements (64 rows,
+// 8192 x 8000: lse 7e-7 off, 1.5e-6 with all of them together; 8192 x 32000: 99.7 and 101.0 us).
+constexpr int kFewRange = 32;
 constexpr int kFewAhead = 8;              // stages behind the ring whose part of the table is fetched into L2 meanwhile
 constexpr int kFewRoom = 192 * 1024;
 struct FewControl {
@@ -754,6 +801,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
   const int stage_bytes = few_stage_bytes(n_cols), stages = few_stages(n_cols);
   const int tiles = 2 * p.n_vt;                        // of 128 vocabulary rows
   const int ksteps = int((p.hidden + 127) / 128);
+  const int ranges = (ksteps + kFewRange - 1) / kFewRange;
   if (threadIdx.x == 0) {
     for (int s = 0; s < 8; ++s) {
       mbar_init(&ctl->full[s], 1);
@@ -833,23 +881,26 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
         int shard, row;
         if (rows_of(t, &shard, &row) == 0) continue;
-        const uint32_t b = it & 1u;
-        if (!(ok = wait_few(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, ctl, p, SITE_ACC_EMPTY, t))) break;
-        tc_fence_after_sync();
-        for (int k = 0; k < ksteps; ++k, ++j) {
-          const int slot = j % stages;
-          if (!(ok = wait_few(&ctl->full[slot], uint32_t(j / stages) & 1u, ctl, p, SITE_FULL, t))) break;
+        for (int r = 0; ok && r < ranges; ++r) {
+          const int steps = min(kFewRange, ksteps - r * kFewRange);
+          const uint32_t b = it & 1u;
+          if (!(ok = wait_few(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, ctl, p, SITE_ACC_EMPTY, t))) break;
           tc_fence_after_sync();
-          const uint64_t da = desc + uint64_t((slot * stage_bytes) >> 4), db = da + uint64_t((2 * kChunkBytes) >> 4);
+          for (int k = 0; k < steps; ++k, ++j) {
+            const int slot = j % stages;
+            if (!(ok = wait_few(&ctl->full[slot], uint32_t(j / stages) & 1u, ctl, p, SITE_FULL, t))) break;
+            tc_fence_after_sync();
+            const uint64_t da = desc + uint64_t((slot * stage_bytes) >> 4), db = da + uint64_t((2 * kChunkBytes) >> 4);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            umma_bf16(tmem_base + (b * kFewParts + k % kFewParts) * kFewRows, da + uint64_t((i >> 2) * (kChunkBytes >> 4) + (i & 3) * 2),
-                      db + uint64_t((i >> 2) * ((n_cols * BK * 2) >> 4) + (i & 3) * 2), idesc, k >= kFewParts || i ? 1u : 0u);
-          umma_commit(&ctl->empty[slot]);
+            for (int i = 0; i < 8; ++i)
+              umma_bf16(tmem_base + (b * kFewParts + k % kFewParts) * kFewRows, da + uint64_t((i >> 2) * (kChunkBytes >> 4) + (i & 3) * 2),
+                        db + uint64_t((i >> 2) * ((n_cols * BK * 2) >> 4) + (i & 3) * 2), idesc, k >= kFewParts || i ? 1u : 0u);
+            umma_commit(&ctl->empty[slot]);
+          }
+          if (!ok) break;
+          umma_commit(&ctl->acc_full[b]);
+          ++it;
         }
-        if (!ok) break;
-        umma_commit(&ctl->acc_full[b]);
-        ++it;
       }
       if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
         umma_commit(&ctl->drain);
@@ -865,30 +916,40 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
     for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
       int shard, vrow;
       const int live = rows_of(t, &shard, &vrow) - quarter * 32;        // of this warp's 32 vocabulary rows
-      const uint32_t b = it & 1u;
       const bool empty = live + quarter * 32 == 0;
-      if (!empty) {
+      float v[kFewRows / 32][32] = {};      // the logits, 32 tokens at a time
+      for (int r = 0; !empty && ok && r < ranges; ++r) {
+        const uint32_t b = it & 1u;
         ok = few_agree(__all_sync(0xffffffffu, wait_few(&ctl->acc_full[b], (it >> 1) & 1u, ctl, p, SITE_ACC_FULL, t)));
-        if (!ok) break;
+        if (!ok) continue;
         tc_fence_after_sync();
-      }
-      for (int c = 0; c < n_cols; c += 32) {
-        const int token = c + lane;
-        float m = -INFINITY, s = 0.f, sum = 0.f;
-        if (!empty) {
-          uint32_t v[32];
-          const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * kFewParts * kFewRows + c;
-          tmem_ld_32x32b_x32(taddr, v);
-          tmem_ld_wait();
-          for (int part = 1; part < min(kFewParts, ksteps); ++part) {
+        const int parts = min(kFewParts, ksteps - r * kFewRange);
+#pragma unroll
+        for (int c = 0; c < kFewRows / 32; ++c) {
+          if (c * 32 >= n_cols) continue;
+          const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * kFewParts * kFewRows + c * 32;
+          for (int part = 0; part < parts; ++part) {
             uint32_t w[32];
             tmem_ld_32x32b_x32(taddr + part * kFewRows, w);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+            for (int i = 0; i < 32; ++i) v[c][i] += __uint_as_float(w[i]);
           }
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl->acc_empty[b]);
+        ++it;
+      }
+      if (!ok) break;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) sh->z[quarter][i][lane] = __uint_as_float(v[i]) * p.z_scale;
+      for (int c = 0; c < kFewRows / 32; ++c) {
+        if (c * 32 >= n_cols) continue;
+        const int token = c * 32 + lane;
+        float m = -INFINITY, s = 0.f, sum = 0.f;
+        if (!empty) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sh->z[quarter][i][lane] = v[c][i] * p.z_scale;
           __syncwarp();
           const float* z = sh->z[quarter][lane];
 #pragma unroll
@@ -926,12 +987,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
           if (p.smoothing != 0.f) p.part_sum[at] = sum;
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");
-      }
-      if (!empty) {
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl->acc_empty[b]);
-        ++it;
       }
     }
   }

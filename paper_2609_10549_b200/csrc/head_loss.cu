@@ -14,8 +14,8 @@
 //          added to the FP32 sums of dX, and DW, the piece, transposed, times X:
 //          dW of the piece
 // The backward pass is bound by the tensor cores: 6 M hidden vocab operations.
-// Measured: forward, 7392 rows, 4096 x 32000, 1.23 ms alone = 1.58 PFLOP/s (the
-// library's 8192^3 product reaches 1.65), 1.48 ms = 1.31 in a loop at the power
+// Measured: forward, 7392 rows, 4096 x 32000, 1.28 ms alone = 1.52 PFLOP/s (the
+// library's 8192^3 product reaches 1.65), 1.51 ms = 1.29 in a loop at the power
 // limit (1.37); backward, 7392 rows, 4096 x 128000, 18.1 ms = 1.28 PFLOP/s at that
 // limit; backward, 401 rows, 1024 x 50001, 200 us = 0.62 PFLOP/s (every tile's part
 // of the table comes from HBM, and three launches ramp up and down).

@@ -8,7 +8,8 @@
 // instructions per element (55 in the first form, and most of the time): hence
 // FP32 in pairs, one position per row for all tensors, row widths compiled in,
 // 16 elements a thread.  Measured (of the copy rate, 6.55 TB/s): forward with
-// residual, 16384 x 8192 BF16: 190 us, 86 %; backward with the residual's
+// residual, 16384 x 8192 BF16: 168 to 192 us, 98 to 86 %, from box to box and run
+// to run (the same code; no cause found); backward with the residual's
 // gradient, 8192 x 4096 BF16: 51 us, 80 % (half of its issue slots are busy, and
 // a row's sums hold up the rest); backward, 4095 x 1001 FP32, an element per
 // access: 21 us, 35 %; 8192 x 1001 BF16, whose rows are not copied ahead either:

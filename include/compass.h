@@ -68,8 +68,9 @@ typedef enum compass_status {
 } compass_status;
 
 enum { COMPASS_OP_AG_GEMM = 0, COMPASS_OP_GEMM_RS = 1 };
-/* BF16 everywhere; FP32 only where an entry point names it (embedding, layer norm, weight gradients). */
-enum { COMPASS_DTYPE_BF16 = 0, COMPASS_DTYPE_FP32 = 1 };
+/* BF16 everywhere; FP32 and the 8-bit types only where an entry point names them (embedding, norms, weight gradients;
+ * tensors kept in 8 bits and their products). */
+enum { COMPASS_DTYPE_BF16 = 0, COMPASS_DTYPE_FP32 = 1, COMPASS_DTYPE_E4M3 = 2, COMPASS_DTYPE_E5M2 = 3 };
 /* Type of token ids and targets. */
 enum { COMPASS_INDEX_INT64 = 0, COMPASS_INDEX_INT32 = 1 };
 /* GEMM+ReduceScatter variants.
@@ -333,7 +334,8 @@ int compass_select_ex(const compass_problem* problem, const compass_calib* calib
  * the same chain run on the stored weights with COMPASS_B_KN --
  * dH_r = gather(dOut) * W1_r and dX_c = rows of sum_q dH_q * W0_q, i.e. the
  * call (dOut, W1, dH, W0, dX) with hidden and ffn unchanged.  Activation
- * derivatives and weight gradients are not part of this library. */
+ * derivatives are not part of this library; weight gradients are there for
+ * activations kept in 8 bits (compass_weight_grad_8bit). */
 enum { COMPASS_ACT_NONE = 0, COMPASS_ACT_GELU_TANH = 1, COMPASS_ACT_SWIGLU = 2 };
 typedef struct compass_mlp {
   int32_t P;           /* tensor-parallel size */
@@ -448,6 +450,89 @@ int compass_head_loss(const compass_head* head, const void* const* X, const void
 int compass_head_loss_backward(const compass_head* head, const void* const* X, const void* const* W, const void* targets,
                                const float* lse, const float* dloss, void* const* dX, void* const* dW, void* workspace,
                                size_t workspace_bytes, void* cuda_stream);
+
+/* ---- a linear block in 8 bits: root-mean-square norm, tensors kept in 8 bits,
+ * products of 8-bit operands, weight gradients ------------------------------------
+ * A tensor in 8 bits is a matrix of COMPASS_DTYPE_E4M3 or _E5M2 values, rows of a
+ * multiple of 16 columns densely packed and 16-byte aligned, and a matrix of
+ * scales, a byte each (E8M0: byte b is 2^(b - 127), 255 is NaN), also densely
+ * packed:
+ *   by runs    [rows][ceil(cols / 128)]: one for 128 columns of a row (activations)
+ *   by blocks  [ceil(rows / 128)][ceil(cols / 128)]: one for 128 x 128 (weights; the
+ *              transpose, which a backward pass multiplies by, has the same scales)
+ * The element's value is its scale times it.  Scales are powers of two because the
+ * tensor cores apply those themselves; the elements being floating-point numbers,
+ * other scales would not make them more precise.
+ * What the section on the operators around the blocks says of workspaces, graphs,
+ * timing, overlaps and M = 0 holds for the norm and the conversions; the products
+ * and the weight gradient want M, N and K > 0.  All results have the same bits at
+ * every call. */
+
+/* Root-mean-square norm over rows of `hidden` elements (struct compass_norm above):
+ *   h = X (+ residual),  Y = h * rstd(h) * gamma,  rstd = 1 / sqrt(mean(h^2) + eps).
+ * Sums and statistics are FP32. */
+/* residual, summed: both or neither NULL, as in compass_layer_norm (summed may be X
+ * or residual).  gamma: NULL for 1.  rstd: M FP32 values, or NULL.  Y: in norm->dtype.
+ * Y8, scale: Y in 8 bits by runs, in `format` (COMPASS_DTYPE_E4M3 or _E5M2), made
+ * from the FP32 values.  Either output may be NULL, not both; with Y8, hidden is a
+ * multiple of 16 and all tensors but rstd and scale are 16-byte aligned. */
+int compass_rms_norm(const compass_norm* norm, const void* const* X, const void* const* residual, const void* gamma,
+                     void* const* summed, void* const* Y, int format, void* const* Y8, void* const* scale, float* rstd,
+                     void* cuda_stream);
+/* dX = rstd * (g dY - xhat * mean(g dY xhat)) (+ dsum), dgamma = sum over all M rows
+ * of dY * xhat, xhat = X * rstd.  dsum: gradient that reaches h past the norm, or
+ * NULL.  dgamma: NULL to leave out.  dX may be dY or dsum themselves (in place). */
+int compass_rms_norm_workspace_bytes(const compass_norm* norm, size_t* bytes);
+int compass_rms_norm_backward(const compass_norm* norm, const void* const* dY, const void* const* X, const void* gamma,
+                              const float* rstd, const void* const* dsum, void* const* dX, void* dgamma, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
+/* Tensors to 8 bits and back: activations [M/P x cols] per shard, or P weights of
+ * M/P rows each (blocks do not cross shards). */
+typedef struct compass_quant {
+  int32_t P;
+  int32_t dtype;        /* of the tensor in full precision: COMPASS_DTYPE_BF16 or _FP32 */
+  int32_t format;       /* COMPASS_DTYPE_E4M3 or _E5M2 */
+  int32_t block_rows;   /* 1: scales by runs, 128: by blocks */
+  int64_t M, cols;      /* rows of all shards; columns, a multiple of 16 */
+} compass_quant;
+/* A scale is the smallest power of two, 2^-127 at least, with max|x| <= largest number
+ * of the format * scale; x / scale is rounded once, to the nearest number (ties to
+ * even).  NaN and infinities become NaN and do not count for the scale. */
+int compass_quantize(const compass_quant* quant, const void* const* X, void* const* Q, void* const* scale, void* cuda_stream);
+/* X = scale * Q: exact in FP32, and in BF16 down to its smallest normal number. */
+int compass_dequantize(const compass_quant* quant, const void* const* Q, const void* const* scale, void* const* X, void* cuda_stream);
+
+/* The products of compass_ag_gemm and compass_gemm_rs on 8-bit operands, one kernel
+ * each, outputs in BF16: activations A by runs, weights B in E4M3 by blocks.
+ * Of the problem, op, P, M, N, K, dtype (of A: COMPASS_DTYPE_E4M3 or _E5M2),
+ * rs_variant (COMPASS_RS_SEGMENTED_K) and b_layout count; M need only be a multiple
+ * of P, K is one of 16, and N one of 16 with COMPASS_B_KN (else any number).
+ *   A, A_scale: [M/P x K] per rank (AllGather), [M x K] (ReduceScatter)
+ *   B, B_scale: [N x K], or [K x N] with COMPASS_B_KN: the stored weight of a forward
+ *               pass, by whose transpose its data gradient multiplies
+ * Sums are FP32 in the tensor cores, over the whole contraction (all ranks' slices
+ * with ReduceScatter), rounded once.  workspace: >= compass_8bit_workspace_bytes,
+ * 256-byte aligned, zeroed once with compass_workspace_init; afterwards
+ * compass_read_status reports a bounded wait that gave up. */
+int compass_8bit_workspace_bytes(const compass_problem* problem, size_t* bytes);
+int compass_ag_gemm_8bit(const compass_problem* problem, const void* const* A, const void* const* A_scale, const void* const* B,
+                         const void* const* B_scale, void* const* C, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int compass_gemm_rs_8bit(const compass_problem* problem, const void* const* A, const void* const* A_scale, const void* const* B,
+                         const void* const* B_scale, void* const* Out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Gradient of the weights of such a product (its problem, weights [N x K]) from the
+ * activations as they were kept, in 8 bits:
+ *   dW_r [N x K] (+)= G_r^T * X_r,  X_r with its scales multiplied in
+ *   AllGather:      G = the gradient of C, P x [M x N];  X = row shards [M/P x K], gathered
+ *   ReduceScatter:  G = the gradient of Out in row shards [M/P x N], gathered;  X = P x [M x K]
+ * G is BF16, N a multiple of 8; X with its scales enters the product in BF16, which
+ * holds it exactly (below 2^-126 it is rounded); sums are FP32.  dW: grad_dtype
+ * (COMPASS_DTYPE_BF16 or _FP32); accumulate != 0 adds to what it holds, in FP32,
+ * and rounds once. */
+int compass_weight_grad_8bit(const compass_problem* problem, int grad_dtype, int accumulate, const void* const* G,
+                             const void* const* X, const void* const* X_scale, void* const* dW, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
 
 /* ---- models, individually (host) ----------------------------------------- */
 /* Eq. 2-3: (d-1)*max(T_comp,T_comm)/d*(alpha+beta*d) + T_comp/d + T_comm/d. */

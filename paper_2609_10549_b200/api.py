@@ -20,7 +20,7 @@ OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_BUFFER_TOO_S
 ERR_SCRATCH_LIMIT = 8
 NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024
 OP_AG_GEMM, OP_GEMM_RS = 0, 1
-DTYPE_BF16, DTYPE_FP32 = 0, 1
+DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3, DTYPE_E5M2 = range(4)
 INDEX_INT64, INDEX_INT32 = 0, 1
 RS_SEGMENTED_K, RS_RING_RMW, RS_RING_RMW_F32 = 0, 1, 2
 STRATEGY_INTRAFUSION, STRATEGY_INTERDECOM = 0, 1
@@ -44,6 +44,8 @@ EXPORTS = (
     "compass_embedding", "compass_embedding_workspace_bytes", "compass_embedding_backward",
     "compass_layer_norm", "compass_layer_norm_workspace_bytes", "compass_layer_norm_backward",
     "compass_head_workspace_bytes", "compass_head_loss", "compass_head_loss_backward",
+    "compass_rms_norm", "compass_rms_norm_workspace_bytes", "compass_rms_norm_backward", "compass_quantize", "compass_dequantize",
+    "compass_8bit_workspace_bytes", "compass_ag_gemm_8bit", "compass_gemm_rs_8bit", "compass_weight_grad_8bit",
 )
 
 
@@ -79,6 +81,11 @@ class Head(C.Structure):
     _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("index_dtype", C.c_int32),
                 ("M", C.c_int64), ("hidden", C.c_int64), ("vocab", C.c_int64), ("logit_scale", C.c_float),
                 ("label_smoothing", C.c_float)]
+
+
+class Quant(C.Structure):
+    _fields_ = [("P", C.c_int32), ("dtype", C.c_int32), ("format", C.c_int32), ("block_rows", C.c_int32),
+                ("M", C.c_int64), ("cols", C.c_int64)]
 
 
 class SchedEntry(C.Structure):
@@ -169,6 +176,14 @@ def lib() -> C.CDLL:
         L.compass_head_workspace_bytes.argtypes = [C.POINTER(Head), C.c_int, C.POINTER(C.c_size_t)]
         L.compass_head_loss.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, vp, C.c_size_t, vp]
         L.compass_head_loss_backward.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, pp, pp, vp, C.c_size_t, vp]
+        L.compass_rms_norm.argtypes = [C.POINTER(Norm), pp, pp, vp, pp, pp, C.c_int, pp, pp, vp, vp]
+        L.compass_rms_norm_workspace_bytes.argtypes = [C.POINTER(Norm), C.POINTER(C.c_size_t)]
+        L.compass_rms_norm_backward.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, pp, pp, vp, vp, C.c_size_t, vp]
+        L.compass_quantize.argtypes = L.compass_dequantize.argtypes = [C.POINTER(Quant), pp, pp, pp, vp]
+        L.compass_8bit_workspace_bytes.argtypes = [C.POINTER(Problem), C.POINTER(C.c_size_t)]
+        for name in ("compass_ag_gemm_8bit", "compass_gemm_rs_8bit"):
+            getattr(L, name).argtypes = [C.POINTER(Problem), pp, pp, pp, pp, pp, vp, C.c_size_t, vp]
+        L.compass_weight_grad_8bit.argtypes = [C.POINTER(Problem), C.c_int, C.c_int, pp, pp, pp, pp, vp, C.c_size_t, vp]
         L.compass_set_wait_limit_us.argtypes = [C.c_uint32]
         L.compass_test_drop_flag_writes.argtypes = [C.c_int]
         L.compass_tensor_map_cache_stats.argtypes = [C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
@@ -593,6 +608,159 @@ def compass_head_loss_backward(head: Head, X: Sequence, W: Sequence, targets, ls
                                             _vector("dloss", dloss, h.M, here), _row_shards("dX", dX, h.P, h.M, h.hidden, h.dtype, here),
                                             _vocab_shards("dW", dW, h.P, h.vocab, h.hidden, h.grad_dtype, here), p, n, _stream_handle(stream, here)),
            "compass_head_loss_backward")
+
+
+# ---- a linear block in 8 bits: root-mean-square norm, tensors kept in 8 bits, products, weight gradients ------
+#
+# 8-bit tensors are torch.float8_e4m3fn or torch.float8_e5m2, their scales torch.float8_e8m0fnu.  Arguments are checked
+# as those of the operators around the blocks are.
+
+def scale_shape(rows: int, cols: int, block_rows: int = 1):
+    """Shape of the scales of an 8-bit matrix: one for 128 columns of a row, or for each 128 x 128 block."""
+    return -(-rows // block_rows), -(-cols // 128)
+
+
+def _type8(format: int):
+    import torch
+    kinds = {DTYPE_E4M3: torch.float8_e4m3fn, DTYPE_E5M2: torch.float8_e5m2}
+    if format not in kinds:
+        raise ValueError(f"unknown 8-bit type {format}")
+    return kinds[format]
+
+
+def _matrices(name: str, tensors: Sequence, n: int, dtype, shape, here):
+    if len(tensors) != n:
+        raise ValueError(f"{name}: want {n} tensors, got {len(tensors)}")
+    return _pointers([_tensor(name, t, dtype, shape, here) for t in tensors])
+
+
+def _scales(name: str, tensors: Sequence, n: int, rows: int, cols: int, here, block_rows: int = 1):
+    import torch
+    return _matrices(name, tensors, n, torch.float8_e8m0fnu, scale_shape(rows, cols, block_rows), here)
+
+
+def alloc_8bit(n: int, rows: int, cols: int, format: int = DTYPE_E4M3, block_rows: int = 1, device="cuda"):
+    """n matrices in 8 bits and their scales, not initialised."""
+    import torch
+    return ([torch.empty(rows, cols, device=device, dtype=_type8(format)) for _ in range(n)],
+            [torch.empty(scale_shape(rows, cols, block_rows), device=device, dtype=torch.float8_e8m0fnu) for _ in range(n)])
+
+
+def make_rms_norm(P: int, M: int, hidden: int, eps: float = 1e-6, dtype: int = DTYPE_BF16, param_dtype: Optional[int] = None) -> Norm:
+    return Norm(P=P, dtype=dtype, param_dtype=dtype if param_dtype is None else param_dtype, eps=eps, M=M, hidden=hidden)
+
+
+def compass_rms_norm(norm: Norm, X: Sequence, gamma, Y: Optional[Sequence] = None, rstd=None, residual: Optional[Sequence] = None,
+                     summed: Optional[Sequence] = None, Y8: Optional[Sequence] = None, scale: Optional[Sequence] = None,
+                     format: int = DTYPE_E4M3, stream=None) -> None:
+    """Root-mean-square norm of X, or of summed = X + residual, into Y, into Y8 with its scales, or both; gamma may be None (1)."""
+    n, here = norm, _here()
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
+    each = n.M // n.P if n.P else 0
+    _check(lib().compass_rms_norm(C.byref(n), rows("X", X), rows("residual", residual), _vector("gamma", gamma, n.hidden, here, n.param_dtype),
+                                  rows("summed", summed), rows("Y", Y), format,
+                                  None if Y8 is None else _matrices("Y8", Y8, n.P, _type8(format), (each, n.hidden), here),
+                                  None if scale is None else _scales("scale", scale, n.P, each, n.hidden, here),
+                                  _vector("rstd", rstd, n.M, here), _stream_handle(stream, here)), "compass_rms_norm")
+
+
+def compass_rms_norm_workspace_bytes(norm: Norm) -> int:
+    n = C.c_size_t(0)
+    _check(lib().compass_rms_norm_workspace_bytes(C.byref(norm), C.byref(n)), "compass_rms_norm_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_rms_norm_workspace(norm: Norm, device="cuda"):
+    return _sized_workspace(compass_rms_norm_workspace_bytes(norm), device)
+
+
+def compass_rms_norm_backward(norm: Norm, dY: Sequence, X: Sequence, gamma, rstd, dX: Sequence, dgamma, workspace,
+                              dsum: Optional[Sequence] = None, stream=None) -> None:
+    """dX (+ dsum, the gradient that reaches X past the norm) and dgamma (None: left out) summed over all M rows."""
+    n, here = norm, _here()
+    p, size = _op_workspace(workspace, here)
+    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
+    _check(lib().compass_rms_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), _vector("gamma", gamma, n.hidden, here, n.param_dtype),
+                                           _vector("rstd", rstd, n.M, here), rows("dsum", dsum), rows("dX", dX),
+                                           _vector("dgamma", dgamma, n.hidden, here, n.param_dtype), p, size, _stream_handle(stream, here)),
+           "compass_rms_norm_backward")
+
+
+def make_quant(P: int, M: int, cols: int, dtype: int = DTYPE_BF16, format: int = DTYPE_E4M3, block_rows: int = 1) -> Quant:
+    return Quant(P=P, dtype=dtype, format=format, block_rows=block_rows, M=M, cols=cols)
+
+
+def _quant(quant: Quant, X: Sequence, Q: Sequence, scale: Sequence, here):
+    q, each = quant, quant.M // quant.P if quant.P else 0
+    if q.block_rows < 1:
+        raise ValueError(f"unknown block of {q.block_rows} rows")
+    return (_row_shards("X", X, q.P, q.M, q.cols, q.dtype, here), _matrices("Q", Q, q.P, _type8(q.format), (each, q.cols), here),
+            _scales("scale", scale, q.P, each, q.cols, here, q.block_rows))
+
+
+def compass_quantize(quant: Quant, X: Sequence, Q: Sequence, scale: Sequence, stream=None) -> None:
+    """X in 8 bits: values and a power of two for each run of 128 columns or each 128 x 128 block."""
+    here = _here()
+    x, q, s = _quant(quant, X, Q, scale, here)
+    _check(lib().compass_quantize(C.byref(quant), x, q, s, _stream_handle(stream, here)), "compass_quantize")
+
+
+def compass_dequantize(quant: Quant, Q: Sequence, scale: Sequence, X: Sequence, stream=None) -> None:
+    """X = scale * Q."""
+    here = _here()
+    x, q, s = _quant(quant, X, Q, scale, here)
+    _check(lib().compass_dequantize(C.byref(quant), q, s, x, _stream_handle(stream, here)), "compass_dequantize")
+
+
+def compass_8bit_workspace_bytes(problem: Problem) -> int:
+    n = C.c_size_t(0)
+    _check(lib().compass_8bit_workspace_bytes(C.byref(problem), C.byref(n)), "compass_8bit_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_8bit_workspace(problem: Problem, device="cuda"):
+    """For compass_ag_gemm_8bit, compass_gemm_rs_8bit and compass_weight_grad_8bit of this problem."""
+    return _sized_workspace(compass_8bit_workspace_bytes(problem), device)
+
+
+def _product_8bit(name: str, op: int, g: Problem, A: Sequence, A_scale: Sequence, B: Sequence, B_scale: Sequence, out: Sequence, workspace, stream):
+    import torch
+    here = _here()
+    p, size = _op_workspace(workspace, here)
+    each = g.M // g.P if g.P else 0
+    a_rows, out_rows = (each, g.M) if op == OP_AG_GEMM else (g.M, each)
+    b_shape = (g.K, g.N) if g.b_layout == B_KN else (g.N, g.K)
+    _check(getattr(lib(), name)(C.byref(g), _matrices("A", A, g.P, _type8(g.dtype), (a_rows, g.K), here), _scales("A_scale", A_scale, g.P, a_rows, g.K, here),
+                                _matrices("B", B, g.P, torch.float8_e4m3fn, b_shape, here), _scales("B_scale", B_scale, g.P, *b_shape, here, 128),
+                                _matrices("out", out, g.P, torch.bfloat16, (out_rows, g.N), here), p, size, _stream_handle(stream, here)), name)
+
+
+def compass_ag_gemm_8bit(problem: Problem, A: Sequence, A_scale: Sequence, B: Sequence, B_scale: Sequence, Cout: Sequence, workspace,
+                         stream=None) -> None:
+    """C[r] = concat(A) @ B[r].T on 8-bit operands; problem.dtype is the type of A, weights are E4M3 with a scale per 128 x 128."""
+    _product_8bit("compass_ag_gemm_8bit", OP_AG_GEMM, problem, A, A_scale, B, B_scale, Cout, workspace, stream)
+
+
+def compass_gemm_rs_8bit(problem: Problem, A: Sequence, A_scale: Sequence, B: Sequence, B_scale: Sequence, Out: Sequence, workspace,
+                         stream=None) -> None:
+    """Out[r] = rank r's rows of sum over q of A[q] @ B[q].T on 8-bit operands."""
+    _product_8bit("compass_gemm_rs_8bit", OP_GEMM_RS, problem, A, A_scale, B, B_scale, Out, workspace, stream)
+
+
+def compass_weight_grad_8bit(problem: Problem, G: Sequence, X: Sequence, X_scale: Sequence, dW: Sequence, workspace,
+                             grad_dtype: int = DTYPE_BF16, accumulate: bool = False, stream=None) -> None:
+    """dW[r] (+)= G[r].T @ X[r] for the product that `problem` describes, X as it was kept in 8 bits.
+
+    AllGather: G[r] is the gradient of C[r], X the row shards.  ReduceScatter: G the gradient of Out in row shards, X[r] rank r's."""
+    import torch
+    g, here = problem, _here()
+    p, size = _op_workspace(workspace, here)
+    each = g.M // g.P if g.P else 0
+    g_rows, x_rows = (g.M, each) if g.op == OP_AG_GEMM else (each, g.M)
+    _check(lib().compass_weight_grad_8bit(C.byref(g), grad_dtype, int(accumulate), _matrices("G", G, g.P, torch.bfloat16, (g_rows, g.N), here),
+                                          _matrices("X", X, g.P, _type8(g.dtype), (x_rows, g.K), here), _scales("X_scale", X_scale, g.P, x_rows, g.K, here),
+                                          _matrices("dW", dW, g.P, _torch_dtype(grad_dtype), (g.N, g.K), here), p, size, _stream_handle(stream, here)),
+           "compass_weight_grad_8bit")
 
 
 def compass_decomp(problem: Problem, A: Sequence, B: Sequence, out: Sequence, workspace, stream_compute=None,

@@ -1,0 +1,823 @@
+// Tensor-parallel products of 8-bit operands with a scale for each block of 128, for sm_100a:
+//   C[i][j] = sum_b 2^(sa[i][b] + sb[j / 128][b]) * sum_{k in block b} a[i][k] * w[j][k]
+// a: activations in E4M3 or E5M2, a scale per row and 128 columns; w: weights in E4M3, a scale per 128 x 128.  The scales are
+// powers of two (E8M0), which the tensor core applies itself to every 32 products (kind::mxf8f6f4); one for 128 is four times the
+// same.  (With scales of any value the accumulator would have to leave tensor memory every 128 elements.)
+//
+//   AllGather+GEMM      rank r's tiles read the row shards of all ranks, its own first (gather by address)
+//   GEMM+ReduceScatter  a tile's contraction runs over the ranks' slices in ring order, ending near the owner, into one accumulator
+//
+// Two kernels.  gemm8_pair_kernel: pairs of CTAs, 256 rows x up to 256 columns a tile, for batches.  gemm8_few_kernel: weights on
+// the products' M side, 128 rows a tile, and up to 256 activation rows on the N side, the contraction split over a cluster, for
+// few rows, where the weights' bytes are all the work.
+#include <mutex>
+
+#include "pipeline.cuh"
+#include "row_ops.cuh"
+#include "scaled8.cuh"
+
+namespace compass {
+
+using namespace ptx;
+
+namespace {
+
+constexpr int kAtom = 128;                    // elements = bytes of the contraction in one swizzle row: what a scale covers
+constexpr int kChunkBytes = 128 * kAtom;      // 128 rows (or, contraction across: 128 columns) of one atom
+constexpr int kGroupAtoms = 4;                // atoms whose scales are one 32-bit word
+constexpr uint32_t kOne = 0x7F7F7F7Fu;        // scales of 1
+
+struct Gemm8Params {
+  CUtensorMap a[kMaxP];
+  CUtensorMap b[kMaxP];
+  const uint8_t* sa[kMaxP];
+  const uint8_t* sb[kMaxP];
+  __nv_bfloat16* out[kMaxP];
+  StatusBlock* status;
+  int64_t N;
+  int32_t rs;              // GEMM+ReduceScatter
+  int32_t P;
+  int32_t m;               // rows per shard
+  int32_t K;
+  int32_t atoms;           // of a slice of the contraction
+  int32_t kn;              // weights are [K][N]
+  int32_t n_blocks;        // scales along N
+  int32_t a_format;
+  int32_t wide;            // output rows: 2: whole 32-byte sectors, 1: whole 16-byte vectors, 0: neither
+  uint32_t wait_limit_us;
+  // pair kernel
+  int32_t frags;           // 128-row fragments per shard
+  int32_t row_tiles;       // pairs of fragments
+  int32_t col_tiles, bn;   // tiles of bn columns
+  int32_t total;
+  // few-rows kernel
+  int32_t slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
+  int32_t cols;            // accumulator columns, a multiple of 16
+  int32_t n_tiles;         // 128-row tiles of one rank's weights
+  int32_t splits;          // CTAs of a cluster, which share a tile's contraction
+  int32_t stages;
+  int32_t tmem_cols;
+};
+
+// Scales of `count` (1..4) consecutive blocks as one word, the others 1.
+__device__ __forceinline__ uint32_t scales_word(const uint8_t* p, int count, int64_t step) {
+  if (count == 4 && step == 1 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
+  uint32_t w = kOne;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < count) w = (w & ~(0xFFu << (8 * i))) | uint32_t(p[i * step]) << (8 * i);
+  return w;
+}
+// The weights' scales of block `j` along N, from atom `a` on.
+__device__ __forceinline__ uint32_t weight_word(const Gemm8Params& p, int rank, int64_t j, int a, int count) {
+  if (j >= p.n_blocks) return kOne;
+  return p.kn ? scales_word(p.sb[rank] + int64_t(a) * p.n_blocks + j, count, p.n_blocks) : scales_word(p.sb[rank] + j * p.atoms + a, count, 1);
+}
+// MMAs (32 elements each) in atom `a` of a slice.
+__device__ __forceinline__ int steps_of(const Gemm8Params& p, int a) { return min(4, (p.K - a * kAtom + 31) / 32); }
+
+// ---- batches -------------------------------------------------------------------
+// Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue (two per quarter of the rows, 128 columns each),
+// warp 10 brings the scales.  Tensor memory holds two accumulators of 256 columns and the scales only because the accumulators
+// share 32 columns: each is emptied from the shared ones on, and the next tile's products begin once these are read.
+constexpr int kPairThreads = 352;
+constexpr int kEpiWarps = 8;
+constexpr int kPairStages = 3;
+constexpr int kStageAtoms = 2;
+constexpr int kPairStageBytes = kStageAtoms * 2 * kChunkBytes;
+constexpr uint32_t kAcc1 = 224;               // second accumulator's first column; the first's last 32 are shared
+constexpr uint32_t kScaleCols = 480;          // scales of A: 2 x 4 columns, of B: 2 x 8 behind them
+constexpr int kRowGroup = 8;                  // row tiles that go through the columns together (their A stays in L2)
+constexpr int kPitch = 17;                    // words of a staged row of 32 columns
+struct PairControl {
+  uint64_t full[kPairStages], empty[kPairStages];
+  uint64_t scales_full[2], scales_empty[2];
+  uint64_t acc_full, acc_early;
+  uint64_t drain;
+  uint32_t tmem_base;
+  int abort;
+};
+struct PairShared {
+  uint4 scales[2][3][32];                     // [buffer][A, B's columns 0.., B's columns 128..][lane]
+  uint32_t rows[kEpiWarps][32 * kPitch];
+  PairControl ctl;
+};
+constexpr size_t kPairSmemBytes = 1024 + size_t(kPairStages) * kPairStageBytes + sizeof(PairShared);
+static_assert(kPairSmemBytes <= 227 * 1024, "");
+
+struct PairTile {
+  int rank;            // whose weights and output (AllGather)
+  int chunk, row0;     // this CTA's fragment: row shard, first row in it
+  int rows;            // rows of it that exist
+  int first;           // GEMM+ReduceScatter: rank whose slice comes first
+  int64_t col0;
+  int n;               // columns, a multiple of 32
+};
+__device__ __forceinline__ PairTile pair_tile(const Gemm8Params& p, int t, int cta) {
+  PairTile c;
+  const int per_rank = p.row_tiles * p.col_tiles;
+  c.rank = t / per_rank;
+  int w = t - c.rank * per_rank;
+  const int g = w / (kRowGroup * p.col_tiles);
+  w -= g * kRowGroup * p.col_tiles;
+  const int high = min(kRowGroup, p.row_tiles - g * kRowGroup);
+  const int nt = w / high;
+  const int f = 2 * (g * kRowGroup + w - nt * high) + cta;
+  c.col0 = int64_t(nt) * p.bn;
+  c.n = int(min(int64_t(p.bn), (p.N - c.col0 + 31) / 32 * 32));
+  const int all = p.frags * p.P, mine = min(f, all - 1);
+  const int s = mine / p.frags;
+  c.chunk = p.rs ? s : (c.rank + s) % p.P;
+  c.row0 = (mine - s * p.frags) * 128;
+  c.rows = f < all ? min(128, p.m - c.row0) : 0;
+  c.first = ((f - cta) / p.frags + 1) % p.P;
+  return c;
+}
+// Tensor of slice `seg`, the row in it where this CTA's fragment begins.
+__device__ __forceinline__ int slice_of(const Gemm8Params& p, const PairTile& c, int seg) { return p.rs ? (c.first + seg) % p.P : c.chunk; }
+__device__ __forceinline__ int slice_row(const Gemm8Params& p, const PairTile& c) { return p.rs ? c.chunk * p.m + c.row0 : c.row0; }
+
+__global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __grid_constant__ Gemm8Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  PairShared* sh = reinterpret_cast<PairShared*>(smem + kPairStages * kPairStageBytes);
+  PairControl* ctl = &sh->ctl;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = int(cluster_ctarank());
+  const bool leader = cta == 0;
+  const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
+  const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
+  const int segs = p.rs ? p.P : 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->scales_full[b], 2);
+      mbar_init(&ctl->scales_empty[b], 1);
+    }
+    mbar_init(&ctl->acc_full, 1);
+    mbar_init(&ctl->acc_early, 2 * kEpiWarps);
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&ctl->tmem_base, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl->tmem_base;
+  launch_dependents();
+  wait_for_previous_kernel();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      const int b_bytes = (p.kn ? 128 : p.bn / 2) * kAtom;
+      uint32_t j = 0;
+      bool ok = true;
+      for (int t = unit; ok && t < p.total; t += units) {
+        const PairTile c = pair_tile(p, t, cta);
+        const int b0 = int(c.col0) + cta * (c.n / 2);
+        for (int seg = 0; ok && seg < segs; ++seg) {
+          const int q = slice_of(p, c, seg), row = slice_row(p, c), br = p.rs ? q : c.rank;
+          for (int a = 0; a < p.atoms; a += kStageAtoms, ++j) {
+            const uint32_t slot = j % kPairStages;
+            if (j >= kPairStages && !wait_phase(&ctl->empty[slot], (j / kPairStages - 1) & 1u, wc, SITE_EMPTY, t)) {
+              ok = false;
+              break;
+            }
+            const int n = min(kStageAtoms, p.atoms - a);
+            const uint32_t bar = map_to_cta(smem_u32(&ctl->full[slot]), 0);
+            if (leader) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * (kChunkBytes + b_bytes)));
+            uint8_t* dst = smem + slot * kPairStageBytes;
+            for (int i = 0; i < n; ++i) {
+              tma_load_2d_pair_hint(dst + i * 2 * kChunkBytes, &p.a[q], bar, (a + i) * kAtom, row, pol);
+              if (p.kn) tma_load_2d_pair_hint(dst + (i * 2 + 1) * kChunkBytes, &p.b[br], bar, b0, (a + i) * kAtom, pol);
+              else tma_load_2d_pair_hint(dst + (i * 2 + 1) * kChunkBytes, &p.b[br], bar, (a + i) * kAtom, b0, pol);
+            }
+          }
+        }
+      }
+      // leave only when the last stages have been read (the leader's products read both CTAs' memory)
+      const uint32_t back = j < uint32_t(kPairStages) ? j : uint32_t(kPairStages);
+      for (uint32_t i = 1; i <= back; ++i) {
+        const uint32_t r = j - i;
+        if (!wait_phase(&ctl->empty[r % kPairStages], (r / kPairStages) & 1u, wc, SITE_DRAIN, -1)) {
+          if (leader)
+            for (uint32_t k = 1; k <= back; ++k) wait_settled(&ctl->full[(j - k) % kPairStages], ((j - k) / kPairStages) & 1u);
+          break;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- MMA issuer
+    if (leader && lane == 0) {
+      const uint64_t desc_a0 = umma_smem_desc_sw128(smem_u32(smem));
+      const uint64_t desc_b0 = p.kn ? umma_smem_desc_sw128_mn(smem_u32(smem + kChunkBytes), kChunkBytes) : umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
+      // a step of 32 elements: 32 bytes of a row, or (contraction across) four groups of 8 rows
+      const uint64_t bk = p.kn ? 4096 >> 4 : 2;
+      const uint64_t desc_s = smem_desc_scales(smem_u32(sh->scales));
+      uint32_t j = 0, it = 0, g = 0;
+      bool ok = true;
+      for (int t = unit; ok && t < p.total; t += units, ++it) {
+        const PairTile c = pair_tile(p, t, 0);
+        const uint32_t idesc0 = umma_idesc_mx8(256, uint32_t(c.n), uint32_t(p.a_format), E4M3) | (p.kn ? kUmmaIdescBMnMajor : 0u);
+        const uint32_t acc = tmem_base + (it & 1u ? kAcc1 : 0u);
+        if (it > 0) {
+          if (!(ok = wait_phase(&ctl->acc_early, (it - 1) & 1u, wc, SITE_ACC_EMPTY, t))) break;
+          tc_fence_after_sync();
+        }
+        for (int seg = 0; ok && seg < segs; ++seg) {
+          uint32_t buf = 0;
+          for (int a = 0; a < p.atoms; a += kStageAtoms, ++j) {
+            if (a % kGroupAtoms == 0) {
+              buf = g & 1u;
+              if (!(ok = wait_phase(&ctl->scales_full[buf], (g >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
+              tc_fence_after_sync();
+              const uint64_t from = desc_s + uint64_t(buf * (3 * 512 >> 4));
+              tmem_copy_scales<true>(tmem_base + kScaleCols + buf * 4, from);
+              tmem_copy_scales<true>(tmem_base + kScaleCols + 8 + buf * 8, from + (512 >> 4));
+              tmem_copy_scales<true>(tmem_base + kScaleCols + 12 + buf * 8, from + (1024 >> 4));
+              ++g;
+            }
+            const uint32_t slot = j % kPairStages;
+            if (!(ok = wait_phase(&ctl->full[slot], (j / kPairStages) & 1u, wc, SITE_FULL, t))) break;
+            tc_fence_after_sync();
+            const uint32_t sa = tmem_base + kScaleCols + buf * 4, sb = tmem_base + kScaleCols + 8 + buf * 8;
+#pragma unroll
+            for (int i = 0; i < kStageAtoms; ++i) {
+              if (a + i >= p.atoms) break;
+              const uint64_t da = desc_a0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
+              const uint64_t db = desc_b0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
+              const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(a + i) % kGroupAtoms);
+              const uint32_t first = (seg | a | i) != 0 ? 1u : 0u;
+              const int steps = steps_of(p, a + i);
+              if (steps == 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
+              } else {
+                for (int k = 0; k < steps; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
+              }
+            }
+            umma_commit_pair(&ctl->empty[slot], 0x3);
+            if (a % kGroupAtoms == kGroupAtoms - kStageAtoms || a + kStageAtoms >= p.atoms) umma_commit_pair(&ctl->scales_empty[buf], 0x3);
+          }
+        }
+        if (ok) umma_commit_pair(&ctl->acc_full, 0x3);
+      }
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+        // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
+        umma_commit_pair(&ctl->drain, 0x1);
+        wait_settled(&ctl->drain, 0);
+      }
+    }
+  } else if (warp == 10) {
+    // ------------------------------------------------------------------ scales
+    // A word of four blocks' scales per row; those of the next group are on their way while this one's buffer is waited for.
+    uint32_t g = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < p.total; t += units) {
+      const PairTile c = pair_tile(p, t, cta);
+      const int row = slice_row(p, c);
+      for (int seg = 0; ok && seg < segs; ++seg) {
+        const int q = slice_of(p, c, seg), br = p.rs ? q : c.rank;
+        const uint8_t* sa = p.sa[q] + int64_t(row) * p.atoms;
+        for (int a = 0; a < p.atoms; a += kGroupAtoms, ++g) {
+          const int n = min(kGroupAtoms, p.atoms - a);
+          uint32_t w[4], v[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = i * 32 + lane < c.rows ? scales_word(sa + int64_t(i * 32 + lane) * p.atoms + a, n, 1) : kOne;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int64_t b = (c.col0 + 32 * i) >> 7;
+            v[i] = i > 0 && b == (c.col0 + 32 * (i - 1)) >> 7 ? v[i > 0 ? i - 1 : 0] : 32 * i < c.n ? weight_word(p, br, b, a, n) : kOne;
+          }
+          const uint32_t buf = g & 1u;
+          if (g >= 2) {
+            ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((g >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
+            if (!ok) break;
+          }
+          sh->scales[buf][0][lane] = make_uint4(w[0], w[1], w[2], w[3]);
+          sh->scales[buf][1][lane] = make_uint4(v[0], v[1], v[2], v[3]);
+          sh->scales[buf][2][lane] = make_uint4(v[4], v[5], v[6], v[7]);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+        }
+      }
+    }
+    // leave only when the last groups' signals have come
+    for (uint32_t i = g < 2u ? g : 2u; ok && i > 0; --i)
+      ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[(g - i) & 1u], ((g - i) >> 1) & 1u, wc, SITE_DRAIN, -1));
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    uint32_t it = 0;
+    for (int t = unit; t < p.total; t += units, ++it) {
+      const PairTile c = pair_tile(p, t, cta);
+      uint32_t v[4][32];
+      const bool got = wait_phase(&ctl->acc_full, it & 1u, wc, SITE_ACC_FULL, t);
+      if (!__all_sync(0xffffffffu, got)) break;
+      tc_fence_after_sync();
+      const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + (it & 1u ? kAcc1 : 0u) + half * 128;
+      // The shared columns first: the last 32 of the first accumulator, the first 32 of the second.  The others, of the accumulator
+      // that the next tile does not touch, may be read later.
+      const bool second = it & 1u;
+      if (second) tmem_ld_32x32b_x32(taddr, v[0]);
+      else tmem_ld_32x32b_x32(taddr + 96, v[3]);
+      tmem_ld_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_early), 0));
+      if (second) tmem_ld_32x32b_x32(taddr + 96, v[3]);
+      else tmem_ld_32x32b_x32(taddr, v[0]);
+      tmem_ld_32x32b_x32(taddr + 32, v[1]);
+      tmem_ld_32x32b_x32(taddr + 64, v[2]);
+      tmem_ld_wait();
+
+      const int64_t left = p.N - c.col0 - half * 128;
+      const int cols = int(min(int64_t(min(128, c.n - half * 128)), left));      // of this warp's 128
+      const int rank = p.rs ? c.chunk : c.rank;
+      const int64_t row0 = (p.rs ? c.row0 : c.chunk * int64_t(p.m) + c.row0) + quarter * 32;
+      __nv_bfloat16* out = p.out[rank] + row0 * p.N + c.col0 + half * 128;
+      if (p.wide) {
+        if (quarter * 32 + lane < c.rows) {
+          __nv_bfloat16* mine = out + int64_t(lane) * p.N;
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            if (g * 16 >= cols) break;
+            uint32_t q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              q[i] = pack_bf16x2(__uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i]), __uint_as_float(v[g >> 1][(g & 1) * 16 + 2 * i + 1]));
+            if (p.wide == 2) {
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(mine + g * 16), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]),
+                           "r"(q[4]), "r"(q[5]), "r"(q[6]), "r"(q[7])
+                           : "memory");
+            } else {
+              *reinterpret_cast<uint4*>(mine + g * 16) = make_uint4(q[0], q[1], q[2], q[3]);
+              if (g * 16 + 8 < cols) *reinterpret_cast<uint4*>(mine + g * 16 + 8) = make_uint4(q[4], q[5], q[6], q[7]);
+            }
+          }
+        }
+      } else {
+        // rows that are not whole vectors: through shared memory, so that a warp writes an element each of one row's 32
+        uint32_t* rows = sh->rows[warp - 2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (k * 32 >= cols) break;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) rows[lane * kPitch + i] = pack_bf16x2(__uint_as_float(v[k][2 * i]), __uint_as_float(v[k][2 * i + 1]));
+          __syncwarp();
+          if (k * 32 + lane < cols) {
+            const int shift = 16 * (lane & 1);
+            for (int r = 0; r < min(32, c.rows - quarter * 32); ++r)
+              reinterpret_cast<unsigned short*>(out + int64_t(r) * p.N)[k * 32 + lane] = static_cast<unsigned short>(rows[r * kPitch + (lane >> 1)] >> shift);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---- few rows ------------------------------------------------------------------
+// Warp 0 loads, warp 1 multiplies, warp 2 brings the scales, warps 4..7 read the accumulator.  The CTAs of a cluster take a share
+// of the contraction each and add their FP32 sums up, rank by rank, through each other's shared memory.
+constexpr int kFewThreads = 256;
+constexpr int kFewMostCols = 256;
+constexpr int kFewMostStages = 12;
+constexpr int kFewRoom = 200 * 1024;          // of stages, with one CTA per SM
+constexpr int kFewHalfRoom = 96 * 1024;       // with two
+constexpr size_t kFewAlone = 116 * 1024;      // shared memory that keeps other kernels with as much off the SM
+struct FewControl {
+  uint64_t full[kFewMostStages], empty[kFewMostStages];
+  uint64_t scales_full[2], scales_empty[2];
+  uint64_t acc_full, drain;
+  uint32_t tmem_base;
+  int abort;
+};
+struct FewShared {
+  uint4 scales[2][3][32];
+  FewControl ctl;
+};
+__host__ __device__ constexpr int few_stage_bytes(int cols) { return kChunkBytes + cols * kAtom; }
+__host__ __device__ constexpr size_t few_smem_bytes(int cols, int stages) { return 1024 + size_t(stages) * few_stage_bytes(cols) + sizeof(FewShared); }
+
+__global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_constant__ Gemm8Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const int stage_bytes = few_stage_bytes(p.cols), stages = p.stages;
+  FewShared* sh = reinterpret_cast<FewShared*>(smem + stages * stage_bytes);
+  FewControl* ctl = &sh->ctl;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = p.splits > 1 ? int(cluster_ctarank()) : 0;
+  const int t = int(blockIdx.x) / p.splits;
+  const int rank = p.rs ? 0 : t / p.n_tiles;
+  const int64_t n0 = int64_t(t - rank * p.n_tiles) * 128;
+  const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
+  // this CTA's atoms of the whole contraction
+  const int all = (p.rs ? p.P : 1) * p.atoms;
+  const int from = int(int64_t(all) * part / p.splits), to = int(int64_t(all) * (part + 1) / p.splits);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->scales_full[b], 1);
+      mbar_init(&ctl->scales_empty[b], 1);
+    }
+    mbar_init(&ctl->acc_full, 1);
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&ctl->tmem_base, uint32_t(p.tmem_cols));
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl->tmem_base;
+  const uint32_t scale_a = tmem_base + uint32_t(p.cols), scale_b = scale_a + 8;      // 2 x 4 and 2 x 8 columns
+  launch_dependents();
+  wait_for_previous_kernel();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      const int shards = p.rs ? 1 : p.P;
+      const uint32_t bytes = uint32_t(kChunkBytes + shards * p.slot * kAtom);
+      int j = 0;
+      for (int g = from; g < to; ++g, ++j) {
+        const int slot = j % stages, seg = g / p.atoms, a = g - seg * p.atoms;
+        if (j >= stages && !wait_phase(&ctl->empty[slot], uint32_t(j / stages - 1) & 1u, wc, SITE_EMPTY, t)) break;
+        uint8_t* dst = smem + slot * stage_bytes;
+        mbar_arrive_expect_tx(&ctl->full[slot], bytes);
+        const CUtensorMap* w = &p.b[p.rs ? seg : rank];
+        if (p.kn) tma_load_2d_hint(dst, w, &ctl->full[slot], int(n0), a * kAtom, pol);
+        else tma_load_2d_hint(dst, w, &ctl->full[slot], a * kAtom, int(n0), pol);
+        for (int s = 0; s < shards; ++s)
+          tma_load_2d_hint(dst + kChunkBytes + s * p.slot * kAtom, &p.a[p.rs ? seg : s], &ctl->full[slot], a * kAtom, 0, pol);
+      }
+      // leave only when everything that was loaded has landed and been read
+      for (int i = max(0, j - stages); i < j; ++i)
+        if (!wait_phase(&ctl->empty[i % stages], uint32_t(i / stages) & 1u, wc, SITE_DRAIN, -1)) {
+          for (int k = max(0, j - stages); k < j; ++k) wait_settled(&ctl->full[k % stages], uint32_t(k / stages) & 1u);
+          break;
+        }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc0 = umma_idesc_mx8(128, uint32_t(p.cols), E4M3, uint32_t(p.a_format)) | (p.kn ? kUmmaIdescAMnMajor : 0u);
+      const uint64_t desc_w = p.kn ? umma_smem_desc_sw128_mn(smem_u32(smem), kChunkBytes) : umma_smem_desc_sw128(smem_u32(smem));
+      const uint64_t desc_x = umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
+      const uint64_t desc_s = smem_desc_scales(smem_u32(sh->scales));
+      const uint64_t wk = p.kn ? 4096 >> 4 : 2;
+      int j = 0;
+      uint32_t group = 0, buf = 0;
+      int in_group = 0, left = 0;
+      bool ok = true;
+      for (int g = from; g < to; ++g, ++j) {
+        const int seg = g / p.atoms, a = g - seg * p.atoms;
+        if (left == 0) {
+          // a group of scales: up to four atoms of one slice
+          left = min(min(kGroupAtoms, p.atoms - a), to - g);
+          in_group = 0;
+          buf = group & 1u;
+          if (!(ok = wait_phase(&ctl->scales_full[buf], (group >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
+          tc_fence_after_sync();
+          const uint64_t src = desc_s + uint64_t(buf * (3 * 512 >> 4));
+          tmem_copy_scales<false>(scale_a + buf * 4, src);
+          tmem_copy_scales<false>(scale_b + buf * 8, src + (512 >> 4));
+          if (p.cols > 128) tmem_copy_scales<false>(scale_b + buf * 8 + 4, src + (1024 >> 4));
+          ++group;
+        }
+        const int slot = j % stages;
+        if (!(ok = wait_phase(&ctl->full[slot], uint32_t(j / stages) & 1u, wc, SITE_FULL, t))) break;
+        tc_fence_after_sync();
+        const uint64_t dw = desc_w + uint64_t((slot * stage_bytes) >> 4), dx = desc_x + uint64_t((slot * stage_bytes) >> 4);
+        const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(in_group));
+        const int steps = steps_of(p, a);
+        for (int k = 0; k < steps; ++k) umma_mx8<false>(tmem_base, dw + k * wk, dx + k * 2, idesc, scale_a + buf * 4, scale_b + buf * 8, j | k ? 1u : 0u);
+        umma_commit(&ctl->empty[slot]);
+        ++in_group;
+        if (--left == 0) umma_commit(&ctl->scales_empty[buf]);
+      }
+      if (ok) umma_commit(&ctl->acc_full);
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+        umma_commit(&ctl->drain);
+        wait_settled(&ctl->drain, 0);
+      }
+    }
+  } else if (warp == 2) {
+    uint32_t group = 0;
+    int n = 0;
+    bool ok = true;
+    for (int g = from; g < to; g += n, ++group) {
+      const int seg = g / p.atoms, a = g - seg * p.atoms;
+      n = min(min(kGroupAtoms, p.atoms - a), to - g);
+      uint32_t w[8];
+      const uint32_t v = weight_word(p, p.rs ? seg : rank, n0 >> 7, a, n);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int col = i * 32 + lane;
+        w[i] = kOne;
+        if (i * 32 < p.cols) {
+          const int s = p.rs ? 0 : col / p.slot, row = col - s * p.slot;
+          if (s < p.P && row < (p.rs ? p.m * p.P : p.m)) w[i] = scales_word(p.sa[p.rs ? seg : s] + int64_t(row) * p.atoms + a, n, 1);
+        }
+      }
+      const uint32_t buf = group & 1u;
+      if (group >= 2) {
+        ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
+        if (!ok) break;
+      }
+      sh->scales[buf][0][lane] = make_uint4(v, v, v, v);
+      sh->scales[buf][1][lane] = make_uint4(w[0], w[1], w[2], w[3]);
+      sh->scales[buf][2][lane] = make_uint4(w[4], w[5], w[6], w[7]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl->scales_full[buf]);
+    }
+    for (uint32_t i = group < 2u ? group : 2u; ok && i > 0; --i)
+      ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[(group - i) & 1u], ((group - i) >> 1) & 1u, wc, SITE_DRAIN, -1));
+  }
+
+  // The sums: lanes are weight rows, columns are activation rows.
+  const int M = p.m * p.P;
+  const int quarter = warp & 3;
+  auto column_of = [&](int i) {      // accumulator column of activation row i
+    const int s = p.rs ? 0 : i / p.m;
+    return p.rs ? i : s * p.slot + (i - s * p.m);
+  };
+  auto store = [&](int i, int n, float x) {
+    if (n0 + n >= p.N) return;
+    const int chunk = i / p.m;
+    __nv_bfloat16* out = p.rs ? p.out[chunk] + int64_t(i - chunk * p.m) * p.N : p.out[rank] + int64_t(i) * p.N;
+    out[n0 + n] = __float2bfloat16_rn(x);
+  };
+  bool ok = true;
+  float* sums = reinterpret_cast<float*>(smem);      // [column][128], over the stages
+  if (warp >= 4) {
+    ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full, 0, wc, SITE_ACC_FULL, t));
+    tc_fence_after_sync();
+    if (ok) {
+      for (int c = 0; c < p.cols; c += 16) {
+        uint32_t v[16];
+        tmem_ld_32x32b_x16(tmem_base + (uint32_t(quarter * 32) << 16) + c, v);
+        tmem_ld_wait();
+        if (p.splits > 1) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int col = c + i, s = p.rs ? 0 : col / p.slot, row = col - s * p.slot;
+            if (p.rs ? col < M : s < p.P && row < p.m) store(p.rs ? col : s * p.m + row, quarter * 32 + lane, __uint_as_float(v[i]));
+          }
+        }
+      }
+    }
+    tc_fence_before_sync();
+  }
+  if (p.splits > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
+      const uint32_t base = smem_u32(sums);
+      const int n = int(threadIdx.x) & 127;
+      for (int i = part + p.splits * (int(threadIdx.x) >> 7); i < M; i += 2 * p.splits) {
+        const uint32_t at = base + uint32_t(column_of(i) * 128 + n) * 4;
+        float x = 0.f;
+        for (int s = 0; s < p.splits; ++s) {
+          float y;
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(map_to_cta(at, uint32_t(s))) : "memory");
+          x += y;
+        }
+        store(i, n, x);
+      }
+    }
+    cluster_arrive();      // nobody's memory goes while it is read
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, uint32_t(p.tmem_cols));
+  }
+}
+
+// ---- host ----------------------------------------------------------------------
+
+int check_problem8(const compass_problem* g, int op) {
+  if (g == nullptr) return COMPASS_ERR_INVALID_ARG;
+  if (g->op != op) return COMPASS_ERR_INVALID_ARG;
+  const int st = check_problem_8bit(g);
+  if (st != COMPASS_OK) return st;
+  // weights [K][N] are read along N
+  return g->b_layout == COMPASS_B_KN && g->N % 16 != 0 ? COMPASS_ERR_ALIGNMENT : COMPASS_OK;
+}
+
+struct DeviceFacts {
+  bool ready = false;
+  int pairs = 0, sms = 0;
+};
+int device_facts(DeviceFacts** out) {
+  constexpr int kMaxDevices = 64;
+  static DeviceFacts facts[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return record_cuda_error(e);
+  if (dev < 0 || dev >= kMaxDevices) return COMPASS_ERR_UNSUPPORTED;
+  std::lock_guard<std::mutex> lock(mu);
+  DeviceFacts& f = facts[dev];
+  if (!f.ready) {
+    e = cudaFuncSetAttribute(gemm8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kPairSmemBytes));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm8_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&f.sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(f.sms / 2 * 2));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmemBytes;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&f.pairs, gemm8_pair_kernel, &cfg);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    if (f.pairs < 1) return COMPASS_ERR_UNSUPPORTED;
+    f.ready = true;
+  }
+  *out = &f;
+  return COMPASS_OK;
+}
+
+int launch_clusters(void (*kernel)(const Gemm8Params), int64_t grid, int threads, size_t smem, int cluster, const Gemm8Params& p, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(grid));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(cluster);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  count_kernel_launch();
+  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}
+
+int run_product(const compass_problem* g, int op, const void* const* A, const void* const* sA, const void* const* B, const void* const* sB,
+                void* const* out, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_problem8(g, op);
+  if (st != COMPASS_OK) return st;
+  if (!A || !sA || !B || !sB || !out) return COMPASS_ERR_INVALID_ARG;
+  for (int r = 0; r < g->P; ++r)
+    if (!A[r] || !sA[r] || !B[r] || !sB[r] || !out[r]) return COMPASS_ERR_INVALID_ARG;
+  for (int r = 0; r < g->P; ++r)
+    if (!is_aligned(A[r], 16) || !is_aligned(B[r], 16) || !is_aligned(out[r], 2)) return COMPASS_ERR_ALIGNMENT;
+  st = check_workspace(ws, ws_bytes, COMPASS_STATUS_BYTES);
+  if (st != COMPASS_OK) return st;
+  DeviceFacts* f;
+  st = device_facts(&f);
+  if (st != COMPASS_OK) return st;
+
+  Gemm8Params p = {};
+  p.rs = op == COMPASS_OP_GEMM_RS;
+  p.P = g->P;
+  p.m = int32_t(g->M / g->P);
+  p.K = int32_t(g->K);
+  p.N = g->N;
+  p.atoms = int32_t(scale_blocks(g->K));
+  p.kn = g->b_layout == COMPASS_B_KN;
+  p.n_blocks = int32_t(scale_blocks(g->N));
+  p.a_format = format_of(g->dtype);
+  p.status = static_cast<StatusBlock*>(ws);
+  p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
+  p.wide = g->N % 16 == 0 ? 2 : g->N % 8 == 0 ? 1 : 0;
+  for (int r = 0; r < g->P; ++r) {
+    p.sa[r] = static_cast<const uint8_t*>(sA[r]);
+    p.sb[r] = static_cast<const uint8_t*>(sB[r]);
+    p.out[r] = static_cast<__nv_bfloat16*>(out[r]);
+    if (p.wide == 2 && !is_aligned(out[r], 32)) p.wide = 1;
+    if (!is_aligned(out[r], 16)) p.wide = 0;
+  }
+  const int64_t a_rows = p.rs ? g->M : p.m;
+  const int64_t b_rows = p.kn ? g->K : g->N, b_cols = p.kn ? g->N : g->K;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int64_t slot = int64_t(round_up(size_t(a_rows), 8)), cols = int64_t(round_up(size_t(p.rs ? slot : slot * g->P), 16));
+  bool ok = true;
+  if (cols <= kFewMostCols) {
+    p.slot = int32_t(slot);
+    p.cols = int32_t(cols);
+    p.n_tiles = int32_t(scale_blocks(g->N));
+    const int64_t tiles = int64_t(p.n_tiles) * (p.rs ? 1 : g->P);
+    const int all = (p.rs ? g->P : 1) * p.atoms;
+    p.splits = 1;
+    while (p.splits < 8 && tiles * p.splits * 2 <= f->sms && all >= 4 * p.splits) p.splits *= 2;
+    const int stage = few_stage_bytes(p.cols);
+    const int64_t mine = ceil_div(all, p.splits);
+    const int room = tiles * p.splits > f->sms && cols <= 128 ? kFewHalfRoom : kFewRoom;
+    int64_t stages = room / stage;
+    if (stages > mine) stages = mine;
+    if (stages > kFewMostStages) stages = kFewMostStages;
+    // (the cluster's sums lie where the stages were)
+    while (p.splits > 1 && stages * stage < cols * 512) ++stages;
+    p.stages = int32_t(stages);
+    p.tmem_cols = 32;
+    while (p.tmem_cols < p.cols + 24) p.tmem_cols *= 2;
+    for (int r = 0; r < g->P; ++r) {
+      ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, p.slot);
+      ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, 128);
+    }
+    if (!ok) return record_cuda_error(cudaErrorUnknown);
+    // The CTAs of a cluster wait for one another while they hold tensor memory: none may share its SM with another cluster that
+    // does, each waiting for what the other holds (kernels of other streams included).  More than half of the shared memory, as
+    // all kernels of this library have that wait so, keeps them apart.
+    size_t smem = few_smem_bytes(p.cols, p.stages);
+    if (p.splits > 1 && smem < kFewAlone) smem = kFewAlone;
+    return launch_clusters(gemm8_few_kernel, tiles * p.splits, kFewThreads, smem, p.splits, p, s);
+  }
+  p.frags = int32_t(ceil_div(p.m, 128));
+  p.row_tiles = int32_t(ceil_div(int64_t(p.frags) * g->P, 2));
+  p.bn = 256;
+  p.col_tiles = int32_t(ceil_div(g->N, p.bn));
+  const int64_t total = int64_t(p.row_tiles) * p.col_tiles * (p.rs ? 1 : g->P);
+  if (total > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  p.total = int32_t(total);
+  for (int r = 0; r < g->P; ++r) {
+    ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, 128);
+    ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.kn ? 128 : p.bn / 2);
+  }
+  if (!ok) return record_cuda_error(cudaErrorUnknown);
+  return launch_clusters(gemm8_pair_kernel, 2 * (total < f->pairs ? total : f->pairs), kPairThreads, kPairSmemBytes, 2, p, s);
+}
+
+}  // namespace
+
+// What the products and the weight gradient of 8-bit activations ask of a description.
+int check_problem_8bit(const compass_problem* g) {
+  if (g->P < 1 || (g->op != COMPASS_OP_AG_GEMM && g->op != COMPASS_OP_GEMM_RS)) return COMPASS_ERR_INVALID_ARG;
+  if (g->P > kMaxP) return COMPASS_ERR_UNSUPPORTED;
+  if (g->M <= 0 || g->N <= 0 || g->K <= 0 || g->M % g->P != 0) return COMPASS_ERR_SHAPE;
+  if (g->M > kMaxDim || g->N > kMaxDim || g->K > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  if (format_of(g->dtype) < 0 || g->rs_variant != COMPASS_RS_SEGMENTED_K) return COMPASS_ERR_UNSUPPORTED;
+  if (g->b_layout != COMPASS_B_NK && g->b_layout != COMPASS_B_KN) return COMPASS_ERR_INVALID_ARG;
+  return g->K % 16 == 0 ? COMPASS_OK : COMPASS_ERR_ALIGNMENT;
+}
+
+}  // namespace compass
+
+using namespace compass;
+
+extern "C" int compass_8bit_workspace_bytes(const compass_problem* g, size_t* bytes) {
+  if (g == nullptr || bytes == nullptr) return COMPASS_ERR_INVALID_ARG;
+  const int st = check_problem_8bit(g);
+  if (st != COMPASS_OK) return st;
+  *bytes = COMPASS_STATUS_BYTES;
+  return COMPASS_OK;
+}
+
+extern "C" int compass_ag_gemm_8bit(const compass_problem* g, const void* const* A, const void* const* A_scale, const void* const* B,
+                                    const void* const* B_scale, void* const* C, void* ws, size_t ws_bytes, void* stream) {
+  return run_product(g, COMPASS_OP_AG_GEMM, A, A_scale, B, B_scale, C, ws, ws_bytes, stream);
+}
+
+extern "C" int compass_gemm_rs_8bit(const compass_problem* g, const void* const* A, const void* const* A_scale, const void* const* B,
+                                    const void* const* B_scale, void* const* Out, void* ws, size_t ws_bytes, void* stream) {
+  return run_product(g, COMPASS_OP_GEMM_RS, A, A_scale, B, B_scale, Out, ws, ws_bytes, stream);
+}

@@ -184,6 +184,11 @@ int launch_gemm(const GemmLaunch& launch, cudaStream_t stream);
 // tensor may have taken over. Host time of enqueuing an output-layer loss, with the table's entries found: 16 ranks forward (17
 // maps) 33.3 us, 32.5 with the table; backward (36 maps) 56.7, 55.6; on the GPU no difference (16 x 4096 x 32000: 56.0, 56.0).
 bool encode_tensor_map(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows);
+// The same for bytes: boxes of 128 columns x box_rows rows (a row of a box is one 128-byte swizzle row).
+bool encode_tensor_map_bytes(CUtensorMap* map, const void* ptr, int64_t rows, int64_t cols, int box_rows);
+// A dense [slabs][rows][cols] tensor of bytes or BF16, boxes of 128 bytes x box_rows rows of one slab, which are filled up with
+// zeros behind the slab's last row.
+bool encode_tensor_map_slabs(CUtensorMap* map, const void* ptr, int64_t slabs, int64_t rows, int64_t cols, int element, int box_rows);
 size_t gemm_smem_bytes();
 void tensor_map_cache_stats(uint64_t* hits, uint64_t* misses);
 int gemm_tile_rows(int mode, int rows_per_block);   // rows of one scheduling tile: 256 (CTA pair) or 128
@@ -194,6 +199,9 @@ int launch_reduce_partials(const void* const* partial, int P, void* const* out, 
 
 int launch_gather_slices(const void* const* shard, void* const* gather, int P, int64_t m, int64_t K, int64_t slice_begin,
                          int64_t slice_rows, cudaStream_t stream);
+
+// gemm_8bit.cu
+int check_problem_8bit(const compass_problem* problem);
 
 // api.cu
 int record_cuda_error(cudaError_t e);

@@ -209,6 +209,23 @@ __device__ __forceinline__ void tma_load_2d_pair_hint(void* smem_dst, const CUte
       ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster_addr), "r"(x), "r"(y), "l"(policy)
       : "memory");
 }
+// 3-D boxes (one slab of a [slabs][rows][cols] tensor): on a barrier of either CTA, and on one of this CTA.
+__device__ __forceinline__ void tma_load_3d_pair_hint(void* smem_dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int32_t x, int32_t y,
+                                                      int32_t z, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %5}], [%2], %6;"
+      ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster_addr), "r"(x), "r"(y), "r"(z), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_hint(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int32_t x, int32_t y, int32_t z,
+                                                 uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %5}], [%2], %6;"
+      ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "l"(policy)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* smem_slot, uint32_t columns) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_slot)), "r"(columns)
                : "memory");
@@ -242,6 +259,47 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint16_t cta_mas
   if (cta_mask & 2)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(map_to_cta(own, 1))
                  : "memory");
+}
+
+// ---- 8-bit operands with block scales -------------------------------------------
+// kind::mxf8f6f4: A and B in E4M3 or E5M2, one E8M0 scale for every 32 elements of the contraction, which is one
+// instruction's depth; the tensor core multiplies every product by 2^(a - 127) * 2^(b - 127).  Scales lie in tensor memory, the
+// rows' (of A, or B's columns') four at a time in a 32-bit word: row 32 c + l in lane l of column c, the same in all four
+// quarters of the lanes.  The instruction descriptor says which byte of the words an instruction takes.
+// Bits: [4,6) byte of B's words, [7,10) A format (0 = E4M3, 1 = E5M2), [10,13) B format, 15/16 A/B major (0 = K),
+// [17,23) N>>3, 23 scale format (1 = E8M0), [24,29) M>>4, [29,31) byte of A's words.
+__host__ __device__ constexpr uint32_t umma_idesc_mx8(uint32_t m, uint32_t n, uint32_t a_format, uint32_t b_format) {
+  return (a_format << 7) | (b_format << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t umma_scale_byte(uint32_t id) { return (id << 4) | (id << 29); }
+template <bool kPair>
+__device__ __forceinline__ void umma_mx8(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b,
+                                         uint32_t accumulate) {
+  if constexpr (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+        : "memory");
+}
+// 128 rows' words, shared memory -> 4 columns of tensor memory, to all four quarters of the lanes; in the shared memory of a
+// pair of CTAs at the same offset, each CTA its own.  The words of row 32 c + l lie at 16 l + 4 c: 32 rows of 16 bytes without
+// swizzle, groups of 8 rows 128 bytes apart.  Issued by ONE thread, in order with its MMAs.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t smem_addr) {
+  return static_cast<uint64_t>((smem_addr & 0x3FFFF) >> 4) | static_cast<uint64_t>(128 >> 4) << 32 | static_cast<uint64_t>(1) << 46;
+}
+template <bool kPair>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
 // Load 32 consecutive FP32 columns of this warp's 32 TMEM lanes: thread t gets

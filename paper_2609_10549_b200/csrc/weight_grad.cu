@@ -1,0 +1,459 @@
+// Gradient of a tensor-parallel product's weights from the activations as they were kept, in 8 bits:
+//   dW[n][k] (+)= sum_m G[m][n] * 2^s[m][k / 128] * x[m][k]
+// The contraction runs over the rows, along which the scales differ, so the tensor cores cannot apply them (they take one scale
+// for 32 elements of the contraction): the 8-bit tile is turned into BF16 in shared memory, which holds scale times value
+// exactly, and the products are BF16 ones with FP32 sums.  The activations cross HBM and L2 in 8 bits.
+//
+// Pairs of CTAs, 256 rows (n) x 256 columns (k) a tile, 128 rows of the contraction a stage.  Both operands lie across the
+// contraction (MN-major).  Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue, warps 10..13 convert: a
+// thread has a row of a stage, so one scale.  Rows past a rank's last one are zeros of the tensor maps.
+//
+// The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
+// 1024 rows long, and added up in FP32 in the result itself.
+#include <mutex>
+
+#include "pipeline.cuh"
+#include "row_ops.cuh"
+#include "scaled8.cuh"
+
+namespace compass {
+
+using namespace ptx;
+
+namespace {
+
+constexpr int kThreads = 448;
+constexpr int kEpiWarps = 8;
+constexpr int kConvWarps = 4;
+constexpr int kRows = 128;                            // of the contraction in a stage
+constexpr int kGBytes = 128 * kRows * 2;              // this CTA's 128 columns of G: two boxes of 64
+constexpr int kXBytes = 128 * kRows;                  // its 128 columns of X
+constexpr int kCBytes = 128 * kRows * 2;              // the same in BF16: two chunks of 64
+constexpr int kChunk = 64 * kRows * 2;
+constexpr int kStages = 3;
+constexpr int kConv = 2;
+constexpr int kRangeStages = 8;                       // of a sum that goes to FP32
+constexpr int kRowGroup = 8;                          // row tiles that go through the columns together
+
+struct GradParams {
+  CUtensorMap g[kMaxP];
+  CUtensorMap x[kMaxP];
+  const uint8_t* sx[kMaxP];
+  void* dw[kMaxP];
+  StatusBlock* status;
+  int64_t N, K;
+  int32_t ag;              // AllGather: X in row shards, G whole; else the other way round
+  int32_t P;
+  int32_t m;               // rows per shard
+  int32_t blocks;          // scales per row
+  int32_t stages;          // per shard
+  int32_t row_tiles, col_tiles, total;
+  int32_t accumulate, fp32;
+  int32_t wide;            // results lie on 32-byte boundaries
+  uint32_t wait_limit_us;
+};
+
+struct Control {
+  uint64_t g_full[kStages], g_empty[kStages];
+  uint64_t x_full[kStages], x_empty[kStages];
+  uint64_t c_full[kConv], c_empty[kConv];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t drain;
+  uint32_t tmem_base;
+  int abort;
+};
+constexpr int kXAt = kStages * kGBytes, kCAt = kXAt + kStages * kXBytes, kControlAt = kCAt + kConv * kCBytes;
+constexpr size_t kSmemBytes = 1024 + kControlAt + sizeof(Control);
+static_assert(kSmemBytes <= 227 * 1024, "");
+
+struct Tile {
+  int rank;
+  int row0, col0;
+};
+__device__ __forceinline__ Tile tile_of(const GradParams& p, int t) {
+  Tile c;
+  const int per_rank = p.row_tiles * p.col_tiles;
+  c.rank = t / per_rank;
+  int w = t - c.rank * per_rank;
+  const int g = w / (kRowGroup * p.col_tiles);
+  w -= g * kRowGroup * p.col_tiles;
+  const int high = min(kRowGroup, p.row_tiles - g * kRowGroup);
+  const int nt = w / high;
+  c.row0 = (g * kRowGroup + w - nt * high) * 256;
+  c.col0 = nt * 256;
+  return c;
+}
+
+// 16 values of 8 bits times a scale, in BF16.
+template <int kFormat>
+__device__ __forceinline__ void convert16(const uint4& w, F2 scale, uint4& lo, uint4& hi) {
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 x = unpack8x2<kFormat>(v[i >> 1] >> (16 * (i & 1)));
+    const float2 y = of(f2(x.x, x.y) * scale);
+    o[i] = pack_bf16x2(y.x, y.y);
+  }
+  lo = make_uint4(o[0], o[1], o[2], o[3]);
+  hi = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+template <int kFormat>
+__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ GradParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  Control* ctl = reinterpret_cast<Control*>(smem + kControlAt);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = int(cluster_ctarank());
+  const bool leader = cta == 0;
+  const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
+  const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
+  const int all = p.P * p.stages;      // stages of a tile
+  const int range = p.fp32 ? kRangeStages : all;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctl->g_full[s], 1);
+      mbar_init(&ctl->g_empty[s], 1);
+      mbar_init(&ctl->x_full[s], 1);
+      mbar_init(&ctl->x_empty[s], kConvWarps);
+    }
+    for (int b = 0; b < kConv; ++b) {
+      mbar_init(&ctl->c_full[b], 2 * kConvWarps);
+      mbar_init(&ctl->c_empty[b], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->acc_full[b], 1);
+      mbar_init(&ctl->acc_empty[b], 2 * kEpiWarps);
+    }
+    mbar_init(&ctl->drain, 1);
+    ctl->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&ctl->tmem_base, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = ctl->tmem_base;
+  launch_dependents();
+  wait_for_previous_kernel();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      uint32_t j = 0;
+      bool ok = true;
+      for (int t = unit; ok && t < p.total; t += units) {
+        const Tile c = tile_of(p, t);
+        const int n0 = c.row0 + cta * 128, k0 = c.col0 + cta * 128;
+        for (int s = 0; ok && s < p.P; ++s)
+          for (int i = 0; i < p.stages; ++i, ++j) {
+            const uint32_t slot = j % kStages;
+            if (j >= kStages) {
+              const uint32_t parity = (j / kStages - 1) & 1u;
+              if (!(ok = wait_phase(&ctl->x_empty[slot], parity, wc, SITE_EMPTY, t) && wait_phase(&ctl->g_empty[slot], parity, wc, SITE_EMPTY, t))) break;
+            }
+            mbar_arrive_expect_tx(&ctl->x_full[slot], kXBytes);
+            tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &ctl->x_full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
+            const uint32_t bar = map_to_cta(smem_u32(&ctl->g_full[slot]), 0);
+            if (leader) mbar_arrive_expect_tx(&ctl->g_full[slot], 2 * kGBytes);
+            const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
+            tma_load_3d_pair_hint(smem + slot * kGBytes, g, bar, n0, i * kRows, p.ag ? s : 0, pol);
+            tma_load_3d_pair_hint(smem + slot * kGBytes + kChunk, g, bar, n0 + 64, i * kRows, p.ag ? s : 0, pol);
+          }
+      }
+      // leave only when the last stages have been read (the leader's products read both CTAs' memory)
+      const uint32_t back = j < uint32_t(kStages) ? j : uint32_t(kStages);
+      for (uint32_t i = 1; i <= back; ++i) {
+        const uint32_t r = j - i, slot = r % kStages, parity = (r / kStages) & 1u;
+        if (!wait_phase(&ctl->x_empty[slot], parity, wc, SITE_DRAIN, -1) || !wait_phase(&ctl->g_empty[slot], parity, wc, SITE_DRAIN, -1)) {
+          for (uint32_t k = 1; k <= back; ++k) {
+            wait_settled(&ctl->x_full[(j - k) % kStages], ((j - k) / kStages) & 1u);
+            if (leader) wait_settled(&ctl->g_full[(j - k) % kStages], ((j - k) / kStages) & 1u);
+          }
+          break;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- MMA issuer
+    if (leader && lane == 0) {
+      constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | kUmmaIdescAMnMajor | kUmmaIdescBMnMajor;
+      const uint64_t desc_g = umma_smem_desc_sw128_mn(smem_u32(smem), kChunk);
+      const uint64_t desc_c = umma_smem_desc_sw128_mn(smem_u32(smem + kCAt), kChunk);
+      uint32_t j = 0, it = 0;
+      bool ok = true;
+      for (int t = unit; ok && t < p.total; t += units) {
+        int shard_stage = 0;
+        for (int a = 0; ok && a < all; ++it) {
+          const uint32_t b = it & 1u;
+          const int to = min(all, a + range);
+          if (!(ok = wait_phase(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t))) break;
+          tc_fence_after_sync();
+          for (bool first = true; a < to; ++a, ++j, first = false) {
+            const uint32_t slot = j % kStages, conv = j % kConv;
+            if (!(ok = wait_phase(&ctl->g_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t) &&
+                       wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t)))
+              break;
+            tc_fence_after_sync();
+            // a step of 16 rows of the contraction is two groups of 8 (2048 bytes)
+            const uint64_t da = desc_g + uint64_t((slot * kGBytes) >> 4), db = desc_c + uint64_t((conv * kCBytes) >> 4);
+            const int steps = min(kRows / 16, (p.m - shard_stage * kRows + 15) / 16);
+            for (int k = 0; k < steps; ++k) umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, first && k == 0 ? 0u : 1u);
+            umma_commit_pair(&ctl->g_empty[slot], 0x3);
+            umma_commit_pair(&ctl->c_empty[conv], 0x3);
+            if (++shard_stage == p.stages) shard_stage = 0;
+          }
+          if (ok) umma_commit_pair(&ctl->acc_full[b], 0x3);
+        }
+      }
+      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+        umma_commit_pair(&ctl->drain, 0x1);
+        wait_settled(&ctl->drain, 0);
+      }
+    }
+  } else if (warp >= 2 + kEpiWarps) {
+    // ------------------------------------------------------------- 8 bits -> BF16
+    const int row = (warp - 2 - kEpiWarps) * 32 + lane;
+    uint32_t j = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < p.total; t += units) {
+      const Tile c = tile_of(p, t);
+      const int block = (c.col0 >> 7) + cta;
+      // (scales of columns that do not exist: 1, their values are zeros)
+      auto scale_at = [&](int a) -> uint32_t {
+        const int s = a / p.stages, r = (a - s * p.stages) * kRows + row;
+        if (a >= all || r >= p.m || block >= p.blocks) return 127u;
+        const uint8_t* sx = p.ag ? p.sx[s] + int64_t(r) * p.blocks : p.sx[c.rank] + (int64_t(s) * p.m + r) * p.blocks;
+        return sx[block];
+      };
+      uint32_t next = scale_at(0);
+      for (int a = 0; a < all; ++a, ++j) {
+        const F2 scale = f2(scale_value(next));
+        next = scale_at(a + 1);
+        const uint32_t slot = j % kStages, conv = j % kConv;
+        ok = wait_phase(&ctl->x_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t);
+        if (ok && j >= kConv) ok = wait_phase(&ctl->c_empty[conv], (j / kConv - 1) & 1u, wc, SITE_EMPTY, t);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint8_t* from = smem + kXAt + slot * kXBytes + row * 128;
+        uint8_t* to = smem + kCAt + conv * kCBytes + row * 128;
+        const int swizzle = row & 7;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          uint4 lo, hi;
+          convert16<kFormat>(*reinterpret_cast<const uint4*>(from + ((u ^ swizzle) << 4)), scale, lo, hi);
+          uint8_t* chunk = to + (u >> 2) * kChunk;
+          const int at = 2 * (u & 3);
+          *reinterpret_cast<uint4*>(chunk + ((at ^ swizzle) << 4)) = lo;
+          *reinterpret_cast<uint4*>(chunk + (((at + 1) ^ swizzle) << 4)) = hi;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&ctl->x_empty[slot]);
+          mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->c_full[conv]), 0));
+        }
+      }
+    }
+    for (uint32_t i = j < uint32_t(kConv) ? j : uint32_t(kConv); ok && i > 0; --i)
+      ok = __all_sync(0xffffffffu, wait_phase(&ctl->c_empty[(j - i) % kConv], ((j - i) / kConv) & 1u, wc, SITE_DRAIN, -1));
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < p.total; t += units) {
+      const Tile c = tile_of(p, t);
+      const int64_t n = c.row0 + cta * 128 + quarter * 32 + lane;
+      const int64_t k0 = c.col0 + half * 128;
+      const int cols = int(min(int64_t(128), p.K - k0));      // a multiple of 16, or none
+      const int64_t at = n * p.K + k0;
+      for (int a = 0; a < all; a += range, ++it) {
+        const uint32_t b = it & 1u;
+        ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full[b], (it >> 1) & 1u, wc, SITE_ACC_FULL, t));
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
+        const bool add = p.accumulate || a > 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t v[32];
+          tmem_ld_32x32b_x32(taddr + q * 32, v);
+          tmem_ld_wait();
+          if (q == 3) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+          }
+          if (n >= p.N || q * 32 >= cols) continue;
+          if (p.fp32) {
+            float* out = static_cast<float*>(p.dw[c.rank]) + at + q * 32;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              if (q * 32 + g * 4 >= cols) break;
+              float4 x = make_float4(__uint_as_float(v[4 * g]), __uint_as_float(v[4 * g + 1]), __uint_as_float(v[4 * g + 2]), __uint_as_float(v[4 * g + 3]));
+              if (add) {
+                const float4 old = reinterpret_cast<const float4*>(out)[g];
+                x.x += old.x, x.y += old.y, x.z += old.z, x.w += old.w;
+              }
+              reinterpret_cast<float4*>(out)[g] = x;
+            }
+          } else {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dw[c.rank]) + at + q * 32;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              if (q * 32 + g * 16 >= cols) break;
+              float x[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(v[g * 16 + i]);
+              if (add) {
+                float old[8];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  unpack_bf16x8(old, reinterpret_cast<const uint4*>(out + g * 16)[h]);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) x[h * 8 + i] += old[i];
+                }
+              }
+              uint32_t w[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+              if (p.wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + g * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                             "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                             : "memory");
+              } else {
+                reinterpret_cast<uint4*>(out + g * 16)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4*>(out + g * 16)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---- host ----------------------------------------------------------------------
+
+int device_pairs(int* out) {
+  constexpr int kMaxDevices = 64;
+  static int pairs[kMaxDevices] = {};
+  static std::mutex mu;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return record_cuda_error(e);
+  if (dev < 0 || dev >= kMaxDevices) return COMPASS_ERR_UNSUPPORTED;
+  std::lock_guard<std::mutex> lock(mu);
+  if (pairs[dev] == 0) {
+    e = cudaFuncSetAttribute(weight_grad_kernel<E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(weight_grad_kernel<E5M2>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(sms / 2 * 2));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, weight_grad_kernel<E4M3>, &cfg);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    if (n < 1) return COMPASS_ERR_UNSUPPORTED;
+    pairs[dev] = n;
+  }
+  *out = pairs[dev];
+  return COMPASS_OK;
+}
+
+}  // namespace
+
+}  // namespace compass
+
+using namespace compass;
+
+extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype, int accumulate, const void* const* G, const void* const* X,
+                                        const void* const* X_scale, void* const* dW, void* ws, size_t ws_bytes, void* stream) {
+  if (g == nullptr) return COMPASS_ERR_INVALID_ARG;
+  int st = check_problem_8bit(g);
+  if (st == COMPASS_OK) st = check_dtype(grad_dtype, true);
+  if (st != COMPASS_OK) return st;
+  if (g->b_layout != COMPASS_B_NK) return COMPASS_ERR_UNSUPPORTED;
+  if (g->N % 8 != 0) return COMPASS_ERR_ALIGNMENT;
+  if (!G || !X || !X_scale || !dW) return COMPASS_ERR_INVALID_ARG;
+  for (int r = 0; r < g->P; ++r)
+    if (!G[r] || !X[r] || !X_scale[r] || !dW[r]) return COMPASS_ERR_INVALID_ARG;
+  for (int r = 0; r < g->P; ++r)
+    if (!is_aligned(G[r], 16) || !is_aligned(X[r], 16) || !is_aligned(dW[r], 16)) return COMPASS_ERR_ALIGNMENT;
+  st = check_workspace(ws, ws_bytes, COMPASS_STATUS_BYTES);
+  if (st != COMPASS_OK) return st;
+  const int64_t row_tiles = ceil_div(g->N, 256), col_tiles = ceil_div(g->K, 256);
+  if (row_tiles * col_tiles * g->P > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  int pairs = 0;
+  st = device_pairs(&pairs);
+  if (st != COMPASS_OK) return st;
+  GradParams p = {};
+  p.ag = g->op == COMPASS_OP_AG_GEMM;
+  p.P = g->P;
+  p.m = int32_t(g->M / g->P);
+  p.N = g->N;
+  p.K = g->K;
+  p.blocks = int32_t(scale_blocks(g->K));
+  p.stages = int32_t(ceil_div(p.m, kRows));
+  p.row_tiles = int32_t(row_tiles);
+  p.col_tiles = int32_t(col_tiles);
+  p.total = int32_t(row_tiles * col_tiles * g->P);
+  p.accumulate = accumulate != 0;
+  p.fp32 = grad_dtype == COMPASS_DTYPE_FP32;
+  p.wide = 1;
+  p.status = static_cast<StatusBlock*>(ws);
+  p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
+  bool ok = true;
+  for (int r = 0; r < g->P; ++r) {
+    p.sx[r] = static_cast<const uint8_t*>(X_scale[r]);
+    p.dw[r] = dW[r];
+    if (!is_aligned(dW[r], 32)) p.wide = 0;
+    ok = ok && encode_tensor_map_slabs(&p.g[r], G[r], p.ag ? g->P : 1, p.m, g->N, 2, kRows);
+    ok = ok && encode_tensor_map_slabs(&p.x[r], X[r], p.ag ? 1 : g->P, p.m, g->K, 1, kRows);
+  }
+  if (!ok) return record_cuda_error(cudaErrorUnknown);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(2 * (p.total < pairs ? p.total : pairs)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = format_of(g->dtype) == E4M3 ? cudaLaunchKernelEx(&cfg, weight_grad_kernel<E4M3>, p) : cudaLaunchKernelEx(&cfg, weight_grad_kernel<E5M2>, p);
+  count_kernel_launch();
+  return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
+}

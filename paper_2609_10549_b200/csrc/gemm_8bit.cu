@@ -43,6 +43,7 @@ struct Gemm8Params {
   int32_t kn;              // weights are [K][N]
   int32_t n_blocks;        // scales along N
   int32_t a_format;
+  int32_t whole_words;     // rows of the activations' scales are whole aligned words of four
   int32_t wide;            // output rows: 2: whole 32-byte sectors, 1: whole 16-byte vectors, 0: neither
   uint32_t wait_limit_us;
   // pair kernel
@@ -51,7 +52,8 @@ struct Gemm8Params {
   int32_t col_tiles, bn;   // tiles of bn columns
   int32_t total;
   // few-rows kernel
-  int32_t slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
+  FastDiv slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
+  FastDiv each;            // rows per shard
   int32_t cols;            // accumulator columns, a multiple of 16
   int32_t n_tiles;         // 128-row tiles of one rank's weights
   int32_t splits;          // CTAs of a cluster, which share a tile's contraction
@@ -59,19 +61,33 @@ struct Gemm8Params {
   int32_t tmem_cols;
 };
 
-// Scales of `count` (1..4) consecutive blocks as one word, the others 1.
-__device__ __forceinline__ uint32_t scales_word(const uint8_t* p, int count, int64_t step) {
-  if (count == 4 && step == 1 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t*>(p);
-  uint32_t w = kOne;
+// The scales of a row's `count` (1..4) blocks from `p` on, as they are loaded: a word where rows are whole aligned words (`words`,
+// the same for a warp), else bytes (past the last one that again: not used).  Nothing is done with them before word() is called, and
+// no lane leaves a load out, so that all of a group's loads are in flight together: waiting for each in turn, the scales took longer
+// than the products (4096 x 4736, contraction 4224 instead of 4096: 1.50 and 1.80 PFLOP/s).
+struct RowScales {
+  uint32_t b[4];
+  __device__ __forceinline__ void load(const uint8_t* p, int count, bool words) {
+    if (words) {
+      b[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < count) w = (w & ~(0xFFu << (8 * i))) | uint32_t(p[i * step]) << (8 * i);
-  return w;
+      for (int i = 0; i < 4; ++i) b[i] = p[min(i, count - 1)];
+    }
+  }
+  __device__ __forceinline__ uint32_t word(bool words) const { return words ? b[0] : b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24; }
+};
+// The weights' scales of 8 blocks along N from `j` on, for `count` blocks of the contraction from atom `a` on: a byte a lane, and
+// the word of block j + k from lanes 4 k on.
+__device__ __forceinline__ uint32_t weight_byte(const Gemm8Params& p, int rank, int64_t j, int a, int count, int lane) {
+  const int64_t n = min(j + (lane >> 2), int64_t(p.n_blocks - 1));
+  const int at = a + min(lane & 3, count - 1);
+  return p.sb[rank][p.kn ? int64_t(at) * p.n_blocks + n : n * p.atoms + at];
 }
-// The weights' scales of block `j` along N, from atom `a` on.
-__device__ __forceinline__ uint32_t weight_word(const Gemm8Params& p, int rank, int64_t j, int a, int count) {
-  if (j >= p.n_blocks) return kOne;
-  return p.kn ? scales_word(p.sb[rank] + int64_t(a) * p.n_blocks + j, count, p.n_blocks) : scales_word(p.sb[rank] + j * p.atoms + a, count, 1);
+__device__ __forceinline__ uint32_t weight_words(uint32_t byte, int lane) {
+  uint32_t w = byte << (8 * (lane & 3));
+  w |= __shfl_xor_sync(0xffffffffu, w, 1);
+  return w | __shfl_xor_sync(0xffffffffu, w, 2);
 }
 // MMAs (32 elements each) in atom `a` of a slice.
 __device__ __forceinline__ int steps_of(const Gemm8Params& p, int a) { return min(4, (p.K - a * kAtom + 31) / 32); }
@@ -282,38 +298,61 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
     }
   } else if (warp == 10) {
     // ------------------------------------------------------------------ scales
-    // A word of four blocks' scales per row; those of the next group are on their way while this one's buffer is waited for.
+    // A word of four blocks' scales per row; the loads of the next group are in flight while this one's buffer is waited for.
+    struct Group {
+      RowScales a[4];
+      uint32_t b;
+      int64_t col0;
+    };
+    struct Cursor {
+      int t, seg, a;
+    };
+    PairTile c = {};
+    auto load = [&](const Cursor& at, Group& x) {
+      if (at.t >= p.total) return;
+      if (at.seg == 0 && at.a == 0) c = pair_tile(p, at.t, cta);
+      const int q = slice_of(p, c, at.seg), n = min(kGroupAtoms, p.atoms - at.a);
+      const uint8_t* sa = p.sa[q] + int64_t(slice_row(p, c)) * p.atoms + at.a;
+      const int last = max(c.rows - 1, 0);      // (the scales of rows that do not exist do not matter)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x.a[i].load(sa + int64_t(min(i * 32 + lane, last)) * p.atoms, n, p.whole_words);
+      x.b = weight_byte(p, p.rs ? q : c.rank, c.col0 >> 7, at.a, n, lane);
+      x.col0 = c.col0;
+    };
     uint32_t g = 0;
     bool ok = true;
-    for (int t = unit; ok && t < p.total; t += units) {
-      const PairTile c = pair_tile(p, t, cta);
-      const int row = slice_row(p, c);
-      for (int seg = 0; ok && seg < segs; ++seg) {
-        const int q = slice_of(p, c, seg), br = p.rs ? q : c.rank;
-        const uint8_t* sa = p.sa[q] + int64_t(row) * p.atoms;
-        for (int a = 0; a < p.atoms; a += kGroupAtoms, ++g) {
-          const int n = min(kGroupAtoms, p.atoms - a);
-          uint32_t w[4], v[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = i * 32 + lane < c.rows ? scales_word(sa + int64_t(i * 32 + lane) * p.atoms + a, n, 1) : kOne;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int64_t b = (c.col0 + 32 * i) >> 7;
-            v[i] = i > 0 && b == (c.col0 + 32 * (i - 1)) >> 7 ? v[i > 0 ? i - 1 : 0] : 32 * i < c.n ? weight_word(p, br, b, a, n) : kOne;
-          }
-          const uint32_t buf = g & 1u;
-          if (g >= 2) {
-            ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((g >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
-            if (!ok) break;
-          }
-          sh->scales[buf][0][lane] = make_uint4(w[0], w[1], w[2], w[3]);
-          sh->scales[buf][1][lane] = make_uint4(v[0], v[1], v[2], v[3]);
-          sh->scales[buf][2][lane] = make_uint4(v[4], v[5], v[6], v[7]);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+    Cursor at{unit, 0, 0};
+    Group x, next;
+    load(at, x);
+    for (; at.t < p.total; ++g) {
+      const int t = at.t;
+      at.a += kGroupAtoms;
+      if (at.a >= p.atoms) {
+        at.a = 0;
+        if (++at.seg == segs) {
+          at.seg = 0;
+          at.t += units;
         }
       }
+      load(at, next);
+      uint32_t a[4], b[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = x.a[i].word(p.whole_words);
+      const uint32_t w = weight_words(x.b, lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = __shfl_sync(0xffffffffu, w, 4 * int(((x.col0 + 32 * i + lane) >> 7) - (x.col0 >> 7)));
+      const uint32_t buf = g & 1u;
+      if (g >= 2) {
+        ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((g >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
+        if (!ok) break;
+      }
+      sh->scales[buf][0][lane] = make_uint4(a[0], a[1], a[2], a[3]);
+      sh->scales[buf][1][lane] = make_uint4(b[0], b[1], b[2], b[3]);
+      sh->scales[buf][2][lane] = make_uint4(b[4], b[5], b[6], b[7]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+      x = next;
     }
     // leave only when the last groups' signals have come
     for (uint32_t i = g < 2u ? g : 2u; ok && i > 0; --i)
@@ -407,7 +446,10 @@ constexpr int kFewMostCols = 256;
 constexpr int kFewMostStages = 12;
 constexpr int kFewRoom = 200 * 1024;          // of stages, with one CTA per SM
 constexpr int kFewHalfRoom = 96 * 1024;       // with two
+constexpr int kMostSplits = 8;
+constexpr int kSplitCost = 3;
 constexpr size_t kFewAlone = 116 * 1024;      // shared memory that keeps other kernels with as much off the SM
+constexpr size_t kFewTwo = 78 * 1024;         // that lets two such CTAs share it, each with half of tensor memory
 struct FewControl {
   uint64_t full[kFewMostStages], empty[kFewMostStages];
   uint64_t scales_full[2], scales_empty[2];
@@ -468,7 +510,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     if (lane == 0) {
       const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
       const int shards = p.rs ? 1 : p.P;
-      const uint32_t bytes = uint32_t(kChunkBytes + shards * p.slot * kAtom);
+      const uint32_t bytes = uint32_t(kChunkBytes + (p.rs ? p.P : shards) * p.m * kAtom);
       int j = 0;
       for (int g = from; g < to; ++g, ++j) {
         const int slot = j % stages, seg = g / p.atoms, a = g - seg * p.atoms;
@@ -479,7 +521,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         if (p.kn) tma_load_2d_hint(dst, w, &ctl->full[slot], int(n0), a * kAtom, pol);
         else tma_load_2d_hint(dst, w, &ctl->full[slot], a * kAtom, int(n0), pol);
         for (int s = 0; s < shards; ++s)
-          tma_load_2d_hint(dst + kChunkBytes + s * p.slot * kAtom, &p.a[p.rs ? seg : s], &ctl->full[slot], a * kAtom, 0, pol);
+          tma_load_2d_hint(dst + kChunkBytes + s * p.slot.d * kAtom, &p.a[p.rs ? seg : s], &ctl->full[slot], a * kAtom, 0, pol);
       }
       // leave only when everything that was loaded has landed and been read
       for (int i = max(0, j - stages); i < j; ++i)
@@ -532,23 +574,40 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       }
     }
   } else if (warp == 2) {
-    uint32_t group = 0;
-    int n = 0;
-    bool ok = true;
-    for (int g = from; g < to; g += n, ++group) {
-      const int seg = g / p.atoms, a = g - seg * p.atoms;
-      n = min(min(kGroupAtoms, p.atoms - a), to - g);
-      uint32_t w[8];
-      const uint32_t v = weight_word(p, p.rs ? seg : rank, n0 >> 7, a, n);
+    struct Group {
+      RowScales x[8];
+      uint32_t w;
+      bool words;
+    };
+    // the row of activations of column `i * 32 + lane`, in its tensor
+    int tensor[8], row[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int col = i * 32 + lane;
-        w[i] = kOne;
-        if (i * 32 < p.cols) {
-          const int s = p.rs ? 0 : col / p.slot, row = col - s * p.slot;
-          if (s < p.P && row < (p.rs ? p.m * p.P : p.m)) w[i] = scales_word(p.sa[p.rs ? seg : s] + int64_t(row) * p.atoms + a, n, 1);
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int col = i * 32 + lane, s = int(p.slot.div(uint32_t(col)));
+      tensor[i] = min(s, p.rs ? 0 : p.P - 1);
+      row[i] = min(col - s * int(p.slot.d), (p.rs ? p.m * p.P : p.m) - 1);      // (columns without one: any scale)
+    }
+    auto count = [&](int g) { return min(min(kGroupAtoms, p.atoms - g % p.atoms), to - g); };
+    auto load = [&](int g, Group& x) {
+      if (g >= to) return;
+      const int seg = g / p.atoms, a = g - seg * p.atoms, n = count(g);
+      x.words = p.whole_words && n == 4 && (a & 3) == 0;
+      x.w = weight_byte(p, p.rs ? seg : rank, n0 >> 7, a, n, lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i * 32 < p.cols) x.x[i].load(p.sa[p.rs ? seg : tensor[i]] + int64_t(row[i]) * p.atoms + a, n, x.words);
+    };
+    uint32_t group = 0;
+    bool ok = true;
+    Group x, next;
+    load(from, x);
+    for (int g = from; g < to; ++group) {
+      g += count(g);
+      load(g, next);
+      const uint32_t v = __shfl_sync(0xffffffffu, weight_words(x.w, lane), 0);
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = i * 32 < p.cols ? x.x[i].word(x.words) : kOne;
       const uint32_t buf = group & 1u;
       if (group >= 2) {
         ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
@@ -560,6 +619,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl->scales_full[buf]);
+      x = next;
     }
     for (uint32_t i = group < 2u ? group : 2u; ok && i > 0; --i)
       ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[(group - i) & 1u], ((group - i) >> 1) & 1u, wc, SITE_DRAIN, -1));
@@ -568,14 +628,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   // The sums: lanes are weight rows, columns are activation rows.
   const int M = p.m * p.P;
   const int quarter = warp & 3;
-  auto column_of = [&](int i) {      // accumulator column of activation row i
-    const int s = p.rs ? 0 : i / p.m;
-    return p.rs ? i : s * p.slot + (i - s * p.m);
+  // row i of all ranks' activations: its shard, the row in it
+  auto shard_of = [&](int i, int* row) {
+    const int s = int(p.each.div(uint32_t(i)));
+    *row = i - s * p.m;
+    return s;
   };
-  auto store = [&](int i, int n, float x) {
+  auto store = [&](int i, int s, int row, int n, float x) {
     if (n0 + n >= p.N) return;
-    const int chunk = i / p.m;
-    __nv_bfloat16* out = p.rs ? p.out[chunk] + int64_t(i - chunk * p.m) * p.N : p.out[rank] + int64_t(i) * p.N;
+    __nv_bfloat16* out = p.rs ? p.out[s] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N;
     out[n0 + n] = __float2bfloat16_rn(x);
   };
   bool ok = true;
@@ -594,8 +655,16 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int col = c + i, s = p.rs ? 0 : col / p.slot, row = col - s * p.slot;
-            if (p.rs ? col < M : s < p.P && row < p.m) store(p.rs ? col : s * p.m + row, quarter * 32 + lane, __uint_as_float(v[i]));
+            const int col = c + i;
+            int row;
+            if (p.rs) {
+              const int s = shard_of(col, &row);
+              if (col < M) store(col, s, row, quarter * 32 + lane, __uint_as_float(v[i]));
+            } else {
+              const int s = int(p.slot.div(uint32_t(col)));
+              row = col - s * int(p.slot.d);
+              if (s < p.P && row < p.m) store(s * p.m + row, s, row, quarter * 32 + lane, __uint_as_float(v[i]));
+            }
           }
         }
       }
@@ -606,17 +675,33 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     cluster_arrive();
     cluster_wait();
     if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
+      // four neighbouring sums a thread, those of all CTAs in flight together
       const uint32_t base = smem_u32(sums);
-      const int n = int(threadIdx.x) & 127;
-      for (int i = part + p.splits * (int(threadIdx.x) >> 7); i < M; i += 2 * p.splits) {
-        const uint32_t at = base + uint32_t(column_of(i) * 128 + n) * 4;
-        float x = 0.f;
-        for (int s = 0; s < p.splits; ++s) {
-          float y;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(map_to_cta(at, uint32_t(s))) : "memory");
-          x += y;
+      const int n = lane * 4;
+      for (int i = part + p.splits * warp; i < M; i += p.splits * (kFewThreads / 32)) {
+        int row;
+        const int shard = shard_of(i, &row);
+        const uint32_t at = base + uint32_t((p.rs ? i : shard * int(p.slot.d) + row) * 128 + n) * 4;
+        float4 y[kMostSplits];
+#pragma unroll
+        for (int s = 0; s < kMostSplits; ++s)
+          if (s < p.splits)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w)
+                         : "r"(map_to_cta(at, uint32_t(s))));
+        float4 x = y[0];
+#pragma unroll
+        for (int s = 1; s < kMostSplits; ++s)
+          if (s < p.splits) x.x += y[s].x, x.y += y[s].y, x.z += y[s].z, x.w += y[s].w;
+        __nv_bfloat16* out = (p.rs ? p.out[shard] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N) + n0 + n;
+        if (p.wide) {      // (N is a multiple of 8)
+          if (n0 + n < p.N) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+        } else {
+          const float z[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (n0 + n + k < p.N) out[k] = __float2bfloat16_rn(z[k]);
         }
-        store(i, n, x);
       }
     }
     cluster_arrive();      // nobody's memory goes while it is read
@@ -728,6 +813,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   p.a_format = format_of(g->dtype);
   p.status = static_cast<StatusBlock*>(ws);
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
+  p.whole_words = 1;
   p.wide = g->N % 16 == 0 ? 2 : g->N % 8 == 0 ? 1 : 0;
   for (int r = 0; r < g->P; ++r) {
     p.sa[r] = static_cast<const uint8_t*>(sA[r]);
@@ -735,6 +821,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     p.out[r] = static_cast<__nv_bfloat16*>(out[r]);
     if (p.wide == 2 && !is_aligned(out[r], 32)) p.wide = 1;
     if (!is_aligned(out[r], 16)) p.wide = 0;
+    if (p.atoms % 4 != 0 || !is_aligned(sA[r], 4)) p.whole_words = 0;
   }
   const int64_t a_rows = p.rs ? g->M : p.m;
   const int64_t b_rows = p.kn ? g->K : g->N, b_cols = p.kn ? g->N : g->K;
@@ -742,13 +829,23 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   const int64_t slot = int64_t(round_up(size_t(a_rows), 8)), cols = int64_t(round_up(size_t(p.rs ? slot : slot * g->P), 16));
   bool ok = true;
   if (cols <= kFewMostCols) {
-    p.slot = int32_t(slot);
+    p.slot.set(uint32_t(slot));
+    p.each.set(uint32_t(p.m));
     p.cols = int32_t(cols);
     p.n_tiles = int32_t(scale_blocks(g->N));
     const int64_t tiles = int64_t(p.n_tiles) * (p.rs ? 1 : g->P);
     const int all = (p.rs ? g->P : 1) * p.atoms;
+    // The contraction is split so that the SMs' rounds of it are shortest, in atoms; a split costs about as much as kSplitCost of them
+    // (two barriers of the cluster, and the sums).
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= f->sms && all >= 4 * p.splits) p.splits *= 2;
+    int64_t best = ceil_div(tiles, f->sms) * all;
+    for (int s = 2; s <= kMostSplits && 2 * s <= all; ++s) {
+      const int64_t cost = ceil_div(tiles * s, f->sms) * ceil_div(all, s) + kSplitCost;
+      if (tiles * s <= (cols <= 128 ? 2 : 1) * f->sms && cost < best) {
+        best = cost;
+        p.splits = s;
+      }
+    }
     const int stage = few_stage_bytes(p.cols);
     const int64_t mine = ceil_div(all, p.splits);
     const int room = tiles * p.splits > f->sms && cols <= 128 ? kFewHalfRoom : kFewRoom;
@@ -761,15 +858,19 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     p.tmem_cols = 32;
     while (p.tmem_cols < p.cols + 24) p.tmem_cols *= 2;
     for (int r = 0; r < g->P; ++r) {
-      ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, p.slot);
+      // (boxes of the rows that there are: rows outside a matrix of a few made its loads several times as long)
+      ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, int(a_rows));
       ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, 128);
     }
     if (!ok) return record_cuda_error(cudaErrorUnknown);
-    // The CTAs of a cluster wait for one another while they hold tensor memory: none may share its SM with another cluster that
-    // does, each waiting for what the other holds (kernels of other streams included).  More than half of the shared memory, as
-    // all kernels of this library have that wait so, keeps them apart.
+    // The CTAs of a cluster wait for one another while they hold tensor memory, so no two clusters may each wait for what the other
+    // holds (kernels of other streams included).  Shared memory keeps them apart: one CTA an SM with more than half of it, or two
+    // that have half of tensor memory each; the library's other kernels that wait so take more than either leaves.
     size_t smem = few_smem_bytes(p.cols, p.stages);
-    if (p.splits > 1 && smem < kFewAlone) smem = kFewAlone;
+    if (p.splits > 1) {
+      const size_t least = room == kFewHalfRoom ? kFewTwo : kFewAlone;
+      if (smem < least) smem = least;
+    }
     return launch_clusters(gemm8_few_kernel, tiles * p.splits, kFewThreads, smem, p.splits, p, s);
   }
   p.frags = int32_t(ceil_div(p.m, 128));

@@ -5,8 +5,8 @@
 // exactly, and the products are BF16 ones with FP32 sums.  The activations cross HBM and L2 in 8 bits.
 //
 // Pairs of CTAs, 256 rows (n) x 256 columns (k) a tile, 128 rows of the contraction a stage.  Both operands lie across the
-// contraction (MN-major).  Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue, warps 10..13 convert: a
-// thread has a row of a stage, so one scale.  Rows past a rank's last one are zeros of the tensor maps.
+// contraction (MN-major).  Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17 convert: a
+// thread has half a row of a stage, so one scale.  Rows past a rank's last one are zeros of the tensor maps.
 //
 // The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
 // 1024 rows long, and added up in FP32 in the result itself.
@@ -22,9 +22,9 @@ using namespace ptx;
 
 namespace {
 
-constexpr int kThreads = 448;
+constexpr int kThreads = 576;
 constexpr int kEpiWarps = 8;
-constexpr int kConvWarps = 4;
+constexpr int kConvWarps = 8;
 constexpr int kRows = 128;                            // of the contraction in a stage
 constexpr int kGBytes = 128 * kRows * 2;              // this CTA's 128 columns of G: two boxes of 64
 constexpr int kXBytes = 128 * kRows;                  // its 128 columns of X
@@ -56,7 +56,8 @@ struct GradParams {
 struct Control {
   uint64_t g_full[kStages], g_empty[kStages];
   uint64_t x_full[kStages], x_empty[kStages];
-  uint64_t c_full[kConv], c_empty[kConv];
+  uint64_t c_full[kConv], c_empty[kConv];      // of this CTA's converters; of both CTAs
+  uint64_t c_peer[kConv];                      // leader: the other CTA's converters
   uint64_t acc_full[2], acc_empty[2];
   uint64_t drain;
   uint32_t tmem_base;
@@ -84,20 +85,44 @@ __device__ __forceinline__ Tile tile_of(const GradParams& p, int t) {
   return c;
 }
 
-// 16 values of 8 bits times a scale, in BF16.
+// 16 values of 8 bits times a scale, in BF16 (`scale`: two of it).  The bits of an 8-bit number, its exponent moved to where BF16
+// has its own, are that number times 2^-120 (E5M2: 2^-112), subnormal ones too; the two factors are powers of two, so nothing is
+// rounded above BF16's subnormal range.  By the conversion instructions, of which an SM does 16 a clock, this took three quarters
+// of the kernel's time.  (Those are still used where a NaN is among the 16.)
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 template <int kFormat>
-__device__ __forceinline__ void convert16(const uint4& w, F2 scale, uint4& lo, uint4& hi) {
+__device__ __forceinline__ void convert16(const uint4& w, uint32_t scale, uint4& lo, uint4& hi) {
+  constexpr int kShift = kFormat == E4M3 ? 4 : 3;
+  constexpr uint32_t kMask = (0x7F00u >> kShift) * 0x10001u;
+  constexpr uint32_t kBias = kFormat == E4M3 ? 0x7B807B80u : 0x77807780u;       // 2^120, 2^112
+  constexpr uint32_t kNan = kFormat == E4M3 ? 0x01010101u : 0x04040404u;        // what makes bit 7 of a NaN's size
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-  uint32_t o[8];
+  uint32_t o[8], nan = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 x = unpack8x2<kFormat>(v[i >> 1] >> (16 * (i & 1)));
-    const float2 y = of(f2(x.x, x.y) * scale);
-    o[i] = pack_bf16x2(y.x, y.y);
+  for (int i = 0; i < 4; ++i) {
+    nan |= (v[i] & 0x7F7F7F7Fu) + kNan;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t r = __byte_perm(v[i], 0, h ? 0x3424 : 0x1404);             // two numbers, each in the upper byte of a half
+      o[2 * i + h] = mul_bf16x2(mul_bf16x2((r & 0x80008000u) | ((r >> kShift) & kMask), kBias), scale);
+    }
+  }
+  if (nan & 0x80808080u) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 x = unpack8x2<kFormat>(v[i >> 1] >> (16 * (i & 1)));
+      o[i] = mul_bf16x2(pack_bf16x2(x.x, x.y), scale);
+    }
   }
   lo = make_uint4(o[0], o[1], o[2], o[3]);
   hi = make_uint4(o[4], o[5], o[6], o[7]);
 }
+// 2^(b - 127) in BF16, twice; 255 is NaN.
+__device__ __forceinline__ uint32_t scale_bf16x2(uint32_t b) { return (b == 0 ? 0x0040u : b == 255 ? 0x7FC0u : b << 7) * 0x10001u; }
 
 template <int kFormat>
 __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ GradParams p) {
@@ -120,7 +145,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       mbar_init(&ctl->x_empty[s], kConvWarps);
     }
     for (int b = 0; b < kConv; ++b) {
-      mbar_init(&ctl->c_full[b], 2 * kConvWarps);
+      mbar_init(&ctl->c_full[b], kConvWarps);
+      mbar_init(&ctl->c_peer[b], 1);
       mbar_init(&ctl->c_empty[b], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -200,7 +226,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           for (bool first = true; a < to; ++a, ++j, first = false) {
             const uint32_t slot = j % kStages, conv = j % kConv;
             if (!(ok = wait_phase(&ctl->g_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t) &&
-                       wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t)))
+                       wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t) &&
+                       wait_phase(&ctl->c_peer[conv], (j / kConv) & 1u, wc, SITE_FULL, t)))
               break;
             tc_fence_after_sync();
             // a step of 16 rows of the contraction is two groups of 8 (2048 bytes)
@@ -218,10 +245,21 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         umma_commit_pair(&ctl->drain, 0x1);
         wait_settled(&ctl->drain, 0);
       }
+    } else if (!leader && lane == 0) {
+      // Passes on to the leader that this CTA's converters are done.  (An arrival at the other CTA's barrier releases what came before,
+      // and waits for it to land, about 1000 cycles: by the converters themselves it was a third of a stage's time.)
+      uint32_t j = 0;
+      bool ok = true;
+      for (int t = unit; ok && t < p.total; t += units)
+        for (int a = 0; a < all; ++a, ++j) {
+          const uint32_t conv = j % kConv;
+          if (!(ok = wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t))) break;
+          mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->c_peer[conv]), 0));
+        }
     }
   } else if (warp >= 2 + kEpiWarps) {
     // ------------------------------------------------------------- 8 bits -> BF16
-    const int row = (warp - 2 - kEpiWarps) * 32 + lane;
+    const int w = warp - 2 - kEpiWarps, row = (w & 3) * 32 + lane, side = w >> 2;      // 64 columns of a row
     uint32_t j = 0;
     bool ok = true;
     for (int t = unit; ok && t < p.total; t += units) {
@@ -236,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       };
       uint32_t next = scale_at(0);
       for (int a = 0; a < all; ++a, ++j) {
-        const F2 scale = f2(scale_value(next));
+        const uint32_t scale = scale_bf16x2(next);
         next = scale_at(a + 1);
         const uint32_t slot = j % kStages, conv = j % kConv;
         ok = wait_phase(&ctl->x_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t);
@@ -244,22 +282,23 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint8_t* from = smem + kXAt + slot * kXBytes + row * 128;
-        uint8_t* to = smem + kCAt + conv * kCBytes + row * 128;
+        uint8_t* to = smem + kCAt + conv * kCBytes + side * kChunk + row * 128;
         const int swizzle = row & 7;
+        uint4 in[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < 4; ++u) in[u] = *reinterpret_cast<const uint4*>(from + (((side * 4 + u) ^ swizzle) << 4));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
           uint4 lo, hi;
-          convert16<kFormat>(*reinterpret_cast<const uint4*>(from + ((u ^ swizzle) << 4)), scale, lo, hi);
-          uint8_t* chunk = to + (u >> 2) * kChunk;
-          const int at = 2 * (u & 3);
-          *reinterpret_cast<uint4*>(chunk + ((at ^ swizzle) << 4)) = lo;
-          *reinterpret_cast<uint4*>(chunk + (((at + 1) ^ swizzle) << 4)) = hi;
+          convert16<kFormat>(in[u], scale, lo, hi);
+          *reinterpret_cast<uint4*>(to + ((2 * u ^ swizzle) << 4)) = lo;
+          *reinterpret_cast<uint4*>(to + (((2 * u + 1) ^ swizzle) << 4)) = hi;
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl->x_empty[slot]);
-          mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->c_full[conv]), 0));
+          mbar_arrive(&ctl->c_full[conv]);
         }
       }
     }
@@ -296,16 +335,23 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           if (n >= p.N || q * 32 >= cols) continue;
           if (p.fp32) {
             float* out = static_cast<float*>(p.dw[c.rank]) + at + q * 32;
+            if (add) {
+              // (all loads before the first store: each waiting for the last, the kernel took twice as long)
+              float4 old[8];
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-              if (q * 32 + g * 4 >= cols) break;
-              float4 x = make_float4(__uint_as_float(v[4 * g]), __uint_as_float(v[4 * g + 1]), __uint_as_float(v[4 * g + 2]), __uint_as_float(v[4 * g + 3]));
-              if (add) {
-                const float4 old = reinterpret_cast<const float4*>(out)[g];
-                x.x += old.x, x.y += old.y, x.z += old.z, x.w += old.w;
+              for (int g = 0; g < 8; ++g)
+                if (q * 32 + g * 4 < cols) old[g] = reinterpret_cast<const float4*>(out)[g];
+#pragma unroll
+              for (int g = 0; g < 8; ++g) {
+                v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) + old[g].x);
+                v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) + old[g].y);
+                v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) + old[g].z);
+                v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) + old[g].w);
               }
-              reinterpret_cast<float4*>(out)[g] = x;
             }
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+              if (q * 32 + g * 4 < cols) reinterpret_cast<uint4*>(out)[g] = make_uint4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
           } else {
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dw[c.rank]) + at + q * 32;
 #pragma unroll

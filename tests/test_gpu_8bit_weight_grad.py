@@ -77,3 +77,25 @@ def test_long_sums_keep_fp32_precision():
     d, x = inputs(AG, 1, M, N, K, api.DTYPE_E4M3, 3)
     o, e = run(AG, 1, M, N, K, api.DTYPE_E4M3, d, x, api.DTYPE_FP32)[0], exact(AG, 1, d, x)[0]
     assert (o.double() - e).norm() / e.norm() < 1.5e-6
+
+
+@pytest.mark.parametrize("format", [api.DTYPE_E4M3, api.DTYPE_E5M2])
+def test_every_8_bit_number_and_scale(format):
+    """One row each: dW is that row of activations times a gradient of one, in FP32, so every number of 8 bits times every scale comes
+    through as BF16 holds it (E5M2's infinities, which the conversion to 8 bits never makes, count as numbers that are not)."""
+    bits = torch.arange(256, device="cuda", dtype=torch.uint8).view(1, 256)
+    kind = torch.float8_e4m3fn if format == api.DTYPE_E4M3 else torch.float8_e5m2
+    for first in (0, 1, 100, 120, 127, 134, 200, 230, 254):
+        scales = torch.tensor([[first, min(254, first + 7)]], dtype=torch.uint8, device="cuda")
+        x = bits.view(kind), scales.view(torch.float8_e8m0fnu)
+        d = torch.ones(1, 8, device="cuda", dtype=torch.bfloat16)
+        got = run(AG, 1, 1, 8, 256, format, [d], [x], api.DTYPE_FP32)[0]
+        want = values(*x).float().bfloat16().float().expand(8, 256)
+        finite = torch.isfinite(x[0].float()).expand(8, 256)
+        # (a subnormal operand of the tensor core may count as zero)
+        small = want.abs() < torch.finfo(torch.bfloat16).tiny
+        assert torch.equal(got[finite & ~small], want[finite & ~small])
+        assert ((got - want)[finite & small].abs() <= torch.finfo(torch.bfloat16).tiny).all()
+        assert got[x[0].float().isnan().expand(8, 256)].isnan().all()
+    x = bits[:1, :128].contiguous().view(kind), torch.tensor([[255]], dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    assert run(AG, 1, 1, 8, 128, format, [d], [x], api.DTYPE_FP32)[0].isnan().all()

@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
       sh->scales[buf][2][lane] = make_uint4(b[4], b[5], b[6], b[7]);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+      if (lane == 0) mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
       x = next;
     }
     // leave only when the last groups' signals have come

@@ -191,6 +191,12 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// The same behind fence.proxy.async, for an arrival that hands over this CTA's own shared memory to the pair's MMAs: when the fence
+// is over, the writes before it are there for the tensor cores of both CTAs, so nothing is left for a release to the cluster to wait
+// for, which takes 1000 cycles and more all the same.
+__device__ __forceinline__ void mbar_arrive_cluster_fenced(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // TMA load into this CTA's shared memory whose completion is counted on an
 // mbarrier of either CTA of the pair (`bar_cluster_addr`, shared::cluster).
 __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int32_t x,

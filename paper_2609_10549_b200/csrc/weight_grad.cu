@@ -4,9 +4,10 @@
 // for 32 elements of the contraction): the 8-bit tile is turned into BF16 in shared memory, which holds scale times value
 // exactly, and the products are BF16 ones with FP32 sums.  The activations cross HBM and L2 in 8 bits.
 //
-// Pairs of CTAs, 256 rows (n) x 256 columns (k) a tile, 128 rows of the contraction a stage.  Both operands lie across the
-// contraction (MN-major).  Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17 convert: a
-// thread has half a row of a stage, so one scale.  Rows past a rank's last one are zeros of the tensor maps.
+// Pairs of CTAs, 256 rows (n) x 256 columns (k) a tile, 64 rows of the contraction a stage.  Both operands lie across the
+// contraction (MN-major).  Warp 0 loads G (TMA), warp 18 X, warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17
+// convert: two groups, which take the stages in turn; a thread has half a row of a stage, so one scale.  Rows past a rank's last one
+// are zeros of the tensor maps.
 //
 // The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
 // 1024 rows long, and added up in FP32 in the result itself.
@@ -22,17 +23,18 @@ using namespace ptx;
 
 namespace {
 
-constexpr int kThreads = 576;
+constexpr int kThreads = 608;
 constexpr int kEpiWarps = 8;
-constexpr int kConvWarps = 8;
-constexpr int kRows = 128;                            // of the contraction in a stage
+constexpr int kConvWarps = 4;                         // of a group
+constexpr int kGroups = 2;
+constexpr int kRows = 64;                             // of the contraction in a stage
 constexpr int kGBytes = 128 * kRows * 2;              // this CTA's 128 columns of G: two boxes of 64
 constexpr int kXBytes = 128 * kRows;                  // its 128 columns of X
 constexpr int kCBytes = 128 * kRows * 2;              // the same in BF16: two chunks of 64
 constexpr int kChunk = 64 * kRows * 2;
-constexpr int kStages = 3;
-constexpr int kConv = 2;
-constexpr int kRangeStages = 8;                       // of a sum that goes to FP32
+constexpr int kStages = 5;                            // of G and of X in BF16
+constexpr int kXStages = 5;
+constexpr int kRangeStages = 16;                      // of a sum that goes to FP32
 constexpr int kRowGroup = 8;                          // row tiles that go through the columns together
 
 struct GradParams {
@@ -54,16 +56,15 @@ struct GradParams {
 };
 
 struct Control {
-  uint64_t g_full[kStages], g_empty[kStages];
-  uint64_t x_full[kStages], x_empty[kStages];
-  uint64_t c_full[kConv], c_empty[kConv];      // of this CTA's converters; of both CTAs
-  uint64_t c_peer[kConv];                      // leader: the other CTA's converters
+  uint64_t ready[kStages];      // leader's: both CTAs' G has landed and both CTAs' X is converted
+  uint64_t empty[kStages];
+  uint64_t x_full[kXStages], x_empty[kXStages];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t drain;
   uint32_t tmem_base;
   int abort;
 };
-constexpr int kXAt = kStages * kGBytes, kCAt = kXAt + kStages * kXBytes, kControlAt = kCAt + kConv * kCBytes;
+constexpr int kXAt = kStages * kGBytes, kCAt = kXAt + kXStages * kXBytes, kControlAt = kCAt + kStages * kCBytes;
 constexpr size_t kSmemBytes = 1024 + kControlAt + sizeof(Control);
 static_assert(kSmemBytes <= 227 * 1024, "");
 
@@ -85,38 +86,39 @@ __device__ __forceinline__ Tile tile_of(const GradParams& p, int t) {
   return c;
 }
 
-// 16 values of 8 bits times a scale, in BF16 (`scale`: two of it).  The bits of an 8-bit number, its exponent moved to where BF16
-// has its own, are that number times 2^-120 (E5M2: 2^-112), subnormal ones too; the two factors are powers of two, so nothing is
-// rounded above BF16's subnormal range.  By the conversion instructions, of which an SM does 16 a clock, this took three quarters
-// of the kernel's time.  (Those are still used where a NaN is among the 16.)
+// 16 values of 8 bits times a scale, in BF16 (`scale`: two of it), those of each four in the order 0, 2, 1, 3, which the epilogue
+// undoes.  The bits of an 8-bit number, its exponent moved to where BF16 has its own, are that number times 2^-120 (E5M2: 2^-112),
+// subnormal ones too; the factors are powers of two, so nothing is rounded above BF16's subnormal range.  What is not a number in
+// 8 bits has now the size of one past the largest: times kPast it overflows, and infinity times 0 is added.  (By the conversion
+// instructions this took three quarters of the kernel's time; with the NaN looked for among the bits, the integer pipe was full.)
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+template <int kFormat>
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t bits, uint32_t scale) {
+  constexpr uint32_t kBias = kFormat == E4M3 ? 0x7B807B80u : 0x77807780u;       // 2^120, 2^112
+  // E4M3: 448 kPast is finite, 480 kPast is not: 1.109375 * 2^119.  E5M2: 57344 kPast, 65536 kPast: 1.0625 * 2^112.
+  constexpr uint32_t kPast = kFormat == E4M3 ? 0x7B0E7B0Eu : 0x77887788u;
+  const uint32_t y = mul_bf16x2(bits, kBias);
+  return fma_bf16x2(y, scale, mul_bf16x2(mul_bf16x2(y, kPast), 0u));
+}
 template <int kFormat>
 __device__ __forceinline__ void convert16(const uint4& w, uint32_t scale, uint4& lo, uint4& hi) {
   constexpr int kShift = kFormat == E4M3 ? 4 : 3;
   constexpr uint32_t kMask = (0x7F00u >> kShift) * 0x10001u;
-  constexpr uint32_t kBias = kFormat == E4M3 ? 0x7B807B80u : 0x77807780u;       // 2^120, 2^112
-  constexpr uint32_t kNan = kFormat == E4M3 ? 0x01010101u : 0x04040404u;        // what makes bit 7 of a NaN's size
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-  uint32_t o[8], nan = 0;
+  uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    nan |= (v[i] & 0x7F7F7F7Fu) + kNan;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t r = __byte_perm(v[i], 0, h ? 0x3424 : 0x1404);             // two numbers, each in the upper byte of a half
-      o[2 * i + h] = mul_bf16x2(mul_bf16x2((r & 0x80008000u) | ((r >> kShift) & kMask), kBias), scale);
-    }
-  }
-  if (nan & 0x80808080u) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 x = unpack8x2<kFormat>(v[i >> 1] >> (16 * (i & 1)));
-      o[i] = mul_bf16x2(pack_bf16x2(x.x, x.y), scale);
-    }
+    o[2 * i] = scaled_pair<kFormat>(((v[i] << 8) & 0x80008000u) | ((v[i] << (8 - kShift)) & kMask), scale);      // numbers 0 and 2
+    o[2 * i + 1] = scaled_pair<kFormat>((v[i] & 0x80008000u) | ((v[i] >> kShift) & kMask), scale);               // 1 and 3
   }
   lo = make_uint4(o[0], o[1], o[2], o[3]);
   hi = make_uint4(o[4], o[5], o[6], o[7]);
@@ -139,15 +141,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctl->g_full[s], 1);
-      mbar_init(&ctl->g_empty[s], 1);
+      mbar_init(&ctl->ready[s], 2 * kConvWarps + 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int s = 0; s < kXStages; ++s) {
       mbar_init(&ctl->x_full[s], 1);
       mbar_init(&ctl->x_empty[s], kConvWarps);
-    }
-    for (int b = 0; b < kConv; ++b) {
-      mbar_init(&ctl->c_full[b], kConvWarps);
-      mbar_init(&ctl->c_peer[b], 1);
-      mbar_init(&ctl->c_empty[b], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&ctl->acc_full[b], 1);
@@ -170,10 +169,14 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   launch_dependents();
   wait_for_previous_kernel();
 
-  if (warp == 0) {
-    // ------------------------------------------------------------ TMA producer
+  if (warp == 0 || warp == 2 + kEpiWarps + kGroups * kConvWarps) {
+    // ----------------------------------------------------------- TMA producers
     if (lane == 0) {
+      const bool of_g = warp == 0;
       const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+      const uint32_t depth = of_g ? kStages : kXStages;
+      uint64_t* full = of_g ? ctl->ready : ctl->x_full;
+      uint64_t* empty = of_g ? ctl->empty : ctl->x_empty;
       uint32_t j = 0;
       bool ok = true;
       for (int t = unit; ok && t < p.total; t += units) {
@@ -181,29 +184,28 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const int n0 = c.row0 + cta * 128, k0 = c.col0 + cta * 128;
         for (int s = 0; ok && s < p.P; ++s)
           for (int i = 0; i < p.stages; ++i, ++j) {
-            const uint32_t slot = j % kStages;
-            if (j >= kStages) {
-              const uint32_t parity = (j / kStages - 1) & 1u;
-              if (!(ok = wait_phase(&ctl->x_empty[slot], parity, wc, SITE_EMPTY, t) && wait_phase(&ctl->g_empty[slot], parity, wc, SITE_EMPTY, t))) break;
+            const uint32_t slot = j % depth;
+            if (j >= depth && !(ok = wait_phase(&empty[slot], (j / depth - 1) & 1u, wc, SITE_EMPTY, t))) break;
+            if (of_g) {
+              const uint32_t bar = map_to_cta(smem_u32(&full[slot]), 0);
+              if (leader) mbar_arrive_expect_tx(&full[slot], 2 * kGBytes);
+              const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
+              tma_load_3d_pair_hint(smem + slot * kGBytes, g, bar, n0, i * kRows, p.ag ? s : 0, pol);
+              tma_load_3d_pair_hint(smem + slot * kGBytes + kChunk, g, bar, n0 + 64, i * kRows, p.ag ? s : 0, pol);
+            } else {
+              mbar_arrive_expect_tx(&full[slot], kXBytes);
+              tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
             }
-            mbar_arrive_expect_tx(&ctl->x_full[slot], kXBytes);
-            tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &ctl->x_full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
-            const uint32_t bar = map_to_cta(smem_u32(&ctl->g_full[slot]), 0);
-            if (leader) mbar_arrive_expect_tx(&ctl->g_full[slot], 2 * kGBytes);
-            const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
-            tma_load_3d_pair_hint(smem + slot * kGBytes, g, bar, n0, i * kRows, p.ag ? s : 0, pol);
-            tma_load_3d_pair_hint(smem + slot * kGBytes + kChunk, g, bar, n0 + 64, i * kRows, p.ag ? s : 0, pol);
           }
       }
       // leave only when the last stages have been read (the leader's products read both CTAs' memory)
-      const uint32_t back = j < uint32_t(kStages) ? j : uint32_t(kStages);
+      const uint32_t back = j < depth ? j : depth;
       for (uint32_t i = 1; i <= back; ++i) {
-        const uint32_t r = j - i, slot = r % kStages, parity = (r / kStages) & 1u;
-        if (!wait_phase(&ctl->x_empty[slot], parity, wc, SITE_DRAIN, -1) || !wait_phase(&ctl->g_empty[slot], parity, wc, SITE_DRAIN, -1)) {
-          for (uint32_t k = 1; k <= back; ++k) {
-            wait_settled(&ctl->x_full[(j - k) % kStages], ((j - k) / kStages) & 1u);
-            if (leader) wait_settled(&ctl->g_full[(j - k) % kStages], ((j - k) / kStages) & 1u);
-          }
+        const uint32_t r = j - i;
+        if (!wait_phase(&empty[r % depth], (r / depth) & 1u, wc, SITE_DRAIN, -1)) {
+          // (G's copies of both CTAs are counted with the conversions, which may never come: then after the 100 ms)
+          if (!of_g || leader)
+            for (uint32_t k = 1; k <= back; ++k) wait_settled(&full[(j - k) % depth], ((j - k) / depth) & 1u);
           break;
         }
       }
@@ -223,19 +225,22 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           const int to = min(all, a + range);
           if (!(ok = wait_phase(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t))) break;
           tc_fence_after_sync();
-          for (bool first = true; a < to; ++a, ++j, first = false) {
-            const uint32_t slot = j % kStages, conv = j % kConv;
-            if (!(ok = wait_phase(&ctl->g_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t) &&
-                       wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t) &&
-                       wait_phase(&ctl->c_peer[conv], (j / kConv) & 1u, wc, SITE_FULL, t)))
-              break;
+          for (uint32_t first = 0; a < to; ++a, ++j, first = 1) {
+            const uint32_t slot = j % kStages;
+            if (!(ok = wait_phase(&ctl->ready[slot], (j / kStages) & 1u, wc, SITE_FULL, t))) break;
             tc_fence_after_sync();
             // a step of 16 rows of the contraction is two groups of 8 (2048 bytes)
-            const uint64_t da = desc_g + uint64_t((slot * kGBytes) >> 4), db = desc_c + uint64_t((conv * kCBytes) >> 4);
-            const int steps = min(kRows / 16, (p.m - shard_stage * kRows + 15) / 16);
-            for (int k = 0; k < steps; ++k) umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, first && k == 0 ? 0u : 1u);
-            umma_commit_pair(&ctl->g_empty[slot], 0x3);
-            umma_commit_pair(&ctl->c_empty[conv], 0x3);
+            const uint64_t da = desc_g + uint64_t((slot * kGBytes) >> 4), db = desc_c + uint64_t((slot * kCBytes) >> 4);
+            const int rows = p.m - shard_stage * kRows;
+            if (rows >= kRows) {
+#pragma unroll
+              for (int k = 0; k < kRows / 16; ++k)
+                umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
+            } else {
+              for (int k = 0; k < (rows + 15) / 16; ++k)
+                umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
+            }
+            umma_commit_pair(&ctl->empty[slot], 0x3);
             if (++shard_stage == p.stages) shard_stage = 0;
           }
           if (ok) umma_commit_pair(&ctl->acc_full[b], 0x3);
@@ -245,21 +250,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         umma_commit_pair(&ctl->drain, 0x1);
         wait_settled(&ctl->drain, 0);
       }
-    } else if (!leader && lane == 0) {
-      // Passes on to the leader that this CTA's converters are done.  (An arrival at the other CTA's barrier releases what came before,
-      // and waits for it to land, about 1000 cycles: by the converters themselves it was a third of a stage's time.)
-      uint32_t j = 0;
-      bool ok = true;
-      for (int t = unit; ok && t < p.total; t += units)
-        for (int a = 0; a < all; ++a, ++j) {
-          const uint32_t conv = j % kConv;
-          if (!(ok = wait_phase(&ctl->c_full[conv], (j / kConv) & 1u, wc, SITE_FULL, t))) break;
-          mbar_arrive_cluster(map_to_cta(smem_u32(&ctl->c_peer[conv]), 0));
-        }
     }
   } else if (warp >= 2 + kEpiWarps) {
     // ------------------------------------------------------------- 8 bits -> BF16
-    const int w = warp - 2 - kEpiWarps, row = (w & 3) * 32 + lane, side = w >> 2;      // 64 columns of a row
+    const int w = warp - 2 - kEpiWarps, group = w / kConvWarps;
+    const int row = (w & 1) * 32 + lane, side = (w >> 1) & 1;      // 64 columns of a row
+    const int swizzle = row & 7;
     uint32_t j = 0;
     bool ok = true;
     for (int t = unit; ok && t < p.total; t += units) {
@@ -272,18 +268,18 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const uint8_t* sx = p.ag ? p.sx[s] + int64_t(r) * p.blocks : p.sx[c.rank] + (int64_t(s) * p.m + r) * p.blocks;
         return sx[block];
       };
-      uint32_t next = scale_at(0);
-      for (int a = 0; a < all; ++a, ++j) {
+      int a = int((uint32_t(group) - j) & (kGroups - 1));      // this group's first stage of the tile
+      uint32_t next = scale_at(a);
+      for (; a < all; a += kGroups) {
         const uint32_t scale = scale_bf16x2(next);
-        next = scale_at(a + 1);
-        const uint32_t slot = j % kStages, conv = j % kConv;
-        ok = wait_phase(&ctl->x_full[slot], (j / kStages) & 1u, wc, SITE_FULL, t);
-        if (ok && j >= kConv) ok = wait_phase(&ctl->c_empty[conv], (j / kConv - 1) & 1u, wc, SITE_EMPTY, t);
+        next = scale_at(a + kGroups);
+        const uint32_t at = j + uint32_t(a), xs = at % kXStages, slot = at % kStages;
+        ok = wait_phase(&ctl->x_full[xs], (at / kXStages) & 1u, wc, SITE_FULL, t);
+        if (ok && at >= kStages) ok = wait_phase(&ctl->empty[slot], (at / kStages - 1) & 1u, wc, SITE_EMPTY, t);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint8_t* from = smem + kXAt + slot * kXBytes + row * 128;
-        uint8_t* to = smem + kCAt + conv * kCBytes + side * kChunk + row * 128;
-        const int swizzle = row & 7;
+        const uint8_t* from = smem + kXAt + xs * kXBytes + row * 128;
+        uint8_t* to = smem + kCAt + slot * kCBytes + side * kChunk + row * 128;
         uint4 in[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) in[u] = *reinterpret_cast<const uint4*>(from + (((side * 4 + u) ^ swizzle) << 4));
@@ -297,13 +293,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&ctl->x_empty[slot]);
-          mbar_arrive(&ctl->c_full[conv]);
+          mbar_arrive(&ctl->x_empty[xs]);
+          mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->ready[slot]), 0));
         }
       }
+      j += uint32_t(all);
     }
-    for (uint32_t i = j < uint32_t(kConv) ? j : uint32_t(kConv); ok && i > 0; --i)
-      ok = __all_sync(0xffffffffu, wait_phase(&ctl->c_empty[(j - i) % kConv], ((j - i) / kConv) & 1u, wc, SITE_DRAIN, -1));
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -333,6 +328,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
           }
           if (n >= p.N || q * 32 >= cols) continue;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const uint32_t x = v[i + 1];
+            v[i + 1] = v[i + 2];
+            v[i + 2] = x;
+          }
           if (p.fp32) {
             float* out = static_cast<float*>(p.dw[c.rank]) + at + q * 32;
             if (add) {

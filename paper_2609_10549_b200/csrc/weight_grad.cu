@@ -25,8 +25,8 @@ namespace {
 
 constexpr int kThreads = 608;
 constexpr int kEpiWarps = 8;
-constexpr int kConvWarps = 4;                         // of a group
-constexpr int kGroups = 2;
+constexpr int kConvWarps = 2;                         // of a group
+constexpr int kGroups = 4;
 constexpr int kRows = 64;                             // of the contraction in a stage
 constexpr int kGBytes = 128 * kRows * 2;              // this CTA's 128 columns of G: two boxes of 64
 constexpr int kXBytes = 128 * kRows;                  // its 128 columns of X
@@ -66,7 +66,7 @@ struct Control {
 };
 constexpr int kXAt = kStages * kGBytes, kCAt = kXAt + kXStages * kXBytes, kControlAt = kCAt + kStages * kCBytes;
 constexpr size_t kSmemBytes = 1024 + kControlAt + sizeof(Control);
-static_assert(kSmemBytes <= 227 * 1024, "");
+static_assert(kSmemBytes <= 227 * 1024 && kGroups <= kStages && kStages <= kXStages, "");
 
 struct Tile {
   int rank;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   } else if (warp >= 2 + kEpiWarps) {
     // ------------------------------------------------------------- 8 bits -> BF16
     const int w = warp - 2 - kEpiWarps, group = w / kConvWarps;
-    const int row = (w & 1) * 32 + lane, side = (w >> 1) & 1;      // 64 columns of a row
+    const int row = (w & 1) * 32 + lane;
     const int swizzle = row & 7;
     uint32_t j = 0;
     bool ok = true;
@@ -274,21 +274,26 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const uint32_t scale = scale_bf16x2(next);
         next = scale_at(a + kGroups);
         const uint32_t at = j + uint32_t(a), xs = at % kXStages, slot = at % kStages;
-        ok = wait_phase(&ctl->x_full[xs], (at / kXStages) & 1u, wc, SITE_FULL, t);
-        if (ok && at >= kStages) ok = wait_phase(&ctl->empty[slot], (at / kStages - 1) & 1u, wc, SITE_EMPTY, t);
+        // In this order: a parity tells a phase from the one before it only, and the other groups' stages in between may be late.
+        // This group's last stage waited for the products of stage at - kGroups - kStages, so it is the phase before that can be
+        // missing at worst; and when those of stage at - kStages are done, the load before this one into its place has landed.
+        if (at >= kStages) ok = wait_phase(&ctl->empty[slot], (at / kStages - 1) & 1u, wc, SITE_EMPTY, t);
+        if (ok) ok = wait_phase(&ctl->x_full[xs], (at / kXStages) & 1u, wc, SITE_FULL, t);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint8_t* from = smem + kXAt + xs * kXBytes + row * 128;
-        uint8_t* to = smem + kCAt + slot * kCBytes + side * kChunk + row * 128;
-        uint4 in[4];
+        uint8_t* to = smem + kCAt + slot * kCBytes + row * 128;
+        uint4 in[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) in[u] = *reinterpret_cast<const uint4*>(from + (((side * 4 + u) ^ swizzle) << 4));
+        for (int u = 0; u < 8; ++u) in[u] = *reinterpret_cast<const uint4*>(from + ((u ^ swizzle) << 4));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 8; ++u) {
           uint4 lo, hi;
           convert16<kFormat>(in[u], scale, lo, hi);
-          *reinterpret_cast<uint4*>(to + ((2 * u ^ swizzle) << 4)) = lo;
-          *reinterpret_cast<uint4*>(to + (((2 * u + 1) ^ swizzle) << 4)) = hi;
+          uint8_t* chunk = to + (u >> 2) * kChunk;
+          const int at16 = 2 * (u & 3);
+          *reinterpret_cast<uint4*>(chunk + ((at16 ^ swizzle) << 4)) = lo;
+          *reinterpret_cast<uint4*>(chunk + (((at16 + 1) ^ swizzle) << 4)) = hi;
         }
         fence_proxy_async_smem();
         __syncwarp();

@@ -4,13 +4,14 @@
 // for 32 elements of the contraction): the 8-bit tile is turned into BF16 in shared memory, which holds scale times value
 // exactly, and the products are BF16 ones with FP32 sums.  The activations cross HBM and L2 in 8 bits.
 //
-// Pairs of CTAs, 256 rows (n) x 256 columns (k) a tile, 64 rows of the contraction a stage.  Both operands lie across the
-// contraction (MN-major).  Warp 0 loads G (TMA), warp 18 X, warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17
+// Pairs of CTAs, 512 rows (n) x 256 columns (k) a tile as long as they fill whole rounds of the pairs (two accumulators that share
+// one converted tile), 256 x 256 for the rest; 64 rows of the contraction a stage.  Both operands lie across the contraction
+// (MN-major).  Warp 0 loads G (TMA), warp 18 X, warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17
 // convert: two groups, which take the stages in turn; a thread has half a row of a stage, so one scale.  Rows past a rank's last one
 // are zeros of the tensor maps.
 //
 // The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
-// 1024 rows long, and added up in FP32 in the result itself.
+// 1024 rows long, and added up in FP32, in tensor memory: 256 x 256 tiles whose second accumulator keeps the total.
 #include <mutex>
 
 #include "pipeline.cuh"
@@ -28,12 +29,13 @@ constexpr int kEpiWarps = 8;
 constexpr int kConvWarps = 2;                         // of a group
 constexpr int kGroups = 4;
 constexpr int kRows = 64;                             // of the contraction in a stage
-constexpr int kGBytes = 128 * kRows * 2;              // this CTA's 128 columns of G: two boxes of 64
+constexpr int kGBytes = 256 * kRows * 2;              // this CTA's 256 (or 128) columns of G: boxes of 64
 constexpr int kXBytes = 128 * kRows;                  // its 128 columns of X
 constexpr int kCBytes = 128 * kRows * 2;              // the same in BF16: two chunks of 64
 constexpr int kChunk = 64 * kRows * 2;
-constexpr int kStages = 5;                            // of G and of X in BF16
-constexpr int kXStages = 5;
+constexpr int kStages = 4;                            // of G and of X in BF16
+constexpr int kXStages = 4;
+constexpr int kSkew = 3;                              // stages at a 512 x 256 tile's ends in which accumulator 0 runs ahead
 constexpr int kRangeStages = 16;                      // of a sum that goes to FP32
 constexpr int kRowGroup = 8;                          // row tiles that go through the columns together
 
@@ -49,7 +51,10 @@ struct GradParams {
   int32_t m;               // rows per shard
   int32_t blocks;          // scales per row
   int32_t stages;          // per shard
-  int32_t row_tiles, col_tiles, total;
+  int32_t big_rows, col_tiles;      // rows of 512 x 256 tiles
+  int32_t odd;                      // and one more of 256 x 256
+  int32_t n_big, left, total;       // 512 x 256 tiles; places left over, two 256 x 256 tiles each
+  int32_t parts;                    // sums of a tile
   int32_t accumulate, fp32;
   int32_t wide;            // results lie on 32-byte boundaries
   uint32_t wait_limit_us;
@@ -69,19 +74,34 @@ constexpr size_t kSmemBytes = 1024 + kControlAt + sizeof(Control);
 static_assert(kSmemBytes <= 227 * 1024 && kGroups <= kStages && kStages <= kXStages, "");
 
 struct Tile {
+  bool big;
   int rank;
   int row0, col0;
 };
 __device__ __forceinline__ Tile tile_of(const GradParams& p, int t) {
   Tile c;
-  const int per_rank = p.row_tiles * p.col_tiles;
-  c.rank = t / per_rank;
-  int w = t - c.rank * per_rank;
+  c.big = t < p.n_big;
+  int slot = t, half = 0;
+  const int u = t - p.n_big;
+  if (!c.big && u >= 2 * p.left) {
+    const int w = u - 2 * p.left;
+    c.rank = w / p.col_tiles;
+    c.col0 = (w - c.rank * p.col_tiles) * 256;
+    c.row0 = p.big_rows * 512;
+    return c;
+  }
+  if (!c.big) {
+    slot = p.n_big + (u >> 1);
+    half = u & 1;
+  }
+  const int per_rank = p.big_rows * p.col_tiles;
+  c.rank = slot / per_rank;
+  int w = slot - c.rank * per_rank;
   const int g = w / (kRowGroup * p.col_tiles);
   w -= g * kRowGroup * p.col_tiles;
-  const int high = min(kRowGroup, p.row_tiles - g * kRowGroup);
+  const int high = min(kRowGroup, p.big_rows - g * kRowGroup);
   const int nt = w / high;
-  c.row0 = (g * kRowGroup + w - nt * high) * 256;
+  c.row0 = (g * kRowGroup + w - nt * high) * 512 + half * 256;
   c.col0 = nt * 256;
   return c;
 }
@@ -137,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
   const int all = p.P * p.stages;      // stages of a tile
-  const int range = p.fp32 ? kRangeStages : all;
+  const int range = p.parts > 1 ? kRangeStages : all;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -181,17 +201,17 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       bool ok = true;
       for (int t = unit; ok && t < p.total; t += units) {
         const Tile c = tile_of(p, t);
-        const int n0 = c.row0 + cta * 128, k0 = c.col0 + cta * 128;
+        const int boxes = c.big ? 4 : 2, n0 = c.row0 + cta * boxes * 64, k0 = c.col0 + cta * 128;
         for (int s = 0; ok && s < p.P; ++s)
           for (int i = 0; i < p.stages; ++i, ++j) {
             const uint32_t slot = j % depth;
             if (j >= depth && !(ok = wait_phase(&empty[slot], (j / depth - 1) & 1u, wc, SITE_EMPTY, t))) break;
             if (of_g) {
               const uint32_t bar = map_to_cta(smem_u32(&full[slot]), 0);
-              if (leader) mbar_arrive_expect_tx(&full[slot], 2 * kGBytes);
+              if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * kChunk));
               const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
-              tma_load_3d_pair_hint(smem + slot * kGBytes, g, bar, n0, i * kRows, p.ag ? s : 0, pol);
-              tma_load_3d_pair_hint(smem + slot * kGBytes + kChunk, g, bar, n0 + 64, i * kRows, p.ag ? s : 0, pol);
+              for (int b = 0; b < boxes; ++b)
+                tma_load_3d_pair_hint(smem + slot * kGBytes + b * kChunk, g, bar, n0 + b * 64, i * kRows, p.ag ? s : 0, pol);
             } else {
               mbar_arrive_expect_tx(&full[slot], kXBytes);
               tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
@@ -216,34 +236,85 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | kUmmaIdescAMnMajor | kUmmaIdescBMnMajor;
       const uint64_t desc_g = umma_smem_desc_sw128_mn(smem_u32(smem), kChunk);
       const uint64_t desc_c = umma_smem_desc_sw128_mn(smem_u32(smem + kCAt), kChunk);
-      uint32_t j = 0, it = 0;
+      uint32_t j = 0, uses[2] = {0, 0}, small = 0;
       bool ok = true;
-      for (int t = unit; ok && t < p.total; t += units) {
-        int shard_stage = 0;
-        for (int a = 0; ok && a < all; ++it) {
-          const uint32_t b = it & 1u;
-          const int to = min(all, a + range);
-          if (!(ok = wait_phase(&ctl->acc_empty[b], ((it >> 1) & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t))) break;
-          tc_fence_after_sync();
-          for (uint32_t first = 0; a < to; ++a, ++j, first = 1) {
-            const uint32_t slot = j % kStages;
-            if (!(ok = wait_phase(&ctl->ready[slot], (j / kStages) & 1u, wc, SITE_FULL, t))) break;
-            tc_fence_after_sync();
-            // a step of 16 rows of the contraction is two groups of 8 (2048 bytes)
-            const uint64_t da = desc_g + uint64_t((slot * kGBytes) >> 4), db = desc_c + uint64_t((slot * kCBytes) >> 4);
-            const int rows = p.m - shard_stage * kRows;
-            if (rows >= kRows) {
+      int t = unit;
+      auto acc_free = [&](int b) {
+        if (!wait_phase(&ctl->acc_empty[b], (uses[b] & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t)) return false;
+        tc_fence_after_sync();
+        return true;
+      };
+      auto landed = [&](uint32_t s) {
+        if (!wait_phase(&ctl->ready[s % kStages], (s / kStages) & 1u, wc, SITE_FULL, t)) return false;
+        tc_fence_after_sync();
+        return true;
+      };
+      // Products of stage `s` of a tile (the `s0 + s`-th of all) with columns 128 `block` on of G; a step of 16 rows of the contraction
+      // is two groups of 8 (2048 bytes).  `first`: 0 where a sum begins.
+      auto issue = [&](uint32_t acc, uint32_t at, int block, int s, uint32_t first) {
+        const uint32_t slot = at % kStages;
+        const uint64_t da = desc_g + uint64_t((slot * kGBytes + block * 2 * kChunk) >> 4), db = desc_c + uint64_t((slot * kCBytes) >> 4);
+        const int rows = p.m - s % p.stages * kRows;
+        if (rows >= kRows) {
 #pragma unroll
-              for (int k = 0; k < kRows / 16; ++k)
-                umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
-            } else {
-              for (int k = 0; k < (rows + 15) / 16; ++k)
-                umma_bf16_pair(tmem_base + b * 256, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
+          for (int k = 0; k < kRows / 16; ++k) umma_bf16_pair(acc, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
+        } else {
+          for (int k = 0; k < (rows + 15) / 16; ++k) umma_bf16_pair(acc, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
+        }
+      };
+      for (; ok && t < p.total; t += units) {
+        if (tile_of(p, t).big) {
+          // Both accumulators are live for the whole tile, so nothing would hide the epilogue's reads if they ended together: for the
+          // first and last kSkew stages accumulator 0's products go first.  It is then complete early (its epilogue runs under
+          // accumulator 1's last products), and the next tile begins on it while accumulator 1 is still being read.
+          const int skew = all >= 2 * kSkew ? kSkew : 0;
+          auto skewed = [&](int s0, bool begin) {
+            for (int s = 0; s < kSkew; ++s) {
+              if (!landed(j + s)) return false;
+              issue(tmem_base, j + s, 0, s0 + s, s0 + s ? 1u : 0u);
             }
-            umma_commit_pair(&ctl->empty[slot], 0x3);
-            if (++shard_stage == p.stages) shard_stage = 0;
+            if (begin) {
+              if (!acc_free(1)) return false;
+            } else {
+              umma_commit_pair(&ctl->acc_full[0], 0x3);
+            }
+            for (int s = 0; s < kSkew; ++s) {
+              issue(tmem_base + 256, j + s, 1, s0 + s, s0 + s ? 1u : 0u);
+              umma_commit_pair(&ctl->empty[(j + s) % kStages], 0x3);
+            }
+            j += kSkew;
+            return true;
+          };
+          ok = acc_free(0);
+          if (ok) ok = skew ? skewed(0, true) : acc_free(1);
+          for (int s = skew; ok && s < all - skew; ++s, ++j) {
+            if (!(ok = landed(j))) break;
+            issue(tmem_base, j, 0, s, s ? 1u : 0u);
+            issue(tmem_base + 256, j, 1, s, s ? 1u : 0u);
+            umma_commit_pair(&ctl->empty[j % kStages], 0x3);
           }
-          if (ok) umma_commit_pair(&ctl->acc_full[b], 0x3);
+          if (ok && skew) ok = skewed(all - skew, false);
+          else if (ok) umma_commit_pair(&ctl->acc_full[0], 0x3);
+          if (!ok) break;
+          umma_commit_pair(&ctl->acc_full[1], 0x3);
+          ++uses[0];
+          ++uses[1];
+        } else {
+          for (int s = 0; ok && s < all;) {
+            // one sum: the accumulators in turn; several: the first goes where the total is kept
+            const int b = p.parts > 1 ? (s == 0 ? 1 : 0) : int(small & 1u);
+            const int from = s, to = min(all, s + range);
+            if (!(ok = acc_free(b))) break;
+            for (; s < to; ++s, ++j) {
+              if (!(ok = landed(j))) break;
+              issue(tmem_base + b * 256, j, 0, s, s != from ? 1u : 0u);
+              umma_commit_pair(&ctl->empty[j % kStages], 0x3);
+            }
+            if (!ok) break;
+            umma_commit_pair(&ctl->acc_full[b], 0x3);
+            ++uses[b];
+          }
+          ++small;
         }
       }
       if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
@@ -307,30 +378,65 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    uint32_t it = 0;
+    uint32_t uses[2] = {0, 0}, small = 0;
     bool ok = true;
+    const uint32_t lanes = tmem_base + (uint32_t(quarter * 32) << 16) + half * 128;
     for (int t = unit; ok && t < p.total; t += units) {
       const Tile c = tile_of(p, t);
-      const int64_t n = c.row0 + cta * 128 + quarter * 32 + lane;
+      auto filled = [&](int b) {
+        ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full[b], uses[b] & 1u, wc, SITE_ACC_FULL, t));
+        tc_fence_after_sync();
+        ++uses[b];
+        return ok;
+      };
+      auto give_back = [&](int b) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+      };
+      if (p.parts > 1) {
+        // the total is in accumulator 1; all sums but the last are added to it
+        if (!filled(1)) break;
+        for (int s = 2; ok && s < p.parts; ++s) {
+          if (!filled(0)) break;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t v[32], w[32];
+            tmem_ld_32x32b_x32(lanes + q * 32, v);
+            tmem_ld_32x32b_x32(lanes + 256 + q * 32, w);
+            tmem_ld_wait();
+            if (q == 3) give_back(0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(v[i]));
+            tmem_st_32x32b_x32(lanes + 256 + q * 32, w);
+          }
+          tmem_st_wait();
+        }
+        if (!ok || !filled(0)) break;
+      }
       const int64_t k0 = c.col0 + half * 128;
       const int cols = int(min(int64_t(128), p.K - k0));      // a multiple of 16, or none
-      const int64_t at = n * p.K + k0;
-      for (int a = 0; a < all; a += range, ++it) {
-        const uint32_t b = it & 1u;
-        ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full[b], (it >> 1) & 1u, wc, SITE_ACC_FULL, t));
-        if (!ok) break;
-        tc_fence_after_sync();
-        const uint32_t taddr = tmem_base + (uint32_t(quarter * 32) << 16) + b * 256 + half * 128;
-        const bool add = p.accumulate || a > 0;
-#pragma unroll
+      const bool add = p.accumulate;
+      for (int block = 0; block < (c.big ? 2 : 1); ++block) {
+        const int b = p.parts > 1 ? 0 : c.big ? block : int(small & 1u);
+        if (p.parts == 1 && !filled(b)) break;
+        const int64_t n = c.row0 + (c.big ? cta * 256 + block * 128 : cta * 128) + quarter * 32 + lane;
+        const int64_t at = n * p.K + k0;
+#pragma unroll 1
         for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
-          tmem_ld_32x32b_x32(taddr + q * 32, v);
+          tmem_ld_32x32b_x32(lanes + b * 256 + q * 32, v);
           tmem_ld_wait();
+          if (p.parts > 1) {
+            uint32_t w[32];
+            tmem_ld_32x32b_x32(lanes + 256 + q * 32, w);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(v[i]));
+          }
           if (q == 3) {
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+            give_back(b);
+            if (p.parts > 1) give_back(1);
           }
           if (n >= p.N || q * 32 >= cols) continue;
 #pragma unroll
@@ -342,17 +448,21 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           if (p.fp32) {
             float* out = static_cast<float*>(p.dw[c.rank]) + at + q * 32;
             if (add) {
-              // (all loads before the first store: each waiting for the last, the kernel took twice as long)
-              float4 old[8];
+              // the loads of 16 columns before the first store
 #pragma unroll
-              for (int g = 0; g < 8; ++g)
-                if (q * 32 + g * 4 < cols) old[g] = reinterpret_cast<const float4*>(out)[g];
+              for (int h = 0; h < 2; ++h) {
+                if (q * 32 + h * 16 >= cols) break;
+                float4 old[4];
 #pragma unroll
-              for (int g = 0; g < 8; ++g) {
-                v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) + old[g].x);
-                v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) + old[g].y);
-                v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) + old[g].z);
-                v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) + old[g].w);
+                for (int g = 0; g < 4; ++g) old[g] = reinterpret_cast<const float4*>(out)[h * 4 + g];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                  uint32_t* x = v + h * 16 + g * 4;
+                  x[0] = __float_as_uint(__uint_as_float(x[0]) + old[g].x);
+                  x[1] = __float_as_uint(__uint_as_float(x[1]) + old[g].y);
+                  x[2] = __float_as_uint(__uint_as_float(x[2]) + old[g].z);
+                  x[3] = __float_as_uint(__uint_as_float(x[3]) + old[g].w);
+                }
               }
             }
 #pragma unroll
@@ -390,6 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           }
         }
       }
+      if (!c.big) ++small;
     }
   }
 
@@ -462,7 +573,7 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   st = check_workspace(ws, ws_bytes, COMPASS_STATUS_BYTES);
   if (st != COMPASS_OK) return st;
   const int64_t row_tiles = ceil_div(g->N, 256), col_tiles = ceil_div(g->K, 256);
-  if (row_tiles * col_tiles * g->P > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
+  if (row_tiles * col_tiles * g->P > kMaxDim || g->M + 2 * kRows * g->P > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
   int pairs = 0;
   st = device_pairs(&pairs);
   if (st != COMPASS_OK) return st;
@@ -474,11 +585,17 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   p.K = g->K;
   p.blocks = int32_t(scale_blocks(g->K));
   p.stages = int32_t(ceil_div(p.m, kRows));
-  p.row_tiles = int32_t(row_tiles);
-  p.col_tiles = int32_t(col_tiles);
-  p.total = int32_t(row_tiles * col_tiles * g->P);
   p.accumulate = accumulate != 0;
   p.fp32 = grad_dtype == COMPASS_DTYPE_FP32;
+  p.parts = p.fp32 ? int32_t(ceil_div(int64_t(p.stages) * g->P, kRangeStages)) : 1;
+  // whole rounds of the pairs take 512 x 256 tiles, what is left, and all where a tile has several sums, 256 x 256 ones
+  p.big_rows = int32_t(row_tiles / 2);
+  p.odd = int32_t(row_tiles % 2);
+  p.col_tiles = int32_t(col_tiles);
+  const int32_t places = int32_t(p.big_rows * col_tiles * g->P);
+  p.left = p.parts > 1 ? places : places % pairs;
+  p.n_big = places - p.left;
+  p.total = int32_t(p.n_big + 2 * p.left + p.odd * col_tiles * g->P);
   p.wide = 1;
   p.status = static_cast<StatusBlock*>(ws);
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;

@@ -50,6 +50,7 @@ struct Gemm8Params {
   int32_t frags;           // 128-row fragments per shard
   int32_t row_tiles;       // pairs of fragments
   int32_t col_tiles, bn;   // tiles of bn columns
+  int32_t n_step;          // whose number is a multiple of this, at the end too: both CTAs load half of them from a 16-byte boundary on
   int32_t total;
   // few-rows kernel
   FastDiv slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
@@ -127,7 +128,7 @@ struct PairTile {
   int rows;            // rows of it that exist
   int first;           // GEMM+ReduceScatter: rank whose slice comes first
   int64_t col0;
-  int n;               // columns, a multiple of 32
+  int n;               // columns, a multiple of n_step
 };
 __device__ __forceinline__ PairTile pair_tile(const Gemm8Params& p, int t, int cta) {
   PairTile c;
@@ -140,7 +141,7 @@ __device__ __forceinline__ PairTile pair_tile(const Gemm8Params& p, int t, int c
   const int nt = w / high;
   const int f = 2 * (g * kRowGroup + w - nt * high) + cta;
   c.col0 = int64_t(nt) * p.bn;
-  c.n = int(min(int64_t(p.bn), (p.N - c.col0 + 31) / 32 * 32));
+  c.n = int(min(int64_t(p.bn), (p.N - c.col0 + p.n_step - 1) / p.n_step * p.n_step));
   const int all = p.frags * p.P, mine = min(f, all - 1);
   const int s = mine / p.frags;
   c.chunk = p.rs ? s : (c.rank + s) % p.P;
@@ -236,7 +237,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
     }
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issuer
-    if (leader && lane == 0) {
+    // The whole warp goes through the loop and one lane issues: descriptors and addresses are then the warp's, in the registers that
+    // the instructions take them from.  (With the loop in one lane, each was moved there for every MMA: 180 cycles each, whatever
+    // their size; a full one takes 128.)
+    if (leader) {
       const uint64_t desc_a0 = umma_smem_desc_sw128(smem_u32(smem));
       const uint64_t desc_b0 = p.kn ? umma_smem_desc_sw128_mn(smem_u32(smem + kChunkBytes), kChunkBytes) : umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
       // a step of 32 elements: 32 bytes of a row, or (contraction across) four groups of 8 rows
@@ -249,7 +253,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
         const uint32_t idesc0 = umma_idesc_mx8(256, uint32_t(c.n), uint32_t(p.a_format), E4M3) | (p.kn ? kUmmaIdescBMnMajor : 0u);
         const uint32_t acc = tmem_base + (it & 1u ? kAcc1 : 0u);
         if (it > 0) {
-          if (!(ok = wait_phase(&ctl->acc_early, (it - 1) & 1u, wc, SITE_ACC_EMPTY, t))) break;
+          if (!(ok = wait_warp(&ctl->acc_early, (it - 1) & 1u, wc, SITE_ACC_EMPTY, t))) break;
           tc_fence_after_sync();
         }
         for (int seg = 0; ok && seg < segs; ++seg) {
@@ -257,42 +261,48 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
           for (int a = 0; a < p.atoms; a += kStageAtoms, ++j) {
             if (a % kGroupAtoms == 0) {
               buf = g & 1u;
-              if (!(ok = wait_phase(&ctl->scales_full[buf], (g >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
+              if (!(ok = wait_warp(&ctl->scales_full[buf], (g >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
               tc_fence_after_sync();
               const uint64_t from = desc_s + uint64_t(buf * (3 * 512 >> 4));
-              tmem_copy_scales<true>(tmem_base + kScaleCols + buf * 4, from);
-              tmem_copy_scales<true>(tmem_base + kScaleCols + 8 + buf * 8, from + (512 >> 4));
-              tmem_copy_scales<true>(tmem_base + kScaleCols + 12 + buf * 8, from + (1024 >> 4));
+              if (elect_one()) {
+                tmem_copy_scales<true>(tmem_base + kScaleCols + buf * 4, from);
+                tmem_copy_scales<true>(tmem_base + kScaleCols + 8 + buf * 8, from + (512 >> 4));
+                tmem_copy_scales<true>(tmem_base + kScaleCols + 12 + buf * 8, from + (1024 >> 4));
+              }
               ++g;
             }
             const uint32_t slot = j % kPairStages;
-            if (!(ok = wait_phase(&ctl->full[slot], (j / kPairStages) & 1u, wc, SITE_FULL, t))) break;
+            if (!(ok = wait_warp(&ctl->full[slot], (j / kPairStages) & 1u, wc, SITE_FULL, t))) break;
             tc_fence_after_sync();
             const uint32_t sa = tmem_base + kScaleCols + buf * 4, sb = tmem_base + kScaleCols + 8 + buf * 8;
+            if (elect_one()) {
 #pragma unroll
-            for (int i = 0; i < kStageAtoms; ++i) {
-              if (a + i >= p.atoms) break;
-              const uint64_t da = desc_a0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
-              const uint64_t db = desc_b0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
-              const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(a + i) % kGroupAtoms);
-              const uint32_t first = (seg | a | i) != 0 ? 1u : 0u;
-              const int steps = steps_of(p, a + i);
-              if (steps == 4) {
+              for (int i = 0; i < kStageAtoms; ++i) {
+                if (a + i >= p.atoms) break;
+                const uint64_t da = desc_a0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
+                const uint64_t db = desc_b0 + uint64_t((slot * kPairStageBytes + i * 2 * kChunkBytes) >> 4);
+                const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(a + i) % kGroupAtoms);
+                const uint32_t first = (seg | a | i) != 0 ? 1u : 0u;
+                const int steps = steps_of(p, a + i);
+                if (steps == 4) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
-              } else {
-                for (int k = 0; k < steps; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
+                  for (int k = 0; k < 4; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
+                } else {
+                  for (int k = 0; k < steps; ++k) umma_mx8<true>(acc, da + k * 2, db + k * bk, idesc, sa, sb, k ? 1u : first);
+                }
               }
+              umma_commit_pair(&ctl->empty[slot], 0x3);
+              if (a % kGroupAtoms == kGroupAtoms - kStageAtoms || a + kStageAtoms >= p.atoms) umma_commit_pair(&ctl->scales_empty[buf], 0x3);
             }
-            umma_commit_pair(&ctl->empty[slot], 0x3);
-            if (a % kGroupAtoms == kGroupAtoms - kStageAtoms || a + kStageAtoms >= p.atoms) umma_commit_pair(&ctl->scales_empty[buf], 0x3);
+            __syncwarp();
           }
         }
-        if (ok) umma_commit_pair(&ctl->acc_full, 0x3);
+        if (ok && elect_one()) umma_commit_pair(&ctl->acc_full, 0x3);
+        __syncwarp();
       }
-      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
+      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
         // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
-        umma_commit_pair(&ctl->drain, 0x1);
+        if (elect_one()) umma_commit_pair(&ctl->drain, 0x1);
         wait_settled(&ctl->drain, 0);
       }
     }
@@ -343,7 +353,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
       for (int i = 0; i < 8; ++i) b[i] = __shfl_sync(0xffffffffu, w, 4 * int(((x.col0 + 32 * i + lane) >> 7) - (x.col0 >> 7)));
       const uint32_t buf = g & 1u;
       if (g >= 2) {
-        ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((g >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
+        ok = wait_warp(&ctl->scales_empty[buf], ((g >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t);
         if (!ok) break;
       }
       sh->scales[buf][0][lane] = make_uint4(a[0], a[1], a[2], a[3]);
@@ -356,7 +366,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
     }
     // leave only when the last groups' signals have come
     for (uint32_t i = g < 2u ? g : 2u; ok && i > 0; --i)
-      ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[(g - i) & 1u], ((g - i) >> 1) & 1u, wc, SITE_DRAIN, -1));
+      ok = wait_warp(&ctl->scales_empty[(g - i) & 1u], ((g - i) >> 1) & 1u, wc, SITE_DRAIN, -1);
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -531,47 +541,53 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc0 = umma_idesc_mx8(128, uint32_t(p.cols), E4M3, uint32_t(p.a_format)) | (p.kn ? kUmmaIdescAMnMajor : 0u);
-      const uint64_t desc_w = p.kn ? umma_smem_desc_sw128_mn(smem_u32(smem), kChunkBytes) : umma_smem_desc_sw128(smem_u32(smem));
-      const uint64_t desc_x = umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
-      const uint64_t desc_s = smem_desc_scales(smem_u32(sh->scales));
-      const uint64_t wk = p.kn ? 4096 >> 4 : 2;
-      int j = 0;
-      uint32_t group = 0, buf = 0;
-      int in_group = 0, left = 0;
-      bool ok = true;
-      for (int g = from; g < to; ++g, ++j) {
-        const int seg = g / p.atoms, a = g - seg * p.atoms;
-        if (left == 0) {
-          // a group of scales: up to four atoms of one slice
-          left = min(min(kGroupAtoms, p.atoms - a), to - g);
-          in_group = 0;
-          buf = group & 1u;
-          if (!(ok = wait_phase(&ctl->scales_full[buf], (group >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
-          tc_fence_after_sync();
-          const uint64_t src = desc_s + uint64_t(buf * (3 * 512 >> 4));
+    // (the whole warp goes through the loop and one lane issues, as above)
+    const uint32_t idesc0 = umma_idesc_mx8(128, uint32_t(p.cols), E4M3, uint32_t(p.a_format)) | (p.kn ? kUmmaIdescAMnMajor : 0u);
+    const uint64_t desc_w = p.kn ? umma_smem_desc_sw128_mn(smem_u32(smem), kChunkBytes) : umma_smem_desc_sw128(smem_u32(smem));
+    const uint64_t desc_x = umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
+    const uint64_t desc_s = smem_desc_scales(smem_u32(sh->scales));
+    const uint64_t wk = p.kn ? 4096 >> 4 : 2;
+    int j = 0;
+    uint32_t group = 0, buf = 0;
+    int in_group = 0, left = 0;
+    bool ok = true;
+    for (int g = from; g < to; ++g, ++j) {
+      const int seg = g / p.atoms, a = g - seg * p.atoms;
+      if (left == 0) {
+        // a group of scales: up to four atoms of one slice
+        left = min(min(kGroupAtoms, p.atoms - a), to - g);
+        in_group = 0;
+        buf = group & 1u;
+        if (!(ok = wait_warp(&ctl->scales_full[buf], (group >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
+        tc_fence_after_sync();
+        const uint64_t src = desc_s + uint64_t(buf * (3 * 512 >> 4));
+        if (elect_one()) {
           tmem_copy_scales<false>(scale_a + buf * 4, src);
           tmem_copy_scales<false>(scale_b + buf * 8, src + (512 >> 4));
           if (p.cols > 128) tmem_copy_scales<false>(scale_b + buf * 8 + 4, src + (1024 >> 4));
-          ++group;
         }
-        const int slot = j % stages;
-        if (!(ok = wait_phase(&ctl->full[slot], uint32_t(j / stages) & 1u, wc, SITE_FULL, t))) break;
-        tc_fence_after_sync();
-        const uint64_t dw = desc_w + uint64_t((slot * stage_bytes) >> 4), dx = desc_x + uint64_t((slot * stage_bytes) >> 4);
-        const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(in_group));
-        const int steps = steps_of(p, a);
+        ++group;
+      }
+      const int slot = j % stages;
+      if (!(ok = wait_warp(&ctl->full[slot], uint32_t(j / stages) & 1u, wc, SITE_FULL, t))) break;
+      tc_fence_after_sync();
+      const uint64_t dw = desc_w + uint64_t((slot * stage_bytes) >> 4), dx = desc_x + uint64_t((slot * stage_bytes) >> 4);
+      const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(in_group));
+      const int steps = steps_of(p, a);
+      ++in_group;
+      --left;
+      if (elect_one()) {
         for (int k = 0; k < steps; ++k) umma_mx8<false>(tmem_base, dw + k * wk, dx + k * 2, idesc, scale_a + buf * 4, scale_b + buf * 8, j | k ? 1u : 0u);
         umma_commit(&ctl->empty[slot]);
-        ++in_group;
-        if (--left == 0) umma_commit(&ctl->scales_empty[buf]);
+        if (left == 0) umma_commit(&ctl->scales_empty[buf]);
       }
-      if (ok) umma_commit(&ctl->acc_full);
-      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
-        umma_commit(&ctl->drain);
-        wait_settled(&ctl->drain, 0);
-      }
+      __syncwarp();
+    }
+    if (ok && elect_one()) umma_commit(&ctl->acc_full);
+    __syncwarp();
+    if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
+      if (elect_one()) umma_commit(&ctl->drain);
+      wait_settled(&ctl->drain, 0);
     }
   } else if (warp == 2) {
     struct Group {
@@ -610,7 +626,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       for (int i = 0; i < 8; ++i) w[i] = i * 32 < p.cols ? x.x[i].word(x.words) : kOne;
       const uint32_t buf = group & 1u;
       if (group >= 2) {
-        ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t));
+        ok = wait_warp(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t);
         if (!ok) break;
       }
       sh->scales[buf][0][lane] = make_uint4(v, v, v, v);
@@ -622,7 +638,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       x = next;
     }
     for (uint32_t i = group < 2u ? group : 2u; ok && i > 0; --i)
-      ok = __all_sync(0xffffffffu, wait_phase(&ctl->scales_empty[(group - i) & 1u], ((group - i) >> 1) & 1u, wc, SITE_DRAIN, -1));
+      ok = wait_warp(&ctl->scales_empty[(group - i) & 1u], ((group - i) >> 1) & 1u, wc, SITE_DRAIN, -1);
   }
 
   // The sums: lanes are weight rows, columns are activation rows.
@@ -642,7 +658,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   bool ok = true;
   float* sums = reinterpret_cast<float*>(smem);      // [column][128], over the stages
   if (warp >= 4) {
-    ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full, 0, wc, SITE_ACC_FULL, t));
+    ok = wait_warp(&ctl->acc_full, 0, wc, SITE_ACC_FULL, t);
     tc_fence_after_sync();
     if (ok) {
       for (int c = 0; c < p.cols; c += 16) {
@@ -766,6 +782,25 @@ int device_facts(DeviceFacts** out) {
   return COMPASS_OK;
 }
 
+// Columns of a pair's tile.  An atom of it takes the tensor cores 2 cycles a column, and its operands, 128 rows of A and half of its
+// columns of B for each CTA, 2.1 cycles a row (about 60 bytes a clock from L2); the tile that ends the rounds of the pairs soonest.
+// Tiles are of equal width as far as n_step allows, so that none is a narrow rest that still loads all of A.
+int pair_columns(int64_t N, int64_t row_tiles, int step, int pairs) {
+  int best = 256;
+  double least = 0;
+  for (int most = 256; most >= 64; most -= 32) {
+    const int64_t tiles = ceil_div(N, most);
+    const int bn = int(ceil_div(ceil_div(N, tiles), step) * step);
+    const double atom = 2.0 * bn > 2.1 * (128 + bn / 2) ? 2.0 * bn : 2.1 * (128 + bn / 2);
+    const double cost = double(ceil_div(row_tiles * ceil_div(N, bn), pairs)) * atom;
+    if (least == 0 || cost < 0.98 * least) {
+      least = cost;
+      best = bn;
+    }
+  }
+  return best;
+}
+
 int launch_clusters(void (*kernel)(const Gemm8Params), int64_t grid, int threads, size_t smem, int cluster, const Gemm8Params& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(grid));
@@ -875,7 +910,8 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   }
   p.frags = int32_t(ceil_div(p.m, 128));
   p.row_tiles = int32_t(ceil_div(int64_t(p.frags) * g->P, 2));
-  p.bn = 256;
+  p.n_step = p.kn ? 32 : 16;
+  p.bn = pair_columns(g->N, int64_t(p.row_tiles) * (p.rs ? 1 : g->P), p.n_step, f->pairs);
   p.col_tiles = int32_t(ceil_div(g->N, p.bn));
   const int64_t total = int64_t(p.row_tiles) * p.col_tiles * (p.rs ? 1 : g->P);
   if (total > kMaxDim) return COMPASS_ERR_UNSUPPORTED;

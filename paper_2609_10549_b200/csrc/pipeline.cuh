@@ -35,6 +35,11 @@ __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, const
   return false;
 }
 
+// The same for a whole warp, which goes on or gives up as one.
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, const WaitContext& w, int site, int tile) {
+  return __all_sync(0xffffffffu, wait_phase(bar, parity, w, site, tile));
+}
+
 // After giving up: copies or products in flight, whatever the others do, before this CTA's memory may go (100 ms at most).
 __device__ __forceinline__ void wait_settled(uint64_t* bar, uint32_t parity) {
   const uint64_t t0 = ptx::globaltimer_ns();

@@ -232,7 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     }
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issuer
-    if (leader && lane == 0) {
+    // (the whole warp goes through the loop and one lane issues, as in the products of 8-bit operands)
+    if (leader) {
       constexpr uint32_t idesc = umma_idesc_bf16_f32(256, 256) | kUmmaIdescAMnMajor | kUmmaIdescBMnMajor;
       const uint64_t desc_g = umma_smem_desc_sw128_mn(smem_u32(smem), kChunk);
       const uint64_t desc_c = umma_smem_desc_sw128_mn(smem_u32(smem + kCAt), kChunk);
@@ -240,12 +241,16 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       bool ok = true;
       int t = unit;
       auto acc_free = [&](int b) {
-        if (!wait_phase(&ctl->acc_empty[b], (uses[b] & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t)) return false;
+        if (!wait_warp(&ctl->acc_empty[b], (uses[b] & 1u) ^ 1u, wc, SITE_ACC_EMPTY, t)) return false;
         tc_fence_after_sync();
         return true;
       };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) umma_commit_pair(bar, 0x3);
+        __syncwarp();
+      };
       auto landed = [&](uint32_t s) {
-        if (!wait_phase(&ctl->ready[s % kStages], (s / kStages) & 1u, wc, SITE_FULL, t)) return false;
+        if (!wait_warp(&ctl->ready[s % kStages], (s / kStages) & 1u, wc, SITE_FULL, t)) return false;
         tc_fence_after_sync();
         return true;
       };
@@ -255,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const uint32_t slot = at % kStages;
         const uint64_t da = desc_g + uint64_t((slot * kGBytes + block * 2 * kChunk) >> 4), db = desc_c + uint64_t((slot * kCBytes) >> 4);
         const int rows = p.m - s % p.stages * kRows;
+        if (!elect_one()) return;
         if (rows >= kRows) {
 #pragma unroll
           for (int k = 0; k < kRows / 16; ++k) umma_bf16_pair(acc, da + k * (2048 >> 4), db + k * (2048 >> 4), idesc, k ? 1u : first);
@@ -276,11 +282,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (begin) {
               if (!acc_free(1)) return false;
             } else {
-              umma_commit_pair(&ctl->acc_full[0], 0x3);
+              commit(&ctl->acc_full[0]);
             }
             for (int s = 0; s < kSkew; ++s) {
               issue(tmem_base + 256, j + s, 1, s0 + s, s0 + s ? 1u : 0u);
-              umma_commit_pair(&ctl->empty[(j + s) % kStages], 0x3);
+              commit(&ctl->empty[(j + s) % kStages]);
             }
             j += kSkew;
             return true;
@@ -291,12 +297,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (!(ok = landed(j))) break;
             issue(tmem_base, j, 0, s, s ? 1u : 0u);
             issue(tmem_base + 256, j, 1, s, s ? 1u : 0u);
-            umma_commit_pair(&ctl->empty[j % kStages], 0x3);
+            commit(&ctl->empty[j % kStages]);
           }
           if (ok && skew) ok = skewed(all - skew, false);
-          else if (ok) umma_commit_pair(&ctl->acc_full[0], 0x3);
+          else if (ok) commit(&ctl->acc_full[0]);
           if (!ok) break;
-          umma_commit_pair(&ctl->acc_full[1], 0x3);
+          commit(&ctl->acc_full[1]);
           ++uses[0];
           ++uses[1];
         } else {
@@ -308,17 +314,17 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             for (; s < to; ++s, ++j) {
               if (!(ok = landed(j))) break;
               issue(tmem_base + b * 256, j, 0, s, s != from ? 1u : 0u);
-              umma_commit_pair(&ctl->empty[j % kStages], 0x3);
+              commit(&ctl->empty[j % kStages]);
             }
             if (!ok) break;
-            umma_commit_pair(&ctl->acc_full[b], 0x3);
+            commit(&ctl->acc_full[b]);
             ++uses[b];
           }
           ++small;
         }
       }
-      if (*reinterpret_cast<volatile int*>(&ctl->abort)) {
-        umma_commit_pair(&ctl->drain, 0x1);
+      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
+        if (elect_one()) umma_commit_pair(&ctl->drain, 0x1);
         wait_settled(&ctl->drain, 0);
       }
     }
@@ -384,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     for (int t = unit; ok && t < p.total; t += units) {
       const Tile c = tile_of(p, t);
       auto filled = [&](int b) {
-        ok = __all_sync(0xffffffffu, wait_phase(&ctl->acc_full[b], uses[b] & 1u, wc, SITE_ACC_FULL, t));
+        ok = wait_warp(&ctl->acc_full[b], uses[b] & 1u, wc, SITE_ACC_FULL, t);
         tc_fence_after_sync();
         ++uses[b];
         return ok;

@@ -52,12 +52,15 @@ struct Gemm8Params {
   int32_t col_tiles, bn;   // tiles of bn columns
   int32_t n_step;          // whose number is a multiple of this, at the end too: both CTAs load half of them from a 16-byte boundary on
   int32_t total;
+  FastDiv per_rank, per_group, by_frags;      // tiles of a rank, of a group of rows
   // few-rows kernel
   FastDiv slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
   FastDiv each;            // rows per shard
   int32_t cols;            // accumulator columns, a multiple of 16
   int32_t n_tiles;         // 128-row tiles of one rank's weights
   int32_t splits;          // CTAs of a cluster, which share a tile's contraction
+  int32_t all;             // atoms of the whole contraction
+  FastDiv by_splits, by_tiles;
   int32_t stages;
   int32_t tmem_cols;
 };
@@ -132,26 +135,28 @@ struct PairTile {
 };
 __device__ __forceinline__ PairTile pair_tile(const Gemm8Params& p, int t, int cta) {
   PairTile c;
-  const int per_rank = p.row_tiles * p.col_tiles;
-  c.rank = t / per_rank;
-  int w = t - c.rank * per_rank;
-  const int g = w / (kRowGroup * p.col_tiles);
-  w -= g * kRowGroup * p.col_tiles;
+  c.rank = int(p.per_rank.div(uint32_t(t)));
+  int w = t - c.rank * int(p.per_rank.d);
+  const int g = int(p.per_group.div(uint32_t(w)));
+  w -= g * int(p.per_group.d);
   const int high = min(kRowGroup, p.row_tiles - g * kRowGroup);
-  const int nt = w / high;
+  const int nt = high == kRowGroup ? w / kRowGroup : w / high;
   const int f = 2 * (g * kRowGroup + w - nt * high) + cta;
   c.col0 = int64_t(nt) * p.bn;
   c.n = int(min(int64_t(p.bn), (p.N - c.col0 + p.n_step - 1) / p.n_step * p.n_step));
   const int all = p.frags * p.P, mine = min(f, all - 1);
-  const int s = mine / p.frags;
-  c.chunk = p.rs ? s : (c.rank + s) % p.P;
+  const int s = int(p.by_frags.div(uint32_t(mine)));
+  c.chunk = p.rs ? s : c.rank + s - (c.rank + s >= p.P ? p.P : 0);
   c.row0 = (mine - s * p.frags) * 128;
   c.rows = f < all ? min(128, p.m - c.row0) : 0;
-  c.first = ((f - cta) / p.frags + 1) % p.P;
+  c.first = int(p.by_frags.div(uint32_t(f - cta))) + 1;
+  if (c.first == p.P) c.first = 0;
   return c;
 }
 // Tensor of slice `seg`, the row in it where this CTA's fragment begins.
-__device__ __forceinline__ int slice_of(const Gemm8Params& p, const PairTile& c, int seg) { return p.rs ? (c.first + seg) % p.P : c.chunk; }
+__device__ __forceinline__ int slice_of(const Gemm8Params& p, const PairTile& c, int seg) {
+  return p.rs ? c.first + seg - (c.first + seg >= p.P ? p.P : 0) : c.chunk;
+}
 __device__ __forceinline__ int slice_row(const Gemm8Params& p, const PairTile& c) { return p.rs ? c.chunk * p.m + c.row0 : c.row0; }
 
 __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __grid_constant__ Gemm8Params p) {
@@ -471,6 +476,29 @@ struct FewShared {
   uint4 scales[2][3][32];
   FewControl ctl;
 };
+// This CTA's atoms one after the other: slice, atom in it, place in the ring and its turn.  (By divisions, about 100 cycles each, an
+// atom took the issuing warp 1000 cycles.)
+struct FewWalk {
+  int seg, a, left, slot;
+  uint32_t turn;
+  __device__ __forceinline__ FewWalk(const Gemm8Params& p, int from, int to) : left(to - from), slot(0), turn(0) {
+    seg = from >= p.atoms ? from / p.atoms : 0;
+    a = from - seg * p.atoms;
+  }
+  __device__ __forceinline__ void next(const Gemm8Params& p) {
+    --left;
+    if (++a == p.atoms) {
+      a = 0;
+      ++seg;
+    }
+    if (++slot == p.stages) {
+      slot = 0;
+      ++turn;
+    }
+  }
+  // atoms of the group of scales that begins here
+  __device__ __forceinline__ int group(const Gemm8Params& p) const { return min(min(kGroupAtoms, p.atoms - a), left); }
+};
 __host__ __device__ constexpr int few_stage_bytes(int cols) { return kChunkBytes + cols * kAtom; }
 __host__ __device__ constexpr size_t few_smem_bytes(int cols, int stages) { return 1024 + size_t(stages) * few_stage_bytes(cols) + sizeof(FewShared); }
 
@@ -482,14 +510,17 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   FewControl* ctl = &sh->ctl;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int part = p.splits > 1 ? int(cluster_ctarank()) : 0;
-  const int t = int(blockIdx.x) / p.splits;
-  const int rank = p.rs ? 0 : t / p.n_tiles;
+  const int t = int(p.by_splits.div(blockIdx.x));
+  const int rank = p.rs ? 0 : int(p.by_tiles.div(uint32_t(t)));
   const int64_t n0 = int64_t(t - rank * p.n_tiles) * 128;
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
   // this CTA's atoms of the whole contraction
-  const int all = (p.rs ? p.P : 1) * p.atoms;
-  const int from = int(int64_t(all) * part / p.splits), to = int(int64_t(all) * (part + 1) / p.splits);
+  const int from = int(p.by_splits.div(uint32_t(p.all * part))), to = int(p.by_splits.div(uint32_t(p.all * (part + 1))));
 
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&p.b[rank]);
+    prefetch_tensormap(&p.a[0]);
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
       mbar_init(&ctl->full[s], 1);
@@ -521,23 +552,28 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
       const int shards = p.rs ? 1 : p.P;
       const uint32_t bytes = uint32_t(kChunkBytes + (p.rs ? p.P : shards) * p.m * kAtom);
-      int j = 0;
-      for (int g = from; g < to; ++g, ++j) {
-        const int slot = j % stages, seg = g / p.atoms, a = g - seg * p.atoms;
-        if (j >= stages && !wait_phase(&ctl->empty[slot], uint32_t(j / stages - 1) & 1u, wc, SITE_EMPTY, t)) break;
-        uint8_t* dst = smem + slot * stage_bytes;
-        mbar_arrive_expect_tx(&ctl->full[slot], bytes);
-        const CUtensorMap* w = &p.b[p.rs ? seg : rank];
-        if (p.kn) tma_load_2d_hint(dst, w, &ctl->full[slot], int(n0), a * kAtom, pol);
-        else tma_load_2d_hint(dst, w, &ctl->full[slot], a * kAtom, int(n0), pol);
+      FewWalk w(p, from, to);
+      for (; w.left > 0; w.next(p)) {
+        if (w.turn > 0 && !wait_phase(&ctl->empty[w.slot], (w.turn - 1) & 1u, wc, SITE_EMPTY, t)) break;
+        uint8_t* dst = smem + w.slot * stage_bytes;
+        mbar_arrive_expect_tx(&ctl->full[w.slot], bytes);
+        const CUtensorMap* b = &p.b[p.rs ? w.seg : rank];
+        if (p.kn) tma_load_2d_hint(dst, b, &ctl->full[w.slot], int(n0), w.a * kAtom, pol);
+        else tma_load_2d_hint(dst, b, &ctl->full[w.slot], w.a * kAtom, int(n0), pol);
         for (int s = 0; s < shards; ++s)
-          tma_load_2d_hint(dst + kChunkBytes + s * p.slot.d * kAtom, &p.a[p.rs ? seg : s], &ctl->full[slot], a * kAtom, 0, pol);
+          tma_load_2d_hint(dst + kChunkBytes + s * p.slot.d * kAtom, &p.a[p.rs ? w.seg : s], &ctl->full[w.slot], w.a * kAtom, 0, pol);
       }
-      // leave only when everything that was loaded has landed and been read
-      for (int i = max(0, j - stages); i < j; ++i)
-        if (!wait_phase(&ctl->empty[i % stages], uint32_t(i / stages) & 1u, wc, SITE_DRAIN, -1)) {
-          for (int k = max(0, j - stages); k < j; ++k) wait_settled(&ctl->full[k % stages], uint32_t(k / stages) & 1u);
-          break;
+      // leave only when everything that was loaded has landed and been read: the last turn's places before this one's, the one's before
+      // it from here on
+      bool ok = true;
+      for (int i = 0; i < stages; ++i) {
+        const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
+        if (turn >= 0 && !(ok = wait_phase(&ctl->empty[i], uint32_t(turn) & 1u, wc, SITE_DRAIN, -1))) break;
+      }
+      if (!ok)
+        for (int i = 0; i < stages; ++i) {
+          const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
+          if (turn >= 0) wait_settled(&ctl->full[i], uint32_t(turn) & 1u);
         }
     }
   } else if (warp == 1) {
@@ -547,15 +583,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     const uint64_t desc_x = umma_smem_desc_sw128(smem_u32(smem + kChunkBytes));
     const uint64_t desc_s = smem_desc_scales(smem_u32(sh->scales));
     const uint64_t wk = p.kn ? 4096 >> 4 : 2;
-    int j = 0;
-    uint32_t group = 0, buf = 0;
+    uint32_t group = 0, buf = 0, more = 0;
     int in_group = 0, left = 0;
     bool ok = true;
-    for (int g = from; g < to; ++g, ++j) {
-      const int seg = g / p.atoms, a = g - seg * p.atoms;
+    for (FewWalk w(p, from, to); w.left > 0; w.next(p)) {
       if (left == 0) {
         // a group of scales: up to four atoms of one slice
-        left = min(min(kGroupAtoms, p.atoms - a), to - g);
+        left = w.group(p);
         in_group = 0;
         buf = group & 1u;
         if (!(ok = wait_warp(&ctl->scales_full[buf], (group >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
@@ -568,20 +602,25 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         }
         ++group;
       }
-      const int slot = j % stages;
-      if (!(ok = wait_warp(&ctl->full[slot], uint32_t(j / stages) & 1u, wc, SITE_FULL, t))) break;
+      if (!(ok = wait_warp(&ctl->full[w.slot], w.turn & 1u, wc, SITE_FULL, t))) break;
       tc_fence_after_sync();
-      const uint64_t dw = desc_w + uint64_t((slot * stage_bytes) >> 4), dx = desc_x + uint64_t((slot * stage_bytes) >> 4);
+      const uint64_t dw = desc_w + uint64_t((w.slot * stage_bytes) >> 4), dx = desc_x + uint64_t((w.slot * stage_bytes) >> 4);
       const uint32_t idesc = idesc0 | umma_scale_byte(uint32_t(in_group));
-      const int steps = steps_of(p, a);
+      const int steps = steps_of(p, w.a);
       ++in_group;
       --left;
       if (elect_one()) {
-        for (int k = 0; k < steps; ++k) umma_mx8<false>(tmem_base, dw + k * wk, dx + k * 2, idesc, scale_a + buf * 4, scale_b + buf * 8, j | k ? 1u : 0u);
-        umma_commit(&ctl->empty[slot]);
+        if (steps == 4) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_mx8<false>(tmem_base, dw + k * wk, dx + k * 2, idesc, scale_a + buf * 4, scale_b + buf * 8, k ? 1u : more);
+        } else {
+          for (int k = 0; k < steps; ++k) umma_mx8<false>(tmem_base, dw + k * wk, dx + k * 2, idesc, scale_a + buf * 4, scale_b + buf * 8, k ? 1u : more);
+        }
+        umma_commit(&ctl->empty[w.slot]);
         if (left == 0) umma_commit(&ctl->scales_empty[buf]);
       }
       __syncwarp();
+      more = 1;
     }
     if (ok && elect_one()) umma_commit(&ctl->acc_full);
     __syncwarp();
@@ -603,23 +642,29 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       tensor[i] = min(s, p.rs ? 0 : p.P - 1);
       row[i] = min(col - s * int(p.slot.d), (p.rs ? p.m * p.P : p.m) - 1);      // (columns without one: any scale)
     }
-    auto count = [&](int g) { return min(min(kGroupAtoms, p.atoms - g % p.atoms), to - g); };
-    auto load = [&](int g, Group& x) {
-      if (g >= to) return;
-      const int seg = g / p.atoms, a = g - seg * p.atoms, n = count(g);
+    FewWalk at(p, from, to);
+    auto load = [&](Group& x) {      // of the group that begins here, and on behind it
+      if (at.left == 0) return;
+      const int a = at.a, n = at.group(p);
       x.words = p.whole_words && n == 4 && (a & 3) == 0;
-      x.w = weight_byte(p, p.rs ? seg : rank, n0 >> 7, a, n, lane);
+      x.w = weight_byte(p, p.rs ? at.seg : rank, n0 >> 7, a, n, lane);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i * 32 < p.cols) x.x[i].load(p.sa[p.rs ? seg : tensor[i]] + int64_t(row[i]) * p.atoms + a, n, x.words);
+        if (i * 32 < p.cols) x.x[i].load(p.sa[p.rs ? at.seg : tensor[i]] + int64_t(row[i]) * p.atoms + a, n, x.words);
+      at.a += n;
+      at.left -= n;
+      if (at.a == p.atoms) {
+        at.a = 0;
+        ++at.seg;
+      }
     };
     uint32_t group = 0;
-    bool ok = true;
+    bool ok = true, more = to > from;
     Group x, next;
-    load(from, x);
-    for (int g = from; g < to; ++group) {
-      g += count(g);
-      load(g, next);
+    load(x);
+    for (; more; ++group) {
+      more = at.left > 0;
+      load(next);
       const uint32_t v = __shfl_sync(0xffffffffu, weight_words(x.w, lane), 0);
       uint32_t w[8];
 #pragma unroll
@@ -866,6 +911,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   if (cols <= kFewMostCols) {
     p.slot.set(uint32_t(slot));
     p.each.set(uint32_t(p.m));
+    p.by_tiles.set(uint32_t(scale_blocks(g->N)));
     p.cols = int32_t(cols);
     p.n_tiles = int32_t(scale_blocks(g->N));
     const int64_t tiles = int64_t(p.n_tiles) * (p.rs ? 1 : g->P);
@@ -881,6 +927,8 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
         p.splits = s;
       }
     }
+    p.all = all;
+    p.by_splits.set(uint32_t(p.splits));
     const int stage = few_stage_bytes(p.cols);
     const int64_t mine = ceil_div(all, p.splits);
     const int room = tiles * p.splits > f->sms && cols <= 128 ? kFewHalfRoom : kFewRoom;
@@ -916,6 +964,9 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   const int64_t total = int64_t(p.row_tiles) * p.col_tiles * (p.rs ? 1 : g->P);
   if (total > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
   p.total = int32_t(total);
+  p.per_rank.set(uint32_t(p.row_tiles) * uint32_t(p.col_tiles));
+  p.per_group.set(uint32_t(kRowGroup) * uint32_t(p.col_tiles));
+  p.by_frags.set(uint32_t(p.frags));
   for (int r = 0; r < g->P; ++r) {
     ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, 128);
     ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.kn ? 128 : p.bn / 2);

@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import sys
+from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -176,14 +177,15 @@ def lib() -> C.CDLL:
         L.compass_head_workspace_bytes.argtypes = [C.POINTER(Head), C.c_int, C.POINTER(C.c_size_t)]
         L.compass_head_loss.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, vp, C.c_size_t, vp]
         L.compass_head_loss_backward.argtypes = [C.POINTER(Head), pp, pp, vp, vp, vp, pp, pp, vp, C.c_size_t, vp]
-        L.compass_rms_norm.argtypes = [C.POINTER(Norm), pp, pp, vp, pp, pp, C.c_int, pp, pp, vp, vp]
+        # (arrays of pointers by their address: several lie in one)
+        L.compass_rms_norm.argtypes = [C.POINTER(Norm), vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, vp]
         L.compass_rms_norm_workspace_bytes.argtypes = [C.POINTER(Norm), C.POINTER(C.c_size_t)]
-        L.compass_rms_norm_backward.argtypes = [C.POINTER(Norm), pp, pp, vp, vp, pp, pp, vp, vp, C.c_size_t, vp]
-        L.compass_quantize.argtypes = L.compass_dequantize.argtypes = [C.POINTER(Quant), pp, pp, pp, vp]
+        L.compass_rms_norm_backward.argtypes = [C.POINTER(Norm), vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.compass_quantize.argtypes = L.compass_dequantize.argtypes = [C.POINTER(Quant), vp, vp, vp, vp]
         L.compass_8bit_workspace_bytes.argtypes = [C.POINTER(Problem), C.POINTER(C.c_size_t)]
         for name in ("compass_ag_gemm_8bit", "compass_gemm_rs_8bit"):
-            getattr(L, name).argtypes = [C.POINTER(Problem), pp, pp, pp, pp, pp, vp, C.c_size_t, vp]
-        L.compass_weight_grad_8bit.argtypes = [C.POINTER(Problem), C.c_int, C.c_int, pp, pp, pp, pp, vp, C.c_size_t, vp]
+            getattr(L, name).argtypes = [C.POINTER(Problem), vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.compass_weight_grad_8bit.argtypes = [C.POINTER(Problem), C.c_int, C.c_int, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.compass_set_wait_limit_us.argtypes = [C.c_uint32]
         L.compass_test_drop_flag_writes.argtypes = [C.c_int]
         L.compass_tensor_map_cache_stats.argtypes = [C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
@@ -620,30 +622,51 @@ def scale_shape(rows: int, cols: int, block_rows: int = 1):
     return -(-rows // block_rows), -(-cols // 128)
 
 
-def _type8(format: int):
-    import torch
-    kinds = {DTYPE_E4M3: torch.float8_e4m3fn, DTYPE_E5M2: torch.float8_e5m2}
-    if format not in kinds:
-        raise ValueError(f"unknown 8-bit type {format}")
-    return kinds[format]
+_TYPES: dict = {}
 
 
-def _matrices(name: str, tensors: Sequence, n: int, dtype, shape, here):
-    if len(tensors) != n:
-        raise ValueError(f"{name}: want {n} tensors, got {len(tensors)}")
-    return _pointers([_tensor(name, t, dtype, shape, here) for t in tensors])
+def _types():
+    """torch's types by the library's numbers, and that of the scales."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({DTYPE_BF16: torch.bfloat16, DTYPE_FP32: torch.float32, DTYPE_E4M3: torch.float8_e4m3fn, DTYPE_E5M2: torch.float8_e5m2,
+                       "scale": torch.float8_e8m0fnu})
+    return _TYPES
 
 
-def _scales(name: str, tensors: Sequence, n: int, rows: int, cols: int, here, block_rows: int = 1):
-    import torch
-    return _matrices(name, tensors, n, torch.float8_e8m0fnu, scale_shape(rows, cols, block_rows), here)
+_FULL, _EIGHT = (DTYPE_BF16, DTYPE_FP32), (DTYPE_E4M3, DTYPE_E5M2)
+
+
+def _type(kind: int, which: tuple):
+    if kind not in which:
+        raise ValueError(f"unknown {'8-bit' if which is _EIGHT else 'element'} type {kind}")
+    return _types()[kind]
+
+
+def _arrays(P: int, here, *groups):
+    """Arrays of P pointers to (name, tensors or None, type, shape), one behind the other: what keeps them, and their addresses."""
+    flat, at = [], []
+    for name, tensors, dtype, shape in groups:
+        if tensors is None:
+            at.append(None)
+            continue
+        if len(tensors) != P:
+            raise ValueError(f"{name}: want {P} tensors, got {len(tensors)}")
+        at.append(len(flat))
+        for t in tensors:
+            if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != here):
+                _tensor(name, t, dtype, shape, here)       # raises (None is the library's to refuse)
+            flat.append(0 if t is None else t.data_ptr())
+    kept = array("Q", flat)        # (a quarter of the time of a ctypes array)
+    base = kept.buffer_info()[0]
+    return kept, [None if i is None else base + 8 * i for i in at]
 
 
 def alloc_8bit(n: int, rows: int, cols: int, format: int = DTYPE_E4M3, block_rows: int = 1, device="cuda"):
     """n matrices in 8 bits and their scales, not initialised."""
     import torch
-    return ([torch.empty(rows, cols, device=device, dtype=_type8(format)) for _ in range(n)],
-            [torch.empty(scale_shape(rows, cols, block_rows), device=device, dtype=torch.float8_e8m0fnu) for _ in range(n)])
+    return ([torch.empty(rows, cols, device=device, dtype=_type(format, _EIGHT)) for _ in range(n)],
+            [torch.empty(scale_shape(rows, cols, block_rows), device=device, dtype=_types()["scale"]) for _ in range(n)])
 
 
 def make_rms_norm(P: int, M: int, hidden: int, eps: float = 1e-6, dtype: int = DTYPE_BF16, param_dtype: Optional[int] = None) -> Norm:
@@ -655,13 +678,12 @@ def compass_rms_norm(norm: Norm, X: Sequence, gamma, Y: Optional[Sequence] = Non
                      format: int = DTYPE_E4M3, stream=None) -> None:
     """Root-mean-square norm of X, or of summed = X + residual, into Y, into Y8 with its scales, or both; gamma may be None (1)."""
     n, here = norm, _here()
-    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
-    each = n.M // n.P if n.P else 0
-    _check(lib().compass_rms_norm(C.byref(n), rows("X", X), rows("residual", residual), _vector("gamma", gamma, n.hidden, here, n.param_dtype),
-                                  rows("summed", summed), rows("Y", Y), format,
-                                  None if Y8 is None else _matrices("Y8", Y8, n.P, _type8(format), (each, n.hidden), here),
-                                  None if scale is None else _scales("scale", scale, n.P, each, n.hidden, here),
-                                  _vector("rstd", rstd, n.M, here), _stream_handle(stream, here)), "compass_rms_norm")
+    P, M, H, kind = n.P, n.M, n.hidden, _type(n.dtype, _FULL)
+    rows = (M // P if P else 0, H)
+    kept, at = _arrays(P, here, ("X", X, kind, rows), ("residual", residual, kind, rows), ("summed", summed, kind, rows), ("Y", Y, kind, rows),
+                       ("Y8", Y8, None if Y8 is None else _type(format, _EIGHT), rows), ("scale", scale, _types()["scale"], (rows[0], -(-H // 128))))
+    _check(lib().compass_rms_norm(C.byref(n), at[0], at[1], _vector("gamma", gamma, H, here, n.param_dtype), at[2], at[3], format, at[4], at[5],
+                                  _vector("rstd", rstd, M, here), _stream_handle(stream, here)), "compass_rms_norm")
 
 
 def compass_rms_norm_workspace_bytes(norm: Norm) -> int:
@@ -679,10 +701,11 @@ def compass_rms_norm_backward(norm: Norm, dY: Sequence, X: Sequence, gamma, rstd
     """dX (+ dsum, the gradient that reaches X past the norm) and dgamma (None: left out) summed over all M rows."""
     n, here = norm, _here()
     p, size = _op_workspace(workspace, here)
-    rows = lambda name, t: _row_shards(name, t, n.P, n.M, n.hidden, n.dtype, here)  # noqa: E731
-    _check(lib().compass_rms_norm_backward(C.byref(n), rows("dY", dY), rows("X", X), _vector("gamma", gamma, n.hidden, here, n.param_dtype),
-                                           _vector("rstd", rstd, n.M, here), rows("dsum", dsum), rows("dX", dX),
-                                           _vector("dgamma", dgamma, n.hidden, here, n.param_dtype), p, size, _stream_handle(stream, here)),
+    P, M, H, kind = n.P, n.M, n.hidden, _type(n.dtype, _FULL)
+    rows = (M // P if P else 0, H)
+    kept, at = _arrays(P, here, ("dY", dY, kind, rows), ("X", X, kind, rows), ("dsum", dsum, kind, rows), ("dX", dX, kind, rows))
+    _check(lib().compass_rms_norm_backward(C.byref(n), at[0], at[1], _vector("gamma", gamma, H, here, n.param_dtype), _vector("rstd", rstd, M, here),
+                                           at[2], at[3], _vector("dgamma", dgamma, H, here, n.param_dtype), p, size, _stream_handle(stream, here)),
            "compass_rms_norm_backward")
 
 
@@ -691,24 +714,25 @@ def make_quant(P: int, M: int, cols: int, dtype: int = DTYPE_BF16, format: int =
 
 
 def _quant(quant: Quant, X: Sequence, Q: Sequence, scale: Sequence, here):
-    q, each = quant, quant.M // quant.P if quant.P else 0
+    q, P = quant, quant.P
     if q.block_rows < 1:
         raise ValueError(f"unknown block of {q.block_rows} rows")
-    return (_row_shards("X", X, q.P, q.M, q.cols, q.dtype, here), _matrices("Q", Q, q.P, _type8(q.format), (each, q.cols), here),
-            _scales("scale", scale, q.P, each, q.cols, here, q.block_rows))
+    rows = (q.M // P if P else 0, q.cols)
+    return _arrays(P, here, ("X", X, _type(q.dtype, _FULL), rows), ("Q", Q, _type(q.format, _EIGHT), rows),
+                   ("scale", scale, _types()["scale"], scale_shape(*rows, q.block_rows)))
 
 
 def compass_quantize(quant: Quant, X: Sequence, Q: Sequence, scale: Sequence, stream=None) -> None:
     """X in 8 bits: values and a power of two for each run of 128 columns or each 128 x 128 block."""
     here = _here()
-    x, q, s = _quant(quant, X, Q, scale, here)
+    kept, (x, q, s) = _quant(quant, X, Q, scale, here)
     _check(lib().compass_quantize(C.byref(quant), x, q, s, _stream_handle(stream, here)), "compass_quantize")
 
 
 def compass_dequantize(quant: Quant, Q: Sequence, scale: Sequence, X: Sequence, stream=None) -> None:
     """X = scale * Q."""
     here = _here()
-    x, q, s = _quant(quant, X, Q, scale, here)
+    kept, (x, q, s) = _quant(quant, X, Q, scale, here)
     _check(lib().compass_dequantize(C.byref(quant), q, s, x, _stream_handle(stream, here)), "compass_dequantize")
 
 
@@ -724,15 +748,16 @@ def alloc_8bit_workspace(problem: Problem, device="cuda"):
 
 
 def _product_8bit(name: str, op: int, g: Problem, A: Sequence, A_scale: Sequence, B: Sequence, B_scale: Sequence, out: Sequence, workspace, stream):
-    import torch
     here = _here()
     p, size = _op_workspace(workspace, here)
-    each = g.M // g.P if g.P else 0
-    a_rows, out_rows = (each, g.M) if op == OP_AG_GEMM else (g.M, each)
-    b_shape = (g.K, g.N) if g.b_layout == B_KN else (g.N, g.K)
-    _check(getattr(lib(), name)(C.byref(g), _matrices("A", A, g.P, _type8(g.dtype), (a_rows, g.K), here), _scales("A_scale", A_scale, g.P, a_rows, g.K, here),
-                                _matrices("B", B, g.P, torch.float8_e4m3fn, b_shape, here), _scales("B_scale", B_scale, g.P, *b_shape, here, 128),
-                                _matrices("out", out, g.P, torch.bfloat16, (out_rows, g.N), here), p, size, _stream_handle(stream, here)), name)
+    P, M, N, K, kinds = g.P, g.M, g.N, g.K, _types()
+    each = M // P if P else 0
+    a_rows, out_rows = (each, M) if op == OP_AG_GEMM else (M, each)
+    b_shape = (K, N) if g.b_layout == B_KN else (N, K)
+    kept, at = _arrays(P, here, ("A", A, _type(g.dtype, _EIGHT), (a_rows, K)), ("A_scale", A_scale, kinds["scale"], (a_rows, -(-K // 128))),
+                       ("B", B, kinds[DTYPE_E4M3], b_shape), ("B_scale", B_scale, kinds["scale"], (-(-b_shape[0] // 128), -(-b_shape[1] // 128))),
+                       ("out", out, kinds[DTYPE_BF16], (out_rows, N)))
+    _check(getattr(lib(), name)(C.byref(g), *at, p, size, _stream_handle(stream, here)), name)
 
 
 def compass_ag_gemm_8bit(problem: Problem, A: Sequence, A_scale: Sequence, B: Sequence, B_scale: Sequence, Cout: Sequence, workspace,
@@ -752,14 +777,14 @@ def compass_weight_grad_8bit(problem: Problem, G: Sequence, X: Sequence, X_scale
     """dW[r] (+)= G[r].T @ X[r] for the product that `problem` describes, X as it was kept in 8 bits.
 
     AllGather: G[r] is the gradient of C[r], X the row shards.  ReduceScatter: G the gradient of Out in row shards, X[r] rank r's."""
-    import torch
     g, here = problem, _here()
     p, size = _op_workspace(workspace, here)
-    each = g.M // g.P if g.P else 0
-    g_rows, x_rows = (g.M, each) if g.op == OP_AG_GEMM else (each, g.M)
-    _check(lib().compass_weight_grad_8bit(C.byref(g), grad_dtype, int(accumulate), _matrices("G", G, g.P, torch.bfloat16, (g_rows, g.N), here),
-                                          _matrices("X", X, g.P, _type8(g.dtype), (x_rows, g.K), here), _scales("X_scale", X_scale, g.P, x_rows, g.K, here),
-                                          _matrices("dW", dW, g.P, _torch_dtype(grad_dtype), (g.N, g.K), here), p, size, _stream_handle(stream, here)),
+    P, M, N, K, kinds = g.P, g.M, g.N, g.K, _types()
+    each = M // P if P else 0
+    g_rows, x_rows = (M, each) if g.op == OP_AG_GEMM else (each, M)
+    kept, at = _arrays(P, here, ("G", G, kinds[DTYPE_BF16], (g_rows, N)), ("X", X, _type(g.dtype, _EIGHT), (x_rows, K)),
+                       ("X_scale", X_scale, kinds["scale"], (x_rows, -(-K // 128))), ("dW", dW, _type(grad_dtype, _FULL), (N, K)))
+    _check(lib().compass_weight_grad_8bit(C.byref(g), grad_dtype, int(accumulate), *at, p, size, _stream_handle(stream, here)),
            "compass_weight_grad_8bit")
 
 

@@ -545,6 +545,17 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   const uint32_t tmem_base = ctl->tmem_base;
   const uint32_t scale_a = tmem_base + uint32_t(p.cols), scale_b = scale_a + 8;      // 2 x 4 and 2 x 8 columns
   launch_dependents();
+  // Scales of the activations in column `i * 32 + lane` (columns without any: any): the row in its tensor, and with AllGather, where the
+  // tensors differ from lane to lane, its address.
+  int64_t row_at[8];
+  if (warp == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int col = i * 32 + lane, s = int(p.slot.div(uint32_t(col)));
+      row_at[i] = int64_t(min(col - s * int(p.slot.d), (p.rs ? p.m * p.P : p.m) - 1)) * p.atoms;
+      if (!p.rs) row_at[i] += reinterpret_cast<int64_t>(p.sa[min(s, p.P - 1)]);
+    }
+  }
   wait_for_previous_kernel();
 
   if (warp == 0) {
@@ -634,23 +645,16 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       uint32_t w;
       bool words;
     };
-    // the row of activations of column `i * 32 + lane`, in its tensor
-    int tensor[8], row[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int col = i * 32 + lane, s = int(p.slot.div(uint32_t(col)));
-      tensor[i] = min(s, p.rs ? 0 : p.P - 1);
-      row[i] = min(col - s * int(p.slot.d), (p.rs ? p.m * p.P : p.m) - 1);      // (columns without one: any scale)
-    }
     FewWalk at(p, from, to);
     auto load = [&](Group& x) {      // of the group that begins here, and on behind it
       if (at.left == 0) return;
       const int a = at.a, n = at.group(p);
       x.words = p.whole_words && n == 4 && (a & 3) == 0;
       x.w = weight_byte(p, p.rs ? at.seg : rank, n0 >> 7, a, n, lane);
+      const int64_t base = p.rs ? reinterpret_cast<int64_t>(p.sa[at.seg]) : 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i * 32 < p.cols) x.x[i].load(p.sa[p.rs ? at.seg : tensor[i]] + int64_t(row[i]) * p.atoms + a, n, x.words);
+        if (i * 32 < p.cols) x.x[i].load(reinterpret_cast<const uint8_t*>(row_at[i] + base) + a, n, x.words);
       at.a += n;
       at.left -= n;
       if (at.a == p.atoms) {
@@ -733,7 +737,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     tc_fence_before_sync();
   }
   if (p.splits > 1) {
-    cluster_arrive();
+    // One warp's release stands for all, behind the block's barrier.  (A warp arrives as one: its threads must not part here.)
+    __syncthreads();
+    if (warp == 0) cluster_arrive();
+    else cluster_arrive_relaxed();
     cluster_wait();
     if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
       // four neighbouring sums a thread, those of all CTAs in flight together
@@ -765,7 +772,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         }
       }
     }
-    cluster_arrive();      // nobody's memory goes while it is read
+    __syncwarp();
+    cluster_arrive_relaxed();      // nobody's memory goes while it is read
     cluster_wait();
   } else {
     __syncthreads();
@@ -920,11 +928,11 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     // (two barriers of the cluster, and the sums).
     p.splits = 1;
     int64_t best = ceil_div(tiles, f->sms) * all;
-    for (int s = 2; s <= kMostSplits && 2 * s <= all; ++s) {
-      const int64_t cost = ceil_div(tiles * s, f->sms) * ceil_div(all, s) + kSplitCost;
-      if (tiles * s <= (cols <= 128 ? 2 : 1) * f->sms && cost < best) {
+    for (int n = 2; n <= kMostSplits && 2 * n <= all; ++n) {
+      const int64_t cost = ceil_div(tiles * n, f->sms) * ceil_div(all, n) + kSplitCost;
+      if (tiles * n <= (cols <= 128 ? 2 : 1) * f->sms && cost < best) {
         best = cost;
-        p.splits = s;
+        p.splits = n;
       }
     }
     p.all = all;

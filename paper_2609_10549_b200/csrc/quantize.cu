@@ -13,6 +13,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnit = 16;            // elements of a thread's unit: 8 units are a run of 128
 constexpr int kItems = 4;            // units of a thread that are in flight together
+constexpr int kRowItems = 2;         // the same where runs are brought to 8 bits: fewer registers, more blocks (16384 x 8192 BF16, 2, 4, 8: 64, 77, 71 us)
 constexpr int kChunkUnits = 1024;    // units of a row that one block takes at most
 
 struct QuantParams {
@@ -132,17 +133,17 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_co
   launch_dependents();
   wait_for_previous_kernel();
   const uint32_t n = p.rows * p.units.d;
-  for (uint32_t i0 = threadIdx.x; i0 < n + threadIdx.x; i0 += kThreads * kItems) {      // (the same number of turns for all lanes)
-    Unit<T> u[kItems];
-    Place at[kItems];
+  for (uint32_t i0 = threadIdx.x; i0 < n + threadIdx.x; i0 += kThreads * kRowItems) {      // (the same number of turns for all lanes)
+    Unit<T> u[kRowItems];
+    Place at[kRowItems];
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < kRowItems; ++k) {
       at[k] = place_of(p, i0 + k * kThreads);
       if (at[k].live) u[k].load(p.x.row<T>(at[k].row, p.cols) + at[k].col, p.wide);
       else u[k].zero();
     }
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < kRowItems; ++k) {
       float x[kUnit];
       u[k].get(x);
       float top = largest_of_8(largest(x));
@@ -159,10 +160,11 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_co
   }
 }
 
-// A block of 128 x 128, four units a thread.
+constexpr int kBlockItems = 2, kBlockThreads = 1024 / kBlockItems;
+// A block of 128 x 128, two units a thread.
 template <typename T, int kFormat>
-__global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const __grid_constant__ QuantParams p) {
-  __shared__ float tops[2][kThreads / 32];
+__global__ void __launch_bounds__(kBlockThreads) quantize_blocks_kernel(const __grid_constant__ QuantParams p) {
+  __shared__ float tops[2][kBlockThreads / 32];
   launch_dependents();
   wait_for_previous_kernel();
   const uint32_t line = p.block_cols.div(blockIdx.x), col = blockIdx.x - line * p.block_cols.d;
@@ -170,11 +172,11 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const __grid_
   const T* x = static_cast<const T*>(p.x.ptr[shard]);
   uint8_t* q = static_cast<uint8_t*>(p.q.ptr[shard]);
   const int64_t c = int64_t(col) * 128 + (threadIdx.x & 7) * kUnit;
-  Unit<T> u[kItems];
+  Unit<T> u[kBlockItems];
   float top = 0.f;
-  auto row_of = [&](int k) { return row0 + k * (kThreads / 8) + (threadIdx.x >> 3); };
+  auto row_of = [&](int k) { return row0 + k * (kBlockThreads / 8) + (threadIdx.x >> 3); };
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
+  for (int k = 0; k < kBlockItems; ++k) {
     if (row_of(k) < p.x.rows.d && c < p.cols) u[k].load(x + int64_t(row_of(k)) * p.cols + c, p.wide);
     else u[k].zero();
   }
@@ -184,12 +186,12 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const __grid_
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, part[i]);
+    for (int i = 0; i < kBlockThreads / 32; ++i) m = fmaxf(m, part[i]);
     return m;
   };
   float y[kUnit];
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
+  for (int k = 0; k < kBlockItems; ++k) {
     u[k].get(y);
     top = fmaxf(top, largest(y));
   }
@@ -198,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const __grid_
   if (infinite) {
     top = 0.f;
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < kBlockItems; ++k) {
       u[k].get(y);
       infinite_to_nan(y);
       top = fmaxf(top, largest(y));
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(kThreads) quantize_blocks_kernel(const __grid_
   }
   const uint32_t b = scale_byte_of<kFormat>(__float_as_uint(top));
 #pragma unroll
-  for (int k = 0; k < kItems; ++k) {
+  for (int k = 0; k < kBlockItems; ++k) {
     u[k].get(y);
     if (infinite) infinite_to_nan(y);
     if (row_of(k) < p.x.rows.d && c < p.cols)
@@ -294,7 +296,7 @@ int run_quantize(const compass_quant* q, QuantParams& p, cudaStream_t stream) {
     const int64_t lines = ceil_div(q->M / q->P, 128);
     p.block_rows.set(uint32_t(lines));
     p.block_cols.set(uint32_t(p.blocks));
-    return launch(quantize_blocks_kernel<T, kFormat>, q->P * lines * p.blocks, kThreads, 0, stream, true, p);
+    return launch(quantize_blocks_kernel<T, kFormat>, q->P * lines * p.blocks, kBlockThreads, 0, stream, true, p);
   }
   return launch(quantize_rows_kernel<T, kFormat>, ceil_div(q->M, p.rows) * p.chunks.d, kThreads, 0, stream, true, p);
 }

@@ -31,41 +31,72 @@ struct RmsParams {
 
 constexpr int kNone = -1;      // no output in 8 bits
 
-// V neighbouring values of a run of 128 that lies in 128 / V neighbouring lanes, to 8 bits; all lanes of the warp take part, and
-// `live` ones store.
-template <int kFormat, int V>
-__device__ __forceinline__ void store_8bit(float (&x)[V], uint8_t* to, uint8_t* scale, bool live) {
-  constexpr int kLanes = 128 / V;
+// NVT vectors of V neighbouring values times `factor`, `step` elements apart, to 8 bits; a run of 128 lies in 128 / V neighbouring
+// lanes.  All lanes of the warp take part; the first `live` vectors are stored.  (The factor comes in behind the maximum, which is
+// that of the products all the same: rounding keeps their order.)
+template <int kFormat, int V, int NVT>
+__device__ __forceinline__ void store_8bit(F2 (&x)[V * NVT / 2], float factor, uint8_t* to, uint8_t* scale, int step, int live) {
+  constexpr int kLanes = 128 / V, kPer = V / 2;
+  float top[NVT];
   auto largest = [&] {
-    float m = 0.f;
+    bool infinite = false;
 #pragma unroll
-    for (int j = 0; j < V; ++j) m = fmaxf(m, fabsf(x[j]));
+    for (int i = 0; i < NVT; ++i) {
+      float m = 0.f;
 #pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    return m;
+      for (int j = 0; j < kPer; ++j) {
+        const float2 q = of(x[i * kPer + j]);
+        m = fmaxf(m, fmaxf(fabsf(q.x), fabsf(q.y)));
+      }
+#pragma unroll
+      for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      top[i] = m * factor;
+      infinite |= !(top[i] < INFINITY);
+    }
+    return infinite;
   };
-  float top = largest();
-  if (__any_sync(0xffffffffu, !(top < INFINITY))) {
+  if (__any_sync(0xffffffffu, largest())) {
+    // (times the factor now: a product with it may be what is infinite)
+    auto finite = [&](float a) { return fabsf(a * factor) < INFINITY ? a * factor : __uint_as_float(0x7FC00000u); };
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = fabsf(x[j]) < INFINITY ? x[j] : __uint_as_float(0x7FC00000u);
-    top = largest();
+    for (int j = 0; j < kPer * NVT; ++j) {
+      const float2 q = of(x[j]);
+      x[j] = f2(finite(q.x), finite(q.y));
+    }
+    factor = 1.f;
+    largest();
   }
-  const uint32_t b = scale_byte_of<kFormat>(__float_as_uint(top));
-  const float f = inverse_scale(b);
-  if (!live) return;
-  if constexpr (V == 8)
-    *reinterpret_cast<uint2*>(to) =
-        make_uint2(pack8x4<kFormat>(x[0] * f, x[1] * f, x[2] * f, x[3] * f), pack8x4<kFormat>(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
-  else
-    *reinterpret_cast<uint32_t*>(to) = pack8x4<kFormat>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-  if (threadIdx.x % kLanes == 0) *scale = uint8_t(b);
+#pragma unroll
+  for (int i = 0; i < NVT; ++i) {
+    if (i >= live) break;
+    const uint32_t b = scale_byte_of<kFormat>(__float_as_uint(top[i]));
+    const F2 f = f2(inverse_scale(b));
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const F2 g = f2(factor);
+      const float2 lo = of(x[i * kPer + 2 * j] * g * f), hi = of(x[i * kPer + 2 * j + 1] * g * f);
+      w[j] = pack8x4<kFormat>(lo.x, lo.y, hi.x, hi.y);
+    }
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(to + i * step) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(to + i * step) = w[0];
+    if (threadIdx.x % kLanes == 0) scale[i * step / 128] = uint8_t(b);
+  }
 }
 
 // ---- forward -------------------------------------------------------------------
 // A row per group of kTpr threads, NVT vectors of V elements a thread.  kKeep: gamma stays in registers.
+// Elements of a row per thread: what a row costs every thread is shared by this many.  The output in 8 bits alone is bound by
+// instructions, and takes 32 in BF16; with the residual, four streams of memory, it goes better with more threads a row: to 8 bits, us,
+// 16 and 32: 16384 x 8192: 110 and 80, with the residual 151 and 169; 16384 x 4096: 59 and 41, 78 and 85; 16384 x 1024: 16 and 13, 22 and
+// 21.  In BF16: 16384 x 4096: 44 and 48; 4096 x 8192: 25 and 23.
+template <typename T, int V, bool kResidual, int kFormat>
+constexpr int kForwardElems = V == 8 ? (kFormat != kNone && !kResidual ? 32 : 16) : V == 4 ? 16 : 8;
+template <typename T, int V, int NVT, int kThreads, bool kResidual>
+using ForwardRing = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads, 200 * 1024>;
 template <typename T, int V, int NVT, int kThreads, int kTpr, bool kKeep, bool kResidual, int kFormat>
 __global__ void __launch_bounds__(kThreads, 1) rms_forward_kernel(const __grid_constant__ RmsParams p) {
-  using Ring = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>;
+  using Ring = ForwardRing<T, V, NVT, kThreads, kResidual>;
   __shared__ float red[2][32];
   extern __shared__ uint4 raw[];
   const int groups = blockDim.x / kTpr, group = threadIdx.x / kTpr, t = threadIdx.x - group * kTpr;
@@ -92,6 +123,7 @@ __global__ void __launch_bounds__(kThreads, 1) rms_forward_kernel(const __grid_c
   constexpr int kPairs = V * NVT / 2;
   F2 g[kPairs];
   if constexpr (kKeep) load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, kTpr, t, H);
+  const int own = min(NVT, max(0, (H / V - t + kTpr - 1) / kTpr));      // vectors of a row that this thread holds
   for (uint32_t turn = 0; row < p.M; ++turn, row += stride) {
     const RowAt at = p.x.at(row, H);
     Words<T, V, NVT> x;
@@ -117,24 +149,17 @@ __global__ void __launch_bounds__(kThreads, 1) rms_forward_kernel(const __grid_c
     const float rstd = 1.0f / sqrtf(row_sum(sum_of(sq[0] + sq[1]), kTpr, red[turn & 1]) * inv + p.eps);
     if constexpr (!kKeep) load_params<V, NVT>(g, p.gamma, p.param_fp32, 1.f, kTpr, t, H);
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) h[k] = h[k] * f2(rstd) * g[k];
+    for (int k = 0; k < kPairs; ++k) h[k] = h[k] * g[k];
     if (kFormat == kNone || p.has_y) {
-      x.set(h);
+      F2 y[kPairs];
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k) y[k] = h[k] * f2(rstd);
+      x.set(y);
       x.store(p.y.row<T>(at), kTpr, t, H);
     }
     if constexpr (kFormat != kNone) {
-#pragma unroll
-      for (int i = 0; i < NVT; ++i) {
-        const int c = (i * kTpr + t) * V;
-        float v[V];
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-          const float2 q = of(h[(i * V + j) / 2]);
-          v[j] = q.x;
-          v[j + 1] = q.y;
-        }
-        store_8bit<kFormat, V>(v, p.y8.row<uint8_t>(at) + c, p.scale.row<uint8_t>(row, p.blocks) + (c >> 7), c < H);
-      }
+      uint8_t* scale = static_cast<uint8_t*>(p.scale.ptr[at.shard]) + (row - at.shard * p.x.rows.d) * p.blocks + t * V / 128;
+      store_8bit<kFormat, V, NVT>(h, rstd, p.y8.row<uint8_t>(at) + t * V, scale, kTpr * V, own);
     }
     if (t == 0 && p.rstd) p.rstd[row] = rstd;
   }
@@ -178,7 +203,12 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const __grid_con
       for (int j = 0; j < V; ++j) a[j] = a[j] * rstd * g[j];
       if (kFormat == kNone || p.has_y) store_vec(p.y.row<T>(row, H) + c, a);
     }
-    if constexpr (kFormat != kNone) store_8bit<kFormat, V>(a, p.y8.row<uint8_t>(row, H) + c, p.scale.row<uint8_t>(row, p.blocks) + (c >> 7), live);
+    if constexpr (kFormat != kNone) {
+      F2 x[V / 2];
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) x[j] = f2(a[2 * j], a[2 * j + 1]);
+      store_8bit<kFormat, V, 1>(x, 1.f, p.y8.row<uint8_t>(row, H) + c, p.scale.row<uint8_t>(row, p.blocks) + (c >> 7), 0, live);
+    }
   }
   if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
 }
@@ -424,24 +454,25 @@ BackwardPlan backward_plan(const compass_norm* n, bool whole) {
 
 template <typename T, int V, int NVT, int kThreads, int kTpr, bool kKeep, bool kResidual, int kFormat>
 int run_forward(const RmsParams& p, cudaStream_t stream) {
-  constexpr size_t smem = RowRing<T, V, NVT, kResidual ? 2 : 1, kThreads>::kSmemBytes;
+  constexpr size_t smem = ForwardRing<T, V, NVT, kThreads, kResidual>::kSmemBytes;
   auto kernel = rms_forward_kernel<T, V, NVT, kThreads, kTpr, kKeep, kResidual, kFormat>;
   static std::atomic<uint64_t> allowed{0};
   const int st = allow_smem(reinterpret_cast<const void*>(kernel), smem, &allowed);
   if (st != COMPASS_OK) return st;
   // few rows: a block each, for the shortest way through; else blocks of several that walk the rows
   const int groups = p.M <= kSms || kTpr * 2 > kThreads ? 1 : rows_per_block(kTpr, kThreads);
-  const int64_t need = ceil_div(p.M, groups), most = smem ? kSms : kSms * (kThreads / (kTpr * groups));
+  const int64_t need = ceil_div(p.M, groups), most = kSms * (smem ? 1 : kThreads / (kTpr * groups));
   return launch(kernel, need < most ? need : most, kTpr * groups, smem, stream, true, p);
 }
 
-// Up to 8192 elements a row: gamma in registers.  Up to 16384: 16 elements per thread.
+// Up to 8192 elements a row (or 16384, at 32 a thread): gamma in registers.  Up to 16384: 16 elements per thread.
 template <typename T, int V, bool kResidual, int kFormat>
 int pick_forward(const RmsParams& p, cudaStream_t stream) {
-  const int64_t H = p.hidden;
-  constexpr int E = kElems<T, V>, kThreads = int(kWidest) / E;
-  if (H > kWidest) return run_forward<T, V, 16 / V, 1024, 1024, false, kResidual, kFormat>(p, stream);
-  return with_tpr<kThreads>(threads_per_row(H, E), [&](auto tpr) {
+  constexpr int E = kForwardElems<T, V, kResidual, kFormat>, kThreads = V == 1 ? 1024 : 512;
+  if constexpr (E * kThreads < 2 * kWidest) {
+    if (p.hidden > kWidest) return run_forward<T, V, 16 / V, 1024, 1024, false, kResidual, kFormat>(p, stream);
+  }
+  return with_tpr<kThreads>(threads_per_row(p.hidden, E), [&](auto tpr) {
     return run_forward<T, V, E / V, kThreads, decltype(tpr)::value, true, kResidual, kFormat>(p, stream);
   });
 }

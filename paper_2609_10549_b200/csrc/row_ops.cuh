@@ -136,12 +136,11 @@ struct Raw {
 // The next rows of kArrays tensors on their way from HBM: every thread copies its own elements to shared memory, kDepth rows
 // ahead, and reads back only what it copied, so that no barrier is needed and nothing is held in registers.  Elements of two
 // bytes (rows that are not whole vectors) cannot be copied this way: those are loaded when they are taken.
-template <typename T, int V, int NVT, int kArrays, int kThreads>
+template <typename T, int V, int NVT, int kArrays, int kThreads, int kRoom = 160 * 1024>
 struct RowRing {
   static constexpr int kBytes = V * int(sizeof(T));
   static constexpr bool kAsync = kBytes >= 4;
   static constexpr int kRowBytes = kArrays * NVT * kThreads * kBytes;
-  static constexpr int kRoom = 160 * 1024;
   static constexpr int kDepth = !kAsync ? 1 : kRoom / kRowBytes > 8 ? 8 : kRoom / kRowBytes < 1 ? 1 : kRoom / kRowBytes;
   static constexpr size_t kSmemBytes = kAsync ? size_t(kDepth) * kRowBytes : 0;
   uint32_t base;      // this thread's slot 0

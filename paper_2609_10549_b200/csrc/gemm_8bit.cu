@@ -647,11 +647,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       RowScales x[8];
       uint32_t w;
       bool words;
+      int n;         // 0: behind the last
     };
     FewWalk at(p, from, to);
     auto load = [&](Group& x) {      // of the group that begins here, and on behind it
+      x.n = 0;
       if (at.left == 0) return;
-      const int a = at.a, n = at.group(p);
+      const int a = at.a, n = x.n = at.group(p);
       x.words = p.whole_words && n == 4 && (a & 3) == 0;
       x.w = weight_byte(p, p.rs ? at.seg : rank, n0 >> 7, a, n, lane);
       const int64_t base = p.rs ? reinterpret_cast<int64_t>(p.sa[at.seg]) : 0;
@@ -666,28 +668,32 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       }
     };
     uint32_t group = 0;
-    bool ok = true, more = to > from;
-    Group x, next;
-    load(x);
-    for (; more; ++group) {
-      more = at.left > 0;
-      load(next);
-      const uint32_t v = __shfl_sync(0xffffffffu, weight_words(x.w, lane), 0);
-      uint32_t w[8];
+    bool ok = true;
+    Group x[2];      // (two, so that what is on its way is not moved)
+    load(x[0]);
+    load(x[1]);
+    while (ok && x[0].n > 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = i * 32 < p.cols ? x.x[i].word(x.words) : kOne;
-      const uint32_t buf = group & 1u;
-      if (group >= 2) {
-        ok = wait_warp(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t);
-        if (!ok) break;
+      for (int u = 0; u < 2; ++u) {
+        if (!ok || x[u].n == 0) break;
+        const uint32_t v = __shfl_sync(0xffffffffu, weight_words(x[u].w, lane), 0);
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i * 32 < p.cols ? x[u].x[i].word(x[u].words) : kOne;
+        load(x[u]);
+        const uint32_t buf = group & 1u;
+        if (group >= 2) {
+          ok = wait_warp(&ctl->scales_empty[buf], ((group >> 1) - 1) & 1u, wc, SITE_SCALES_EMPTY, t);
+          if (!ok) break;
+        }
+        sh->scales[buf][0][lane] = make_uint4(v, v, v, v);
+        sh->scales[buf][1][lane] = make_uint4(w[0], w[1], w[2], w[3]);
+        sh->scales[buf][2][lane] = make_uint4(w[4], w[5], w[6], w[7]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl->scales_full[buf]);
+        ++group;
       }
-      sh->scales[buf][0][lane] = make_uint4(v, v, v, v);
-      sh->scales[buf][1][lane] = make_uint4(w[0], w[1], w[2], w[3]);
-      sh->scales[buf][2][lane] = make_uint4(w[4], w[5], w[6], w[7]);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl->scales_full[buf]);
-      x = next;
     }
     for (uint32_t i = group < 2u ? group : 2u; ok && i > 0; --i)
       ok = wait_warp(&ctl->scales_empty[(group - i) & 1u], ((group - i) >> 1) & 1u, wc, SITE_DRAIN, -1);
@@ -702,11 +708,6 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     *row = i - s * p.m;
     return s;
   };
-  auto store = [&](int i, int s, int row, int n, float x) {
-    if (n0 + n >= p.N) return;
-    __nv_bfloat16* out = p.rs ? p.out[s] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N;
-    out[n0 + n] = __float2bfloat16_rn(x);
-  };
   bool ok = true;
   float* sums = reinterpret_cast<float*>(smem);      // [column][128], over the stages
   if (warp >= 4) {
@@ -717,69 +718,53 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
         uint32_t v[16];
         tmem_ld_32x32b_x16(tmem_base + (uint32_t(quarter * 32) << 16) + c, v);
         tmem_ld_wait();
-        if (p.splits > 1) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int col = c + i;
-            int row;
-            if (p.rs) {
-              const int s = shard_of(col, &row);
-              if (col < M) store(col, s, row, quarter * 32 + lane, __uint_as_float(v[i]));
-            } else {
-              const int s = int(p.slot.div(uint32_t(col)));
-              row = col - s * int(p.slot.d);
-              if (s < p.P && row < p.m) store(s * p.m + row, s, row, quarter * 32 + lane, __uint_as_float(v[i]));
-            }
-          }
-        }
+        for (int i = 0; i < 16; ++i) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
       }
     }
     tc_fence_before_sync();
   }
+  __syncthreads();
   if (p.splits > 1) {
     // One warp's release stands for all, behind the block's barrier.  (A warp arrives as one: its threads must not part here.)
-    __syncthreads();
     if (warp == 0) cluster_arrive();
     else cluster_arrive_relaxed();
     cluster_wait();
-    if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
-      // four neighbouring sums a thread, those of all CTAs in flight together
-      const uint32_t base = smem_u32(sums);
-      const int n = lane * 4;
-      for (int i = part + p.splits * warp; i < M; i += p.splits * (kFewThreads / 32)) {
-        int row;
-        const int shard = shard_of(i, &row);
-        const uint32_t at = base + uint32_t((p.rs ? i : shard * int(p.slot.d) + row) * 128 + n) * 4;
-        float4 y[kMostSplits];
+  }
+  if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
+    // four neighbouring sums a thread, those of all CTAs of a cluster in flight together
+    const uint32_t base = smem_u32(sums);
+    const int n = lane * 4;
+    for (int i = part + p.splits * warp; i < M; i += p.splits * (kFewThreads / 32)) {
+      int row;
+      const int shard = shard_of(i, &row);
+      const uint32_t at = base + uint32_t((p.rs ? i : shard * int(p.slot.d) + row) * 128 + n) * 4;
+      float4 y[kMostSplits];
 #pragma unroll
-        for (int s = 0; s < kMostSplits; ++s)
-          if (s < p.splits)
-            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w)
-                         : "r"(map_to_cta(at, uint32_t(s))));
-        float4 x = y[0];
+      for (int s = 0; s < kMostSplits; ++s)
+        if (s < p.splits)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w)
+                       : "r"(map_to_cta(at, uint32_t(s))));
+      float4 x = y[0];
 #pragma unroll
-        for (int s = 1; s < kMostSplits; ++s)
-          if (s < p.splits) x.x += y[s].x, x.y += y[s].y, x.z += y[s].z, x.w += y[s].w;
-        __nv_bfloat16* out = (p.rs ? p.out[shard] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N) + n0 + n;
-        if (p.wide) {      // (N is a multiple of 8)
-          if (n0 + n < p.N) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
-        } else {
-          const float z[4] = {x.x, x.y, x.z, x.w};
+      for (int s = 1; s < kMostSplits; ++s)
+        if (s < p.splits) x.x += y[s].x, x.y += y[s].y, x.z += y[s].z, x.w += y[s].w;
+      __nv_bfloat16* out = (p.rs ? p.out[shard] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N) + n0 + n;
+      if (p.wide) {      // (N is a multiple of 8)
+        if (n0 + n < p.N) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+      } else {
+        const float z[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (n0 + n + k < p.N) out[k] = __float2bfloat16_rn(z[k]);
-        }
+        for (int k = 0; k < 4; ++k)
+          if (n0 + n + k < p.N) out[k] = __float2bfloat16_rn(z[k]);
       }
     }
+  }
+  if (p.splits > 1) {
     __syncwarp();
     cluster_arrive_relaxed();      // nobody's memory goes while it is read
     cluster_wait();
-  } else {
-    __syncthreads();
   }
   if (warp == 1) {
     __syncwarp();
@@ -946,8 +931,8 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     int64_t stages = room / stage;
     if (stages > mine) stages = mine;
     if (stages > kFewMostStages) stages = kFewMostStages;
-    // (the cluster's sums lie where the stages were)
-    while (p.splits > 1 && stages * stage < cols * 512) ++stages;
+    // (the sums lie where the stages were)
+    while (stages * stage < cols * 512) ++stages;
     p.stages = int32_t(stages);
     p.tmem_cols = 32;
     while (p.tmem_cols < p.cols + 24) p.tmem_cols *= 2;

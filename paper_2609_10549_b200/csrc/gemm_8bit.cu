@@ -9,7 +9,8 @@
 //
 // Two kernels.  gemm8_pair_kernel: pairs of CTAs, 256 rows x up to 256 columns a tile, for batches.  gemm8_few_kernel: weights on
 // the products' M side, 128 rows a tile, and up to 256 activation rows on the N side, the contraction split over a cluster, for
-// few rows, where the weights' bytes are all the work.
+// few rows, where the weights' bytes are all the work, and for few tiles of a long contraction.  Which one by what they are estimated
+// to take (few_plan, pair_plan).
 #include <mutex>
 
 #include "pipeline.cuh"
@@ -52,10 +53,17 @@ struct Gemm8Params {
   int32_t col_tiles, bn;   // tiles of bn columns
   int32_t n_step;          // whose number is a multiple of this, at the end too: both CTAs load half of them from a 16-byte boundary on
   int32_t total;
+  // rows of a load, those of a matrix of fewer (rows outside one made its loads several times as long); [K][N] weights: 128 of the
+  // contraction, zero behind it
+  int32_t a_box, b_box;
   FastDiv per_rank, per_group, by_frags;      // tiles of a rank, of a group of rows
   // few-rows kernel
-  FastDiv slot;            // accumulator columns per shard (AllGather) or of all rows: rows rounded up to 8
   FastDiv each;            // rows per shard
+  FastDiv by_rows;         // row tiles of a rank's 128-row tile of weights
+  FastDiv pieces;          // of a shard's rows, a row tile each
+  int32_t tile_shards;     // shards of a row tile (AllGather, shards in one piece)
+  int32_t tile_rows;       // rows of a shard in it, what is loaded together
+  FastDiv slot;            // accumulator columns for them: rounded up to 8
   int32_t cols;            // accumulator columns, a multiple of 16
   int32_t n_tiles;         // 128-row tiles of one rank's weights
   int32_t splits;          // CTAs of a cluster, which share a tile's contraction
@@ -165,7 +173,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
   PairShared* sh = reinterpret_cast<PairShared*>(smem + kPairStages * kPairStageBytes);
   PairControl* ctl = &sh->ctl;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int cta = int(cluster_ctarank());
+  const int cta = int(blockIdx.x & 1);      // (the rank in the cluster, known to be the same for all threads)
   const bool leader = cta == 0;
   const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
@@ -195,51 +203,52 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
   cluster_arrive();
   cluster_wait();
   tc_fence_after_sync();
-  const uint32_t tmem_base = ctl->tmem_base;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
   launch_dependents();
   wait_for_previous_kernel();
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
-    if (lane == 0) {
-      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
-      const int b_bytes = (p.kn ? 128 : p.bn / 2) * kAtom;
-      uint32_t j = 0;
-      bool ok = true;
-      for (int t = unit; ok && t < p.total; t += units) {
-        const PairTile c = pair_tile(p, t, cta);
-        const int b0 = int(c.col0) + cta * (c.n / 2);
-        for (int seg = 0; ok && seg < segs; ++seg) {
-          const int q = slice_of(p, c, seg), row = slice_row(p, c), br = p.rs ? q : c.rank;
-          for (int a = 0; a < p.atoms; a += kStageAtoms, ++j) {
-            const uint32_t slot = j % kPairStages;
-            if (j >= kPairStages && !wait_phase(&ctl->empty[slot], (j / kPairStages - 1) & 1u, wc, SITE_EMPTY, t)) {
-              ok = false;
-              break;
-            }
+    // (the whole warp goes through the loop and one lane issues, as below)
+    const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+    const int bytes = (p.a_box + p.b_box) * kAtom;
+    uint32_t j = 0, slot = 0, turn = 0;
+    bool ok = true;
+    for (int t = unit; ok && t < p.total; t += units) {
+      const PairTile c = pair_tile(p, t, cta);
+      const int b0 = int(c.col0) + cta * (c.n / 2);
+      for (int seg = 0; ok && seg < segs; ++seg) {
+        const int q = slice_of(p, c, seg), row = slice_row(p, c), br = p.rs ? q : c.rank;
+        for (int a = 0; a < p.atoms; a += kStageAtoms) {
+          if (turn > 0 && !(ok = wait_warp(&ctl->empty[slot], (turn - 1) & 1u, wc, SITE_EMPTY, t))) break;
+          if (elect_one()) {
             const int n = min(kStageAtoms, p.atoms - a);
             const uint32_t bar = map_to_cta(smem_u32(&ctl->full[slot]), 0);
-            if (leader) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * (kChunkBytes + b_bytes)));
+            if (leader) mbar_arrive_expect_tx(&ctl->full[slot], uint32_t(2 * n * bytes));
             uint8_t* dst = smem + slot * kPairStageBytes;
-            for (int i = 0; i < n; ++i) {
+#pragma unroll
+            for (int i = 0; i < kStageAtoms; ++i) {
+              if (i >= n) break;
               tma_load_2d_pair_hint(dst + i * 2 * kChunkBytes, &p.a[q], bar, (a + i) * kAtom, row, pol);
               if (p.kn) tma_load_2d_pair_hint(dst + (i * 2 + 1) * kChunkBytes, &p.b[br], bar, b0, (a + i) * kAtom, pol);
               else tma_load_2d_pair_hint(dst + (i * 2 + 1) * kChunkBytes, &p.b[br], bar, (a + i) * kAtom, b0, pol);
             }
           }
-        }
-      }
-      // leave only when the last stages have been read (the leader's products read both CTAs' memory)
-      const uint32_t back = j < uint32_t(kPairStages) ? j : uint32_t(kPairStages);
-      for (uint32_t i = 1; i <= back; ++i) {
-        const uint32_t r = j - i;
-        if (!wait_phase(&ctl->empty[r % kPairStages], (r / kPairStages) & 1u, wc, SITE_DRAIN, -1)) {
-          if (leader)
-            for (uint32_t k = 1; k <= back; ++k) wait_settled(&ctl->full[(j - k) % kPairStages], ((j - k) / kPairStages) & 1u);
-          break;
+          __syncwarp();
+          ++j;
+          if (++slot == kPairStages) {
+            slot = 0;
+            ++turn;
+          }
         }
       }
     }
+    // leave only when the last stages have been read (the leader's products read both CTAs' memory)
+    const uint32_t back = j < uint32_t(kPairStages) ? j : uint32_t(kPairStages);
+    ok = true;
+    for (uint32_t i = 1; ok && i <= back; ++i) ok = wait_warp(&ctl->empty[(j - i) % kPairStages], ((j - i) / kPairStages) & 1u, wc, SITE_DRAIN, -1);
+    if (!ok && leader)
+      for (uint32_t k = 1; k <= back; ++k) wait_settled(&ctl->full[(j - k) % kPairStages], ((j - k) / kPairStages) & 1u);
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issuer
     // The whole warp goes through the loop and one lane issues: descriptors and addresses are then the warp's, in the registers that
@@ -462,7 +471,6 @@ constexpr int kFewMostStages = 12;
 constexpr int kFewRoom = 200 * 1024;          // of stages, with one CTA per SM
 constexpr int kFewHalfRoom = 96 * 1024;       // with two
 constexpr int kMostSplits = 8;
-constexpr int kSplitCost = 3;
 // Shared memory of a cluster's CTA at least, by its part of tensor memory.  Of 228 KB, 1 KB of which goes with each CTA, there is room
 // for two with half of tensor memory, and for none beside one with all of it.
 constexpr size_t kFewHalf = 78 * 1024, kFewAll = 152 * 1024;
@@ -512,10 +520,17 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   FewShared* sh = reinterpret_cast<FewShared*>(smem + stages * stage_bytes);
   FewControl* ctl = &sh->ctl;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int part = p.splits > 1 ? int(cluster_ctarank()) : 0;
-  const int t = int(p.by_splits.div(blockIdx.x));
-  const int rank = p.rs ? 0 : int(p.by_tiles.div(uint32_t(t)));
-  const int64_t n0 = int64_t(t - rank * p.n_tiles) * 128;
+  // (the rank in the cluster by the block's index, which is known to be the same for all threads: what goes by it stays in the
+  // registers that the issuing instructions take)
+  const int t = int(p.by_splits.div(blockIdx.x)), part = int(blockIdx.x) - t * p.splits;
+  const int wt = int(p.by_rows.div(uint32_t(t))), rt = t - wt * int(p.by_rows.d);
+  const int rank = p.rs ? 0 : int(p.by_tiles.div(uint32_t(wt)));
+  const int64_t n0 = int64_t(wt - rank * p.n_tiles) * 128;
+  // the tile's activation rows: `rows` from row0 on of `shards` shards (GEMM+ReduceScatter: of all rows)
+  const int piece = p.rs ? rt : int(p.pieces.d) == 1 ? 0 : rt - int(p.pieces.div(uint32_t(rt))) * int(p.pieces.d);
+  const int shard0 = p.rs ? 0 : int(p.pieces.div(uint32_t(rt))) * p.tile_shards, row0 = piece * p.tile_rows;
+  const int shards = p.rs ? 1 : min(p.tile_shards, p.P - shard0);
+  const int rows = min(p.tile_rows, (p.rs ? p.m * p.P : p.m) - row0);
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
   // this CTA's atoms of the whole contraction
   const int from = int(p.by_splits.div(uint32_t(p.all * part))), to = int(p.by_splits.div(uint32_t(p.all * (part + 1))));
@@ -545,7 +560,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem_base = ctl->tmem_base;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
   const uint32_t scale_a = tmem_base + uint32_t(p.cols), scale_b = scale_a + 8;      // 2 x 4 and 2 x 8 columns
   launch_dependents();
   // Scales of the activations in column `i * 32 + lane` (columns without any: any): the row in its tensor, and with AllGather, where the
@@ -555,40 +570,39 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int col = i * 32 + lane, s = int(p.slot.div(uint32_t(col)));
-      row_at[i] = int64_t(min(col - s * int(p.slot.d), (p.rs ? p.m * p.P : p.m) - 1)) * p.atoms;
-      if (!p.rs) row_at[i] += reinterpret_cast<int64_t>(p.sa[min(s, p.P - 1)]);
+      row_at[i] = int64_t(row0 + min(col - s * int(p.slot.d), rows - 1)) * p.atoms;
+      if (!p.rs) row_at[i] += reinterpret_cast<int64_t>(p.sa[shard0 + min(s, shards - 1)]);
     }
   }
   wait_for_previous_kernel();
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
-      const int shards = p.rs ? 1 : p.P;
-      const uint32_t bytes = uint32_t(kChunkBytes + (p.rs ? p.P : shards) * p.m * kAtom);
-      FewWalk w(p, from, to);
-      for (; w.left > 0; w.next(p)) {
-        if (w.turn > 0 && !wait_phase(&ctl->empty[w.slot], (w.turn - 1) & 1u, wc, SITE_EMPTY, t)) break;
+    const uint64_t pol = make_l2_policy(L2_EVICT_NORMAL);
+    const uint32_t bytes = uint32_t((p.b_box + shards * p.tile_rows) * kAtom);
+    FewWalk w(p, from, to);
+    for (; w.left > 0; w.next(p)) {
+      if (w.turn > 0 && !wait_warp(&ctl->empty[w.slot], (w.turn - 1) & 1u, wc, SITE_EMPTY, t)) break;
+      if (elect_one()) {
         uint8_t* dst = smem + w.slot * stage_bytes;
         mbar_arrive_expect_tx(&ctl->full[w.slot], bytes);
         const CUtensorMap* b = &p.b[p.rs ? w.seg : rank];
         if (p.kn) tma_load_2d_hint(dst, b, &ctl->full[w.slot], int(n0), w.a * kAtom, pol);
         else tma_load_2d_hint(dst, b, &ctl->full[w.slot], w.a * kAtom, int(n0), pol);
         for (int s = 0; s < shards; ++s)
-          tma_load_2d_hint(dst + kChunkBytes + s * p.slot.d * kAtom, &p.a[p.rs ? w.seg : s], &ctl->full[w.slot], w.a * kAtom, 0, pol);
+          tma_load_2d_hint(dst + kChunkBytes + s * p.slot.d * kAtom, &p.a[p.rs ? w.seg : shard0 + s], &ctl->full[w.slot], w.a * kAtom, row0, pol);
       }
-      // leave only when everything that was loaded has landed and been read: the last turn's places before this one's, the one's before
-      // it from here on
-      bool ok = true;
-      for (int i = 0; i < stages; ++i) {
-        const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
-        if (turn >= 0 && !(ok = wait_phase(&ctl->empty[i], uint32_t(turn) & 1u, wc, SITE_DRAIN, -1))) break;
-      }
-      if (!ok)
-        for (int i = 0; i < stages; ++i) {
-          const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
-          if (turn >= 0) wait_settled(&ctl->full[i], uint32_t(turn) & 1u);
-        }
+      __syncwarp();
+    }
+    // leave only when everything that was loaded has landed and been read: the last turn's places before this one's, the one's before
+    // it from here on
+    bool ok = true;
+    for (int i = 0; ok && i < stages; ++i) {
+      const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
+      if (turn >= 0) ok = wait_warp(&ctl->empty[i], uint32_t(turn) & 1u, wc, SITE_DRAIN, -1);
+    }
+    for (int i = 0; !ok && i < stages; ++i) {
+      const int turn = int(w.turn) - (i < w.slot ? 0 : 1);
+      if (turn >= 0) wait_settled(&ctl->full[i], uint32_t(turn) & 1u);
     }
   } else if (warp == 1) {
     // (the whole warp goes through the loop and one lane issues, as above)
@@ -700,14 +714,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
   }
 
   // The sums: lanes are weight rows, columns are activation rows.
-  const int M = p.m * p.P;
   const int quarter = warp & 3;
-  // row i of all ranks' activations: its shard, the row in it
-  auto shard_of = [&](int i, int* row) {
-    const int s = int(p.each.div(uint32_t(i)));
-    *row = i - s * p.m;
-    return s;
-  };
   bool ok = true;
   float* sums = reinterpret_cast<float*>(smem);      // [column][128], over the stages
   if (warp >= 4) {
@@ -735,22 +742,29 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
     // four neighbouring sums a thread, those of all CTAs of a cluster in flight together
     const uint32_t base = smem_u32(sums);
     const int n = lane * 4;
-    for (int i = part + p.splits * warp; i < M; i += p.splits * (kFewThreads / 32)) {
-      int row;
-      const int shard = shard_of(i, &row);
-      const uint32_t at = base + uint32_t((p.rs ? i : shard * int(p.slot.d) + row) * 128 + n) * 4;
+    for (int i = part + p.splits * warp; i < shards * rows; i += p.splits * (kFewThreads / 32)) {
+      // the i-th row of the tile: of which shard, and its accumulator column
+      const int s = shards == 1 ? 0 : int(p.each.div(uint32_t(i))), row = i - s * rows;
+      const uint32_t at = base + uint32_t((s * int(p.slot.d) + row) * 128 + n) * 4;
       float4 y[kMostSplits];
 #pragma unroll
-      for (int s = 0; s < kMostSplits; ++s)
-        if (s < p.splits)
+      for (int k = 0; k < kMostSplits; ++k)
+        if (k < p.splits)
           asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w)
-                       : "r"(map_to_cta(at, uint32_t(s))));
+                       : "=f"(y[k].x), "=f"(y[k].y), "=f"(y[k].z), "=f"(y[k].w)
+                       : "r"(map_to_cta(at, uint32_t(k))));
       float4 x = y[0];
 #pragma unroll
-      for (int s = 1; s < kMostSplits; ++s)
-        if (s < p.splits) x.x += y[s].x, x.y += y[s].y, x.z += y[s].z, x.w += y[s].w;
-      __nv_bfloat16* out = (p.rs ? p.out[shard] + int64_t(row) * p.N : p.out[rank] + int64_t(i) * p.N) + n0 + n;
+      for (int k = 1; k < kMostSplits; ++k)
+        if (k < p.splits) x.x += y[k].x, x.y += y[k].y, x.z += y[k].z, x.w += y[k].w;
+      __nv_bfloat16* out;
+      if (p.rs) {
+        const int chunk = int(p.each.div(uint32_t(row0 + row)));
+        out = p.out[chunk] + int64_t(row0 + row - chunk * p.m) * p.N;
+      } else {
+        out = p.out[rank] + (int64_t(shard0 + s) * p.m + row0 + row) * p.N;
+      }
+      out += n0 + n;
       if (p.wide) {      // (N is a multiple of 8)
         if (n0 + n < p.N) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
       } else {
@@ -823,23 +837,68 @@ int device_facts(DeviceFacts** out) {
   return COMPASS_OK;
 }
 
-// Columns of a pair's tile.  An atom of it takes the tensor cores 2 cycles a column, and its operands, 128 rows of A and half of its
-// columns of B for each CTA, 2.1 cycles a row (about 60 bytes a clock from L2); the tile that ends the rounds of the pairs soonest.
-// Tiles are of equal width as far as n_step allows, so that none is a narrow rest that still loads all of A.
-int pair_columns(int64_t N, int64_t row_tiles, int step, int pairs) {
-  int best = 256;
-  double least = 0;
+// How long a call takes, in cycles, by what an atom of a tile takes: the products, or its operands at 60 bytes a clock from L2 (2.1
+// cycles a row of 128 bytes), whatever is more; and what a tile takes besides.  Of the widths, splits and kernels the one with the
+// shortest time is taken.  Measured, the pair kernel against the other: 1024 x 1024 x 256 rows 5.6 us : 14, 4096 x 4096 x 512 rows 13.0 :
+// 18.5, 2 ranks' 5003 x 2064 x 59 rows 12.8 : 15.9; GEMM+ReduceScatter of 8 ranks 752 x 4096 x 1136 rows 66 : 36, [K][N] 87 : 39; 82 x
+// 7392 x 1571 rows 17.6 : 12.0, 4096 x 4096 x 1 row 17 : 7.
+double atom_cycles(double products, double rows) { return products > 2.1 * rows ? products : 2.1 * rows; }
+
+// Columns of a pair's tile: 2 cycles of products each.  For each CTA 128 rows of A and half of its columns of B, or (weights [K][N])
+// 128 of the contraction whatever the width.  Tiles are of equal width as far as n_step allows, so that none is a narrow rest that
+// still loads all of A.
+struct PairPlan {
+  int bn;
+  double cost;
+};
+PairPlan pair_plan(int64_t N, int64_t row_tiles, int64_t atoms, int step, bool kn, int pairs) {
+  PairPlan best = {256, 0};
   for (int most = 256; most >= 64; most -= 32) {
     const int64_t tiles = ceil_div(N, most);
     const int bn = int(ceil_div(ceil_div(N, tiles), step) * step);
-    const double atom = 2.0 * bn > 2.1 * (128 + bn / 2) ? 2.0 * bn : 2.1 * (128 + bn / 2);
-    const double cost = double(ceil_div(row_tiles * ceil_div(N, bn), pairs)) * atom;
-    if (least == 0 || cost < 0.98 * least) {
-      least = cost;
-      best = bn;
-    }
+    const double tile = double(atoms) * atom_cycles(2.0 * bn, 128 + (kn ? 128 : bn / 2)) + 1500;
+    const double cost = double(ceil_div(row_tiles * ceil_div(N, bn), pairs)) * tile;
+    if (best.cost == 0 || cost < 0.98 * best.cost) best = {bn, cost};
   }
   return best;
+}
+
+// The other kernel's row tiles: whole shards, as many as fit, or equal pieces of one; and over how many CTAs each one's contraction is
+// split.  Their sums cost two barriers of the cluster and some 30 cycles a column.
+struct FewPlan {
+  int64_t shards, pieces, rows, slot, cols, row_tiles;
+  int splits;
+  double cost;
+};
+FewPlan few_plan(bool rs, int P, int64_t m, int64_t n_tiles, int64_t all, int sms) {
+  FewPlan f = {};
+  const int64_t whole = rs ? m * P : m;      // rows of a tensor of activations
+  f.shards = f.pieces = 1;
+  f.rows = whole;
+  if (whole > kFewMostCols) {
+    f.pieces = ceil_div(whole, kFewMostCols);
+    f.rows = int64_t(round_up(size_t(ceil_div(whole, f.pieces)), 8));
+    f.pieces = ceil_div(whole, f.rows);
+  }
+  f.slot = int64_t(round_up(size_t(f.rows), 8));
+  if (!rs && f.pieces == 1) {
+    f.shards = kFewMostCols / f.slot < P ? kFewMostCols / f.slot : P;
+    f.shards = ceil_div(P, ceil_div(P, f.shards));
+  }
+  f.cols = int64_t(round_up(size_t(f.shards * f.slot), 16));
+  f.row_tiles = f.pieces * (rs ? 1 : ceil_div(P, f.shards));
+  const int64_t tiles = n_tiles * f.row_tiles * (rs ? 1 : P);
+  double atom = atom_cycles(2.0 * double(f.cols), 128 + double(f.shards * f.rows));
+  if (atom < 550) atom = 550;      // (measured, whatever the columns)
+  for (int n = 1; n <= kMostSplits && (n == 1 || 2 * n <= all); ++n) {
+    if (n > 1 && tiles * n > (f.cols <= 128 ? 2 : 1) * sms) break;
+    const double cost = double(ceil_div(tiles * n, sms)) * (double(ceil_div(all, n)) * atom + 1500) + (n > 1 ? 2000.0 + 30.0 * double(f.cols) : 10.0 * double(f.cols));
+    if (f.splits == 0 || cost < f.cost) {
+      f.splits = n;
+      f.cost = cost;
+    }
+  }
+  return f;
 }
 
 int launch_clusters(void (*kernel)(const Gemm8Params), int64_t grid, int threads, size_t smem, int cluster, const Gemm8Params& p, cudaStream_t stream) {
@@ -902,28 +961,27 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   const int64_t a_rows = p.rs ? g->M : p.m;
   const int64_t b_rows = p.kn ? g->K : g->N, b_cols = p.kn ? g->N : g->K;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int64_t slot = int64_t(round_up(size_t(a_rows), 8)), cols = int64_t(round_up(size_t(p.rs ? slot : slot * g->P), 16));
   bool ok = true;
-  if (cols <= kFewMostCols) {
-    p.slot.set(uint32_t(slot));
+  const int64_t n_tiles = scale_blocks(g->N), ranks = p.rs ? 1 : g->P, all = (p.rs ? g->P : 1) * int64_t(p.atoms);
+  const FewPlan few = few_plan(p.rs, g->P, p.m, n_tiles, all, f->sms);
+  p.frags = int32_t(ceil_div(p.m, 128));
+  p.row_tiles = int32_t(ceil_div(int64_t(p.frags) * g->P, 2));
+  p.n_step = p.kn ? 32 : 16;
+  const PairPlan pair = pair_plan(g->N, p.row_tiles * ranks, all, p.n_step, p.kn, f->pairs);
+  const int64_t few_tiles = n_tiles * few.row_tiles * ranks;
+  if (few.cost < pair.cost && few_tiles <= kMaxDim) {
+    p.tile_shards = int32_t(few.shards);
+    p.tile_rows = int32_t(few.rows);
+    p.slot.set(uint32_t(few.slot));
+    p.pieces.set(uint32_t(p.rs ? 1 : few.pieces));
+    p.by_rows.set(uint32_t(few.row_tiles));
     p.each.set(uint32_t(p.m));
-    p.by_tiles.set(uint32_t(scale_blocks(g->N)));
-    p.cols = int32_t(cols);
-    p.n_tiles = int32_t(scale_blocks(g->N));
-    const int64_t tiles = int64_t(p.n_tiles) * (p.rs ? 1 : g->P);
-    const int all = (p.rs ? g->P : 1) * p.atoms;
-    // The contraction is split so that the SMs' rounds of it are shortest, in atoms; a split costs about as much as kSplitCost of them
-    // (two barriers of the cluster, and the sums).
-    p.splits = 1;
-    int64_t best = ceil_div(tiles, f->sms) * all;
-    for (int n = 2; n <= kMostSplits && 2 * n <= all; ++n) {
-      const int64_t cost = ceil_div(tiles * n, f->sms) * ceil_div(all, n) + kSplitCost;
-      if (tiles * n <= (cols <= 128 ? 2 : 1) * f->sms && cost < best) {
-        best = cost;
-        p.splits = n;
-      }
-    }
-    p.all = all;
+    p.by_tiles.set(uint32_t(n_tiles));
+    p.cols = int32_t(few.cols);
+    p.n_tiles = int32_t(n_tiles);
+    p.splits = few.splits;
+    const int64_t cols = few.cols, tiles = few_tiles;
+    p.all = int32_t(all);
     p.by_splits.set(uint32_t(p.splits));
     const int stage = few_stage_bytes(p.cols);
     const int64_t mine = ceil_div(all, p.splits);
@@ -936,10 +994,10 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     p.stages = int32_t(stages);
     p.tmem_cols = 32;
     while (p.tmem_cols < p.cols + 24) p.tmem_cols *= 2;
+    p.b_box = p.kn || g->N > 128 ? 128 : int32_t(g->N);
     for (int r = 0; r < g->P; ++r) {
-      // (boxes of the rows that there are: rows outside a matrix of a few made its loads several times as long)
-      ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, int(a_rows));
-      ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, 128);
+      ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, p.tile_rows);
+      ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.b_box);
     }
     if (!ok) return record_cuda_error(cudaErrorUnknown);
     // The CTAs of a cluster wait for one another while they hold tensor memory, so no two clusters may each wait for what the other
@@ -952,10 +1010,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     }
     return launch_clusters(gemm8_few_kernel, tiles * p.splits, kFewThreads, smem, p.splits, p, s);
   }
-  p.frags = int32_t(ceil_div(p.m, 128));
-  p.row_tiles = int32_t(ceil_div(int64_t(p.frags) * g->P, 2));
-  p.n_step = p.kn ? 32 : 16;
-  p.bn = pair_columns(g->N, int64_t(p.row_tiles) * (p.rs ? 1 : g->P), p.n_step, f->pairs);
+  p.bn = pair.bn;
   p.col_tiles = int32_t(ceil_div(g->N, p.bn));
   const int64_t total = int64_t(p.row_tiles) * p.col_tiles * (p.rs ? 1 : g->P);
   if (total > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
@@ -963,9 +1018,11 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   p.per_rank.set(uint32_t(p.row_tiles) * uint32_t(p.col_tiles));
   p.per_group.set(uint32_t(kRowGroup) * uint32_t(p.col_tiles));
   p.by_frags.set(uint32_t(p.frags));
+  p.a_box = a_rows < 128 ? int32_t(a_rows) : 128;
+  p.b_box = p.kn ? 128 : g->N < p.bn / 2 ? int32_t(g->N) : p.bn / 2;
   for (int r = 0; r < g->P; ++r) {
-    ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, 128);
-    ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.kn ? 128 : p.bn / 2);
+    ok = ok && encode_tensor_map_bytes(&p.a[r], A[r], a_rows, g->K, p.a_box);
+    ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.b_box);
   }
   if (!ok) return record_cuda_error(cudaErrorUnknown);
   return launch_clusters(gemm8_pair_kernel, 2 * (total < f->pairs ? total : f->pairs), kPairThreads, kPairSmemBytes, 2, p, s);

@@ -74,6 +74,16 @@ def test_weights_along_n(op, P, M, N, K):
     compare(op, P, M, N, K, api.B_KN, api.DTYPE_E5M2)
 
 
+# few tiles of a long contraction: rows in pieces, several shards a tile and a last tile of fewer, boundaries of ranks inside a tile
+@pytest.mark.parametrize("layout", [api.B_NK, api.B_KN])
+@pytest.mark.parametrize("op,P,M,N,K", [
+    (AG, 1, 257, 80, 4112), (AG, 2, 1202, 112, 8192), (AG, 16, 640, 64, 4112), (AG, 16, 1600, 80, 6160), (AG, 5, 95, 16, 16400),
+    (RS, 8, 600, 112, 2064), (RS, 3, 807, 48, 4096), (RS, 16, 4112, 16, 2048), (RS, 8, 152, 96, 3120),
+])
+def test_row_tiles(op, P, M, N, K, layout):
+    compare(op, P, M, N, K, layout, api.DTYPE_E4M3)
+
+
 @pytest.mark.parametrize("layout", [api.B_NK, api.B_KN])
 @pytest.mark.parametrize("format", [api.DTYPE_E4M3, api.DTYPE_E5M2])
 @pytest.mark.parametrize("op,P,M,N,K", [(AG, 2, 20, 400, 1040), (RS, 2, 20, 400, 1040), (AG, 2, 700, 400, 1040), (RS, 4, 700, 400, 528)])

@@ -51,6 +51,7 @@ struct GradParams {
   int32_t m;               // rows per shard
   int32_t blocks;          // scales per row
   int32_t stages;          // per shard
+  int32_t box;             // rows of a load
   int32_t big_rows, col_tiles;      // rows of 512 x 256 tiles
   int32_t odd;                      // and one more of 256 x 256
   int32_t n_big, left, total;       // 512 x 256 tiles; places left over, two 256 x 256 tiles each
@@ -176,6 +177,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     ctl->abort = 0;
     fence_mbar_init();
   }
+  if (p.box < kRows) {
+    // Shards of fewer rows than a stage has: loads bring those that there are (rows outside a matrix of a few made them several times
+    // as long), the others are zeros from the start.
+    for (int i = threadIdx.x; i < kCAt / 16; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
   if (warp == 1) {
     tmem_alloc_pair(&ctl->tmem_base, 512);
     tmem_relinquish_pair();
@@ -208,12 +215,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (j >= depth && !(ok = wait_phase(&empty[slot], (j / depth - 1) & 1u, wc, SITE_EMPTY, t))) break;
             if (of_g) {
               const uint32_t bar = map_to_cta(smem_u32(&full[slot]), 0);
-              if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * kChunk));
+              if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * p.box * 128));
               const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
               for (int b = 0; b < boxes; ++b)
                 tma_load_3d_pair_hint(smem + slot * kGBytes + b * kChunk, g, bar, n0 + b * 64, i * kRows, p.ag ? s : 0, pol);
             } else {
-              mbar_arrive_expect_tx(&full[slot], kXBytes);
+              mbar_arrive_expect_tx(&full[slot], uint32_t(p.box * 128));
               tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
             }
           }
@@ -591,6 +598,7 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   p.K = g->K;
   p.blocks = int32_t(scale_blocks(g->K));
   p.stages = int32_t(ceil_div(p.m, kRows));
+  p.box = p.m < kRows ? p.m : kRows;
   p.accumulate = accumulate != 0;
   p.fp32 = grad_dtype == COMPASS_DTYPE_FP32;
   p.parts = p.fp32 ? int32_t(ceil_div(int64_t(p.stages) * g->P, kRangeStages)) : 1;
@@ -610,8 +618,8 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
     p.sx[r] = static_cast<const uint8_t*>(X_scale[r]);
     p.dw[r] = dW[r];
     if (!is_aligned(dW[r], 32)) p.wide = 0;
-    ok = ok && encode_tensor_map_slabs(&p.g[r], G[r], p.ag ? g->P : 1, p.m, g->N, 2, kRows);
-    ok = ok && encode_tensor_map_slabs(&p.x[r], X[r], p.ag ? 1 : g->P, p.m, g->K, 1, kRows);
+    ok = ok && encode_tensor_map_slabs(&p.g[r], G[r], p.ag ? g->P : 1, p.m, g->N, 2, p.box);
+    ok = ok && encode_tensor_map_slabs(&p.x[r], X[r], p.ag ? 1 : g->P, p.m, g->K, 1, p.box);
   }
   if (!ok) return record_cuda_error(cudaErrorUnknown);
   cudaLaunchConfig_t cfg = {};

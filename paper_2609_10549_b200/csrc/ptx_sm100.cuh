@@ -277,6 +277,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint16_t cta_mas
                  : "memory");
 }
 
+// The same to this CTA's mbarrier and to CTA `peer`'s.
+__device__ __forceinline__ void umma_commit_both(uint64_t* bar, uint32_t peer) {
+  umma_commit_pair(bar, 0x1);
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(map_to_cta(smem_u32(bar), peer)) : "memory");
+}
+
 // ---- 8-bit operands with block scales -------------------------------------------
 // kind::mxf8f6f4: A and B in E4M3 or E5M2, one E8M0 scale for every 32 elements of the contraction, which is one
 // instruction's depth; the tensor core multiplies every product by 2^(a - 127) * 2^(b - 127).  Scales lie in tensor memory, the

@@ -37,6 +37,7 @@ constexpr int kStages = 4;                            // of G and of X in BF16
 constexpr int kXStages = 4;
 constexpr int kSkew = 3;                              // stages at a 512 x 256 tile's ends in which accumulator 0 runs ahead
 constexpr int kRangeStages = 16;                      // of a sum that goes to FP32
+constexpr int kMostSplits = 4;                        // pairs of a cluster
 constexpr int kRowGroup = 8;                          // row tiles that go through the columns together
 
 struct GradParams {
@@ -55,7 +56,7 @@ struct GradParams {
   int32_t big_rows, col_tiles;      // rows of 512 x 256 tiles
   int32_t odd;                      // and one more of 256 x 256
   int32_t n_big, left, total;       // 512 x 256 tiles; places left over, two 256 x 256 tiles each
-  int32_t parts;                    // sums of a tile
+  int32_t splits;                   // pairs of a cluster, which share a tile's contraction
   int32_t accumulate, fp32;
   int32_t wide;            // results lie on 32-byte boundaries
   uint32_t wait_limit_us;
@@ -147,18 +148,23 @@ __device__ __forceinline__ void convert16(const uint4& w, uint32_t scale, uint4&
 // 2^(b - 127) in BF16, twice; 255 is NaN.
 __device__ __forceinline__ uint32_t scale_bf16x2(uint32_t b) { return (b == 0 ? 0x0040u : b == 255 ? 0x7FC0u : b << 7) * 0x10001u; }
 
-template <int kFormat>
+// kSplit: tiles shared by the pairs of a cluster (of its own, for the instructions: 0.4 us a call otherwise).
+template <int kFormat, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   Control* ctl = reinterpret_cast<Control*>(smem + kControlAt);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int cta = int(cluster_ctarank());
+  // (ranks by the block's index, which is known to be the same for all threads)
+  const int splits = kSplit ? p.splits : 1;
+  const int unit = int(blockIdx.x) / (2 * splits), units = int(gridDim.x) / (2 * splits), place = int(blockIdx.x) - unit * 2 * splits;
+  const int cta = place & 1, pair = place >> 1;
+  const uint32_t first_cta = uint32_t(2 * pair);      // of this pair in its cluster
   const bool leader = cta == 0;
-  const int unit = int(blockIdx.x >> 1), units = int(gridDim.x >> 1);
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
-  const int all = p.P * p.stages;      // stages of a tile
-  const int range = p.parts > 1 ? kRangeStages : all;
+  // this pair's stages of a tile
+  const int from = p.P * p.stages * pair / splits, all = p.P * p.stages * (pair + 1) / splits - from;
+  const int range = p.fp32 ? kRangeStages : all, parts = (all + range - 1) / range;      // of one sum, and how many sums
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -192,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   cluster_arrive();
   cluster_wait();
   tc_fence_after_sync();
-  const uint32_t tmem_base = ctl->tmem_base;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
   launch_dependents();
   wait_for_previous_kernel();
 
@@ -209,12 +215,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       for (int t = unit; ok && t < p.total; t += units) {
         const Tile c = tile_of(p, t);
         const int boxes = c.big ? 4 : 2, n0 = c.row0 + cta * boxes * 64, k0 = c.col0 + cta * 128;
-        for (int s = 0; ok && s < p.P; ++s)
-          for (int i = 0; i < p.stages; ++i, ++j) {
+        int s = from / p.stages, i = from - s * p.stages;
+        for (int a = 0; a < all; ++a, ++j) {
             const uint32_t slot = j % depth;
             if (j >= depth && !(ok = wait_phase(&empty[slot], (j / depth - 1) & 1u, wc, SITE_EMPTY, t))) break;
             if (of_g) {
-              const uint32_t bar = map_to_cta(smem_u32(&full[slot]), 0);
+              const uint32_t bar = map_to_cta(smem_u32(&full[slot]), first_cta);
               if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * p.box * 128));
               const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
               for (int b = 0; b < boxes; ++b)
@@ -223,7 +229,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
               mbar_arrive_expect_tx(&full[slot], uint32_t(p.box * 128));
               tma_load_3d_hint(smem + kXAt + slot * kXBytes, &p.x[p.ag ? s : c.rank], &full[slot], k0, i * kRows, p.ag ? 0 : s, pol);
             }
-          }
+            if (++i == p.stages) {
+              i = 0;
+              ++s;
+            }
+        }
       }
       // leave only when the last stages have been read (the leader's products read both CTAs' memory)
       const uint32_t back = j < depth ? j : depth;
@@ -253,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         return true;
       };
       auto commit = [&](uint64_t* bar) {
-        if (elect_one()) umma_commit_pair(bar, 0x3);
+        if (elect_one()) umma_commit_both(bar, first_cta + 1);
         __syncwarp();
       };
       auto landed = [&](uint32_t s) {
@@ -266,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       auto issue = [&](uint32_t acc, uint32_t at, int block, int s, uint32_t first) {
         const uint32_t slot = at % kStages;
         const uint64_t da = desc_g + uint64_t((slot * kGBytes + block * 2 * kChunk) >> 4), db = desc_c + uint64_t((slot * kCBytes) >> 4);
-        const int rows = p.m - s % p.stages * kRows;
+        const int rows = p.m - (from + s) % p.stages * kRows;
         if (!elect_one()) return;
         if (rows >= kRows) {
 #pragma unroll
@@ -315,12 +325,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         } else {
           for (int s = 0; ok && s < all;) {
             // one sum: the accumulators in turn; several: the first goes where the total is kept
-            const int b = p.parts > 1 ? (s == 0 ? 1 : 0) : int(small & 1u);
-            const int from = s, to = min(all, s + range);
+            const int b = parts > 1 ? (s == 0 ? 1 : 0) : int(small & 1u);
+            const int begin = s, to = min(all, s + range);
             if (!(ok = acc_free(b))) break;
             for (; s < to; ++s, ++j) {
               if (!(ok = landed(j))) break;
-              issue(tmem_base + b * 256, j, 0, s, s != from ? 1u : 0u);
+              issue(tmem_base + b * 256, j, 0, s, s != begin ? 1u : 0u);
               commit(&ctl->empty[j % kStages]);
             }
             if (!ok) break;
@@ -347,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       const int block = (c.col0 >> 7) + cta;
       // (scales of columns that do not exist: 1, their values are zeros)
       auto scale_at = [&](int a) -> uint32_t {
-        const int s = a / p.stages, r = (a - s * p.stages) * kRows + row;
+        const int s = (from + a) / p.stages, r = (from + a - s * p.stages) * kRows + row;
         if (a >= all || r >= p.m || block >= p.blocks) return 127u;
         const uint8_t* sx = p.ag ? p.sx[s] + int64_t(r) * p.blocks : p.sx[c.rank] + (int64_t(s) * p.m + r) * p.blocks;
         return sx[block];
@@ -383,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl->x_empty[xs]);
-          mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->ready[slot]), 0));
+          mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->ready[slot]), first_cta));
         }
       }
       j += uint32_t(all);
@@ -405,12 +415,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       auto give_back = [&](int b) {
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), 0));
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_empty[b]), first_cta));
       };
-      if (p.parts > 1) {
+      if (parts > 1) {
         // the total is in accumulator 1; all sums but the last are added to it
         if (!filled(1)) break;
-        for (int s = 2; ok && s < p.parts; ++s) {
+        for (int s = 2; ok && s < parts; ++s) {
           if (!filled(0)) break;
 #pragma unroll 1
           for (int q = 0; q < 4; ++q) {
@@ -431,8 +441,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       const int cols = int(min(int64_t(128), p.K - k0));      // a multiple of 16, or none
       const bool add = p.accumulate;
       for (int block = 0; block < (c.big ? 2 : 1); ++block) {
-        const int b = p.parts > 1 ? 0 : c.big ? block : int(small & 1u);
-        if (p.parts == 1 && !filled(b)) break;
+        const int b = parts > 1 ? 0 : c.big ? block : int(small & 1u);
+        if (parts == 1 && !filled(b)) break;
         const int64_t n = c.row0 + (c.big ? cta * 256 + block * 128 : cta * 128) + quarter * 32 + lane;
         const int64_t at = n * p.K + k0;
 #pragma unroll 1
@@ -440,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           uint32_t v[32];
           tmem_ld_32x32b_x32(lanes + b * 256 + q * 32, v);
           tmem_ld_wait();
-          if (p.parts > 1) {
+          if (parts > 1) {
             uint32_t w[32];
             tmem_ld_32x32b_x32(lanes + 256 + q * 32, w);
             tmem_ld_wait();
@@ -449,14 +459,23 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           }
           if (q == 3) {
             give_back(b);
-            if (p.parts > 1) give_back(1);
+            if (parts > 1) give_back(1);
           }
-          if (n >= p.N || q * 32 >= cols) continue;
+          if (!kSplit && (n >= p.N || q * 32 >= cols)) continue;
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
             const uint32_t x = v[i + 1];
             v[i + 1] = v[i + 2];
             v[i + 2] = x;
+          }
+          if constexpr (kSplit) {
+            // to the cluster: 128 rows of 256, over G's stages, which have been read
+            const int row = quarter * 32 + lane;
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+              *reinterpret_cast<uint4*>(smem + row * 1024 + (((half * 32 + q * 8 + g) ^ (row & 7)) << 4)) =
+                  make_uint4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+            continue;
           }
           if (p.fp32) {
             float* out = static_cast<float*>(p.dw[c.rank]) + at + q * 32;
@@ -517,9 +536,58 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     }
   }
 
+  if constexpr (kSplit) {
+    // The pairs' sums of the cluster's tile: each adds up its part of the rows, in the pairs' order, eight columns a thread.
+    __syncthreads();
+    if (warp == 0) cluster_arrive();
+    else cluster_arrive_relaxed();
+    cluster_wait();
+    if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
+      const Tile c = tile_of(p, unit);
+      const int64_t k = c.col0 + lane * 8;
+      for (int row = pair + splits * warp; row < 128; row += splits * (kThreads / 32)) {
+        const int64_t n = c.row0 + cta * 128 + row;
+        if (n >= p.N || k >= p.K) break;
+        const uint32_t at = smem_u32(smem + row * 1024);
+        float y[kMostSplits][8];
+#pragma unroll
+        for (int q = 0; q < kMostSplits; ++q)
+          if (q < splits)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                           : "=f"(y[q][4 * h]), "=f"(y[q][4 * h + 1]), "=f"(y[q][4 * h + 2]), "=f"(y[q][4 * h + 3])
+                           : "r"(map_to_cta(at + (uint32_t((2 * lane + h) ^ (row & 7)) << 4), uint32_t(2 * q + cta))));
+        float* x = y[0];
+#pragma unroll
+        for (int q = 1; q < kMostSplits; ++q)
+          if (q < splits)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] += y[q][i];
+        if (p.fp32) {
+          float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.dw[c.rank]) + n * p.K + k);
+          if (p.accumulate) {
+            const float4 a = out[0], b = out[1];
+            x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+          }
+          out[0] = make_float4(x[0], x[1], x[2], x[3]);
+          out[1] = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+          uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.dw[c.rank]) + n * p.K + k);
+          if (p.accumulate) {
+            float old[8];
+            unpack_bf16x8(old, *out);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] += old[i];
+          }
+          *out = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+        }
+      }
+    }
+  }
   tc_fence_before_sync();
   __syncthreads();
-  cluster_arrive();
+  cluster_arrive_relaxed();      // nobody's memory goes while it is read
   cluster_wait();
   if (warp == 1) {
     tc_fence_after_sync();
@@ -529,38 +597,50 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 
 // ---- host ----------------------------------------------------------------------
 
-int device_pairs(int* out) {
+using GradKernel = void (*)(const GradParams);
+GradKernel grad_kernel(int format, bool split) {
+  if (format == E4M3) return split ? weight_grad_kernel<E4M3, true> : weight_grad_kernel<E4M3, false>;
+  return split ? weight_grad_kernel<E5M2, true> : weight_grad_kernel<E5M2, false>;
+}
+
+// Clusters of n pairs that the device holds at once, in [n].
+struct Clusters {
+  int of[kMostSplits + 1];
+};
+int device_clusters(Clusters* out) {
   constexpr int kMaxDevices = 64;
-  static int pairs[kMaxDevices] = {};
+  static Clusters known[kMaxDevices] = {};
   static std::mutex mu;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return record_cuda_error(e);
   if (dev < 0 || dev >= kMaxDevices) return COMPASS_ERR_UNSUPPORTED;
   std::lock_guard<std::mutex> lock(mu);
-  if (pairs[dev] == 0) {
-    e = cudaFuncSetAttribute(weight_grad_kernel<E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(weight_grad_kernel<E5M2>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
+  if (known[dev].of[1] == 0) {
+    for (GradKernel k : {grad_kernel(E4M3, false), grad_kernel(E5M2, false), grad_kernel(E4M3, true), grad_kernel(E5M2, true)})
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemBytes));
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return record_cuda_error(e);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(sms / 2 * 2));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2;
-    attr.val.clusterDim.y = 1;
-    attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, weight_grad_kernel<E4M3>, &cfg);
-    if (e != cudaSuccess) return record_cuda_error(e);
-    if (n < 1) return COMPASS_ERR_UNSUPPORTED;
-    pairs[dev] = n;
+    Clusters found = {};
+    for (int n = 1; n <= kMostSplits; ++n) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(unsigned(sms / (2 * n) * 2 * n));
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = kSmemBytes;
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = unsigned(2 * n);
+      attr.val.clusterDim.y = 1;
+      attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&found.of[n], grad_kernel(E4M3, n > 1), &cfg);
+      if (e != cudaSuccess) return record_cuda_error(e);
+    }
+    if (found.of[1] < 1) return COMPASS_ERR_UNSUPPORTED;
+    known[dev] = found;
   }
-  *out = pairs[dev];
+  *out = known[dev];
   return COMPASS_OK;
 }
 
@@ -587,8 +667,8 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   if (st != COMPASS_OK) return st;
   const int64_t row_tiles = ceil_div(g->N, 256), col_tiles = ceil_div(g->K, 256);
   if (row_tiles * col_tiles * g->P > kMaxDim || g->M + 2 * kRows * g->P > kMaxDim) return COMPASS_ERR_UNSUPPORTED;
-  int pairs = 0;
-  st = device_pairs(&pairs);
+  Clusters clusters;
+  st = device_clusters(&clusters);
   if (st != COMPASS_OK) return st;
   GradParams p = {};
   p.ag = g->op == COMPASS_OP_AG_GEMM;
@@ -601,15 +681,27 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   p.box = p.m < kRows ? p.m : kRows;
   p.accumulate = accumulate != 0;
   p.fp32 = grad_dtype == COMPASS_DTYPE_FP32;
-  p.parts = p.fp32 ? int32_t(ceil_div(int64_t(p.stages) * g->P, kRangeStages)) : 1;
   // whole rounds of the pairs take 512 x 256 tiles, what is left, and all where a tile has several sums, 256 x 256 ones
   p.big_rows = int32_t(row_tiles / 2);
   p.odd = int32_t(row_tiles % 2);
   p.col_tiles = int32_t(col_tiles);
   const int32_t places = int32_t(p.big_rows * col_tiles * g->P);
-  p.left = p.parts > 1 ? places : places % pairs;
+  const int pairs = clusters.of[1];
+  const int64_t stages = int64_t(p.stages) * g->P;
+  p.left = p.fp32 && stages > kRangeStages ? places : places % pairs;
   p.n_big = places - p.left;
   p.total = int32_t(p.n_big + 2 * p.left + p.odd * col_tiles * g->P);
+  // Tiles that leave pairs without work: several pairs share a tile's contraction.  A stage of a tile takes some 770 cycles, the sum
+  // over the cluster some 9000 (and the next kernel begins no earlier on SMs without work).  Measured with one pair and with several: 1024 x
+  // 1024 over 4096 rows 30.9 us : 21.7, 4 ranks' 232 x 480 over 5552 rows 42 : 22, 768 x 768 over 2048 rows in FP32 25.6 : 17.0; 4872 x 96
+  // over 1261 rows 15.7 : 15.1.
+  p.splits = 1;
+  int64_t least = stages * 770;
+  for (int n = 2; n <= kMostSplits && n <= stages; ++n)
+    if (p.n_big == 0 && p.total <= clusters.of[n] && ceil_div(stages, n) * 770 + 9000 < least) {
+      p.splits = n;
+      least = ceil_div(stages, n) * 770 + 9000;
+    }
   p.wide = 1;
   p.status = static_cast<StatusBlock*>(ws);
   p.wait_limit_us = default_wait_limit_us() ? default_wait_limit_us() : 2000000u;
@@ -623,20 +715,20 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   }
   if (!ok) return record_cuda_error(cudaErrorUnknown);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(2 * (p.total < pairs ? p.total : pairs)));
+  cfg.gridDim = dim3(unsigned(2 * p.splits * (p.total < pairs ? p.total : pairs)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmemBytes;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.x = unsigned(2 * p.splits);
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = format_of(g->dtype) == E4M3 ? cudaLaunchKernelEx(&cfg, weight_grad_kernel<E4M3>, p) : cudaLaunchKernelEx(&cfg, weight_grad_kernel<E5M2>, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, grad_kernel(format_of(g->dtype), p.splits > 1), p);
   count_kernel_launch();
   return e == cudaSuccess ? COMPASS_OK : record_cuda_error(e);
 }

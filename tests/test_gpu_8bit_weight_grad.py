@@ -69,6 +69,20 @@ def test_accumulates(op, P, M, N, K, grad):
         assert torch.equal(o, (e + v.double()).to(kind))
 
 
+# few tiles of a long contraction, which several pairs of CTAs share; their boundaries inside a shard and at its ragged end
+@pytest.mark.parametrize("grad", [api.DTYPE_BF16, api.DTYPE_FP32])
+@pytest.mark.parametrize("op,P,M,N,K", [
+    (AG, 1, 1999, 72, 80), (AG, 3, 4053, 520, 272), (RS, 4, 5552, 232, 480), (RS, 16, 4112, 264, 144), (AG, 1, 2100, 1280, 1040), (RS, 1, 3000, 1544, 768),
+])
+def test_shared_contraction(op, P, M, N, K, grad):
+    """In whole numbers, so that only BF16's rounding is left, and added to what is there."""
+    d, x = inputs(op, P, M, N, K, api.DTYPE_E4M3, 4, whole=True)
+    kind = torch.float32 if grad == api.DTYPE_FP32 else torch.bfloat16
+    old = [torch.full((N, K), 3.0, device="cuda", dtype=kind) for _ in range(P)]
+    for o, e in zip(run(op, P, M, N, K, api.DTYPE_E4M3, d, x, grad, old), exact(op, P, d, x)):
+        assert torch.equal(o, (e + 3).to(kind))
+
+
 def test_long_sums_keep_fp32_precision():
     """A result in FP32 over 8192 rows is as close as FP32 arithmetic brings it: 2^-24 per addition of 1024 rows' sums is far below
     1e-6, and the tensor cores' cut-off over 1024 rows is half a unit (2^-24) per 16 of them at the sum's size on average: 64 * 2^-24 /

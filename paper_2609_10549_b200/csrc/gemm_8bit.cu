@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
 
   tc_fence_before_sync();
   __syncthreads();
-  cluster_arrive();
+  cluster_arrive_relaxed();      // nobody's memory goes while it is read
   cluster_wait();
   if (warp == 1) {
     tc_fence_after_sync();

@@ -87,9 +87,10 @@ __device__ __forceinline__ void store_8bit(F2 (&x)[V * NVT / 2], float factor, u
 // ---- forward -------------------------------------------------------------------
 // A row per group of kTpr threads, NVT vectors of V elements a thread.  kKeep: gamma stays in registers.
 // Elements of a row per thread: what a row costs every thread is shared by this many.  The output in 8 bits alone is bound by
-// instructions, and takes 32 in BF16; with the residual, four streams of memory, it goes better with more threads a row: to 8 bits, us,
-// 16 and 32: 16384 x 8192: 110 and 80, with the residual 151 and 169; 16384 x 4096: 59 and 41, 78 and 85; 16384 x 1024: 16 and 13, 22 and
-// 21.  In BF16: 16384 x 4096: 44 and 48; 4096 x 8192: 25 and 23.
+// instructions, and takes 32 in BF16; with the residual, four streams of memory, it goes better with more threads a row.  To 8 bits, us,
+// 16 and 32: 16384 x 8192: 98 and 79, with the residual 140 and 159; 16384 x 4096: 53 and 41, 76 and 81; with the values restored again
+// 16384 x 1024: 23.5 and 22.4, 29.4 and 28.9.  In BF16: 16384 x 4096: 44 and 48, with the residual 95 and 91; 4096 x 8192: 25 and 23, 47
+// and 47.
 template <typename T, int V, bool kResidual, int kFormat>
 constexpr int kForwardElems = V == 8 ? (kFormat != kNone && !kResidual ? 32 : 16) : V == 4 ? 16 : 8;
 template <typename T, int V, int NVT, int kThreads, bool kResidual>

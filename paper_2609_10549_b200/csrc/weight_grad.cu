@@ -554,50 +554,51 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   }
 
   if constexpr (kSplit) {
-    // The pairs' sums of the cluster's tile: each adds up its part of the rows, in the pairs' order, eight columns a thread.
+    // The pairs' sums of the cluster's tile: each adds up its part of the rows, in the pairs' order.  A warp reads 512 bytes in
+    // a row of a CTA's memory at a time (eight neighbouring columns a thread, every other 16 bytes: 3.5 us more).
     __syncthreads();
     if (warp == 0) cluster_arrive();
     else cluster_arrive_relaxed();
     cluster_wait();
     if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
       const Tile c = tile_of(p, unit);
-      const int64_t k = c.col0 + lane * 8;
       for (int row = pair + splits * warp; row < 128; row += splits * (kThreads / 32)) {
         const int64_t n = c.row0 + cta * 128 + row;
-        if (n >= p.N || k >= p.K) break;
+        if (n >= p.N) break;
         const uint32_t at = smem_u32(smem + row * 1024);
-        float y[kMostSplits][8];
+        float4 y[kMostSplits][2];
 #pragma unroll
         for (int q = 0; q < kMostSplits; ++q)
           if (q < splits)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                           : "=f"(y[q][4 * h]), "=f"(y[q][4 * h + 1]), "=f"(y[q][4 * h + 2]), "=f"(y[q][4 * h + 3])
-                           : "r"(map_to_cta(at + (uint32_t((2 * lane + h) ^ (row & 7)) << 4), uint32_t(2 * q + cta))));
-        float* x = y[0];
+                           : "=f"(y[q][h].x), "=f"(y[q][h].y), "=f"(y[q][h].z), "=f"(y[q][h].w)
+                           : "r"(map_to_cta(at + (uint32_t((h * 32 + lane) ^ (row & 7)) << 4), uint32_t(2 * q + cta))));
 #pragma unroll
-        for (int q = 1; q < kMostSplits; ++q)
-          if (q < splits)
+        for (int h = 0; h < 2; ++h) {
+          float4 x = y[0][h];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += y[q][i];
-        if (p.fp32) {
-          float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.dw[c.rank]) + n * p.K + k);
-          if (p.accumulate) {
-            const float4 a = out[0], b = out[1];
-            x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+          for (int q = 1; q < kMostSplits; ++q)
+            if (q < splits) x.x += y[q][h].x, x.y += y[q][h].y, x.z += y[q][h].z, x.w += y[q][h].w;
+          const int64_t k = c.col0 + h * 128 + lane * 4;
+          if (k >= p.K) continue;
+          if (p.fp32) {
+            float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.dw[c.rank]) + n * p.K + k);
+            if (p.accumulate) {
+              const float4 a = *out;
+              x.x += a.x, x.y += a.y, x.z += a.z, x.w += a.w;
+            }
+            *out = x;
+          } else {
+            uint2* out = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.dw[c.rank]) + n * p.K + k);
+            if (p.accumulate) {
+              const uint2 a = *out;
+              x.x += __uint_as_float(a.x << 16), x.y += __uint_as_float(a.x & 0xFFFF0000u);
+              x.z += __uint_as_float(a.y << 16), x.w += __uint_as_float(a.y & 0xFFFF0000u);
+            }
+            *out = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
           }
-          out[0] = make_float4(x[0], x[1], x[2], x[3]);
-          out[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-          uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.dw[c.rank]) + n * p.K + k);
-          if (p.accumulate) {
-            float old[8];
-            unpack_bf16x8(old, *out);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += old[i];
-          }
-          *out = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
         }
       }
     }
@@ -709,15 +710,15 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   p.n_big = places - p.left;
   p.total = int32_t(p.n_big + 2 * p.left + p.odd * col_tiles * g->P);
   // Tiles that leave pairs without work: several pairs share a tile's contraction.  A stage of a tile takes some 770 cycles, the sum
-  // over the cluster some 9000 (and the next kernel begins no earlier on SMs without work).  Measured with one pair and with several: 1024 x
-  // 1024 over 4096 rows 30.9 us : 21.7, 4 ranks' 232 x 480 over 5552 rows 42 : 22, 768 x 768 over 2048 rows in FP32 25.6 : 17.0; 4872 x 96
-  // over 1261 rows 15.7 : 15.1.
+  // over the cluster some 5000 (and the next kernel begins no earlier on SMs without work).  Measured with one pair and with several: 1024 x
+  // 1024 over 4096 rows 30.9 us : 18.2, over 1024 12.4 : 11.9, 4 ranks' 232 x 480 over 5552 rows 42 : 17.8, 768 x 768 over 2048 rows in FP32
+  // 25.6 : 12.6; 512 x 512 over 512 rows 9.0 : 9.8.
   p.splits = 1;
   int64_t least = stages * 770;
   for (int n = 2; n <= kMostSplits && n <= stages; ++n)
-    if (p.n_big == 0 && p.total <= clusters.of[n] && ceil_div(stages, n) * 770 + 9000 < least) {
+    if (p.n_big == 0 && p.total <= clusters.of[n] && ceil_div(stages, n) * 770 + 5000 < least) {
       p.splits = n;
-      least = ceil_div(stages, n) * 770 + 9000;
+      least = ceil_div(stages, n) * 770 + 5000;
     }
   p.wide = 1;
   p.status = static_cast<StatusBlock*>(ws);

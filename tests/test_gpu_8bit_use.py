@@ -267,3 +267,76 @@ def test_a_norm_in_8_bits_beyond_4_gb():
     for i in (0, 139, 279):
         rows = slice(i * 1000, i * 1000 + 1000)
         assert torch.equal(y8[0][rows].view(torch.uint8), one[0].view(torch.uint8)) and torch.equal(scale[0][rows].view(torch.uint8), ones[0].view(torch.uint8))
+
+
+# activation rows in several tiles, several shards a tile, and contractions that CTAs share
+TILED = [(AG, 1, 700, 96, 4112), (AG, 16, 640, 64, 4112), (RS, 8, 600, 112, 2064)]
+
+
+@pytest.mark.parametrize("layout", [api.B_NK, api.B_KN])
+@pytest.mark.parametrize("op,P,M,N,K", TILED)
+def test_row_tiles_read_nothing_else(op, P, M, N, K, layout):
+    a, b = product_inputs(op, P, M, N, K, layout, api.DTYPE_E5M2, 8)
+    want = run_product(op, P, M, N, K, layout, api.DTYPE_E5M2, a, b)
+    a, b = ([(among_nan(q, 255), among_nan(s, 255)) for q, s in t] for t in (a, b))
+    for x, y in zip(want, run_product(op, P, M, N, K, layout, api.DTYPE_E5M2, a, b)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("op,P,M,N,K", TILED)
+def test_what_is_not_a_number_stays_in_its_row_of_a_tile(op, P, M, N, K):
+    """One row of the last rank's last shard, in a value and in a scale."""
+    a, b = product_inputs(op, P, M, N, K, api.B_NK, api.DTYPE_E4M3, 9)
+    clean = run_product(op, P, M, N, K, api.B_NK, api.DTYPE_E4M3, a, b)
+    a[-1][0].view(torch.uint8)[-1, 0] = NAN
+    a[-1][1].view(torch.uint8)[-3, -1] = 255
+    got = run_product(op, P, M, N, K, api.B_NK, api.DTYPE_E4M3, a, b)
+    for r in range(P):
+        bad = torch.zeros_like(clean[r], dtype=torch.bool)
+        if op == AG or r == P - 1:
+            bad[[-1, -3]] = True
+        assert got[r][bad].isnan().all() and torch.equal(got[r][~bad], clean[r][~bad])
+
+
+@pytest.mark.parametrize("grad", [api.DTYPE_BF16, api.DTYPE_FP32])
+@pytest.mark.parametrize("op,P,M,N,K", [(AG, 4, 44, 264, 400), (RS, 16, 16, 72, 272), (RS, 5, 315, 1032, 144), (AG, 1, 4100, 136, 272)])
+def test_weight_gradients_of_short_shards_read_nothing_else(op, P, M, N, K, grad):
+    """Shards of fewer rows than are loaded at a time, and a contraction that CTAs share."""
+    d, x = grad_inputs(op, P, M, N, K, api.DTYPE_E4M3, 10)
+    want = run_grad(op, P, M, N, K, api.DTYPE_E4M3, d, x, grad)
+    d2, x2 = [among_nan(t, 255) for t in d], [(among_nan(q), among_nan(s, 255)) for q, s in x]
+    for a, b in zip(want, run_grad(op, P, M, N, K, api.DTYPE_E4M3, d2, x2, grad)):
+        assert torch.equal(a, b)
+
+
+def test_shared_contractions_at_once():
+    """Products and weight gradients whose CTAs wait for one another, on two streams at a time, many in flight."""
+    made = []
+    for seed, (op, P, M, N, K) in enumerate(TILED + [(AG, 1, 1, 4096, 4096)]):
+        a, b = product_inputs(op, P, M, N, K, api.B_NK, api.DTYPE_E4M3, seed)
+        pr = api.make_problem(op, P, M, N, K, dtype=api.DTYPE_E4M3)
+        out = [torch.empty(M if op == AG else M // P, N, device="cuda", dtype=torch.bfloat16) for _ in range(P)]
+        call = api.compass_ag_gemm_8bit if op == AG else api.compass_gemm_rs_8bit
+        args = [pr, [t[0] for t in a], [t[1] for t in a], [t[0] for t in b], [t[1] for t in b], out, api.alloc_8bit_workspace(pr)]
+        made.append((lambda s, call=call, args=args: call(*args, stream=s), out, args[-1]))
+    for seed, (op, P, M, N, K) in enumerate([(AG, 1, 4100, 512, 512), (RS, 4, 2064, 264, 144)]):
+        d, x = grad_inputs(op, P, M, N, K, api.DTYPE_E4M3, seed)
+        pr = api.make_problem(op, P, M, N, K, dtype=api.DTYPE_E4M3)
+        out = [torch.empty(N, K, device="cuda", dtype=torch.bfloat16) for _ in range(P)]
+        args = [pr, d, [t[0] for t in x], [t[1] for t in x], out, api.alloc_8bit_workspace(pr)]
+        made.append((lambda s, args=args: api.compass_weight_grad_8bit(*args, stream=s), out, args[-1]))
+    for call, _, _ in made:
+        call(None)
+    torch.cuda.synchronize()
+    want = [[t.clone() for t in out] for _, out, _ in made]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    half = len(made) // 2
+    for turn in range(30):
+        # (each call always on the same stream: its workspace and outputs are its own)
+        for i in range(half):
+            made[i][0](streams[0])
+            made[half + (i + turn) % half][0](streams[1])
+    torch.cuda.synchronize()
+    for (_, out, ws), w in zip(made, want):
+        assert api.compass_read_status(ws) == (api.OK, 0)
+        assert all(torch.equal(a, b) for a, b in zip(out, w))

@@ -108,6 +108,9 @@ __device__ __forceinline__ int steps_of(const Gemm8Params& p, int a) { return mi
 // Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue (two per quarter of the rows, 128 columns each),
 // warp 10 brings the scales.  Tensor memory holds two accumulators of 256 columns and the scales only because the accumulators
 // share 32 columns: each is emptied from the shared ones on, and the next tile's products begin once these are read.
+// Bound by the tensor cores, then by the board's power: 8 ranks' 8192 x 1376 x 4096 254 us in a burst (2.9 PFLOP/s, tensor pipe busy 85 % of
+// the cycles) and 310 to 320 in loops; GEMM+ReduceScatter of 4 ranks 8192 x 4096 x 2752, [K][N], 251 and 325.  256 x 256 takes the fewest
+// operand bytes that tensor memory has room for with two accumulators.
 constexpr int kPairThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kPairStages = 3;
@@ -463,6 +466,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
 }
 
 // ---- few rows ------------------------------------------------------------------
+// Bound by the weights' bytes where they are many (one row of 8192 x 8192: 67 MB in 15.6 us), by launch, first loads and the cluster's sum
+// where not (4096 x 4096: 16.8 MB in 7.4 us, of which a kernel that does next to nothing takes 3.5).  Weights on the M side, because the
+// tensor cores take no fewer than 128 rows there but as few columns as 16; the contraction split so that all SMs load.
 // Warp 0 loads, warp 1 multiplies, warp 2 brings the scales, warps 4..7 read the accumulator.  The CTAs of a cluster take a share
 // of the contraction each and add their FP32 sums up, rank by rank, through each other's shared memory.
 constexpr int kFewThreads = 256;

@@ -2,7 +2,8 @@
 // each block of 128 x 128 (weights, whose transpose then has the same scales), and back.
 //
 // Bound by HBM: a BF16 element is 2 bytes read and 1 + 1/128 written, or the reverse.  A thread takes 16 elements, so that 8
-// neighbouring lanes hold a run and its maximum is three shuffles away; four such units a thread are in flight.
+// neighbouring lanes hold a run and its maximum is three shuffles away; two (four, back) such units a thread are in flight.
+// 16384 x 8192 in BF16: 64 us there (6.3 TB/s), 61 back (6.6), 72 by blocks of 128 x 128.
 #include "row_ops.cuh"
 #include "scaled8.cuh"
 

@@ -6,6 +6,8 @@
 // Bound by HBM.  A row is read once into registers; the rows after it are copied ahead through shared memory.  The output in 8
 // bits is made from the FP32 values: a run of 128 columns lies in 16 neighbouring lanes (32 in FP32), so that its maximum is four
 // (five) shuffles away, and it costs 1 + 1/128 bytes an element instead of a second pass over 2.
+// 16384 x 8192 in BF16 with the residual to 8 bits: 138 us, 6.8 TB/s; without 80, by instructions; to BF16 with the residual 185, 5.8
+// TB/s.  Backward with the residual's gradient, 8192 x 4096: 46 us, 5.8 TB/s, both kernels.
 #include "norm_rows.cuh"
 #include "scaled8.cuh"
 

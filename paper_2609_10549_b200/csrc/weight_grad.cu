@@ -12,6 +12,10 @@
 //
 // The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
 // 1024 rows long, and added up in FP32, in tensor memory: 256 x 256 tiles whose second accumulator keeps the total.
+//
+// Bound by the tensor cores and the board's power: 4 ranks' 2752 x 4096 over 8192 rows 505 us in a burst (1.46 PFLOP/s, tensor pipe busy
+// 88 %) and 560 to 590 in loops.  In FP32 8192 x 8192 over 8192 rows takes 1110 against 810 us: the products wait for the sums of 1024 rows,
+// and tiles of 256 x 256 take shared memory's bandwidth (160 bytes a clock).
 #include <mutex>
 
 #include "pipeline.cuh"

@@ -807,6 +807,7 @@ int check_problem8(const compass_problem* g, int op) {
 struct DeviceFacts {
   bool ready = false;
   int pairs = 0, sms = 0;
+  int few[kMostSplits + 1] = {};      // clusters of n CTAs of the few-rows kernel that fit, one CTA per SM
 };
 int device_facts(DeviceFacts** out) {
   constexpr int kMaxDevices = 64;
@@ -837,6 +838,15 @@ int device_facts(DeviceFacts** out) {
     e = cudaOccupancyMaxActiveClusters(&f.pairs, gemm8_pair_kernel, &cfg);
     if (e != cudaSuccess) return record_cuda_error(e);
     if (f.pairs < 1) return COMPASS_ERR_UNSUPPORTED;
+    for (int n = 1; n <= kMostSplits; ++n) {
+      cfg.gridDim = dim3(unsigned(f.sms / n * n));
+      cfg.blockDim = dim3(kFewThreads);
+      cfg.dynamicSmemBytes = 1024 + size_t(kFewRoom) + sizeof(FewShared);
+      attr.val.clusterDim.x = unsigned(n);
+      e = cudaOccupancyMaxActiveClusters(&f.few[n], gemm8_few_kernel, &cfg);
+      if (e != cudaSuccess) return record_cuda_error(e);
+      if (f.few[n] < 1) return COMPASS_ERR_UNSUPPORTED;
+    }
     f.ready = true;
   }
   *out = &f;
@@ -871,12 +881,13 @@ PairPlan pair_plan(int64_t N, int64_t row_tiles, int64_t atoms, int step, bool k
 
 // The other kernel's row tiles: whole shards, as many as fit, or equal pieces of one; and over how many CTAs each one's contraction is
 // split.  Their sums cost two barriers of the cluster and some 30 cycles a column.
+int few_two(int64_t cols, int64_t ctas, int sms) { return ctas > sms && cols <= 128; }      // two CTAs per SM
 struct FewPlan {
   int64_t shards, pieces, rows, slot, cols, row_tiles;
   int splits;
   double cost;
 };
-FewPlan few_plan(bool rs, int P, int64_t m, int64_t n_tiles, int64_t all, int sms) {
+FewPlan few_plan(bool rs, int P, int64_t m, int64_t n_tiles, int64_t all, const DeviceFacts& d) {
   FewPlan f = {};
   const int64_t whole = rs ? m * P : m;      // rows of a tensor of activations
   f.shards = f.pieces = 1;
@@ -897,8 +908,12 @@ FewPlan few_plan(bool rs, int P, int64_t m, int64_t n_tiles, int64_t all, int sm
   double atom = atom_cycles(2.0 * double(f.cols), 128 + double(f.shards * f.rows));
   if (atom < 550) atom = 550;      // (measured, whatever the columns)
   for (int n = 1; n <= kMostSplits && (n == 1 || 2 * n <= all); ++n) {
-    if (n > 1 && tiles * n > (f.cols <= 128 ? 2 : 1) * sms) break;
-    const double cost = double(ceil_div(tiles * n, sms)) * (double(ceil_div(all, n)) * atom + 1500) + (n > 1 ? 2000.0 + 30.0 * double(f.cols) : 10.0 * double(f.cols));
+    // All clusters at once: what is left over takes as long again (2048 x 8192 x 16 rows, 16 clusters of 8 where 15 fit: 13.4 us, of 7 and
+    // 8.8).  With two CTAs per SM a fifteenth more went as well (4096 x 4096 x 1 row, 32 of 8 where 30 fit: 6.0 us, of 4 7.4), more did
+    // not (5120 x 5120 x 32 rows, 40 of 7: 14.3 us, of 6, which fit, 8.4).
+    if (n > 1 && tiles * 15 > d.few[n] * (few_two(f.cols, tiles * n, d.sms) ? 32 : 15)) continue;
+    const double tile = double(ceil_div(all, n)) * atom + 1500;
+    const double cost = n > 1 ? tile + 2000.0 + 30.0 * double(f.cols) : double(ceil_div(tiles, d.sms)) * tile + 10.0 * double(f.cols);
     if (f.splits == 0 || cost < f.cost) {
       f.splits = n;
       f.cost = cost;
@@ -969,7 +984,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   bool ok = true;
   const int64_t n_tiles = scale_blocks(g->N), ranks = p.rs ? 1 : g->P, all = (p.rs ? g->P : 1) * int64_t(p.atoms);
-  const FewPlan few = few_plan(p.rs, g->P, p.m, n_tiles, all, f->sms);
+  const FewPlan few = few_plan(p.rs, g->P, p.m, n_tiles, all, *f);
   p.frags = int32_t(ceil_div(p.m, 128));
   p.row_tiles = int32_t(ceil_div(int64_t(p.frags) * g->P, 2));
   p.n_step = p.kn ? 32 : 16;
@@ -991,7 +1006,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
     p.by_splits.set(uint32_t(p.splits));
     const int stage = few_stage_bytes(p.cols);
     const int64_t mine = ceil_div(all, p.splits);
-    const int room = tiles * p.splits > f->sms && cols <= 128 ? kFewHalfRoom : kFewRoom;
+    const int room = few_two(cols, tiles * p.splits, f->sms) ? kFewHalfRoom : kFewRoom;
     int64_t stages = room / stage;
     if (stages > mine) stages = mine;
     if (stages > kFewMostStages) stages = kFewMostStages;

@@ -466,8 +466,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
 }
 
 // ---- few rows ------------------------------------------------------------------
-// Bound by the weights' bytes where they are many (one row of 8192 x 8192: 67 MB in 15.6 us), by launch, first loads and the cluster's sum
-// where not (4096 x 4096: 16.8 MB in 7.4 us, of which a kernel that does next to nothing takes 3.5).  Weights on the M side, because the
+// Bound by the weights' bytes where they are many (one row of 8192 x 8192: 67 MB in 15 us), by launch, first loads and the cluster's sum
+// where not (4096 x 4096: 16.8 MB in 6.0 us, of which a kernel that does next to nothing takes 3.5).  Weights on the M side, because the
 // tensor cores take no fewer than 128 rows there but as few columns as 16; the contraction split so that all SMs load.
 // Warp 0 loads, warp 1 multiplies, warp 2 brings the scales, warps 4..7 read the accumulator.  The CTAs of a cluster take a share
 // of the contraction each and add their FP32 sums up, rank by rank, through each other's shared memory.
@@ -857,7 +857,7 @@ int device_facts(DeviceFacts** out) {
 // cycles a row of 128 bytes), whatever is more; and what a tile takes besides.  Of the widths, splits and kernels the one with the
 // shortest time is taken.  Measured, the pair kernel against the other: 1024 x 1024 x 256 rows 5.6 us : 14, 4096 x 4096 x 512 rows 13.0 :
 // 18.5, 2 ranks' 5003 x 2064 x 59 rows 12.8 : 15.9; GEMM+ReduceScatter of 8 ranks 752 x 4096 x 1136 rows 66 : 36, [K][N] 87 : 39; 82 x
-// 7392 x 1571 rows 17.6 : 12.0, 4096 x 4096 x 1 row 17 : 7.
+// 7392 x 1571 rows 17.6 : 12.0, 4096 x 4096 x 1 row 17 : 6.
 double atom_cycles(double products, double rows) { return products > 2.1 * rows ? products : 2.1 * rows; }
 
 // Columns of a pair's tile: 2 cycles of products each.  For each CTA 128 rows of A and half of its columns of B, or (weights [K][N])

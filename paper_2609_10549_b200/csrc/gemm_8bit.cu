@@ -317,6 +317,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
         if (ok && elect_one()) umma_commit_pair(&ctl->acc_full, 0x3);
         __syncwarp();
       }
+      // leave only when the last tile's signals have come: the other CTA's may be on their way to this one's memory still
+      if (ok && it > 0) wait_warp(&ctl->acc_early, (it - 1) & 1u, wc, SITE_DRAIN, -1);
       if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
         // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
         if (elect_one()) umma_commit_pair(&ctl->drain, 0x1);

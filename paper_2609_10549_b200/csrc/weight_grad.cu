@@ -355,6 +355,9 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           ++small;
         }
       }
+      // leave only when the accumulators' last signals have come: the other CTA's may be on their way to this one's memory still
+      for (int b = 0; ok && b < 2; ++b)
+        if (uses[b] > 0) ok = wait_warp(&ctl->acc_empty[b], (uses[b] - 1) & 1u, wc, SITE_DRAIN, -1);
       if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
         if (elect_one()) umma_commit_pair(&ctl->drain, 0x1);
         wait_settled(&ctl->drain, 0);

@@ -122,9 +122,10 @@ constexpr int kRowGroup = 16;                 // row tiles that go through the c
 constexpr int kPitch = 17;                    // words of a staged row of 32 columns
 struct PairControl {
   uint64_t full[kPairStages], empty[kPairStages];
-  uint64_t scales_full[2], scales_empty[2];
+  uint64_t scales_full[2], scales_empty[2];      // (full: the leader's, by both CTAs)
   uint64_t acc_full, acc_early;
   uint64_t drain;
+  uint32_t signal;
   uint32_t tmem_base;
   int abort;
 };
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
       mbar_init(&ctl->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&ctl->scales_full[b], 2);
+      mbar_init(&ctl->scales_full[b], 1);
       mbar_init(&ctl->scales_empty[b], 1);
     }
     mbar_init(&ctl->acc_full, 1);
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
           for (int a = 0; a < p.atoms; a += kStageAtoms, ++j) {
             if (a % kGroupAtoms == 0) {
               buf = g & 1u;
-              if (!(ok = wait_warp(&ctl->scales_full[buf], (g >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
+              if (!(ok = wait_warp<true>(&ctl->scales_full[buf], (g >> 1) & 1u, wc, SITE_SCALES_FULL, t))) break;
               tc_fence_after_sync();
               const uint64_t from = desc_s + uint64_t(buf * (3 * 512 >> 4));
               if (elect_one()) {
@@ -380,7 +381,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
       sh->scales[buf][2][lane] = make_uint4(b[4], b[5], b[6], b[7]);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+      if (lane == 0) {
+        if (leader) mbar_arrive_expect_tx(&ctl->scales_full[buf], kSignalBytes);
+        else mbar_signal_cluster(map_to_cta(smem_u32(&ctl->signal), 0), map_to_cta(smem_u32(&ctl->scales_full[buf]), 0));
+      }
       x = next;
     }
     // leave only when the last groups' signals have come

@@ -14,13 +14,16 @@ struct WaitContext {
   uint32_t limit_us;
 };
 
-// Waits for an mbarrier's phase; gives up after the limit, or when another role of this CTA has.
+// Waits for an mbarrier's phase; gives up after the limit, or when another role of this CTA has.  kCluster: for one by which another
+// CTA hands over what it wrote.
+template <bool kCluster = false>
 __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, const WaitContext& w, int site, int tile) {
-  if (ptx::mbar_try_wait(bar, parity)) return true;
+  auto there = [&] { return kCluster ? ptx::mbar_try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity); };
+  if (there()) return true;
   const uint64_t t0 = ptx::globaltimer_ns();
   const uint64_t limit = uint64_t(w.limit_us) * 1000ull;
   for (uint32_t spins = 1; spins < (1u << 30); ++spins) {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
+    if (there()) return true;
     if ((spins & 0xFF) == 0) {
       if (*reinterpret_cast<volatile int*>(w.abort)) return false;
       if (ptx::globaltimer_ns() - t0 > limit) break;
@@ -36,8 +39,9 @@ __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, const
 }
 
 // The same for a whole warp, which goes on or gives up as one.
+template <bool kCluster = false>
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, const WaitContext& w, int site, int tile) {
-  return __all_sync(0xffffffffu, wait_phase(bar, parity, w, site, tile));
+  return __all_sync(0xffffffffu, wait_phase<kCluster>(bar, parity, w, site, tile));
 }
 
 // After giving up: copies or products in flight, whatever the others do, before this CTA's memory may go (100 ms at most).

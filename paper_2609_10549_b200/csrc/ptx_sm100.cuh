@@ -41,6 +41,19 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return done != 0;
 }
 
+// The same where what is waited for came from another CTA of the cluster.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
 // One lane of a converged warp, the same one every time.
 __device__ __forceinline__ bool elect_one() {
   uint32_t is;
@@ -201,12 +214,15 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// The same behind fence.proxy.async, for an arrival that hands over this CTA's own shared memory to the pair's MMAs: when the fence
-// is over, the writes before it are there for the tensor cores of both CTAs, so nothing is left for a release to the cluster to wait
-// for, which takes 1000 cycles and more all the same.
-__device__ __forceinline__ void mbar_arrive_cluster_fenced(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+// Hands this CTA's shared memory over to another CTA's MMAs, behind the writes and fence.proxy.async: four bytes on an mbarrier of that
+// CTA, counted (expect_tx) like a copy's, as an asynchronous store to a word beside it (both shared::cluster addresses).  The
+// store's completion is a release at the scope of the cluster, and the writes precede its issue.  The thread does not wait for it, as it
+// would for an arrival with that release: 1000 cycles and more, 12 to 20 % of the batches' products and weight gradients (passed on by
+// another thread of the CTA: 10 to 35 %).
+__device__ __forceinline__ void mbar_signal_cluster(uint32_t word, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(word), "r"(0u), "r"(bar) : "memory");
 }
+constexpr uint32_t kSignalBytes = 4;
 // TMA load into this CTA's shared memory whose completion is counted on an
 // mbarrier of either CTA of the pair (`bar_cluster_addr`, shared::cluster).
 __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int32_t x,

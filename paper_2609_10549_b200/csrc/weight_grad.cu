@@ -72,6 +72,7 @@ struct Control {
   uint64_t x_full[kXStages], x_empty[kXStages];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t drain;
+  uint32_t signal[kGroups * kConvWarps];
   uint32_t tmem_base;
   int abort;
 };
@@ -183,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctl->ready[s], 2 * kConvWarps + 1);
+      mbar_init(&ctl->ready[s], kConvWarps + 1);
       mbar_init(&ctl->empty[s], 1);
     }
     for (int s = 0; s < kXStages; ++s) {
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
             if (j >= depth && !(ok = wait_phase(&empty[slot], (j / depth - 1) & 1u, wc, SITE_EMPTY, t))) break;
             if (of_g) {
               const uint32_t bar = map_to_cta(smem_u32(&full[slot]), first_cta);
-              if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * p.box * 128));
+              if (leader) mbar_arrive_expect_tx(&full[slot], uint32_t(2 * boxes * p.box * 128) + kConvWarps * kSignalBytes);
               const CUtensorMap* g = &p.g[p.ag ? c.rank : s];
               for (int b = 0; b < boxes; ++b)
                 tma_load_3d_pair_hint(smem + slot * kGBytes + b * kChunk, g, bar, n0 + b * 64, i * kRows, p.ag ? s : 0, pol);
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         __syncwarp();
       };
       auto landed = [&](uint32_t s) {
-        if (!wait_warp(&ctl->ready[s % kStages], (s / kStages) & 1u, wc, SITE_FULL, t)) return false;
+        if (!wait_warp<true>(&ctl->ready[s % kStages], (s / kStages) & 1u, wc, SITE_FULL, t)) return false;
         tc_fence_after_sync();
         return true;
       };
@@ -411,7 +412,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&ctl->x_empty[xs]);
-          mbar_arrive_cluster_fenced(map_to_cta(smem_u32(&ctl->ready[slot]), first_cta));
+          if (leader) mbar_arrive(&ctl->ready[slot]);
+          else mbar_signal_cluster(map_to_cta(smem_u32(&ctl->signal[w]), first_cta), map_to_cta(smem_u32(&ctl->ready[slot]), first_cta));
         }
       }
       j += uint32_t(all);

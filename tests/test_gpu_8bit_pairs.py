@@ -55,3 +55,27 @@ def test_weight_gradients_right_behind_one_another(op, P, M, N, K, grad):
         for out in outs:
             bad += wrong(out, want)
     assert bad.item() == 0 and api.compass_read_status(ws) == (api.OK, 0)
+
+
+def test_no_launch_sees_what_the_one_before_left():
+    """Products and weight gradients of inputs that change from launch to launch: a second CTA's scales or activations that the first
+    one's products took too early would be those of the launch (or of the group) before."""
+    P, M, N, K, sets = 1, 1100, 2048, 2064, 5
+    pr = api.make_problem(AG, P, M, N, K, dtype=api.DTYPE_E4M3)
+    ws, bad = api.alloc_8bit_workspace(pr), torch.zeros((), device="cuda", dtype=torch.int64)
+    made = []
+    for i in range(sets):
+        a, b = product_inputs(AG, P, M, N, K, api.B_NK, api.DTYPE_E4M3, 30 + i, whole=True)
+        d, x = grad_inputs(AG, P, M, N, K, api.DTYPE_E4M3, 40 + i, whole=True)
+        made.append((a, b, d, x, [e.to(torch.bfloat16) for e in product_of(AG, P, a, b, api.B_NK)], [e.float() for e in grad_of(AG, P, d, x)]))
+    c = [[torch.full((M, N), float("nan"), device="cuda", dtype=torch.bfloat16)] for _ in range(sets)]
+    dw = [[torch.full((N, K), float("nan"), device="cuda")] for _ in range(sets)]
+    split = lambda t: ([q for q, _ in t], [s for _, s in t])  # noqa: E731
+    for _ in range(30):
+        for i, (a, b, d, x, _, _) in enumerate(made):
+            api.compass_ag_gemm_8bit(pr, *split(a), *split(b), c[i], ws)
+        for i, (a, b, d, x, _, _) in enumerate(made):
+            api.compass_weight_grad_8bit(pr, d, *split(x), dw[i], ws, grad_dtype=api.DTYPE_FP32)
+        for i in range(sets):
+            bad += wrong(c[i], made[i][4]) + wrong(dw[i], made[i][5])
+    assert bad.item() == 0 and api.compass_read_status(ws) == (api.OK, 0)

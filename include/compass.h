@@ -512,7 +512,9 @@ int compass_dequantize(const compass_quant* quant, const void* const* Q, const v
  *   B, B_scale: [N x K], or [K x N] with COMPASS_B_KN: the stored weight of a forward
  *               pass, by whose transpose its data gradient multiplies
  * Sums are FP32 in the tensor cores, over the whole contraction (all ranks' slices
- * with ReduceScatter), rounded once.  workspace: >= compass_8bit_workspace_bytes,
+ * with ReduceScatter), rounded once.  The tensor cores cut off, at every 32 products,
+ * up to 2^-23 of the sum so far: contractions beyond some 100000 lose a part of BF16's
+ * half step by it.  workspace: >= compass_8bit_workspace_bytes,
  * 256-byte aligned, zeroed once with compass_workspace_init; afterwards
  * compass_read_status reports a bounded wait that gave up. */
 int compass_8bit_workspace_bytes(const compass_problem* problem, size_t* bytes);
@@ -527,7 +529,9 @@ int compass_gemm_rs_8bit(const compass_problem* problem, const void* const* A, c
  *   AllGather:      G = the gradient of C, P x [M x N];  X = row shards [M/P x K], gathered
  *   ReduceScatter:  G = the gradient of Out in row shards [M/P x N], gathered;  X = P x [M x K]
  * G is BF16, N a multiple of 8; X with its scales enters the product in BF16, which
- * holds it exactly (below 2^-126 it is rounded); sums are FP32.  dW: grad_dtype
+ * holds it exactly (below 2^-126 it is rounded); sums are FP32, in the tensor cores
+ * over 65536 rows at most (1024 for a result in FP32), beyond that of such sums.
+ * dW: grad_dtype
  * (COMPASS_DTYPE_BF16 or _FP32); accumulate != 0 adds to what it holds, in FP32,
  * and rounds once. */
 int compass_weight_grad_8bit(const compass_problem* problem, int grad_dtype, int accumulate, const void* const* G,

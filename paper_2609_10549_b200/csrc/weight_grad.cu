@@ -10,8 +10,11 @@
 // convert: two groups, which take the stages in turn; a thread has half a row of a stage, so one scale.  Rows past a rank's last one
 // are zeros of the tensor maps.
 //
-// The tensor cores cut off what their FP32 sums cannot hold, a little at each step.  For a result in FP32 the sums are therefore
-// 1024 rows long, and added up in FP32, in tensor memory: 256 x 256 tiles whose second accumulator keeps the total.
+// The tensor cores cut off what their FP32 sums cannot hold, a little at each step: up to 2^-23 of the sum so far for 16 rows.  For a
+// result in FP32 the sums are therefore 1024 rows long, and added up in FP32, in tensor memory: 256 x 256 tiles whose second accumulator
+// keeps the total.  For one in BF16 the same is done with sums of 65536 rows, in which the cut-off stays below 2^-12 of growing sums, an
+// eighth of BF16's half step (as one sum each, the shares of 4 million positive rows came out up to 0.6 % too small, where half a step is 0.2 %;
+// sums of 65536 rows cost 4096 x 4096 over 131072 rows 4350 us instead of 3880, having no 512 x 256 tiles).
 //
 // Bound by the tensor cores and the board's power: 4 ranks' 2752 x 4096 over 8192 rows 505 us in a burst (1.46 PFLOP/s, tensor pipe busy
 // 88 %) and 560 to 590 in loops.  In FP32 8192 x 8192 over 8192 rows takes 1110 against 810 us: the products wait for the sums of 1024 rows,
@@ -40,7 +43,8 @@ constexpr int kChunk = 64 * kRows * 2;
 constexpr int kStages = 4;                            // of G and of X in BF16
 constexpr int kXStages = 4;
 constexpr int kSkew = 3;                              // stages at a 512 x 256 tile's ends in which accumulator 0 runs ahead
-constexpr int kRangeStages = 16;                      // of a sum that goes to FP32
+// Stages of one sum: of one that goes to FP32, and of one that is rounded to BF16 (65536 rows).
+constexpr int kFp32Range = 16, kBf16Range = 1024;
 constexpr int kMostSplits = 4;                        // pairs of a cluster
 constexpr int kRowGroup = 8;                          // row tiles that go through the columns together
 
@@ -62,6 +66,7 @@ struct GradParams {
   int32_t n_big, left, total;       // 512 x 256 tiles; places left over, two 256 x 256 tiles each
   int32_t splits;                   // pairs of a cluster, which share a tile's contraction
   int32_t accumulate, fp32;
+  int32_t range;           // stages of one sum at most
   int32_t wide;            // results lie on 32-byte boundaries
   uint32_t wait_limit_us;
 };
@@ -180,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   const WaitContext wc{p.status, &ctl->abort, p.wait_limit_us};
   // this pair's stages of a tile
   const int from = p.P * p.stages * pair / splits, all = p.P * p.stages * (pair + 1) / splits - from;
-  const int range = p.fp32 ? kRangeStages : all, parts = (all + range - 1) / range;      // of one sum, and how many sums
+  const int range = p.range, parts = (all + range - 1) / range;      // stages of one sum, and how many sums
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -715,7 +720,8 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   const int32_t places = int32_t(p.big_rows * col_tiles * g->P);
   const int pairs = clusters.of[1];
   const int64_t stages = int64_t(p.stages) * g->P;
-  p.left = p.fp32 && stages > kRangeStages ? places : places % pairs;
+  p.range = p.fp32 ? kFp32Range : kBf16Range;
+  p.left = stages > p.range ? places : places % pairs;
   p.n_big = places - p.left;
   p.total = int32_t(p.n_big + 2 * p.left + p.odd * col_tiles * g->P);
   // Tiles that leave pairs without work: several pairs share a tile's contraction.  A stage of a tile takes some 770 cycles, the sum

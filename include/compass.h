@@ -460,7 +460,7 @@ int compass_head_loss_backward(const compass_head* head, const void* const* X, c
  *   by runs    [rows][ceil(cols / 128)]: one for 128 columns of a row (activations)
  *   by blocks  [ceil(rows / 128)][ceil(cols / 128)]: one for 128 x 128 (weights; the
  *              transpose, which a backward pass multiplies by, has the same scales)
- * The element's value is its scale times it.  Scales are powers of two because the
+ * The element's value is its scale times it (E5M2's infinities are infinite).  Scales are powers of two because the
  * tensor cores apply those themselves; the elements being floating-point numbers,
  * other scales would not make them more precise.
  * What the section on the operators around the blocks says of workspaces, graphs,
@@ -531,9 +531,8 @@ int compass_gemm_rs_8bit(const compass_problem* problem, const void* const* A, c
  * G is BF16, N a multiple of 8; X with its scales enters the product in BF16, which
  * holds it exactly (below 2^-126 it is rounded); sums are FP32, in the tensor cores
  * over 65536 rows at most (1024 for a result in FP32), beyond that of such sums.
- * dW: grad_dtype
- * (COMPASS_DTYPE_BF16 or _FP32); accumulate != 0 adds to what it holds, in FP32,
- * and rounds once. */
+ * dW: grad_dtype (COMPASS_DTYPE_BF16 or _FP32); accumulate != 0 adds to what it
+ * holds, in FP32, and rounds once. */
 int compass_weight_grad_8bit(const compass_problem* problem, int grad_dtype, int accumulate, const void* const* G,
                              const void* const* X, const void* const* X_scale, void* const* dW, void* workspace,
                              size_t workspace_bytes, void* cuda_stream);

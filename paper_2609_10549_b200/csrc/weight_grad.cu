@@ -121,7 +121,8 @@ __device__ __forceinline__ Tile tile_of(const GradParams& p, int t) {
 // 16 values of 8 bits times a scale, in BF16 (`scale`: two of it), those of each four in the order 0, 2, 1, 3, which the epilogue
 // undoes.  The bits of an 8-bit number, its exponent moved to where BF16 has its own, are that number times 2^-120 (E5M2: 2^-112),
 // subnormal ones too; the factors are powers of two, so nothing is rounded above BF16's subnormal range.  What is not a number in
-// 8 bits has now the size of one past the largest: times kPast it overflows, and infinity times 0 is added.  (By the conversion
+// 8 bits has now the size of one past the largest: times kPast it overflows, and infinity times 0 is added, in E4M3 to the value, in E5M2,
+// whose infinities are to stay such, to `odd`: a row with any is converted again by convert16_rare.  (By the conversion
 // instructions this took three quarters of the kernel's time; with the NaN looked for among the bits, the integer pipe was full.)
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -145,23 +146,41 @@ __device__ __forceinline__ void ld_global_f32x8(float* v, const float* from) {
                : "memory");
 }
 template <int kFormat>
-__device__ __forceinline__ uint32_t scaled_pair(uint32_t bits, uint32_t scale) {
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t bits, uint32_t scale, uint32_t& odd) {
   constexpr uint32_t kBias = kFormat == E4M3 ? 0x7B807B80u : 0x77807780u;       // 2^120, 2^112
   // E4M3: 448 kPast is finite, 480 kPast is not: 1.109375 * 2^119.  E5M2: 57344 kPast, 65536 kPast: 1.0625 * 2^112.
   constexpr uint32_t kPast = kFormat == E4M3 ? 0x7B0E7B0Eu : 0x77887788u;
   const uint32_t y = mul_bf16x2(bits, kBias);
+  if constexpr (kFormat == E5M2) {
+    odd = fma_bf16x2(mul_bf16x2(y, kPast), 0u, odd);
+    return mul_bf16x2(y, scale);
+  }
   return fma_bf16x2(y, scale, mul_bf16x2(mul_bf16x2(y, kPast), 0u));
 }
 template <int kFormat>
-__device__ __forceinline__ void convert16(const uint4& w, uint32_t scale, uint4& lo, uint4& hi) {
+__device__ __forceinline__ void convert16(const uint4& w, uint32_t scale, uint4& lo, uint4& hi, uint32_t& odd) {
   constexpr int kShift = kFormat == E4M3 ? 4 : 3;
   constexpr uint32_t kMask = (0x7F00u >> kShift) * 0x10001u;
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
   uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    o[2 * i] = scaled_pair<kFormat>(((v[i] << 8) & 0x80008000u) | ((v[i] << (8 - kShift)) & kMask), scale);      // numbers 0 and 2
-    o[2 * i + 1] = scaled_pair<kFormat>((v[i] & 0x80008000u) | ((v[i] >> kShift) & kMask), scale);               // 1 and 3
+    o[2 * i] = scaled_pair<kFormat>(((v[i] << 8) & 0x80008000u) | ((v[i] << (8 - kShift)) & kMask), scale, odd);      // numbers 0 and 2
+    o[2 * i + 1] = scaled_pair<kFormat>((v[i] & 0x80008000u) | ((v[i] >> kShift) & kMask), scale, odd);               // 1 and 3
+  }
+  lo = make_uint4(o[0], o[1], o[2], o[3]);
+  hi = make_uint4(o[4], o[5], o[6], o[7]);
+}
+// The same by the conversion instructions, of E5M2 with what is infinite or no number.
+__device__ __forceinline__ void convert16_rare(const uint4& w, uint32_t scale, uint4& lo, uint4& hi) {
+  const float s = __uint_as_float(scale << 16);
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 a = unpack8x2<E5M2>(v[i]), b = unpack8x2<E5M2>(v[i] >> 16);
+    o[2 * i] = bf16x2_of(a.x * s, b.x * s);
+    o[2 * i + 1] = bf16x2_of(a.y * s, b.y * s);
   }
   lo = make_uint4(o[0], o[1], o[2], o[3]);
   hi = make_uint4(o[4], o[5], o[6], o[7]);
@@ -404,14 +423,26 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         uint4 in[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) in[u] = *reinterpret_cast<const uint4*>(from + ((u ^ swizzle) << 4));
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          uint4 lo, hi;
-          convert16<kFormat>(in[u], scale, lo, hi);
+        auto put = [&](int u, const uint4& lo, const uint4& hi) {
           uint8_t* chunk = to + (u >> 2) * kChunk;
           const int at16 = 2 * (u & 3);
           *reinterpret_cast<uint4*>(chunk + ((at16 ^ swizzle) << 4)) = lo;
           *reinterpret_cast<uint4*>(chunk + (((at16 + 1) ^ swizzle) << 4)) = hi;
+        };
+        uint4 lo, hi;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          convert16<kFormat>(in[u], scale, lo, hi, odd);
+          put(u, lo, hi);
+        }
+        // (0 times anything finite has added nothing)
+        if (kFormat == E5M2 && (odd & 0x7FFF7FFFu) != 0) {
+#pragma unroll 1
+          for (int u = 0; u < 8; ++u) {
+            convert16_rare(*reinterpret_cast<const uint4*>(from + ((u ^ swizzle) << 4)), scale, lo, hi);
+            put(u, lo, hi);
+          }
         }
         fence_proxy_async_smem();
         __syncwarp();

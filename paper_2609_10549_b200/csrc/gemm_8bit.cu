@@ -887,7 +887,17 @@ PairPlan pair_plan(int64_t N, int64_t row_tiles, int64_t atoms, int step, bool k
 
 // The other kernel's row tiles: whole shards, as many as fit, or equal pieces of one; and over how many CTAs each one's contraction is
 // split.  Their sums cost two barriers of the cluster and some 30 cycles a column.
-int few_two(int64_t cols, int64_t ctas, int sms) { return ctas > sms && cols <= 128; }      // two CTAs per SM
+bool few_two(int64_t cols, int64_t ctas, int sms) { return ctas > sms && cols <= 128; }      // two CTAs per SM
+// Clusters of n CTAs that run at once.  The occupancy query answers for one CTA per SM, whatever its shared memory.  With two, twice as many
+// fit, and some on what is left of the SMs: one for n SMs, but no more than there are clusters of n / 2, whose SMs one of n takes; where n
+// is odd, two thirds of that.  Clusters of 2, 3 .. 8: 148, 92, 70, 54, 45, 34, 33, where in time 148, 92, 71, 55, 45, 37, 33 do (one more, and
+// a token's product takes 9.5 to 10 us instead of 5.6 to 6.1).
+int64_t few_fit(const DeviceFacts& d, int n, bool two) {
+  if (!two) return d.few[n];
+  const int left = d.sms - n * d.few[n];
+  if (n % 2 != 0) return 2 * d.few[n] + 2 * left / n / 3;
+  return 2 * d.few[n] + left / n < d.few[n / 2] ? 2 * d.few[n] + left / n : d.few[n / 2];
+}
 struct FewPlan {
   int64_t shards, pieces, rows, slot, cols, row_tiles;
   int splits;
@@ -914,12 +924,11 @@ FewPlan few_plan(bool rs, int P, int64_t m, int64_t n_tiles, int64_t all, const 
   double atom = atom_cycles(2.0 * double(f.cols), 128 + double(f.shards * f.rows));
   if (atom < 550) atom = 550;      // (measured, whatever the columns)
   for (int n = 1; n <= kMostSplits && (n == 1 || 2 * n <= all); ++n) {
-    // All clusters at once: what is left over takes as long again (2048 x 8192 x 16 rows, 16 clusters of 8 where 15 fit: 13.4 us, of 7 and
-    // 8.8).  With two CTAs per SM a fifteenth more went as well (4096 x 4096 x 1 row, 32 of 8 where 30 fit: 6.0 us, of 4 7.4), more did
-    // not (5120 x 5120 x 32 rows, 40 of 7: 14.3 us, of 6, which fit, 8.4).
-    if (n > 1 && tiles * 15 > d.few[n] * (few_two(f.cols, tiles * n, d.sms) ? 32 : 15)) continue;
+    // Clusters that do not fit at once take as long again (2048 x 8192 x 16 rows, 16 clusters of 8 where 15 fit: 13.4 us, of 6 8.8; two CTAs
+    // per SM, 4096 x 5760 x 1 row, 45 of 6: 7.6 us, 46 12.8), which can still be the least (4096 x 25600 x 1 row, 200 of 2: 26.7 us, of 1 29).
     const double tile = double(ceil_div(all, n)) * atom + 1500;
-    const double cost = n > 1 ? tile + 2000.0 + 30.0 * double(f.cols) : double(ceil_div(tiles, d.sms)) * tile + 10.0 * double(f.cols);
+    const double cost = n > 1 ? double(ceil_div(tiles, few_fit(d, n, few_two(f.cols, tiles * n, d.sms)))) * (tile + 2000.0 + 30.0 * double(f.cols))
+                              : double(ceil_div(tiles, d.sms)) * tile + 10.0 * double(f.cols);
     if (f.splits == 0 || cost < f.cost) {
       f.splits = n;
       f.cost = cost;

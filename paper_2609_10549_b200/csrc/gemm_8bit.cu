@@ -483,11 +483,8 @@ constexpr int kFewMostStages = 12;
 constexpr int kFewRoom = 200 * 1024;          // of stages, with one CTA per SM
 constexpr int kFewHalfRoom = 96 * 1024;       // with two
 constexpr int kMostSplits = 8;
-// Shared memory of a cluster's CTA at least, by its part of tensor memory.  Of 228 KB, 1 KB of which goes with each CTA, there is room
-// for two with half of tensor memory, and for none beside one with all of it.
-constexpr size_t kFewHalf = 78 * 1024, kFewAll = 152 * 1024;
-static_assert(3 * (kFewHalf + 1024) > 228 * 1024 && kFewHalf + kFewAll + 2048 > 228 * 1024, "");
-static_assert(kPairSmemBytes + kFewHalf + 2048 > 228 * 1024, "");
+constexpr size_t kFewAll = 152 * 1024;        // shared memory of a cluster's CTA with more than half of tensor memory, at least
+static_assert(keeps_tmem_apart(kFewAll) && keeps_tmem_apart(kPairSmemBytes), "");
 struct FewControl {
   uint64_t full[kFewMostStages], empty[kFewMostStages];
   uint64_t scales_full[2], scales_empty[2];
@@ -1036,12 +1033,10 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
       ok = ok && encode_tensor_map_bytes(&p.b[r], B[r], b_rows, b_cols, p.b_box);
     }
     if (!ok) return record_cuda_error(cudaErrorUnknown);
-    // The CTAs of a cluster wait for one another while they hold tensor memory, so no two clusters may each wait for what the other
-    // holds (kernels of other streams included).  Shared memory keeps those apart that tensor memory has no room for; the library's
-    // other kernels that wait so take more of it than either leaves.
+    // the CTAs of a cluster wait for one another while they hold tensor memory
     size_t smem = few_smem_bytes(p.cols, p.stages);
     if (p.splits > 1) {
-      const size_t least = p.tmem_cols <= 256 ? kFewHalf : kFewAll;
+      const size_t least = p.tmem_cols <= 256 ? kHalfTmemShared : kFewAll;
       if (smem < least) smem = least;
     }
     return launch_clusters(gemm8_few_kernel, tiles * p.splits, kFewThreads, smem, p.splits, p, s);

@@ -97,6 +97,7 @@ constexpr size_t smem_bytes() {
   return 1024 /*alignment slack*/ + size_t(Cfg<kPair>::kStages) * Cfg<kPair>::kStageBytes + sizeof(Control) + 16 +
          size_t(kEpilogueWarps) * kStageWarpBytes;
 }
+static_assert(keeps_tmem_apart(smem_bytes<false>()) && keeps_tmem_apart(smem_bytes<true>()), "");
 
 __device__ __forceinline__ void report_timeout(const GemmParams& p, Control* ctl, int site, int tile) {
   *reinterpret_cast<volatile int*>(&ctl->abort) = 1;
@@ -771,6 +772,7 @@ constexpr int kChunkBytes = BM * BK * 2;      // 16 KB: one 128-row, 64-column B
 constexpr int kChunks = 12;
 constexpr size_t kMixedSmemBytes =
     1024 + size_t(kChunks) * kChunkBytes + sizeof(Control) + 16 + size_t(kEpilogueWarps) * kStageWarpBytes;
+static_assert(keeps_tmem_apart(kMixedSmemBytes), "");
 
 struct MixedTile {
   int big;        // 1 = 512x256, 0 = 256x256 or 256x128

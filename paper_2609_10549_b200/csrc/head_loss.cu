@@ -129,6 +129,7 @@ struct Control {
 };
 
 constexpr size_t kSmemBytes = 1024 + size_t(kChunks) * kChunkBytes + sizeof(Control);
+static_assert(keeps_tmem_apart(kSmemBytes), "");
 
 enum Site : int { SITE_EMPTY = 1, SITE_FULL = 2, SITE_ACC_EMPTY = 3, SITE_ACC_FULL = 4, SITE_DRAIN = 5 };
 

@@ -200,6 +200,14 @@ int launch_reduce_partials(const void* const* partial, int P, void* const* out, 
 int launch_gather_slices(const void* const* shard, void* const* gather, int P, int64_t m, int64_t K, int64_t slice_begin,
                          int64_t slice_rows, cudaStream_t stream);
 
+// CTAs that wait for others of their cluster or grid while they hold tensor memory must not hold what those wait for, nor may the CTAs
+// of two such kernels (of two streams) hold what the other's wait for.  Their shared memory sees to it: of an SM's 228 KB, 1 KB of which
+// goes with each CTA, there is room for two CTAs that take half of tensor memory, and for none beside one that takes all of it.
+constexpr size_t kSmShared = 228 * 1024, kCtaShared = 1024;
+constexpr size_t kHalfTmemShared = 78 * 1024;      // of a CTA with half of tensor memory, at least
+constexpr bool keeps_tmem_apart(size_t smem) { return smem + kHalfTmemShared + 2 * kCtaShared > kSmShared && 2 * (smem + kCtaShared) > kSmShared; }
+static_assert(3 * (kHalfTmemShared + kCtaShared) > kSmShared, "");
+
 // gemm_8bit.cu
 int check_problem_8bit(const compass_problem* problem);
 

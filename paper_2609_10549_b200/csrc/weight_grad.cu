@@ -83,7 +83,7 @@ struct Control {
 };
 constexpr int kXAt = kStages * kGBytes, kCAt = kXAt + kXStages * kXBytes, kControlAt = kCAt + kStages * kCBytes;
 constexpr size_t kSmemBytes = 1024 + kControlAt + sizeof(Control);
-static_assert(kSmemBytes <= 227 * 1024 && kGroups <= kStages && kStages <= kXStages, "");
+static_assert(kSmemBytes <= 227 * 1024 && keeps_tmem_apart(kSmemBytes) && kGroups <= kStages && kStages <= kXStages, "");
 
 struct Tile {
   bool big;

@@ -1002,7 +1002,7 @@ int run_product(const compass_problem* g, int op, const void* const* A, const vo
   p.n_step = p.kn ? 32 : 16;
   const PairPlan pair = pair_plan(g->N, p.row_tiles * ranks, all, p.n_step, p.kn, f->pairs);
   const int64_t few_tiles = n_tiles * few.row_tiles * ranks;
-  if (few.cost < pair.cost && few_tiles <= kMaxDim) {
+  if (few.cost < pair.cost && few_tiles * few.splits <= kMaxDim) {
     p.tile_shards = int32_t(few.shards);
     p.tile_rows = int32_t(few.rows);
     p.slot.set(uint32_t(few.slot));

@@ -318,8 +318,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
         if (ok && elect_one()) umma_commit_pair(&ctl->acc_full, 0x3);
         __syncwarp();
       }
-      // leave only when the last tile's signals have come: the other CTA's may be on their way to this one's memory still
-      if (ok && it > 0) wait_warp(&ctl->acc_early, (it - 1) & 1u, wc, SITE_DRAIN, -1);
       if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&ctl->abort) != 0)) {
         // gave up somewhere: let the tensor core finish what it still has before tensor memory is released
         if (elect_one()) umma_commit_pair(&ctl->drain, 0x1);
@@ -409,7 +407,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm8_pair_kernel(const __gri
       tmem_ld_wait();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_early), 0));
+      // (not of the last tile: nobody would wait for the signal, and the CTA that it goes to may have left)
+      if (lane == 0 && t + units < p.total) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&ctl->acc_early), 0));
       if (second) tmem_ld_32x32b_x32(taddr + 96, v[3]);
       else tmem_ld_32x32b_x32(taddr, v[0]);
       tmem_ld_32x32b_x32(taddr + 32, v[1]);

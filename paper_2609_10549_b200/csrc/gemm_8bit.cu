@@ -754,6 +754,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       // the i-th row of the tile: of which shard, and its accumulator column
       const int s = shards == 1 ? 0 : int(p.each.div(uint32_t(i))), row = i - s * rows;
       const uint32_t at = base + uint32_t((s * int(p.slot.d) + row) * 128 + n) * 4;
+      if (n0 + n >= p.N) continue;      // (only what is stored is read, and so has been read before the warp says that the others may leave)
       float4 y[kMostSplits];
 #pragma unroll
       for (int k = 0; k < kMostSplits; ++k)
@@ -774,7 +775,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) gemm8_few_kernel(const __grid_
       }
       out += n0 + n;
       if (p.wide) {      // (N is a multiple of 8)
-        if (n0 + n < p.N) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
       } else {
         const float z[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll

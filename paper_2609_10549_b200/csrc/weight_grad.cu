@@ -607,6 +607,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     cluster_wait();
     if (*reinterpret_cast<volatile int*>(&ctl->abort) == 0) {
       const Tile c = tile_of(p, unit);
+      // (128 columns are read only where a lane stores some of them: then they have been read before the warp says that the others may leave.)
+      const bool second = c.col0 + 128 < p.K;
       for (int row = pair + splits * warp; row < 128; row += splits * (kThreads / 32)) {
         const int64_t n = c.row0 + cta * 128 + row;
         if (n >= p.N) break;
@@ -617,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           if (q < splits)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+              if (h == 0 || second) asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                            : "=f"(y[q][h].x), "=f"(y[q][h].y), "=f"(y[q][h].z), "=f"(y[q][h].w)
                            : "r"(map_to_cta(at + (uint32_t((h * 32 + lane) ^ (row & 7)) << 4), uint32_t(2 * q + cta))));
 #pragma unroll

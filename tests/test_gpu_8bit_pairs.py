@@ -41,7 +41,7 @@ def test_products_right_behind_one_another(op, P, M, N, K):
 
 # one accumulator, both in turn, sums of 1024 rows, tiles of 512 rows, a contraction that pairs share
 @pytest.mark.parametrize("grad", [api.DTYPE_BF16, api.DTYPE_FP32])
-@pytest.mark.parametrize("op,P,M,N,K", [(AG, 1, 40, 72, 80), (AG, 1, 300, 6152, 2064), (RS, 2, 2300, 136, 272), (AG, 1, 200, 8192, 2560), (AG, 1, 4100, 264, 144)])
+@pytest.mark.parametrize("op,P,M,N,K", [(AG, 1, 40, 72, 80), (AG, 1, 300, 6152, 2064), (RS, 2, 2300, 136, 272), (AG, 1, 200, 8192, 2560), (AG, 1, 4100, 264, 144), (AG, 1, 4100, 72, 80)])
 def test_weight_gradients_right_behind_one_another(op, P, M, N, K, grad):
     d, x = grad_inputs(op, P, M, N, K, api.DTYPE_E4M3, 21, whole=True)
     kind = torch.float32 if grad == api.DTYPE_FP32 else torch.bfloat16

@@ -7,8 +7,8 @@
 // Pairs of CTAs, 512 rows (n) x 256 columns (k) a tile as long as they fill whole rounds of the pairs (two accumulators that share
 // one converted tile), 256 x 256 for the rest; 64 rows of the contraction a stage.  Both operands lie across the contraction
 // (MN-major).  Warp 0 loads G (TMA), warp 18 X, warp 1 issues the products, warps 2..9 are the epilogue, warps 10..17
-// convert: two groups, which take the stages in turn; a thread has half a row of a stage, so one scale.  Rows past a rank's last one
-// are zeros of the tensor maps.
+// convert: four groups of two warps, which take the stages in turn; a thread has its CTA's 128 columns of one row of a stage, so one
+// scale.  Rows past a rank's last one are zeros of the tensor maps.
 //
 // The tensor cores cut off what their FP32 sums cannot hold, a little at each step: up to 2^-23 of the sum so far for 16 rows.  For a
 // result in FP32 the sums are therefore 1024 rows long, and added up in FP32, in tensor memory: 256 x 256 tiles whose second accumulator

@@ -108,8 +108,8 @@ __device__ __forceinline__ int steps_of(const Gemm8Params& p, int a) { return mi
 // Warp 0 loads (TMA), warp 1 issues the products, warps 2..9 are the epilogue (two per quarter of the rows, 128 columns each),
 // warp 10 brings the scales.  Tensor memory holds two accumulators of 256 columns and the scales only because the accumulators
 // share 32 columns: each is emptied from the shared ones on, and the next tile's products begin once these are read.
-// Bound by the tensor cores, then by the board's power: 8 ranks' 8192 x 1376 x 4096 254 us in a burst (2.9 PFLOP/s, tensor pipe busy 85 % of
-// the cycles) and 310 to 320 in loops; GEMM+ReduceScatter of 4 ranks 8192 x 4096 x 2752, [K][N], 251 and 325.  256 x 256 takes the fewest
+// Bound by the tensor cores, then by the board's power: 8 ranks' 8192 x 1376 x 4096 254 to 264 us in a burst (2.8 to 2.9 PFLOP/s, tensor pipe busy
+// 85 % of the cycles) and 305 to 340 in loops; GEMM+ReduceScatter of 4 ranks 8192 x 4096 x 2752, [K][N], 251 to 263 and 320 to 350.  256 x 256 takes the fewest
 // operand bytes that tensor memory has room for with two accumulators.
 constexpr int kPairThreads = 352;
 constexpr int kEpiWarps = 8;

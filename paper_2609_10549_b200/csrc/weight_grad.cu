@@ -16,8 +16,8 @@
 // eighth of BF16's half step (as one sum each, the shares of 4 million positive rows came out up to 0.6 % too small, where half a step is 0.2 %;
 // sums of 65536 rows cost 4096 x 4096 over 131072 rows 4350 us instead of 3880, having no 512 x 256 tiles).
 //
-// Bound by the tensor cores and the board's power: 4 ranks' 2752 x 4096 over 8192 rows 505 us in a burst (1.46 PFLOP/s, tensor pipe busy
-// 88 %) and 560 to 590 in loops.  In FP32 8192 x 8192 over 8192 rows takes 1110 against 810 us: the products wait for the sums of 1024 rows,
+// Bound by the tensor cores and the board's power: 4 ranks' 2752 x 4096 over 8192 rows 505 to 515 us in a burst (1.45 PFLOP/s, tensor pipe
+// busy 88 %) and 560 to 600 in loops.  In FP32 8192 x 8192 over 8192 rows takes 1060 to 1110 against 790 to 840 us: the products wait for the sums of 1024 rows,
 // and tiles of 256 x 256 take shared memory's bandwidth (160 bytes a clock).
 #include <mutex>
 
@@ -759,7 +759,7 @@ extern "C" int compass_weight_grad_8bit(const compass_problem* g, int grad_dtype
   p.total = int32_t(p.n_big + 2 * p.left + p.odd * col_tiles * g->P);
   // Tiles that leave pairs without work: several pairs share a tile's contraction.  A stage of a tile takes some 770 cycles, the sum
   // over the cluster some 5000 (and the next kernel begins no earlier on SMs without work).  Measured with one pair and with several: 1024 x
-  // 1024 over 4096 rows 30.9 us : 18.2, over 1024 12.4 : 11.9, 4 ranks' 232 x 480 over 5552 rows 42 : 17.8, 768 x 768 over 2048 rows in FP32
+  // 1024 over 4096 rows 30.9 us : 18.6, over 1024 12.5 : 12.2, 4 ranks' 232 x 480 over 5552 rows 42 : 17.8, 768 x 768 over 2048 rows in FP32
   // 25.6 : 12.6; 512 x 512 over 512 rows 9.0 : 9.8.
   p.splits = 1;
   int64_t least = stages * 770;
